@@ -349,7 +349,7 @@ def _plain_adamw(s):
 def _scaled(a, blk, nb, top):
     """a over its block's scale (the block's largest value has the code `top`), the scale by column and by block."""
     big = torch.zeros((a.shape[0], nb), device=DEV, dtype=a.dtype).scatter_reduce_(1, blk, a, "amax")
-    scale = big / (top * top)
+    scale = big * (1.0 / (top * top))
     scale = torch.where(scale > 2.0 ** -100, scale, torch.zeros_like(scale))
     inv = torch.where(scale > 0, 1.0 / scale, torch.zeros_like(scale))
     return (a * inv.gather(1, blk)).clamp(max=top * top), scale.gather(1, blk), scale
