@@ -349,6 +349,117 @@ lsgd_status lsgd_select_pull_static(int32_t W, int64_t P, int64_t ld, int32_t n_
 enum { LSGD_PROBE_READ = 0, LSGD_PROBE_COPY = 1, LSGD_PROBE_UPDATE = 2 };
 lsgd_status lsgd_stream_probe(int32_t kind, float* a, float* b, float* c, int64_t n, void* hip_stream);
 
+/* ---- Operators of token models ------------------------------------------------------------------
+ * What a population of models over tokens needs around its blocks' matrix products and for its step.  As everywhere,
+ * worker w's parameters and gradients are columns of row w of fp32 matrices (x, g), so a pointer into row 0 and the
+ * row stride ld name a parameter tensor of all workers.  None of these needs a population handle; each takes its stream,
+ * device pointers and workspace from the caller, allocates nothing on the device and does not synchronise (except
+ * lsgd_adamw_create).  Strides count elements.  bf16 data are bit patterns; sums, norms and moments' arithmetic are fp32. */
+
+/* Embedding lookup: out[w,t,:] = scale * table_w[tokens[w,t], :], rounded once; zeros where the token lies outside
+ * [0, V) (padding: such a place is never looked up).
+ *   table  device, worker w's [V, D] at table + w*ld_table (fp32 or bf16; ld_table = 0: one table for all workers)
+ *   tokens device int32, worker w's [T] at tokens + w*ld_tokens
+ *   out    device, worker w's [T, D] at out + w*ld_out (fp32 or bf16); must not overlap the inputs
+ * T = 0 is allowed.  T <= 2^24, V < 2^30.                                                              */
+lsgd_status lsgd_embed_lookup(int32_t W, int32_t T, int32_t V, int32_t D, const void* table, int64_t ld_table, int32_t table_is_bf16,
+                              const int32_t* tokens, int64_t ld_tokens, float scale, void* out, int64_t ld_out, int32_t out_is_bf16,
+                              void* hip_stream);
+
+/* Its gradient: dtable_w[v,:] = scale * sum over t with tokens[w,t] = v of dout[w,t,:], summed in fp32 in an order that
+ * depends on the tokens alone (equal calls give equal bits).
+ *   accumulate 0: every row of the table is written, zeros where no token names it; 1: the sum is added to what is there
+ *              (tied weights, several batches a step) and rows that no token names are not touched
+ *   dout       device, worker w's [T, D] at dout + w*ld_dout (fp32 or bf16)
+ *   dtable     device fp32, worker w's [V, D] at dtable + w*ld_dtable, ld_dtable >= V*D; must not overlap the inputs
+ *   workspace  device, >= lsgd_embed_grad_workspace_bytes, 256-byte aligned (may be NULL when T = 0); not kept      */
+size_t lsgd_embed_grad_workspace_bytes(int32_t W, int32_t T, int32_t V, int32_t D); /* 0 on invalid arguments */
+lsgd_status lsgd_embed_grad(int32_t W, int32_t T, int32_t V, int32_t D, const void* dout, int64_t ld_dout, int32_t dout_is_bf16,
+                            const int32_t* tokens, int64_t ld_tokens, float scale, int32_t accumulate, float* dtable, int64_t ld_dtable,
+                            void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Activations [W, T, D] with dense rows: token t of worker w at data + w*worker_stride + t*token_stride. */
+typedef struct {
+    void* data; /* device; NULL: absent */
+    int64_t worker_stride, token_stride;
+} lsgd_rows;
+
+/* Norms after and before a block, fused with its gate and residual sum, D <= 16384:
+ *   r_out = r + scale * sigmoid(gate) o (q_post y o w_post)   q_post = (mean_d y^2 + eps)^-1/2     (when y is given)
+ *   n     = q_pre r_out o w_pre                               q_pre  = (mean_d r_out^2 + eps)^-1/2  (when n is given)
+ * With y absent the second line takes r in r_out's place (a model's first norm); with n absent only the sum is made (its
+ * last).  gate absent: 1.  post_norm = 0: q_post = 1 (blocks without a norm behind them; w_post then scales channels).
+ * n is computed from r_out before that is rounded to its type.  r_out may be r, and n may be y or gate, element for
+ * element; no other overlaps.                                                                              */
+typedef struct {
+    int32_t W, T, D;
+    int32_t is_bf16;              /* type of r, y, gate, r_out, n: 0 fp32, 1 bf16                    */
+    int32_t post_norm;
+    float scale, eps;             /* eps > 0                                                         */
+    lsgd_rows r, y, gate, r_out, n;
+    const float *w_post, *w_pre;  /* device fp32, worker w's [D] at w_post + w*ld_w_post; NULL: ones */
+    int64_t ld_w_post, ld_w_pre;
+    float *q_post, *q_pre;        /* device fp32 [W, T], what the gradient needs; NULL: not wanted   */
+} lsgd_block_norm_args;
+lsgd_status lsgd_block_norm(const lsgd_block_norm_args* args, void* hip_stream);
+
+/* Its gradients from dn (of n; absent: there was no norm before the next block) and dr_out (what reaches r_out past it;
+ * absent: nothing), given what the forward call read and gave:
+ *   dr (of r), dy, dgate     [W, T, D] of the activations' type
+ *   dw_post, dw_pre          device fp32, worker w's [D] at dw + w*ld; NULL: not wanted; accumulate = 1 adds to them
+ * r_out and q_pre are needed with dn, q_post with a post-norm.  dr may be dr_out or dn, dy may be y, dgate may be gate,
+ * element for element.  Sums over tokens are made in an order that depends on the sizes alone.
+ *   workspace  device, >= lsgd_block_norm_grad_workspace_bytes, 256-byte aligned; may be NULL when no dw is wanted   */
+typedef struct {
+    int32_t W, T, D;
+    int32_t is_bf16, post_norm, accumulate;
+    float scale;
+    lsgd_rows dn, dr_out, r_out, y, gate, dr, dy, dgate;
+    const float *w_post, *w_pre;
+    int64_t ld_w_post, ld_w_pre;
+    const float *q_post, *q_pre;
+    float *dw_post, *dw_pre;
+    int64_t ld_dw_post, ld_dw_pre;
+} lsgd_block_norm_grad_args;
+size_t lsgd_block_norm_grad_workspace_bytes(int32_t W, int32_t T, int32_t D); /* 0 on invalid arguments */
+lsgd_status lsgd_block_norm_grad(const lsgd_block_norm_grad_args* args, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* AdamW over a list of tensors, one launch a step.
+ *   m <- b1 m + (1-b1) c g;  v <- b2 v + (1-b2) (c g)^2
+ *   x <- x (1 - lr lr_mult wd) - lr lr_mult/(1-b1^t) * m / (sqrt(v)/sqrt(1-b2^t) + eps)
+ * A tensor is a [rows, n] part of matrices (for a population: rows = W, n = the tensor's elements in a worker's row, the
+ * strides those of x and g); one row stands for any dense tensor.  Tensors must not overlap.
+ * state_bits 32: m, v fp32.  8: m int8 and v uint8 codes with one fp32 scale for every LSGD_ADAMW_BLOCK elements of a
+ * row (the last block may be shorter): m = sign(q) q^2 m_scale, v = (q^2 v_scale)^2; all zeros is the state before the
+ * first step.  Which of the two codes around a value is stored follows from a threshold that the step number sets, so
+ * that slow changes are kept on average; scales are the block's largest value's, and a block whose largest is below about
+ * 2^-100 q_max^2 is held as zeros.  A moment that is not finite is held as the block's largest finite one.            */
+#define LSGD_ADAMW_BLOCK 256
+typedef struct {
+    float* x;                     /* device [rows, n], updated                                         */
+    const void* g;                /* device [rows, n], fp32 or bf16 (the same for all tensors)         */
+    void *m, *v;                  /* device [rows, n] moments, updated                                 */
+    float *m_scale, *v_scale;     /* device [rows, ceil(n / LSGD_ADAMW_BLOCK)]; 8 bits only            */
+    float *m_values, *v_values;   /* device [rows, n], where lsgd_adamw_moments writes; NULL: nowhere  */
+    uint16_t* x_bf16;             /* device [rows, n], kept equal to bf16(x); NULL: none               */
+    int64_t rows, n;
+    int64_t ld_x, ld_g, ld_state, ld_scale, ld_values, ld_bf16; /* row strides (ld_state: m and v)     */
+    double weight_decay, lr_mult;
+} lsgd_adamw_tensor;
+typedef struct lsgd_adamw lsgd_adamw; /* opaque host object */
+
+/* Bytes of the tables a handle keeps in its workspace; 0 on invalid arguments. */
+size_t lsgd_adamw_workspace_bytes(const lsgd_adamw_tensor* tensors, int32_t n_tensors, int32_t state_bits, int32_t g_is_bf16);
+/* Binds caller-owned buffers into a handle; workspace is device memory, 256-byte aligned, owned by the caller for the
+ * life of the handle.  Copies the tables there and synchronises the stream, which all later calls use.            */
+lsgd_status lsgd_adamw_create(const lsgd_adamw_tensor* tensors, int32_t n_tensors, int32_t state_bits, int32_t g_is_bf16, void* workspace,
+                              size_t workspace_bytes, void* hip_stream, lsgd_adamw** out);
+lsgd_status lsgd_adamw_destroy(lsgd_adamw* opt); /* frees the host object only */
+/* step counts from 1; grad_scale is the c above.  All are values of this call: a captured call repeats them. */
+lsgd_status lsgd_adamw_step(lsgd_adamw* opt, double lr, double beta1, double beta2, double eps, int64_t step, double grad_scale);
+/* 8 bits: writes what the stored codes stand for to m_values and v_values of the tensors that have them. */
+lsgd_status lsgd_adamw_moments(lsgd_adamw* opt);
+
 /* Message for the last failing call on this thread ("" if none).  Static storage. */
 const char* lsgd_last_error(void);
 

@@ -55,6 +55,31 @@ class _Batch(C.Structure):
     _fields_ = [("kind", C.c_int32), ("desc", C.c_void_p)]
 
 
+class _Rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("worker_stride", C.c_int64), ("token_stride", C.c_int64)]
+
+
+class _BlockNorm(C.Structure):
+    _fields_ = [("W", C.c_int32), ("T", C.c_int32), ("D", C.c_int32), ("is_bf16", C.c_int32), ("post_norm", C.c_int32),
+                ("scale", C.c_float), ("eps", C.c_float), ("r", _Rows), ("y", _Rows), ("gate", _Rows), ("r_out", _Rows), ("n", _Rows),
+                ("w_post", C.c_void_p), ("w_pre", C.c_void_p), ("ld_w_post", C.c_int64), ("ld_w_pre", C.c_int64),
+                ("q_post", C.c_void_p), ("q_pre", C.c_void_p)]
+
+
+class _BlockNormGrad(C.Structure):
+    _fields_ = [("W", C.c_int32), ("T", C.c_int32), ("D", C.c_int32), ("is_bf16", C.c_int32), ("post_norm", C.c_int32),
+                ("accumulate", C.c_int32), ("scale", C.c_float), ("dn", _Rows), ("dr_out", _Rows), ("r_out", _Rows), ("y", _Rows),
+                ("gate", _Rows), ("dr", _Rows), ("dy", _Rows), ("dgate", _Rows), ("w_post", C.c_void_p), ("w_pre", C.c_void_p),
+                ("ld_w_post", C.c_int64), ("ld_w_pre", C.c_int64), ("q_post", C.c_void_p), ("q_pre", C.c_void_p),
+                ("dw_post", C.c_void_p), ("dw_pre", C.c_void_p), ("ld_dw_post", C.c_int64), ("ld_dw_pre", C.c_int64)]
+
+
+class _AdamWTensor(C.Structure):
+    _fields_ = [(k, C.c_void_p) for k in ("x", "g", "m", "v", "m_scale", "v_scale", "m_values", "v_values", "x_bf16")] + \
+               [(k, C.c_int64) for k in ("rows", "n", "ld_x", "ld_g", "ld_state", "ld_scale", "ld_values", "ld_bf16")] + \
+               [("weight_decay", C.c_double), ("lr_mult", C.c_double)]
+
+
 def lib_path() -> str:
     return os.path.join(_HERE, "liblsgd.so")
 
@@ -98,6 +123,23 @@ def lib():
         L.lsgd_get_leaders.argtypes = [C.c_void_p, C.POINTER(C.c_int32), C.POINTER(C.c_int32)]
         L.lsgd_get_losses.argtypes = [C.c_void_p, C.POINTER(C.c_float)]
         L.lsgd_set_leaders.argtypes = [C.c_void_p, C.POINTER(C.c_int32), C.c_int32]
+        L.lsgd_embed_lookup.argtypes = [C.c_int32] * 4 + [C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_int64, C.c_float, C.c_void_p,
+                                                          C.c_int64, C.c_int32, C.c_void_p]
+        L.lsgd_embed_grad_workspace_bytes.restype = C.c_size_t
+        L.lsgd_embed_grad_workspace_bytes.argtypes = [C.c_int32] * 4
+        L.lsgd_embed_grad.argtypes = [C.c_int32] * 4 + [C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_int64, C.c_float, C.c_int32,
+                                                        C.c_void_p, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.lsgd_block_norm.argtypes = [C.POINTER(_BlockNorm), C.c_void_p]
+        L.lsgd_block_norm_grad_workspace_bytes.restype = C.c_size_t
+        L.lsgd_block_norm_grad_workspace_bytes.argtypes = [C.c_int32] * 3
+        L.lsgd_block_norm_grad.argtypes = [C.POINTER(_BlockNormGrad), C.c_void_p, C.c_size_t, C.c_void_p]
+        L.lsgd_adamw_workspace_bytes.restype = C.c_size_t
+        L.lsgd_adamw_workspace_bytes.argtypes = [C.POINTER(_AdamWTensor), C.c_int32, C.c_int32, C.c_int32]
+        L.lsgd_adamw_create.argtypes = [C.POINTER(_AdamWTensor), C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p,
+                                        C.POINTER(C.c_void_p)]
+        L.lsgd_adamw_destroy.argtypes = [C.c_void_p]
+        L.lsgd_adamw_step.argtypes = [C.c_void_p, C.c_double, C.c_double, C.c_double, C.c_double, C.c_int64, C.c_double]
+        L.lsgd_adamw_moments.argtypes = [C.c_void_p]
         _lib = L
     return _lib
 
@@ -300,3 +342,288 @@ class Population:
         out = (C.c_float * self.W)()
         _check(lib().lsgd_get_losses(self._h, out))
         return list(out)
+
+
+# ------------------------------------------------------------------------------------------------
+# operators of token models
+# ------------------------------------------------------------------------------------------------
+ADAMW_BLOCK = 256
+
+_FLOATS = (torch.float32, torch.bfloat16)
+
+
+def _need(ok, msg):
+    if not ok:
+        raise ValueError(msg)
+
+
+def _on_gpu(who, **tensors):
+    """All tensors that are given lie on one GPU; returns it."""
+    dev = None
+    for name, t in tensors.items():
+        if t is None:
+            continue
+        _need(t.is_cuda, f"{who}: {name} is not on a GPU")
+        _need(dev is None or t.device == dev, f"{who}: {name} is on {t.device}, other tensors on {dev}")
+        dev = t.device
+    return dev
+
+
+def _launch_on(dev, stream):
+    return C.c_void_p((torch.cuda.current_stream(dev) if stream is None else stream).cuda_stream)
+
+
+def _fresh(shape, dtype, dev, stream):
+    """Memory of the stream that the call runs on, as under torch.cuda.stream(stream): whoever used it before, or will after it is
+    freed, is ordered on that stream too."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=dev)
+
+
+def _workspace(who, nbytes, dev, workspace, stream):
+    """The caller's, or memory of this call's own."""
+    if nbytes == 0:
+        raise LsgdError(-1, lib().lsgd_last_error().decode())
+    if workspace is None:
+        workspace = _fresh((nbytes,), torch.uint8, dev, stream)
+    _need(workspace.device == dev and workspace.is_contiguous(), f"{who}: workspace must be contiguous and on {dev}")
+    return workspace, workspace.numel() * workspace.element_size()
+
+
+def _stride0(t):
+    """Row stride of what the library reads by rows; of a single row any will do."""
+    return int(t.stride(0)) if t.shape[0] > 1 else int(t.numel())
+
+
+def _dense_after(t, k):
+    """Whether dimensions k.. of t lie in memory one after the other without gaps."""
+    want = 1
+    for d in range(t.dim() - 1, k - 1, -1):
+        if t.shape[d] > 1 and t.stride(d) != want:
+            return False
+        want *= t.shape[d]
+    return True
+
+
+def _tokens(who, tokens):
+    _need(tokens.dtype == torch.int32 and tokens.dim() == 2, f"{who}: tokens must be int32 [W, T]")
+    _need(tokens.numel() == 0 or _dense_after(tokens, 1), f"{who}: a worker's tokens must be dense")
+
+
+def embed_lookup(table, tokens, scale=1.0, dtype=None, out=None, stream=None):
+    """lsgd_embed_lookup: scale * table[w, tokens[w, t]] as [W, T, D]; zeros where a token lies outside [0, V).
+    table: float32 or bfloat16 [W, V, D], dense within a worker (columns of x: x[:, a:a + V * D].unflatten(1, (V, D)));
+    tokens: int32 [W, T]; dtype: of the result (the table's if None); out: optional result buffer."""
+    who = "embed_lookup"
+    dev = _on_gpu(who, table=table, tokens=tokens, out=out)
+    _tokens(who, tokens)
+    _need(table.dim() == 3 and table.dtype in _FLOATS, f"{who}: table must be float32 or bfloat16 [W, V, D]")
+    W, V, D = table.shape
+    T = tokens.shape[1]
+    _need(tokens.shape[0] == W, f"{who}: {tokens.shape[0]} rows of tokens for {W} workers")
+    _need(_dense_after(table, 1), f"{who}: a worker's table must be dense")
+    if out is None:
+        dtype = table.dtype if dtype is None else dtype
+        _need(dtype in _FLOATS, f"{who}: dtype must be float32 or bfloat16")
+        out = _fresh((W, T, D), dtype, dev, stream)
+    _need(out.shape == (W, T, D) and out.dtype in _FLOATS and (dtype is None or out.dtype == dtype), f"{who}: out must be [W, T, D] of dtype")
+    _need(out.numel() == 0 or _dense_after(out, 1), f"{who}: a worker's part of out must be dense")
+    if tokens.numel() == 0:
+        return out
+    with torch.cuda.device(dev):
+        _check(lib().lsgd_embed_lookup(W, T, V, D, _ptr(table), _stride0(table), int(table.dtype == torch.bfloat16), _ptr(tokens),
+                                       _stride0(tokens), scale, _ptr(out), _stride0(out), int(out.dtype == torch.bfloat16), _launch_on(dev, stream)))
+    return out
+
+
+def embed_grad(dout, tokens, dtable, scale=1.0, accumulate=False, workspace=None, stream=None):
+    """lsgd_embed_grad: the table's gradient of embed_lookup, into dtable (float32 [W, V, D], dense within a worker).
+    dout: float32 or bfloat16 [W, T, D], dense within a worker; accumulate: add to dtable instead of writing all of it."""
+    who = "embed_grad"
+    dev = _on_gpu(who, dout=dout, tokens=tokens, dtable=dtable)
+    _tokens(who, tokens)
+    _need(dtable.dim() == 3 and dtable.dtype == torch.float32, f"{who}: dtable must be float32 [W, V, D]")
+    W, V, D = dtable.shape
+    T = tokens.shape[1]
+    _need(tokens.shape[0] == W and dout.shape == (W, T, D) and dout.dtype in _FLOATS, f"{who}: dout must be float32 or bfloat16 [W, T, D] and tokens [W, T]")
+    _need(_dense_after(dtable, 1), f"{who}: a worker's part of dtable must be dense")
+    _need(dout.numel() == 0 or _dense_after(dout, 1), f"{who}: a worker's part of dout must be dense (an expanded gradient needs .contiguous())")
+    with torch.cuda.device(dev):
+        nbytes = 0
+        if T > 0:
+            workspace, nbytes = _workspace(who, lib().lsgd_embed_grad_workspace_bytes(W, T, V, D), dev, workspace, stream)
+        _check(lib().lsgd_embed_grad(W, T, V, D, _ptr(dout), _stride0(dout) if T else 0, int(dout.dtype == torch.bfloat16), _ptr(tokens),
+                                     _stride0(tokens) if T else 0, scale, int(bool(accumulate)), _ptr(dtable), _stride0(dtable),
+                                     _ptr(workspace) if T else None, nbytes, _launch_on(dev, stream)))
+
+
+def _rows(who, name, t, shape, dtype):
+    if t is None:
+        return _Rows(None, 0, 0)
+    _need(tuple(t.shape) == tuple(shape) and t.dtype == dtype, f"{who}: {name} must be {dtype} {list(shape)}")
+    _need(t.numel() == 0 or t.shape[2] == 1 or t.stride(2) == 1, f"{who}: rows of {name} must be dense")
+    W, T, D = shape
+    # a dimension of one element has no stride that means anything
+    return _Rows(t.data_ptr() or None, t.stride(0) if W > 1 else T * D, t.stride(1) if T > 1 else D)
+
+
+def _weights(who, name, w, W, D):
+    if w is None:
+        return None, 0
+    _need(w.dtype == torch.float32 and tuple(w.shape) == (W, D) and (D == 1 or w.stride(1) == 1), f"{who}: {name} must be float32 [W, D] with dense rows")
+    return w.data_ptr(), w.stride(0) if W > 1 else D
+
+
+def block_norm(r, y=None, gate=None, w_post=None, w_pre=None, scale=1.0, eps=1e-6, post_norm=True, pre_norm=True, r_out=None, n=None,
+               stats=None, stream=None):
+    """lsgd_block_norm: r_out = r + scale * sigmoid(gate) * norm(y) * w_post, n = norm(r_out) * w_pre.
+    r, y, gate: float32 or bfloat16 [W, T, D] with dense rows; w_post, w_pre: float32 [W, D] (columns of x) or None (ones).
+    y None: only n = norm(r) * w_pre.  post_norm False: y itself instead of norm(y).  pre_norm False: no n.
+    Returns (r_out, n, stats); stats: float32 [2, W, T], what block_norm_grad needs.  r_out, n, stats: optional buffers (r_out
+    may be r)."""
+    who = "block_norm"
+    dev = _on_gpu(who, r=r, y=y, gate=gate, w_post=w_post, w_pre=w_pre, r_out=r_out, n=n, stats=stats)
+    _need(r.dim() == 3 and r.dtype in _FLOATS, f"{who}: r must be float32 or bfloat16 [W, T, D]")
+    W, T, D = r.shape
+    _need(y is not None or pre_norm, f"{who}: neither y nor a norm after it: nothing to do")
+    _need(y is not None or (gate is None and r_out is None and w_post is None), f"{who}: gate, w_post and r_out need y")
+    _need(pre_norm or (n is None and w_pre is None), f"{who}: n and w_pre need pre_norm")
+    if y is not None and r_out is None:
+        r_out = _fresh((W, T, D), r.dtype, dev, stream)
+    if pre_norm and n is None:
+        n = _fresh((W, T, D), r.dtype, dev, stream)
+    if stats is None:
+        stats = _fresh((2, W, T), torch.float32, dev, stream)
+    _need(stats.dtype == torch.float32 and tuple(stats.shape) == (2, W, T) and stats.is_contiguous(), f"{who}: stats must be contiguous float32 [2, W, T]")
+    wp, lp = _weights(who, "w_post", w_post, W, D)
+    wn, ln = _weights(who, "w_pre", w_pre, W, D)
+    shape = (W, T, D)
+    a = _BlockNorm(W, T, D, int(r.dtype == torch.bfloat16), int(bool(post_norm)), scale, eps, _rows(who, "r", r, shape, r.dtype),
+                   _rows(who, "y", y, shape, r.dtype), _rows(who, "gate", gate, shape, r.dtype), _rows(who, "r_out", r_out, shape, r.dtype),
+                   _rows(who, "n", n, shape, r.dtype), wp, wn, lp, ln, stats[0].data_ptr() if y is not None else None, stats[1].data_ptr())
+    with torch.cuda.device(dev):
+        _check(lib().lsgd_block_norm(C.byref(a), _launch_on(dev, stream)))
+    return (r if y is None else r_out), n, stats
+
+
+def block_norm_grad(dn, dr_out, r_out, stats, y=None, gate=None, w_post=None, w_pre=None, scale=1.0, post_norm=True, dw_post=None,
+                    dw_pre=None, accumulate=False, dr=None, dy=None, dgate=None, workspace=None, stream=None):
+    """lsgd_block_norm_grad: (dr, dy, dgate) from dn (gradient of n, or None) and dr_out (gradient of r_out past the next
+    block, or None); r_out, stats: what block_norm returned; the rest as given to it.  dw_post, dw_pre: float32 [W, D]
+    (columns of g) that receive the weights' gradients, added to what is there if accumulate; dr, dy, dgate: optional buffers."""
+    who = "block_norm_grad"
+    dev = _on_gpu(who, dn=dn, dr_out=dr_out, r_out=r_out, stats=stats, y=y, gate=gate, w_post=w_post, w_pre=w_pre, dw_post=dw_post,
+                  dw_pre=dw_pre, dr=dr, dy=dy, dgate=dgate)
+    _need(r_out.dim() == 3 and r_out.dtype in _FLOATS, f"{who}: r_out must be float32 or bfloat16 [W, T, D]")
+    W, T, D = shape = tuple(r_out.shape)
+    dt = r_out.dtype
+    _need(dn is not None or dr_out is not None, f"{who}: neither dn nor dr_out is given")
+    _need(y is not None or (gate is None and dw_post is None and dy is None and dgate is None), f"{who}: gate, dw_post, dy and dgate need y")
+    _need(gate is not None or dgate is None, f"{who}: dgate needs gate")
+    _need(stats.dtype == torch.float32 and tuple(stats.shape) == (2, W, T) and stats.is_contiguous(), f"{who}: stats must be contiguous float32 [2, W, T]")
+    if dr is None:
+        dr = _fresh(shape, dt, dev, stream)
+    if y is not None and dy is None:
+        dy = _fresh(shape, dt, dev, stream)
+    if gate is not None and dgate is None:
+        dgate = _fresh(shape, dt, dev, stream)
+    wp, lp = _weights(who, "w_post", w_post, W, D)
+    wn, ln = _weights(who, "w_pre", w_pre, W, D)
+    dwp, ldp = _weights(who, "dw_post", dw_post, W, D)
+    dwn, ldn = _weights(who, "dw_pre", dw_pre, W, D)
+    R = lambda name, t: _rows(who, name, t, shape, dt)
+    a = _BlockNormGrad(W, T, D, int(dt == torch.bfloat16), int(bool(post_norm)), int(bool(accumulate)), scale, R("dn", dn), R("dr_out", dr_out),
+                       R("r_out", r_out), R("y", y), R("gate", gate), R("dr", dr), R("dy", dy), R("dgate", dgate), wp, wn, lp, ln,
+                       stats[0].data_ptr(), stats[1].data_ptr(), dwp, dwn, ldp, ldn)
+    with torch.cuda.device(dev):
+        nbytes = 0
+        if dwp or dwn:
+            workspace, nbytes = _workspace(who, lib().lsgd_block_norm_grad_workspace_bytes(W, T, D), dev, workspace, stream)
+        _check(lib().lsgd_block_norm_grad(C.byref(a), _ptr(workspace), nbytes, _launch_on(dev, stream)))
+    return dr, dy, dgate
+
+
+class AdamWTensor:
+    """One tensor of an AdamW step: float32 x and its gradient g (float32 or bfloat16), both [rows, n] with dense rows (columns of a
+    population's x and g, or any dense tensor, which counts as one row).  Moments m, v of the same shape: float32 for 32 bits;
+    int8 and uint8 for 8 bits with float32 scales m_scale, v_scale [rows, ceil(n / ADAMW_BLOCK)].  x_bf16: optional bfloat16 copy
+    of x that the step keeps current.  m_values, v_values: optional float32 tensors that AdamW.moments() fills."""
+
+    def __init__(self, x, g, m, v, weight_decay=0.0, lr_mult=1.0, x_bf16=None, m_scale=None, v_scale=None, m_values=None, v_values=None):
+        self.t = dict(x=x, g=g, m=m, v=v, m_scale=m_scale, v_scale=v_scale, m_values=m_values, v_values=v_values, x_bf16=x_bf16)
+        self.weight_decay, self.lr_mult = float(weight_decay), float(lr_mult)
+
+    def _c(self, k, bits, g_dtype):
+        who = f"AdamW: tensor {k}"
+        x = self.t["x"]
+        types = {"x": torch.float32, "g": g_dtype, "m": torch.float32 if bits == 32 else torch.int8, "v": torch.float32 if bits == 32 else torch.uint8,
+                 "m_scale": torch.float32, "v_scale": torch.float32, "m_values": torch.float32, "v_values": torch.float32, "x_bf16": torch.bfloat16}
+        for name in ("x", "g", "m", "v"):
+            _need(self.t[name] is not None, f"{who}: {name} is missing")
+        two = x.dim() == 2
+        rows, n = (x.shape if two else (1, x.numel()))
+        got, ld = {}, {}
+        for name, t in self.t.items():
+            if t is None or (bits == 32 and name in ("m_scale", "v_scale", "m_values", "v_values")):
+                got[name], ld[name] = None, 0
+                continue
+            _need(t.dtype == types[name], f"{who}: {name} must be {types[name]}, is {t.dtype}")
+            if name in ("m_scale", "v_scale"):
+                nb = -(-n // ADAMW_BLOCK)
+                t = t if t.dim() == 2 else t.reshape(1, -1)
+                _need(tuple(t.shape) == (rows, nb), f"{who}: {name} must be [{rows}, {nb}]")
+            else:
+                _need(t.shape == x.shape, f"{who}: {name} has shape {list(t.shape)}, x has {list(x.shape)}")
+                if not two:
+                    _need(t.is_contiguous(), f"{who}: {name} must be contiguous")
+                    t = t.view(1, -1)
+            _need(t.numel() == 0 or t.shape[1] == 1 or t.stride(1) == 1, f"{who}: rows of {name} must be dense")
+            got[name], ld[name] = t.data_ptr() or None, (t.stride(0) if t.shape[0] > 1 else t.shape[1])
+        _need(ld["m"] == ld["v"] and ld["m_scale"] == ld["v_scale"] and ld["m_values"] == ld["v_values"],
+              f"{who}: m and v (their scales, their values) must have the same row stride")
+        return _AdamWTensor(got["x"], got["g"], got["m"], got["v"], got["m_scale"], got["v_scale"], got["m_values"], got["v_values"], got["x_bf16"],
+                            rows, n, ld["x"], ld["g"], ld["m"], ld["m_scale"], ld["m_values"], ld["x_bf16"], self.weight_decay, self.lr_mult)
+
+
+class AdamW:
+    """lsgd_adamw_create over a list of AdamWTensor; bits: 32 or 8, how the moments are held.  Keeps the tensors alive."""
+
+    def __init__(self, tensors, bits=32, stream=None, workspace=None):
+        self._h = None
+        self.tensors = list(tensors)
+        _need(self.tensors, "AdamW: no tensors")
+        dev = _on_gpu("AdamW", **{f"{name} of tensor {k}": t for k, a in enumerate(self.tensors) for name, t in a.t.items()})
+        g_dtype = self.tensors[0].t["g"].dtype
+        _need(g_dtype in _FLOATS, "AdamW: g must be float32 or bfloat16")
+        arr = (_AdamWTensor * len(self.tensors))(*[a._c(k, bits, g_dtype) for k, a in enumerate(self.tensors)])
+        self.stream = torch.cuda.current_stream(dev) if stream is None else stream
+        self.device = dev
+        bf = int(g_dtype == torch.bfloat16)
+        with torch.cuda.device(dev):
+            self.workspace, nbytes = _workspace("AdamW", lib().lsgd_adamw_workspace_bytes(arr, len(arr), bits, bf), dev, workspace, stream)
+            h = C.c_void_p()
+            _check(lib().lsgd_adamw_create(arr, len(arr), bits, bf, _ptr(self.workspace), nbytes, C.c_void_p(self.stream.cuda_stream), C.byref(h)))
+        self._h = h
+
+    def close(self):
+        if getattr(self, "_h", None):
+            lib().lsgd_adamw_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def step(self, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=1.0):
+        """One step; `step` counts from 1."""
+        with torch.cuda.device(self.device):
+            _check(lib().lsgd_adamw_step(self._h, lr, beta1, beta2, eps, int(step), grad_scale))
+
+    def moments(self):
+        """8 bits: fills m_values and v_values of the tensors that have them."""
+        with torch.cuda.device(self.device):
+            _check(lib().lsgd_adamw_moments(self._h))

@@ -1,0 +1,535 @@
+// One AdamW step over every tensor of a program at once, moments held in 32 or in 8 bits.
+//
+//   g' = c g;  m <- b1 m + (1-b1) g';  v <- b2 v + (1-b2) g' g'
+//   x <- x (1 - lr wd) - lr/(1-b1^t) * m / (sqrt(v)/sqrt(1-b2^t) + eps)
+//
+// Every product, sum, quotient and root is rounded to fp32 by itself (no fused multiply-add): the stored bits then do
+// not depend on which code path or compiler evaluates the expression, and the 8-bit codes, where one last bit can move
+// a value to the next code, stay reproducible.  The arithmetic hides behind the memory accesses.
+//
+// 8-bit moments.  A block of 256 elements of a tensor's row shares an fp32 scale: m = sign(q) q^2 s_m with |q| <= 127 and
+// sqrt(v) = q^2 s_v with q <= 255, s = (largest in the block) / q_max^2, so the spacing of stored values is 2/q of the
+// value: 1.6 % (0.8 %) near the block's largest, and values down to 1/16129 (1/65025) of it are told from zero.  A moment
+// changes by a fraction 1-b of itself a step, less than the spacing: rounded to nearest it would never move.  So the
+// point between two neighbouring codes above which the upper one is taken walks through (0,1) with the step number by
+// the golden ratio; over any run of steps each code is taken in proportion to how near the value is, and slow drift is
+// kept on average.  Between two codes v (not its root) is interpolated, or the second moment would be biased upwards.
+//
+// Bound by memory: 28 bytes an element (x, m, v read and written, g read) with 32-bit moments, 16 with 8-bit ones.
+#include <cmath>
+#include <cstring>
+#include <new>
+#include <vector>
+
+#include "common.h"
+
+using namespace lsgd;
+
+namespace {
+
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef uint32_t v2u __attribute__((ext_vector_type(2)));
+
+constexpr int kThreads = 256;
+constexpr int kBlock = LSGD_ADAMW_BLOCK;             // elements that share a scale: one wavefront, four each
+static_assert(kBlock == 4 * kWave, "a wavefront holds one block");
+constexpr int kChunk = 4096;                         // elements of one workgroup
+constexpr float kTopM = 127.0f * 127.0f, kTopV = 255.0f * 255.0f;
+
+// A tensor as the kernels see it.
+struct Tensor {
+    float* x;
+    const void* g;
+    void *m, *v;
+    float *m_scale, *v_scale;
+    uint16_t* xb;
+    float *m_values, *v_values;
+    int64_t ld_x, ld_g, ld_s, ld_scale, ld_b, ld_values;
+    int64_t n;
+    double wd, lr_mult;
+    int32_t wide, wide_values;                       // every row of every array starts on a four-element boundary
+};
+
+// What one workgroup does: elements [start, min(start + kChunk, n)) of one row.
+struct Work {
+    int32_t tensor, row;
+    int64_t start;
+};
+
+struct Step {
+    double lr, lr_corrected;                         // lr_corrected = lr / (1 - b1^t)
+    float b1, b2, one_b1, one_b2, inv_c2, eps, gscale;
+    float um, uv;                                    // where between two codes the upper one begins
+};
+
+struct Coef {
+    float decay, rate;
+};
+
+__device__ __forceinline__ Coef coefficients(const Tensor& t, const Step& p)
+{
+#pragma clang fp contract(off)
+    Coef c;
+    c.decay = (float)(1.0 - p.lr * t.lr_mult * t.wd);
+    c.rate = (float)(p.lr_corrected * t.lr_mult);
+    return c;
+}
+
+// One element; m and v are its moments before and after, r the root of the second after.
+__device__ __forceinline__ void update(float& x, float g, float& m, float& v, float& r, const Coef& c, const Step& p)
+{
+#pragma clang fp contract(off)
+    const float gs = g * p.gscale;
+    m = p.b1 * m + p.one_b1 * gs;
+    v = p.b2 * v + p.one_b2 * (gs * gs);
+    r = sqrtf(v);
+    const float den = r * p.inv_c2 + p.eps;
+    x = x * c.decay - (m / den) * c.rate;
+}
+
+template <class G>
+__device__ __forceinline__ float grad1(const void* g, int64_t i)
+{
+    if constexpr (sizeof(G) == 4) return static_cast<const float*>(g)[i];
+    else return bf16_to_f32(static_cast<const uint16_t*>(g)[i]);
+}
+
+template <class G>
+__device__ __forceinline__ v4f grad4(const void* g, int64_t i)
+{
+    if constexpr (sizeof(G) == 4) return *reinterpret_cast<const v4f*>(static_cast<const float*>(g) + i);
+    else {
+        const v2u b = *reinterpret_cast<const v2u*>(static_cast<const uint16_t*>(g) + i);
+        return v4f{__uint_as_float(b.x << 16), __uint_as_float(b.x & 0xFFFF0000u), __uint_as_float(b.y << 16), __uint_as_float(b.y & 0xFFFF0000u)};
+    }
+}
+
+__device__ __forceinline__ v2u shadow4(v4f x) { return v2u{f32x2_to_bf16x2(x.x, x.y), f32x2_to_bf16x2(x.z, x.w)}; }
+
+// ---- 32-bit moments ----
+template <class G>
+__global__ __launch_bounds__(kThreads) void adamw32_kernel(const Tensor* __restrict__ tensors, const Work* __restrict__ works, Step p)
+{
+    const Work w = works[blockIdx.x];
+    const Tensor t = tensors[w.tensor];
+    const Coef c = coefficients(t, p);
+    const int64_t end = w.start + kChunk < t.n ? w.start + kChunk : t.n;
+    float* x = t.x + w.row * t.ld_x;
+    float* m = static_cast<float*>(t.m) + w.row * t.ld_s;
+    float* v = static_cast<float*>(t.v) + w.row * t.ld_s;
+    const void* g = static_cast<const char*>(t.g) + w.row * t.ld_g * (int64_t)sizeof(G);
+    uint16_t* xb = t.xb ? t.xb + w.row * t.ld_b : nullptr;
+    float r;
+    int64_t i = w.start;
+    if (t.wide) {
+        const int64_t end4 = w.start + ((end - w.start) & ~(int64_t)3);
+        for (int64_t k = w.start + 4 * threadIdx.x; k < end4; k += 4 * kThreads) {
+            v4f xv = *reinterpret_cast<const v4f*>(x + k);
+            const v4f gv = grad4<G>(g, k);
+            v4f mv = *reinterpret_cast<const v4f*>(m + k);
+            v4f vv = *reinterpret_cast<const v4f*>(v + k);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float xe = xv[e], me = mv[e], ve = vv[e];
+                update(xe, gv[e], me, ve, r, c, p);
+                xv[e] = xe; mv[e] = me; vv[e] = ve;
+            }
+            *reinterpret_cast<v4f*>(x + k) = xv;
+            *reinterpret_cast<v4f*>(m + k) = mv;
+            *reinterpret_cast<v4f*>(v + k) = vv;
+            if (xb) *reinterpret_cast<v2u*>(xb + k) = shadow4(xv);
+        }
+        i = end4;
+    }
+    for (i += threadIdx.x; i < end; i += kThreads) {
+        float xe = x[i], me = m[i], ve = v[i];
+        update(xe, grad1<G>(g, i), me, ve, r, c, p);
+        x[i] = xe; m[i] = me; v[i] = ve;
+        if (xb) xb[i] = f32_to_bf16_rne(xe);
+    }
+}
+
+// ---- 8-bit moments ----
+__device__ __forceinline__ float wave_max(float a)
+{
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) a = fmaxf(a, __shfl_xor(a, o));
+    return a;
+}
+
+__device__ __forceinline__ bool finite(float a) { return fabsf(a) < __builtin_inff(); }
+
+// Scale of a block whose largest finite value is `big`, and its reciprocal; blocks of next to nothing are held as zero.
+__device__ __forceinline__ float scale_of(float big, float top, float& inv)
+{
+    float s = big * (1.0f / top);
+    if (!(s > 0x1p-100f)) s = 0.0f;
+    inv = s > 0.0f ? 1.0f / s : 0.0f;
+    return s;
+}
+
+// The largest whole c with c*c <= y (0 <= y <= 65025): an approximate root is at most one off.
+__device__ __forceinline__ float floor_root(float y)
+{
+#pragma clang fp contract(off)
+    float c = floorf(__builtin_amdgcn_sqrtf(y));
+    if (c * c > y) c -= 1.0f;
+    if ((c + 1.0f) * (c + 1.0f) <= y) c += 1.0f;
+    return c;
+}
+
+// A value that is not finite is held as the block's largest one (the parameter it belongs to is not finite either).
+__device__ __forceinline__ float code_m(float m, float s, float inv, float u)
+{
+#pragma clang fp contract(off)
+    const float a = fabsf(m);
+    const float y = finite(a) ? fminf(a * inv, kTopM) : (s > 0.0f ? kTopM : 0.0f);
+    float c = floor_root(y);
+    if (y - c * c > u * (2.0f * c + 1.0f)) c += 1.0f;
+    return m < 0.0f ? -c : c;
+}
+
+__device__ __forceinline__ float code_v(float r, float s, float inv, float u)
+{
+#pragma clang fp contract(off)
+    const float y = finite(r) ? fminf(r * inv, kTopV) : (s > 0.0f ? kTopV : 0.0f);
+    float c = floor_root(y);
+    const float c2 = c * c, d2 = (c + 1.0f) * (c + 1.0f);
+    if ((y - c2) * (y + c2) > u * ((d2 - c2) * (d2 + c2))) c += 1.0f;
+    return r > 0.0f && s > 0.0f ? fmaxf(c, 1.0f) : c;        // a second moment that is not zero is not held as zero
+}
+
+__device__ __forceinline__ float value_m(int q, float s)
+{
+    const float c = (float)q;
+    return c * fabsf(c) * s;
+}
+__device__ __forceinline__ float value_r(int q, float s)
+{
+    const float c = (float)q;
+    return c * c * s;
+}
+
+// A wavefront takes whole blocks: its lanes hold four elements each, adjacent ones where the arrays allow wide accesses.
+template <class G>
+__global__ __launch_bounds__(kThreads) void adamw8_kernel(const Tensor* __restrict__ tensors, const Work* __restrict__ works, Step p)
+{
+    const Work w = works[blockIdx.x];
+    const Tensor t = tensors[w.tensor];
+    const Coef c = coefficients(t, p);
+    const int64_t end = w.start + kChunk < t.n ? w.start + kChunk : t.n;
+    float* x = t.x + w.row * t.ld_x;
+    int8_t* m = static_cast<int8_t*>(t.m) + w.row * t.ld_s;
+    uint8_t* v = static_cast<uint8_t*>(t.v) + w.row * t.ld_s;
+    float* ms = t.m_scale + w.row * t.ld_scale;
+    float* vs = t.v_scale + w.row * t.ld_scale;
+    const void* g = static_cast<const char*>(t.g) + w.row * t.ld_g * (int64_t)sizeof(G);
+    uint16_t* xb = t.xb ? t.xb + w.row * t.ld_b : nullptr;
+    const int lane = threadIdx.x & (kWave - 1);
+    for (int64_t b = w.start / kBlock + threadIdx.x / kWave; b * kBlock < end; b += kThreads / kWave) {
+        const int64_t first = b * kBlock;
+        const float sm = ms[b], sv = vs[b];
+        float xe[4], me[4], re[4];
+        const bool wide = t.wide && first + kBlock <= end;
+        const int64_t k = first + 4 * lane;
+        if (wide) {
+            const v4f xv = *reinterpret_cast<const v4f*>(x + k);
+            const v4f gv = grad4<G>(g, k);
+            const uint32_t mq = *reinterpret_cast<const uint32_t*>(m + k), vq = *reinterpret_cast<const uint32_t*>(v + k);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                xe[e] = xv[e];
+                me[e] = value_m((int)(int8_t)(mq >> (8 * e)), sm);
+                const float rr = value_r((int)(vq >> (8 * e) & 255u), sv);
+                float ve = rr * rr;
+                update(xe[e], gv[e], me[e], ve, re[e], c, p);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int64_t i = first + lane + e * kWave;
+                xe[e] = me[e] = re[e] = 0.0f;
+                if (i < end) {
+                    xe[e] = x[i];
+                    me[e] = value_m(m[i], sm);
+                    const float rr = value_r(v[i], sv);
+                    float ve = rr * rr;
+                    update(xe[e], grad1<G>(g, i), me[e], ve, re[e], c, p);
+                }
+            }
+        }
+        float bm = 0.0f, bv = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (finite(me[e])) bm = fmaxf(bm, fabsf(me[e]));
+            if (finite(re[e])) bv = fmaxf(bv, re[e]);
+        }
+        float im, iv;
+        const float nm = scale_of(wave_max(bm), kTopM, im), nv = scale_of(wave_max(bv), kTopV, iv);
+        int qm[4], qv[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            qm[e] = (int)code_m(me[e], nm, im, p.um);
+            qv[e] = (int)code_v(re[e], nv, iv, p.uv);
+        }
+        if (wide) {
+            uint32_t mq = 0, vq = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                mq |= (uint32_t)(qm[e] & 255) << (8 * e);
+                vq |= (uint32_t)qv[e] << (8 * e);
+            }
+            const v4f xv = {xe[0], xe[1], xe[2], xe[3]};
+            *reinterpret_cast<v4f*>(x + k) = xv;
+            *reinterpret_cast<uint32_t*>(m + k) = mq;
+            *reinterpret_cast<uint32_t*>(v + k) = vq;
+            if (xb) *reinterpret_cast<v2u*>(xb + k) = shadow4(xv);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int64_t i = first + lane + e * kWave;
+                if (i < end) {
+                    x[i] = xe[e];
+                    m[i] = (int8_t)qm[e];
+                    v[i] = (uint8_t)qv[e];
+                    if (xb) xb[i] = f32_to_bf16_rne(xe[e]);
+                }
+            }
+        }
+        if (lane == 0) {
+            ms[b] = nm;
+            vs[b] = nv;
+        }
+    }
+}
+
+// The values that the codes stand for.
+__global__ __launch_bounds__(kThreads) void adamw8_values_kernel(const Tensor* __restrict__ tensors, const Work* __restrict__ works)
+{
+#pragma clang fp contract(off)
+    const Work w = works[blockIdx.x];
+    const Tensor t = tensors[w.tensor];
+    if (!t.m_values) return;
+    const int64_t end = w.start + kChunk < t.n ? w.start + kChunk : t.n;
+    const int8_t* m = static_cast<const int8_t*>(t.m) + w.row * t.ld_s;
+    const uint8_t* v = static_cast<const uint8_t*>(t.v) + w.row * t.ld_s;
+    const float* ms = t.m_scale + w.row * t.ld_scale;
+    const float* vs = t.v_scale + w.row * t.ld_scale;
+    float* om = t.m_values + w.row * t.ld_values;
+    float* ov = t.v_values + w.row * t.ld_values;
+    int64_t i = w.start;
+    if (t.wide_values) {
+        const int64_t end4 = w.start + ((end - w.start) & ~(int64_t)3);
+        for (int64_t k = w.start + 4 * threadIdx.x; k < end4; k += 4 * kThreads) {
+            const uint32_t mq = *reinterpret_cast<const uint32_t*>(m + k), vq = *reinterpret_cast<const uint32_t*>(v + k);
+            const float sm = ms[k / kBlock], sv = vs[k / kBlock];
+            v4f a, b;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                a[e] = value_m((int)(int8_t)(mq >> (8 * e)), sm);
+                const float r = value_r((int)(vq >> (8 * e) & 255u), sv);
+                b[e] = r * r;
+            }
+            *reinterpret_cast<v4f*>(om + k) = a;
+            *reinterpret_cast<v4f*>(ov + k) = b;
+        }
+        i = end4;
+    }
+    for (i += threadIdx.x; i < end; i += kThreads) {
+        om[i] = value_m(m[i], ms[i / kBlock]);
+        const float r = value_r(v[i], vs[i / kBlock]);
+        ov[i] = r * r;
+    }
+}
+
+constexpr size_t kAlign = 256;
+size_t align_up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
+
+bool on(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+// Checks the list and counts workgroups.
+lsgd_status check_tensors(const lsgd_adamw_tensor* t, int32_t count, int32_t bits, int32_t g_is_bf16, int64_t* works)
+{
+    if (count < 0) return set_error(LSGD_ERR_SHAPE, "adamw: n_tensors=%d is negative", (int)count);
+    if (count > 0 && !t) return set_error(LSGD_ERR_INVALID_ARG, "adamw: tensors is NULL");
+    if (bits != 32 && bits != 8) return set_error(LSGD_ERR_INVALID_ARG, "adamw: state_bits=%d is neither 32 nor 8", (int)bits);
+    if (g_is_bf16 != 0 && g_is_bf16 != 1) return set_error(LSGD_ERR_INVALID_ARG, "adamw: g_is_bf16 must be 0 or 1");
+    int64_t total = 0;
+    for (int k = 0; k < count; ++k) {
+        const lsgd_adamw_tensor& a = t[k];
+        if (a.rows < 0 || a.n < 0) return set_error(LSGD_ERR_SHAPE, "adamw: tensor %d: negative rows or n", k);
+        if (!std::isfinite(a.weight_decay) || !std::isfinite(a.lr_mult))
+            return set_error(LSGD_ERR_INVALID_ARG, "adamw: tensor %d: weight_decay and lr_mult must be finite", k);
+        if (a.rows == 0 || a.n == 0) continue;
+        if (a.rows > 0x7fffffff) return set_error(LSGD_ERR_SHAPE, "adamw: tensor %d: rows=%lld", k, (long long)a.rows);
+        if (!a.x || !a.g || !a.m || !a.v) return set_error(LSGD_ERR_INVALID_ARG, "adamw: tensor %d: x, g, m and v are required", k);
+        if (!on(a.x, 4) || !on(a.g, g_is_bf16 ? 2 : 4) || !on(a.x_bf16, 2) || (bits == 32 && (!on(a.m, 4) || !on(a.v, 4))) ||
+            !on(a.m_scale, 4) || !on(a.v_scale, 4) || !on(a.m_values, 4) || !on(a.v_values, 4))
+            return set_error(LSGD_ERR_INVALID_ARG, "adamw: tensor %d: a pointer is not aligned to its element", k);
+        if (a.rows > 1 && (a.ld_x < a.n || a.ld_g < a.n || a.ld_state < a.n || (a.x_bf16 && a.ld_bf16 < a.n)))
+            return set_error(LSGD_ERR_SHAPE, "adamw: tensor %d: a row stride is smaller than n=%lld", k, (long long)a.n);
+        if (bits == 8) {
+            if (!a.m_scale || !a.v_scale) return set_error(LSGD_ERR_INVALID_ARG, "adamw: tensor %d: 8-bit moments need m_scale and v_scale", k);
+            if (a.rows > 1 && a.ld_scale < (a.n + kBlock - 1) / kBlock)
+                return set_error(LSGD_ERR_SHAPE, "adamw: tensor %d: ld_scale is smaller than the %lld blocks of a row", k, (long long)((a.n + kBlock - 1) / kBlock));
+            if (!a.m_values != !a.v_values) return set_error(LSGD_ERR_INVALID_ARG, "adamw: tensor %d: give both m_values and v_values or neither", k);
+            if (a.m_values && a.rows > 1 && a.ld_values < a.n) return set_error(LSGD_ERR_SHAPE, "adamw: tensor %d: ld_values is smaller than n", k);
+        }
+        const int64_t per = (a.n - 1) / kChunk + 1;
+        if (per > (int64_t)0x7fffffff / a.rows) return set_error(LSGD_ERR_SHAPE, "adamw: tensor %d is too large for one launch", k);
+        total += per * a.rows;
+        if (total > 0x7fffffff) return set_error(LSGD_ERR_SHAPE, "adamw: the tensors are too large for one launch");
+    }
+    *works = total;
+    return LSGD_OK;
+}
+
+size_t table_bytes(int32_t count, int64_t works)
+{
+    return align_up(sizeof(Tensor) * (size_t)count) + align_up(sizeof(Work) * (size_t)works);
+}
+
+} // namespace
+
+struct lsgd_adamw {
+    const Tensor* tensors;
+    const Work* works;
+    int64_t n_works;
+    int32_t bits, g_is_bf16;
+    bool values;             // some tensor has room for its moments' values
+    hipStream_t stream;
+};
+
+extern "C" {
+
+size_t lsgd_adamw_workspace_bytes(const lsgd_adamw_tensor* tensors, int32_t n_tensors, int32_t state_bits, int32_t g_is_bf16)
+{
+    int64_t works = 0;
+    if (check_tensors(tensors, n_tensors, state_bits, g_is_bf16, &works) != LSGD_OK) return 0;
+    const size_t b = table_bytes(n_tensors, works);
+    return b ? b : kAlign;
+}
+
+lsgd_status lsgd_adamw_create(const lsgd_adamw_tensor* tensors, int32_t n_tensors, int32_t state_bits, int32_t g_is_bf16, void* workspace,
+                              size_t workspace_bytes, void* hip_stream, lsgd_adamw** out)
+{
+    if (!out) return set_error(LSGD_ERR_INVALID_ARG, "adamw: out is NULL");
+    *out = nullptr;
+    int64_t n_works = 0;
+    lsgd_status st = check_tensors(tensors, n_tensors, state_bits, g_is_bf16, &n_works);
+    if (st != LSGD_OK) return st;
+    if (!workspace) return set_error(LSGD_ERR_INVALID_ARG, "adamw: workspace is NULL");
+    if (!on(workspace, kAlign)) return set_error(LSGD_ERR_INVALID_ARG, "adamw: workspace must be 256-byte aligned");
+    if (workspace_bytes < table_bytes(n_tensors, n_works))
+        return set_error(LSGD_ERR_NOMEM, "adamw: workspace of %zu bytes < %zu needed", workspace_bytes, table_bytes(n_tensors, n_works));
+    hipError_t e = hipSuccess;
+    lsgd_adamw* h = nullptr;
+    try {
+        std::vector<Tensor> ts((size_t)n_tensors);
+        std::vector<Work> ws;
+        ws.reserve((size_t)n_works);
+        bool values = false;
+        for (int k = 0; k < n_tensors; ++k) {
+            const lsgd_adamw_tensor& a = tensors[k];
+            Tensor& t = ts[(size_t)k];
+            std::memset(&t, 0, sizeof(t));
+            if (a.rows == 0 || a.n == 0) continue;
+            t.x = a.x; t.g = a.g; t.m = a.m; t.v = a.v;
+            t.xb = a.x_bf16;
+            // one row: its stride is never multiplied by anything, so it does not matter to the alignment either
+            auto ld = [&](int64_t v) { return a.rows > 1 ? v : (int64_t)0; };
+            t.ld_x = ld(a.ld_x); t.ld_g = ld(a.ld_g); t.ld_s = ld(a.ld_state); t.ld_b = a.x_bf16 ? ld(a.ld_bf16) : 0;
+            const uintptr_t es = state_bits == 32 ? 16 : 4;
+            t.wide = on(t.x, 16) && on(t.g, g_is_bf16 ? 8 : 16) && on(t.m, es) && on(t.v, es) && on(t.xb, 8) &&
+                     (t.ld_x | t.ld_g | t.ld_s | t.ld_b) % 4 == 0;
+            if (state_bits == 8) {
+                t.m_scale = a.m_scale; t.v_scale = a.v_scale; t.ld_scale = ld(a.ld_scale);
+                t.m_values = a.m_values; t.v_values = a.v_values; t.ld_values = ld(a.ld_values);
+                t.wide_values = on(t.m, 4) && on(t.v, 4) && on(t.m_values, 16) && on(t.v_values, 16) && (t.ld_s | t.ld_values) % 4 == 0;
+                values |= a.m_values != nullptr;
+            }
+            t.n = a.n;
+            t.wd = a.weight_decay;
+            t.lr_mult = a.lr_mult;
+            for (int64_t row = 0; row < a.rows; ++row)
+                for (int64_t s = 0; s < a.n; s += kChunk) ws.push_back(Work{k, (int32_t)row, s});
+        }
+        h = new (std::nothrow) lsgd_adamw();
+        if (!h) return set_error(LSGD_ERR_NOMEM, "adamw: host allocation failed");
+        char* base = static_cast<char*>(workspace);
+        h->tensors = reinterpret_cast<const Tensor*>(base);
+        h->works = reinterpret_cast<const Work*>(base + align_up(sizeof(Tensor) * (size_t)n_tensors));
+        h->n_works = n_works;
+        h->bits = state_bits;
+        h->g_is_bf16 = g_is_bf16;
+        h->values = values;
+        h->stream = static_cast<hipStream_t>(hip_stream);
+        if (!ws.empty()) {
+            e = hipMemcpyAsync(base, ts.data(), sizeof(Tensor) * ts.size(), hipMemcpyHostToDevice, h->stream);
+            if (e == hipSuccess)
+                e = hipMemcpyAsync(const_cast<Work*>(h->works), ws.data(), sizeof(Work) * ws.size(), hipMemcpyHostToDevice, h->stream);
+            const hipError_t waited = hipStreamSynchronize(h->stream);      // the host vectors were the copy's source
+            if (e == hipSuccess) e = waited;
+        }
+    } catch (const std::bad_alloc&) {
+        delete h;
+        return set_error(LSGD_ERR_NOMEM, "adamw: host allocation failed");
+    }
+    if (e != hipSuccess) {
+        delete h;
+        return set_error(LSGD_ERR_HIP, "adamw: create: %s", hipGetErrorString(e));
+    }
+    *out = h;
+    return LSGD_OK;
+}
+
+lsgd_status lsgd_adamw_destroy(lsgd_adamw* opt)
+{
+    delete opt;
+    return LSGD_OK;
+}
+
+lsgd_status lsgd_adamw_step(lsgd_adamw* opt, double lr, double beta1, double beta2, double eps, int64_t step, double grad_scale)
+{
+    if (!opt) return set_error(LSGD_ERR_INVALID_ARG, "adamw: handle is NULL");
+    if (!std::isfinite(lr) || !std::isfinite(grad_scale)) return set_error(LSGD_ERR_INVALID_ARG, "adamw: lr and grad_scale must be finite");
+    if (!(beta1 >= 0.0 && beta1 < 1.0 && beta2 >= 0.0 && beta2 < 1.0)) return set_error(LSGD_ERR_INVALID_ARG, "adamw: beta1 and beta2 must lie in [0, 1)");
+    if (!std::isfinite(eps) || eps < 0.0) return set_error(LSGD_ERR_INVALID_ARG, "adamw: eps must be finite and >= 0");
+    if (step < 1) return set_error(LSGD_ERR_INVALID_ARG, "adamw: step=%lld counts from 1", (long long)step);
+    if (opt->n_works == 0) return LSGD_OK;
+    Step p;
+    p.lr = lr;
+    p.lr_corrected = lr / (1.0 - std::pow(beta1, (double)step));
+    p.b1 = (float)beta1; p.b2 = (float)beta2;
+    p.one_b1 = (float)(1.0 - beta1); p.one_b2 = (float)(1.0 - beta2);
+    p.inv_c2 = (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, (double)step)));
+    p.eps = (float)eps;
+    p.gscale = (float)grad_scale;
+    constexpr double kGolden = 0.6180339887498949;
+    p.uv = (float)std::fmod((double)step * kGolden, 1.0);
+    p.um = (float)std::fmod((double)step * kGolden + 0.5, 1.0);
+    const dim3 grid((unsigned)opt->n_works), block(kThreads);
+    if (opt->bits == 32) {
+        if (opt->g_is_bf16) hipLaunchKernelGGL((adamw32_kernel<uint16_t>), grid, block, 0, opt->stream, opt->tensors, opt->works, p);
+        else hipLaunchKernelGGL((adamw32_kernel<float>), grid, block, 0, opt->stream, opt->tensors, opt->works, p);
+    } else {
+        if (opt->g_is_bf16) hipLaunchKernelGGL((adamw8_kernel<uint16_t>), grid, block, 0, opt->stream, opt->tensors, opt->works, p);
+        else hipLaunchKernelGGL((adamw8_kernel<float>), grid, block, 0, opt->stream, opt->tensors, opt->works, p);
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return set_error(LSGD_ERR_HIP, "adamw: %s", hipGetErrorString(e));
+    return LSGD_OK;
+}
+
+lsgd_status lsgd_adamw_moments(lsgd_adamw* opt)
+{
+    if (!opt) return set_error(LSGD_ERR_INVALID_ARG, "adamw: handle is NULL");
+    if (opt->bits != 8) return set_error(LSGD_ERR_STATE, "adamw: 32-bit moments are their own values");
+    if (!opt->values) return set_error(LSGD_ERR_STATE, "adamw: no tensor was given m_values and v_values");
+    hipLaunchKernelGGL(adamw8_values_kernel, dim3((unsigned)opt->n_works), dim3(kThreads), 0, opt->stream, opt->tensors, opt->works);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return set_error(LSGD_ERR_HIP, "adamw: moments: %s", hipGetErrorString(e));
+    return LSGD_OK;
+}
+
+} // extern "C"

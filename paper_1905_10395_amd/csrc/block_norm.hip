@@ -1,0 +1,624 @@
+// The norms around a block of a model, fused with the block's gate and its scaled residual sum, and their gradients.
+//
+//   after the block      r' = r + s a o (q_y y o w)       q_y = (mean y^2 + eps)^-1/2, a = sigmoid(u)
+//   before the next one  n  = q_r r' o v                  q_r = (mean r'^2 + eps)^-1/2
+//
+// One pass: a team of lanes holds a token's whole row in registers between the sums and the stores, so r, y and u are
+// read once and r' and n written once; between the two norms r' stays fp32 (it is rounded only where it is stored).
+//
+//   backward, from dn and the gradient dR of r' that comes past the next block; h = q_r r', z = q_y y
+//   dr = dR + q_r (v o dn - h mean(v o dn o h))           dv = sum_t dn o h
+//   e  = s dr o a;  dy = q_y (e o w - z mean(e o w o z))  dw = sum_t e o z     du = s dr o z o w a (1-a)
+//
+// Bound by memory.  Workers' weights are columns of fp32 rows; a team keeps them in registers over the tokens it takes,
+// as it does its part of the sums over tokens, which go to the workspace once a workgroup and are added up in order by a
+// second launch: no atomics, equal calls give equal bits.
+#include <algorithm>
+#include <cmath>
+
+#include "common.h"
+
+using namespace lsgd;
+
+namespace {
+
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+
+constexpr int E = 8;              // elements of a piece: 16 bytes of bf16, twice that of fp32
+
+// [W, T, D] with dense rows
+struct Rows {
+    void* p;
+    int64_t lw, lt;
+};
+
+struct NormArgs {
+    Rows r, y, u, r_out, n;                  // y, u, r_out, n may be absent
+    const float *w_post, *w_pre;             // NULL: ones
+    int64_t ld_w_post, ld_w_pre;
+    float *q_post, *q_pre;                   // [W, T]; may be NULL
+    int T, D, per;                           // tokens of a workgroup
+    float scale, eps, inv_d;
+    int post;                                // the block's output is normed
+};
+
+struct NormGradArgs {
+    Rows dn, dr_out, r, y, u, dr, dy, du;    // dn, dr_out, y, u, dy, du may be absent
+    const float *w_post, *w_pre;
+    int64_t ld_w_post, ld_w_pre;
+    const float *q_post, *q_pre;
+    float* parts;                            // [W][chunks][2][Dp]: dw_post, dw_pre of a workgroup's tokens; NULL: not wanted
+    int T, D, Dp, per, chunks;
+    float scale, inv_d;
+    int post;
+};
+
+__device__ __forceinline__ void load8(const float* p, float (&v)[E])
+{
+    const v4f a = *reinterpret_cast<const v4f*>(p), b = *reinterpret_cast<const v4f*>(p + 4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { v[e] = a[e]; v[e + 4] = b[e]; }
+}
+__device__ __forceinline__ void load8(const uint16_t* p, float (&v)[E])
+{
+    const v4u a = *reinterpret_cast<const v4u*>(p);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        v[2 * e] = __uint_as_float(a[e] << 16);
+        v[2 * e + 1] = __uint_as_float(a[e] & 0xFFFF0000u);
+    }
+}
+__device__ __forceinline__ void store8(float* p, const float (&v)[E])
+{
+    *reinterpret_cast<v4f*>(p) = v4f{v[0], v[1], v[2], v[3]};
+    *reinterpret_cast<v4f*>(p + 4) = v4f{v[4], v[5], v[6], v[7]};
+}
+__device__ __forceinline__ void store8(uint16_t* p, const float (&v)[E])
+{
+    *reinterpret_cast<v4u*>(p) = v4u{f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]), f32x2_to_bf16x2(v[4], v[5]), f32x2_to_bf16x2(v[6], v[7])};
+}
+__device__ __forceinline__ float get1(const float* p) { return *p; }
+__device__ __forceinline__ float get1(const uint16_t* p) { return bf16_to_f32(*p); }
+__device__ __forceinline__ void put1(float* p, float v) { *p = v; }
+__device__ __forceinline__ void put1(uint16_t* p, float v) { *p = f32_to_bf16_rne(v); }
+
+// A lane's N pieces of a row: adjacent elements where rows are aligned for 16-byte accesses (WIDE), else one element
+// every TS columns.  Elements past the row's end read `fill` and are not written.
+template <int TS, int N, bool WIDE>
+struct Piece {
+    static __device__ __forceinline__ int col(int lane, int n, int e) { return WIDE ? (n * TS + lane) * E + e : (n * E + e) * TS + lane; }
+
+    template <class T>
+    static __device__ __forceinline__ void load(const T* p, int lane, int D, float fill, float (&v)[N][E])
+    {
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[n][e] = fill;
+            if constexpr (WIDE) {
+                if (col(lane, n, 0) < D) load8(p + col(lane, n, 0), v[n]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (col(lane, n, e) < D) v[n][e] = get1(p + col(lane, n, e));
+            }
+        }
+    }
+    template <class T>
+    static __device__ __forceinline__ void store(T* p, int lane, int D, const float (&v)[N][E])
+    {
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            if constexpr (WIDE) {
+                if (col(lane, n, 0) < D) store8(p + col(lane, n, 0), v[n]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (col(lane, n, e) < D) put1(p + col(lane, n, e), v[n][e]);
+            }
+        }
+    }
+    // per-column weights of a worker; absent: ones.  Past the row's end zero, so that nothing there enters a sum.
+    static __device__ __forceinline__ void weights(const float* p, int lane, int D, bool wide, float (&v)[N][E])
+    {
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[n][e] = 0.0f;
+        if (WIDE && wide && p) {
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+                if (col(lane, n, 0) < D) load8(p + col(lane, n, 0), v[n]);
+        } else {
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (col(lane, n, e) < D) v[n][e] = p ? p[col(lane, n, e)] : 1.0f;
+        }
+    }
+};
+
+template <int TS>
+struct Team {
+    static constexpr int kThreads = TS < 256 ? 256 : TS;
+    static constexpr int kTeams = kThreads / TS;
+    static constexpr int kWaves = TS / kWave;
+};
+
+__device__ __forceinline__ float wave_sum(float a)
+{
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) a += __shfl_xor(a, o);
+    return a;
+}
+
+// Sum over a team, the same value in all its lanes.  Teams of several wavefronts meet in LDS; two buffers in turn, so that
+// one barrier a sum is enough (a buffer is written again only after the barrier that follows its last read).
+template <int TS>
+__device__ __forceinline__ float team_sum(float a, float (*buf)[16], int& turn)
+{
+    a = wave_sum(a);
+    if constexpr (TS > kWave) {
+        if ((threadIdx.x & (kWave - 1)) == 0) buf[turn][threadIdx.x / kWave] = a;
+        __syncthreads();
+        a = 0.0f;
+#pragma unroll
+        for (int w = 0; w < TS / kWave; ++w) a += buf[turn][w];
+        turn ^= 1;
+    }
+    return a;
+}
+
+__device__ __forceinline__ float sigmoid(float u) { return __builtin_amdgcn_rcpf(1.0f + __expf(-u)); }
+
+template <class T>
+__device__ __forceinline__ T* row_of(const Rows& a, int w, int64_t t) { return static_cast<T*>(a.p) + w * a.lw + t * a.lt; }
+
+template <class T, int TS, int N, bool WIDE>
+__global__ __launch_bounds__(Team<TS>::kThreads) void block_norm_kernel(NormArgs a, int wide_w)
+{
+    using P = Piece<TS, N, WIDE>;
+    __shared__ float buf[2][16];
+    int turn = 0;
+    const int lane = threadIdx.x % TS, team = threadIdx.x / TS, w = blockIdx.y;
+    const int64_t t0 = (int64_t)blockIdx.x * a.per, t1 = t0 + a.per < a.T ? t0 + a.per : a.T;
+    float wp[N][E], wn[N][E];
+    if (a.y.p) P::weights(a.w_post ? a.w_post + w * a.ld_w_post : nullptr, lane, a.D, wide_w & 1, wp);
+    if (a.n.p) P::weights(a.w_pre ? a.w_pre + w * a.ld_w_pre : nullptr, lane, a.D, wide_w & 2, wn);
+    for (int64_t t = t0 + team; t < t1; t += Team<TS>::kTeams) {
+        float r[N][E];
+        P::load(row_of<T>(a.r, w, t), lane, a.D, 0.0f, r);
+        if (a.y.p) {
+            float y[N][E], u[N][E];
+            P::load(row_of<T>(a.y, w, t), lane, a.D, 0.0f, y);
+            if (a.u.p) P::load(row_of<T>(a.u, w, t), lane, a.D, 0.0f, u);
+            float q = 1.0f;
+            if (a.post) {
+                float s = 0.0f;
+#pragma unroll
+                for (int n = 0; n < N; ++n)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) s += y[n][e] * y[n][e];
+                q = 1.0f / sqrtf(team_sum<TS>(s, buf, turn) * a.inv_d + a.eps);
+                if (a.q_post && lane == 0) a.q_post[(int64_t)w * a.T + t] = q;
+            }
+            const float sq = a.scale * q;
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    float b = y[n][e] * sq * wp[n][e];
+                    if (a.u.p) b *= sigmoid(u[n][e]);
+                    r[n][e] += b;
+                }
+            P::store(row_of<T>(a.r_out, w, t), lane, a.D, r);
+        }
+        if (a.n.p) {
+            float s = 0.0f;
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int e = 0; e < E; ++e) s += r[n][e] * r[n][e];
+            const float q = 1.0f / sqrtf(team_sum<TS>(s, buf, turn) * a.inv_d + a.eps);
+            if (a.q_pre && lane == 0) a.q_pre[(int64_t)w * a.T + t] = q;
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int e = 0; e < E; ++e) r[n][e] *= q * wn[n][e];
+            P::store(row_of<T>(a.n, w, t), lane, a.D, r);
+        }
+    }
+}
+
+template <class T, int TS, int N, bool WIDE>
+__global__ __launch_bounds__(Team<TS>::kThreads) void block_norm_grad_kernel(NormGradArgs a, int wide_w)
+{
+    using P = Piece<TS, N, WIDE>;
+    __shared__ float buf[2][16];
+    int turn = 0;
+    const int lane = threadIdx.x % TS, team = threadIdx.x / TS, w = blockIdx.y;
+    const int64_t t0 = (int64_t)blockIdx.x * a.per, t1 = t0 + a.per < a.T ? t0 + a.per : a.T;
+    float wp[N][E], wn[N][E], dwp[N][E], dwn[N][E];
+    if (a.y.p) P::weights(a.w_post ? a.w_post + w * a.ld_w_post : nullptr, lane, a.D, wide_w & 1, wp);
+    if (a.dn.p) P::weights(a.w_pre ? a.w_pre + w * a.ld_w_pre : nullptr, lane, a.D, wide_w & 2, wn);
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int e = 0; e < E; ++e) dwp[n][e] = dwn[n][e] = 0.0f;
+    for (int64_t t = t0 + team; t < t1; t += Team<TS>::kTeams) {
+        float dr[N][E];
+        if (a.dr_out.p) P::load(row_of<T>(a.dr_out, w, t), lane, a.D, 0.0f, dr);
+        else {
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int e = 0; e < E; ++e) dr[n][e] = 0.0f;
+        }
+        if (a.dn.p) {
+            float dn[N][E], h[N][E];
+            P::load(row_of<T>(a.dn, w, t), lane, a.D, 0.0f, dn);
+            P::load(row_of<T>(a.r, w, t), lane, a.D, 0.0f, h);
+            const float q = a.q_pre[(int64_t)w * a.T + t];
+            float s = 0.0f;
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    h[n][e] *= q;
+                    dwn[n][e] += dn[n][e] * h[n][e];
+                    dn[n][e] *= wn[n][e];
+                    s += dn[n][e] * h[n][e];
+                }
+            s = team_sum<TS>(s, buf, turn) * a.inv_d;
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int e = 0; e < E; ++e) dr[n][e] += q * (dn[n][e] - h[n][e] * s);
+        }
+        P::store(row_of<T>(a.dr, w, t), lane, a.D, dr);
+        if (a.y.p) {
+            float z[N][E], u[N][E];
+            P::load(row_of<T>(a.y, w, t), lane, a.D, 0.0f, z);
+            if (a.u.p) P::load(row_of<T>(a.u, w, t), lane, a.D, 0.0f, u);
+            const float q = a.post ? a.q_post[(int64_t)w * a.T + t] : 1.0f;
+            float s = 0.0f;
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    z[n][e] *= q;
+                    float d = a.scale * dr[n][e];                       // e of the formula, gate still missing
+                    if (a.u.p) {
+                        const float g = sigmoid(u[n][e]);
+                        u[n][e] = d * z[n][e] * wp[n][e] * (g * (1.0f - g));
+                        d *= g;
+                    }
+                    dwp[n][e] += d * z[n][e];
+                    dr[n][e] = d * wp[n][e];
+                    s += dr[n][e] * z[n][e];
+                }
+            if (a.u.p) P::store(row_of<T>(a.du, w, t), lane, a.D, u);
+            if (a.post) {
+                s = team_sum<TS>(s, buf, turn) * a.inv_d;
+#pragma unroll
+                for (int n = 0; n < N; ++n)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) dr[n][e] = q * (dr[n][e] - z[n][e] * s);
+            }
+            P::store(row_of<T>(a.dy, w, t), lane, a.D, dr);
+        }
+    }
+    if (!a.parts) return;
+    float* part = a.parts + ((int64_t)w * a.chunks + blockIdx.x) * 2 * a.Dp;
+    if constexpr (Team<TS>::kTeams == 1) {
+        P::store(part, lane, a.D, dwp);
+        P::store(part + a.Dp, lane, a.D, dwn);
+    } else {
+        // the workgroup's teams add up theirs in order
+        __shared__ float sum[Team<TS>::kTeams][TS * N * E];
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int e = 0; e < E; ++e) sum[team][(n * E + e) * TS + lane] = which ? dwn[n][e] : dwp[n][e];
+            __syncthreads();
+            for (int i = threadIdx.x; i < TS * N * E; i += Team<TS>::kThreads) {
+                float s = 0.0f;
+#pragma unroll
+                for (int k = 0; k < Team<TS>::kTeams; ++k) s += sum[k][i];
+                const int c = P::col(i % TS, i / TS / E, i / TS % E);
+                if (c < a.D) part[which * a.Dp + c] = s;
+            }
+            __syncthreads();
+        }
+    }
+}
+
+// dw[w, :] (+)= the sum over a worker's parts, each wavefront a stretch of them.
+constexpr int kJoinThreads = 1024;
+__global__ __launch_bounds__(kJoinThreads) void norm_join_kernel(const float* __restrict__ parts, int chunks, int D, int Dp, float* dw_post,
+                                                                 int64_t ld_post, float* dw_pre, int64_t ld_pre, int accumulate)
+{
+    constexpr int waves = kJoinThreads / kWave;
+    __shared__ float sum[waves][kWave];
+    float* dw = blockIdx.z ? dw_pre : dw_post;
+    if (!dw) return;
+    dw += (int64_t)blockIdx.y * (blockIdx.z ? ld_pre : ld_post);
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, c = blockIdx.x * kWave + lane;
+    const float* p = parts + ((int64_t)blockIdx.y * chunks * 2 + blockIdx.z) * Dp + c;
+    const int per = (chunks + waves - 1) / waves, p0 = wave * per, p1 = p0 + per < chunks ? p0 + per : chunks;
+    float acc = 0.0f;
+    if (c < D) {
+#pragma unroll 8
+        for (int k = p0; k < p1; ++k) acc += p[(int64_t)k * 2 * Dp];
+    }
+    sum[wave][lane] = acc;
+    __syncthreads();
+    if (wave == 0 && c < D) {
+        float s = 0.0f;
+#pragma unroll
+        for (int k = 0; k < waves; ++k) s += sum[k][lane];
+        dw[c] = (accumulate ? dw[c] : 0.0f) + s;
+    }
+}
+
+__global__ __launch_bounds__(256) void norm_zero_kernel(float* dw, int64_t ld, int D)
+{
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    if (c < D) dw[blockIdx.y * ld + c] = 0.0f;
+}
+
+// ---- host ----
+constexpr size_t kAlign = 256;
+constexpr int kMaxWidth = 1024 * 2 * E;
+bool on(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+lsgd_status check_shape(const char* who, int32_t W, int32_t T, int32_t D)
+{
+    if (W <= 0 || W > LSGD_MAX_WORKERS) return set_error(LSGD_ERR_SHAPE, "%s: W=%d outside [1,%d]", who, (int)W, LSGD_MAX_WORKERS);
+    if (T < 0 || D <= 0) return set_error(LSGD_ERR_SHAPE, "%s: T=%d must not be negative, D=%d must be positive", who, (int)T, (int)D);
+    if (D > kMaxWidth) return set_error(LSGD_ERR_UNSUPPORTED, "%s: D=%d beyond the %d columns a workgroup holds", who, (int)D, kMaxWidth);
+    return LSGD_OK;
+}
+
+// One activation tensor: there or not, aligned to its elements, rows that do not overlap.
+lsgd_status check_rows(const char* who, const char* name, const lsgd_rows& a, int W, int T, int D, int es, bool wanted, bool written)
+{
+    if (wanted && !a.data) return set_error(LSGD_ERR_INVALID_ARG, "%s: %s is required", who, name);
+    if (!wanted && a.data) return set_error(LSGD_ERR_INVALID_ARG, "%s: %s has no meaning here and must be NULL", who, name);
+    if (!a.data) return LSGD_OK;
+    if (!on(a.data, es)) return set_error(LSGD_ERR_INVALID_ARG, "%s: %s is not aligned to its element", who, name);
+    const int64_t lt = T > 1 ? a.token_stride : D, lw = a.worker_stride;
+    if (lt < 0 || (W > 1 && lw < 0)) return set_error(LSGD_ERR_SHAPE, "%s: %s has a negative stride", who, name);
+    // what is written must not overlap itself, whichever of the two strides is the larger
+    if (written && ((T > 1 && lt < D) || (W > 1 && lw < D) ||
+                    (T > 1 && W > 1 && lw < (int64_t)(T - 1) * lt + D && lt < (int64_t)(W - 1) * lw + D)))
+        return set_error(LSGD_ERR_SHAPE, "%s: rows of %s overlap", who, name);
+    return LSGD_OK;
+}
+
+bool wide_rows(const lsgd_rows& a, int W, int T, int es)
+{
+    const int64_t per = 16 / es;
+    return !a.data || (on(a.data, 16) && (W == 1 || a.worker_stride % per == 0) && (T <= 1 || a.token_stride % per == 0));
+}
+bool wide_weights(const float* w, int64_t ld, int W) { return on(w, 16) && (W == 1 || ld % 4 == 0); }
+
+Rows rows(const lsgd_rows& a) { return Rows{a.data, a.worker_stride, a.token_stride}; }
+
+struct Shape {
+    int ts, n, teams;
+};
+Shape shape_of(int D)
+{
+    if (D <= 64 * E) return {64, 1, 4};
+    if (D <= 64 * 2 * E) return {64, 2, 4};
+    if (D <= 256 * E) return {256, 1, 1};
+    if (D <= 256 * 2 * E) return {256, 2, 1};
+    if (D <= 1024 * E) return {1024, 1, 1};
+    return {1024, 2, 1};
+}
+
+// Tokens of a workgroup: enough that weights and sums kept in registers pay, while the grid still fills the chip.
+int tokens_per_group(int W, int T, const Shape& s, int workgroups)
+{
+    const int64_t total = (int64_t)W * T;
+    int64_t per = (total + workgroups - 1) / workgroups;
+    per = std::min<int64_t>((per + s.teams - 1) / s.teams * s.teams, 16 * s.teams);
+    per = std::max<int64_t>(per, s.teams);
+    return (int)per;
+}
+constexpr int kGroups = 2048;
+
+struct GradPlan {
+    int per, chunks, Dp;
+    size_t bytes;
+};
+GradPlan grad_plan(int W, int T, int D)
+{
+    GradPlan p;
+    p.per = tokens_per_group(W, T, shape_of(D), kGroups);
+    p.chunks = T ? (T - 1) / p.per + 1 : 0;
+    p.Dp = (D + E - 1) / E * E;
+    p.bytes = std::max<size_t>(kAlign, sizeof(float) * (size_t)W * (size_t)p.chunks * 2 * (size_t)p.Dp);
+    return p;
+}
+
+template <class T, bool WIDE, class A, template <class, int, int, bool> class K>
+void dispatch(const A& a, int D, dim3 grid, int wide_w, hipStream_t s)
+{
+    const Shape sh = shape_of(D);
+    if (sh.ts == 64) {
+        if (sh.n == 1) K<T, 64, 1, WIDE>::go(a, grid, wide_w, s);
+        else K<T, 64, 2, WIDE>::go(a, grid, wide_w, s);
+    } else if (sh.ts == 256) {
+        if (sh.n == 1) K<T, 256, 1, WIDE>::go(a, grid, wide_w, s);
+        else K<T, 256, 2, WIDE>::go(a, grid, wide_w, s);
+    } else {
+        if (sh.n == 1) K<T, 1024, 1, WIDE>::go(a, grid, wide_w, s);
+        else K<T, 1024, 2, WIDE>::go(a, grid, wide_w, s);
+    }
+}
+
+template <class T, int TS, int N, bool WIDE>
+struct Forward {
+    static void go(const NormArgs& a, dim3 grid, int wide_w, hipStream_t s)
+    {
+        hipLaunchKernelGGL((block_norm_kernel<T, TS, N, WIDE>), grid, dim3(Team<TS>::kThreads), 0, s, a, wide_w);
+    }
+};
+template <class T, int TS, int N, bool WIDE>
+struct Backward {
+    static void go(const NormGradArgs& a, dim3 grid, int wide_w, hipStream_t s)
+    {
+        hipLaunchKernelGGL((block_norm_grad_kernel<T, TS, N, WIDE>), grid, dim3(Team<TS>::kThreads), 0, s, a, wide_w);
+    }
+};
+
+template <class A, template <class, int, int, bool> class K>
+void dispatch_type(const A& a, int D, bool bf16, bool wide, dim3 grid, int wide_w, hipStream_t s)
+{
+    if (bf16) {
+        if (wide) dispatch<uint16_t, true, A, K>(a, D, grid, wide_w, s);
+        else dispatch<uint16_t, false, A, K>(a, D, grid, wide_w, s);
+    } else {
+        if (wide) dispatch<float, true, A, K>(a, D, grid, wide_w, s);
+        else dispatch<float, false, A, K>(a, D, grid, wide_w, s);
+    }
+}
+
+#define LSGD_TRY(x)                         \
+    do {                                    \
+        const lsgd_status st_ = (x);        \
+        if (st_ != LSGD_OK) return st_;     \
+    } while (0)
+
+lsgd_status check_weights(const char* who, const char* name, const float* w, int64_t ld, int W, int D, bool written)
+{
+    if (!w) return LSGD_OK;
+    if (!on(w, 4)) return set_error(LSGD_ERR_INVALID_ARG, "%s: %s is not aligned to its element", who, name);
+    if (W > 1 && (ld < 0 || (written && ld < D))) return set_error(LSGD_ERR_SHAPE, "%s: %s: worker stride %lld for D=%d", who, name, (long long)ld, D);
+    return LSGD_OK;
+}
+
+} // namespace
+
+extern "C" {
+
+lsgd_status lsgd_block_norm(const lsgd_block_norm_args* p, void* hip_stream)
+{
+    const char* who = "block_norm";
+    if (!p) return set_error(LSGD_ERR_INVALID_ARG, "%s: arguments are NULL", who);
+    const int W = p->W, T = p->T, D = p->D, es = p->is_bf16 ? 2 : 4;
+    LSGD_TRY(check_shape(who, W, T, D));
+    if (p->is_bf16 & ~1 || p->post_norm & ~1) return set_error(LSGD_ERR_INVALID_ARG, "%s: is_bf16 and post_norm must be 0 or 1", who);
+    if (!std::isfinite(p->scale)) return set_error(LSGD_ERR_INVALID_ARG, "%s: scale must be finite", who);
+    if (!std::isfinite(p->eps) || p->eps <= 0.0f) return set_error(LSGD_ERR_INVALID_ARG, "%s: eps must be finite and positive", who);
+    if (T == 0) return LSGD_OK;
+    const bool sum = p->y.data != nullptr;
+    LSGD_TRY(check_rows(who, "r", p->r, W, T, D, es, true, false));
+    LSGD_TRY(check_rows(who, "y", p->y, W, T, D, es, sum, false));
+    LSGD_TRY(check_rows(who, "gate", p->gate, W, T, D, es, sum && p->gate.data, false));
+    LSGD_TRY(check_rows(who, "r_out", p->r_out, W, T, D, es, sum, true));
+    LSGD_TRY(check_rows(who, "n", p->n, W, T, D, es, !sum || p->n.data, true));
+    LSGD_TRY(check_weights(who, "w_post", p->w_post, p->ld_w_post, W, D, false));
+    LSGD_TRY(check_weights(who, "w_pre", p->w_pre, p->ld_w_pre, W, D, false));
+    if (!on(p->q_post, 4) || !on(p->q_pre, 4)) return set_error(LSGD_ERR_INVALID_ARG, "%s: q_post or q_pre is not aligned to its element", who);
+
+    NormArgs a{};
+    a.r = rows(p->r); a.y = rows(p->y); a.u = rows(p->gate); a.r_out = rows(p->r_out); a.n = rows(p->n);
+    a.w_post = p->w_post; a.ld_w_post = p->ld_w_post;
+    a.w_pre = p->w_pre; a.ld_w_pre = p->ld_w_pre;
+    a.q_post = p->q_post; a.q_pre = p->q_pre;
+    a.T = T; a.D = D;
+    a.per = tokens_per_group(W, T, shape_of(D), kGroups);
+    a.scale = p->scale; a.eps = p->eps; a.inv_d = 1.0f / (float)D;
+    a.post = p->post_norm;
+    bool wide = D % E == 0;
+    for (const lsgd_rows* q : {&p->r, &p->y, &p->gate, &p->r_out, &p->n}) wide = wide && wide_rows(*q, W, T, es);
+    const int wide_w = (wide_weights(p->w_post, p->ld_w_post, W) ? 1 : 0) | (wide_weights(p->w_pre, p->ld_w_pre, W) ? 2 : 0);
+    const dim3 grid((unsigned)((T - 1) / a.per + 1), (unsigned)W);
+    dispatch_type<NormArgs, Forward>(a, D, p->is_bf16, wide, grid, wide_w, static_cast<hipStream_t>(hip_stream));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return set_error(LSGD_ERR_HIP, "%s: %s", who, hipGetErrorString(e));
+    return LSGD_OK;
+}
+
+size_t lsgd_block_norm_grad_workspace_bytes(int32_t W, int32_t T, int32_t D)
+{
+    if (check_shape("block_norm_grad", W, T, D) != LSGD_OK) return 0;
+    return grad_plan(W, T, D).bytes;
+}
+
+lsgd_status lsgd_block_norm_grad(const lsgd_block_norm_grad_args* p, void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+    const char* who = "block_norm_grad";
+    if (!p) return set_error(LSGD_ERR_INVALID_ARG, "%s: arguments are NULL", who);
+    const int W = p->W, T = p->T, D = p->D, es = p->is_bf16 ? 2 : 4;
+    LSGD_TRY(check_shape(who, W, T, D));
+    if (p->is_bf16 & ~1 || p->post_norm & ~1 || p->accumulate & ~1) return set_error(LSGD_ERR_INVALID_ARG, "%s: is_bf16, post_norm and accumulate must be 0 or 1", who);
+    if (!std::isfinite(p->scale)) return set_error(LSGD_ERR_INVALID_ARG, "%s: scale must be finite", who);
+    LSGD_TRY(check_weights(who, "w_post", p->w_post, p->ld_w_post, W, D, false));
+    LSGD_TRY(check_weights(who, "w_pre", p->w_pre, p->ld_w_pre, W, D, false));
+    LSGD_TRY(check_weights(who, "dw_post", p->dw_post, p->ld_dw_post, W, D, true));
+    LSGD_TRY(check_weights(who, "dw_pre", p->dw_pre, p->ld_dw_pre, W, D, true));
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    hipError_t e;
+    if (T == 0) {
+        if (!p->accumulate)
+            for (int k = 0; k < 2; ++k)
+                if (float* dw = k ? p->dw_pre : p->dw_post)
+                    hipLaunchKernelGGL(norm_zero_kernel, dim3((unsigned)((D - 1) / 256 + 1), (unsigned)W), dim3(256), 0, s, dw,
+                                       k ? p->ld_dw_pre : p->ld_dw_post, D);
+        e = hipGetLastError();
+        if (e != hipSuccess) return set_error(LSGD_ERR_HIP, "%s: %s", who, hipGetErrorString(e));
+        return LSGD_OK;
+    }
+    const bool sum = p->y.data != nullptr, norm = p->dn.data != nullptr;
+    if (!norm && !p->dr_out.data) return set_error(LSGD_ERR_INVALID_ARG, "%s: neither dn nor dr_out is given", who);
+    LSGD_TRY(check_rows(who, "dn", p->dn, W, T, D, es, norm, false));
+    LSGD_TRY(check_rows(who, "dr_out", p->dr_out, W, T, D, es, p->dr_out.data, false));
+    LSGD_TRY(check_rows(who, "r_out", p->r_out, W, T, D, es, norm || p->r_out.data, false));
+    LSGD_TRY(check_rows(who, "y", p->y, W, T, D, es, sum, false));
+    LSGD_TRY(check_rows(who, "gate", p->gate, W, T, D, es, sum && p->gate.data, false));
+    LSGD_TRY(check_rows(who, "dr", p->dr, W, T, D, es, true, true));
+    LSGD_TRY(check_rows(who, "dy", p->dy, W, T, D, es, sum, true));
+    LSGD_TRY(check_rows(who, "dgate", p->dgate, W, T, D, es, sum && p->gate.data, true));
+    if (norm && !p->q_pre) return set_error(LSGD_ERR_INVALID_ARG, "%s: q_pre is required", who);
+    if (sum && p->post_norm && !p->q_post) return set_error(LSGD_ERR_INVALID_ARG, "%s: q_post is required", who);
+    if (!on(p->q_post, 4) || !on(p->q_pre, 4)) return set_error(LSGD_ERR_INVALID_ARG, "%s: q_post or q_pre is not aligned to its element", who);
+    if (p->dw_post && !sum) return set_error(LSGD_ERR_INVALID_ARG, "%s: dw_post needs y", who);
+    if (p->dw_pre && !norm) return set_error(LSGD_ERR_INVALID_ARG, "%s: dw_pre needs dn", who);
+    const GradPlan plan = grad_plan(W, T, D);
+    const bool sums = p->dw_post || p->dw_pre;
+    if (sums) {
+        if (!workspace) return set_error(LSGD_ERR_INVALID_ARG, "%s: workspace is NULL", who);
+        if (!on(workspace, kAlign)) return set_error(LSGD_ERR_INVALID_ARG, "%s: workspace must be 256-byte aligned", who);
+        if (workspace_bytes < plan.bytes) return set_error(LSGD_ERR_NOMEM, "%s: workspace of %zu bytes < %zu needed", who, workspace_bytes, plan.bytes);
+    }
+    NormGradArgs a{};
+    a.dn = rows(p->dn); a.dr_out = rows(p->dr_out); a.r = rows(p->r_out); a.y = rows(p->y); a.u = rows(p->gate);
+    a.dr = rows(p->dr); a.dy = rows(p->dy); a.du = rows(p->dgate);
+    a.w_post = p->w_post; a.ld_w_post = p->ld_w_post;
+    a.w_pre = p->w_pre; a.ld_w_pre = p->ld_w_pre;
+    a.q_post = p->q_post; a.q_pre = p->q_pre;
+    a.parts = sums ? static_cast<float*>(workspace) : nullptr;
+    a.T = T; a.D = D; a.Dp = plan.Dp; a.per = plan.per; a.chunks = plan.chunks;
+    a.scale = p->scale; a.inv_d = 1.0f / (float)D;
+    a.post = p->post_norm;
+    bool wide = D % E == 0;
+    for (const lsgd_rows* q : {&p->dn, &p->dr_out, &p->r_out, &p->y, &p->gate, &p->dr, &p->dy, &p->dgate}) wide = wide && wide_rows(*q, W, T, es);
+    const int wide_w = (wide_weights(p->w_post, p->ld_w_post, W) ? 1 : 0) | (wide_weights(p->w_pre, p->ld_w_pre, W) ? 2 : 0);
+    dispatch_type<NormGradArgs, Backward>(a, D, p->is_bf16, wide, dim3((unsigned)plan.chunks, (unsigned)W), wide_w, s);
+    if (sums)
+        hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)((D - 1) / kWave + 1), (unsigned)W, 2), dim3(kJoinThreads), 0, s, a.parts, plan.chunks, D,
+                           plan.Dp, p->dw_post, p->ld_dw_post, p->dw_pre, p->ld_dw_pre, p->accumulate);
+    e = hipGetLastError();
+    if (e != hipSuccess) return set_error(LSGD_ERR_HIP, "%s: %s", who, hipGetErrorString(e));
+    return LSGD_OK;
+}
+
+} // extern "C"

@@ -1,0 +1,349 @@
+"""AdamW over many tensors: 32-bit moments against the formulas in 64 bits, 8-bit ones bit for bit against the same sequence of
+fp32 operations and against what the codes are for."""
+import math
+
+import pytest
+import torch
+
+import paper_1905_10395_amd as L
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+EPS = 2.0 ** -24
+PHI = 0.6180339887498949
+B = L.ADAMW_BLOCK
+CANARY = 55.0
+
+
+def rnd(*shape, seed, std=1.0):
+    return torch.randn(shape, generator=torch.Generator().manual_seed(seed)) * std
+
+
+class Rows:
+    """Tensors of `sizes` elements side by side in the rows of x, g, m, v (and a bf16 copy), the first at column `lead`."""
+
+    def __init__(self, W, sizes, bits, g_dtype=torch.float32, lead=0, shadow=False, seed=0, blank=False):
+        P = lead + sum(sizes)
+        ld = P + 6
+        full = lambda dt=torch.float32, v=CANARY: torch.full((W, ld), v).to(dt)
+        self.x, self.g = full(), full(g_dtype)
+        self.m, self.v = (full(), full()) if bits == 32 else (full(torch.int8), full(torch.uint8))
+        self.xb = full(torch.bfloat16) if shadow else None
+        self.mv, self.vv = (full(), full()) if bits == 8 else (None, None)
+        nb = sum(-(-n // B) for n in sizes)
+        self.ms, self.vs = torch.zeros((W, nb + 2)), torch.zeros((W, nb + 2))
+        g = torch.Generator().manual_seed(seed)
+        cols = slice(lead, P)
+        self.x[:, cols] = torch.randn((W, P - lead), generator=g) * 0.1
+        self.g[:, cols] = (torch.randn((W, P - lead), generator=g) * 0.01).to(g_dtype)
+        if blank:
+            self.m[:, cols], self.v[:, cols] = 0, 0
+        elif bits == 32:
+            self.m[:, cols] = torch.randn((W, P - lead), generator=g) * 0.003
+            self.v[:, cols] = (torch.randn((W, P - lead), generator=g) * 0.01) ** 2
+        else:
+            self.m[:, cols] = torch.randint(-127, 128, (W, P - lead), generator=g).to(torch.int8)
+            self.v[:, cols] = torch.randint(0, 256, (W, P - lead), generator=g).to(torch.uint8)
+            self.ms[:, :nb] = (torch.rand((W, nb), generator=g) + 0.5) * (1e-2 / 127 ** 2)
+            self.vs[:, :nb] = (torch.rand((W, nb), generator=g) + 0.5) * (3e-2 / 255 ** 2)
+        self.parts = []
+        at, b = lead, 0
+        for n in sizes:
+            self.parts.append((slice(at, at + n), slice(b, b + -(-n // B))))
+            at += n
+            b += -(-n // B)
+        self.bits = bits
+        for k in ("x", "g", "m", "v", "xb", "mv", "vv", "ms", "vs"):
+            t = getattr(self, k)
+            setattr(self, k + "0", None if t is None else t.clone())
+            setattr(self, k, None if t is None else t.to(DEV))
+
+    def optimizer(self, wd, mult, **kw):
+        ts = []
+        for k, (c, b) in enumerate(self.parts):
+            cut = lambda t, s: None if t is None else t[:, s]
+            eight = self.bits == 8
+            ts.append(L.AdamWTensor(self.x[:, c], self.g[:, c], self.m[:, c], self.v[:, c], weight_decay=wd[k % len(wd)], lr_mult=mult[k % len(mult)],
+                                    x_bf16=cut(self.xb, c), m_scale=self.ms[:, b] if eight else None, v_scale=self.vs[:, b] if eight else None,
+                                    m_values=cut(self.mv, c), v_values=cut(self.vv, c)))
+        return L.AdamW(ts, bits=self.bits, **kw)
+
+    def untouched(self):
+        """Everything outside the tensors, and the gradient, is as it was."""
+        mask = torch.ones_like(self.x0, dtype=torch.bool)
+        for c, _ in self.parts:
+            mask[:, c] = False
+        for k in ("x", "m", "v", "xb", "mv", "vv"):
+            t = getattr(self, k)
+            if t is not None:
+                assert torch.equal(t.cpu()[mask], getattr(self, k + "0")[mask]), k
+        assert torch.equal(self.g.cpu(), self.g0)
+
+
+def reference64(x, g, m, v, lr, wd, mult, b1, b2, eps, t, c):
+    x, g, m, v = x.double(), g.double() * c, m.double(), v.double()
+    m = b1 * m + (1 - b1) * g
+    v = b2 * v + (1 - b2) * g * g
+    step = (m / (1 - b1 ** t)) / ((v / (1 - b2 ** t)).sqrt() + eps)
+    return x - lr * mult * (step + wd * x), m, v, lr * mult * step.abs()
+
+
+HYPER = dict(lr=2e-3, beta1=0.9, beta2=0.99, eps=1e-6)
+
+
+@pytest.mark.parametrize("W,sizes,lead", [(1, [1], 0), (3, [5, 1, 4, 300], 0), (2, [4096, 64, 8192], 0), (2, [4095, 1, 4097, 12], 3), (1, [20001], 1),
+                                          (5, [0, 7, 0, 260], 2), (32, [96, 10], 0)])
+@pytest.mark.parametrize("g_dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("shadow", [False, True])
+def test_32_bits(W, sizes, lead, g_dtype, shadow):
+    r = Rows(W, sizes, 32, g_dtype, lead, shadow, seed=sum(sizes))
+    wd, mult, t, c = [0.1, 0.0], [1.0, 0.5, 2.0], 3, 0.25
+    r.optimizer(wd, mult).step(step=t, grad_scale=c, **HYPER)
+    for k, (cols, _) in enumerate(r.parts):
+        x, m, v, disp = reference64(r.x0[:, cols], r.g0[:, cols], r.m0[:, cols], r.v0[:, cols], HYPER["lr"], wd[k % 2], mult[k % 3], HYPER["beta1"],
+                                    HYPER["beta2"], HYPER["eps"], t, c)
+        mag = r.m0[:, cols].double().abs() + r.g0[:, cols].double().abs() * c
+        # m: two products, a sum, two rounded coefficients; v: all terms positive; x: a dozen roundings of the step, three of x,
+        # and the step's error from m's (which may cancel)
+        bm = 4 * EPS * mag
+        assert bool(((r.m.cpu()[:, cols].double() - m).abs() <= bm).all())
+        assert bool(((r.v.cpu()[:, cols].double() - v).abs() <= 6 * EPS * v + 1e-44).all())
+        dm = disp * bm / m.abs().clamp(min=1e-300)
+        assert bool(((r.x.cpu()[:, cols].double() - x).abs() <= 16 * EPS * disp + dm + 3 * EPS * (x.abs() + r.x0[:, cols].double().abs())).all())
+        if shadow:
+            assert torch.equal(r.xb.cpu()[:, cols], r.x.cpu()[:, cols].bfloat16())
+    r.untouched()
+
+
+def test_32_bits_against_torch_over_many_steps():
+    W, sizes = 2, [333, 40]
+    r = Rows(W, sizes, 32, blank=True, seed=4)
+    opt = r.optimizer([0.05], [1.0])
+    p = torch.nn.Parameter(r.x0[:, :373].double())
+    ref = torch.optim.AdamW([p], lr=1e-2, betas=(0.9, 0.95), eps=1e-8, weight_decay=0.05)
+    for t in range(1, 31):
+        g = rnd(W, 373, seed=t)
+        r.g[:, :373] = g.to(DEV)
+        opt.step(1e-2, t, beta1=0.9, beta2=0.95)
+        p.grad = g.double()
+        ref.step()
+    # 30 steps of at most ~lr each, each with a relative error of some 20 roundings, and x's own 3 a step
+    assert float((r.x.cpu()[:, :373].double() - p.detach()).abs().max()) <= 30 * (1e-2 * 10 * 20 * EPS + 3 * EPS)
+
+
+def encode(a, top, u, second):
+    """Codes and scale of one block (last dimension) by the stated sequence of fp32 operations."""
+    fin = torch.isfinite(a)
+    big = torch.where(fin, a.abs(), torch.zeros_like(a)).amax(-1, keepdim=True)
+    top2 = torch.tensor(top * top, dtype=torch.float32)
+    s = big * (torch.tensor(1.0) / top2)
+    s = torch.where(s > 2.0 ** -100, s, torch.zeros_like(s))
+    inv = torch.where(s > 0, 1.0 / s, torch.zeros_like(s))
+    y = torch.where(fin, (a.abs() * inv).clamp(max=top * top), torch.where(s > 0, top2, torch.zeros_like(top2)).expand_as(a))
+    c = y.double().sqrt().floor().float()
+    if second:
+        c2, d2 = c * c, (c + 1) * (c + 1)
+        c = c + ((y - c2) * (y + c2) > u * ((d2 - c2) * (d2 + c2))).float()
+        c = torch.where((a > 0) & (s > 0), c.clamp(min=1.0), c)
+    else:
+        c = c + (y - c * c > u * (2 * c + 1)).float()
+        c = torch.where(a < 0, -c, c)
+    return c, s
+
+
+def replica8(x, g, mq, vq, ms, vs, lr, wd, mult, b1, b2, eps, t, c):
+    """One tensor's step, every operation rounded to fp32, blocks of B along the last dimension."""
+    f = lambda a: torch.tensor(a, dtype=torch.float64).float()
+    W, n = x.shape
+    fill = (-n) % B
+    wide = lambda q: torch.cat([q.float(), torch.zeros((W, fill))], 1).view(W, -1, B)
+    x, g, mq, vq = wide(x), wide(g), wide(mq), wide(vq)
+    m = mq * mq.abs() * ms[..., None]
+    r = vq * vq * vs[..., None]
+    v = r * r
+    gs = g * f(c)
+    m = f(b1) * m + f(1 - b1) * gs
+    v = f(b2) * v + f(1 - b2) * (gs * gs)
+    r = v.double().sqrt().float()                                    # correctly rounded (torch's vector root on the CPU is not)
+    den = r * f(1 / math.sqrt(1 - b2 ** t)) + f(eps)
+    x = x * f(1.0 - lr * mult * wd) - (m / den) * f(lr / (1 - b1 ** t) * mult)
+    real = (torch.arange(n + fill) < n).view(-1, B)
+    m, r = torch.where(real, m, torch.zeros_like(m)), torch.where(real, r, torch.zeros_like(r))
+    mq, ms = encode(m, 127.0, f((t * PHI + 0.5) % 1.0), False)
+    vq, vs = encode(r, 255.0, f((t * PHI) % 1.0), True)
+    cut = lambda q: q.reshape(W, -1)[:, :n]
+    r = vq * vq * vs
+    return cut(x), cut(mq), cut(vq), ms[..., 0], vs[..., 0], cut(mq * mq.abs() * ms), cut(r * r)
+
+
+def same(a, b):
+    return torch.equal(torch.nan_to_num(a, nan=-3e33, posinf=4e33, neginf=-4e33), torch.nan_to_num(b, nan=-3e33, posinf=4e33, neginf=-4e33))
+
+
+def check8(r, wd, mult, t, c=1.0, hyper=HYPER):
+    for k, (cols, bl) in enumerate(r.parts):
+        want = replica8(r.x0[:, cols], r.g0[:, cols].float(), r.m0[:, cols], r.v0[:, cols], r.ms0[:, bl], r.vs0[:, bl], hyper["lr"], wd[k % len(wd)],
+                        mult[k % len(mult)], hyper["beta1"], hyper["beta2"], hyper["eps"], t, c)
+        have = (r.x[:, cols], r.m[:, cols].float(), r.v[:, cols].float(), r.ms[:, bl], r.vs[:, bl], r.mv[:, cols], r.vv[:, cols])
+        for name, a, b in zip(("x", "m codes", "v codes", "m scale", "v scale", "m", "v"), have, want):
+            assert same(a.cpu(), b), (k, name, int((a.cpu() != b).sum()))
+
+
+@pytest.mark.parametrize("W,sizes,lead", [(1, [1], 0), (2, [256], 0), (2, [255, 257, 5], 0), (3, [4096, 300, 4100], 0), (2, [1000, 31], 3), (1, [9001], 2),
+                                          (4, [0, 12], 0)])
+@pytest.mark.parametrize("g_dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("t", [1, 2, 12345])
+def test_8_bits_bit_for_bit(W, sizes, lead, g_dtype, t):
+    r = Rows(W, sizes, 8, g_dtype, lead, shadow=True, seed=t)
+    wd, mult = [0.1, 0.0], [1.0, 0.5]
+    opt = r.optimizer(wd, mult)
+    opt.step(step=t, grad_scale=0.5, **HYPER)
+    opt.moments()
+    check8(r, wd, mult, t, 0.5)
+    for cols, _ in r.parts:
+        assert torch.equal(r.xb.cpu()[:, cols], r.x.cpu()[:, cols].bfloat16())
+    r.untouched()
+
+
+def test_8_bits_first_step_from_nothing_and_blocks_of_nothing():
+    r = Rows(1, [3 * B], 8, blank=True, seed=2)
+    r.g0[:, B:2 * B] = 0.0                                           # a block that gets no gradient
+    r.g0[:, 2 * B:3 * B] *= 1e-38                                    # and one of next to none
+    r.g.copy_(r.g0)
+    opt = r.optimizer([0.0], [1.0])
+    opt.step(step=1, **HYPER)
+    opt.moments()
+    check8(r, [0.0], [1.0], 1)
+    assert bool((r.m[:, B:3 * B] == 0).all()) and bool((r.v[:, B:3 * B] == 0).all()) and bool((r.ms[:, 1:3] == 0).all())
+    assert torch.equal(r.x.cpu()[:, B:2 * B], r.x0[:, B:2 * B])
+
+
+def test_8_bits_codes_are_neighbours_of_the_value():
+    """Against 64 bits: a stored moment is one of the two values around the exact one (their spacing: 2q+1 units)."""
+    r = Rows(2, [5000], 8, seed=9)
+    opt = r.optimizer([0.0], [1.0])
+    t = 7
+    opt.step(step=t, **HYPER)
+    opt.moments()
+    (cols, bl), = r.parts
+    blk = torch.arange(5000) // B
+    m0 = r.m0[:, cols].double() * r.m0[:, cols].double().abs() * r.ms0[:, bl].double()[:, blk]
+    r0 = r.v0[:, cols].double() ** 2 * r.vs0[:, bl].double()[:, blk]
+    _, m, v, _ = reference64(r.x0[:, cols], r.g0[:, cols], m0, r0 ** 2, HYPER["lr"], 0.0, 1.0, HYPER["beta1"], HYPER["beta2"], HYPER["eps"], t, 1.0)
+    sm, sv = r.ms.cpu()[:, bl].double()[:, blk], r.vs.cpu()[:, bl].double()[:, blk]
+    qm, qv = r.m.cpu()[:, cols].double().abs(), r.v.cpu()[:, cols].double()
+    lo = lambda q: (q - 1).clamp(min=0) ** 2
+    tiny = 1e-5                                                      # fp32 arithmetic's share, relative to the spacing's unit
+    a = m.abs() / sm
+    assert bool((a >= lo(qm) - tiny * a - tiny).all()) and bool((a <= (qm + 1) ** 2 + tiny * a + tiny).all())
+    a = v.sqrt() / sv
+    assert bool((a >= torch.where(qv == 1, torch.zeros_like(qv), lo(qv)) - tiny * a - tiny).all()) and bool((a <= (qv + 1) ** 2 + tiny * a + tiny).all())
+
+
+def test_8_bits_what_is_not_finite_stays_where_it_is():
+    r = Rows(1, [2 * B], 8, seed=5)
+    r.g0[0, 3], r.g0[0, 9], r.g0[0, 11] = float("nan"), float("inf"), 1e25     # the last: its square overflows
+    r.g.copy_(r.g0)
+    clean = Rows(1, [2 * B], 8, seed=5)
+    for q in (r, clean):
+        opt = q.optimizer([0.0], [1.0])
+        opt.step(step=4, **HYPER)
+        opt.moments()
+    check8(r, [0.0], [1.0], 4)
+    bad = torch.zeros(2 * B, dtype=torch.bool)
+    bad[[3, 9, 11]] = True
+    assert torch.equal(r.x.cpu()[0, :2 * B][~bad], clean.x.cpu()[0, :2 * B][~bad])
+    assert bool(torch.isfinite(r.mv[0, :2 * B]).all()) and bool(torch.isfinite(r.vv[0, :2 * B]).all())
+    assert torch.equal(r.vv[0, B:2 * B], clean.vv[0, B:2 * B])
+
+
+def test_8_bits_slow_changes_are_not_lost():
+    """beta2 = 0.999 moves v by a thousandth a step, the codes are a hundredth and more apart: over 2000 steps of gradients that
+    fell to a tenth, the second moment has to fall by what it does in 32 bits although one element of the block keeps the scale."""
+    n, steps = B, 2000
+    r = Rows(1, [n], 8, blank=True, seed=1)
+    g = torch.full((1, n), 0.1)
+    g[0, 0] = 1.0                                                    # keeps the block's scale
+    opt = r.optimizer([0.0], [1.0])
+    v = torch.zeros((1, n), dtype=torch.float64)
+    # bring v up: one step with beta2 = 0 sets it to g^2 where the elements start at half the largest
+    start = torch.full((1, n), 0.5)
+    start[0, 0] = 1.0
+    r.g[:, :n] = start.to(DEV)
+    opt.step(0.0, 1, beta1=0.9, beta2=0.0)
+    v = start.double() ** 2
+    r.g[:, :n] = g.to(DEV)
+    for t in range(2, steps + 2):
+        opt.step(0.0, t, beta1=0.9, beta2=0.999)
+        v = 0.999 * v + 0.001 * g.double() ** 2
+    opt.moments()
+    got = r.vv.cpu()[0, 1:n].double()
+    # v falls from 0.25 to 0.0424.  Its codes, between q = 116 and 180, are 4/q = 2.2 to 3.5 % of v apart.  The threshold's
+    # sequence has discrepancy of order log(N)/N: codes taken differ from the drift by a few (3) at the end.
+    assert abs(float(got.mean()) / float(v[0, 1]) - 1) <= 3 * 0.035
+    assert float(r.vv[0, 0]) == pytest.approx(1.0, rel=1e-3)
+
+
+def test_many_tensors_one_row_each():
+    """Dense tensors of any shape count as one row."""
+    shapes = [(3, 4, 5), (7,), (16, 16), (1,)]
+    x, g = [rnd(*s, seed=k).to(DEV) for k, s in enumerate(shapes)], [rnd(*s, seed=50 + k).to(DEV) for k, s in enumerate(shapes)]
+    m, v = [torch.zeros_like(a) for a in x], [torch.zeros_like(a) for a in x]
+    x0 = [a.cpu() for a in x]
+    opt = L.AdamW([L.AdamWTensor(*q) for q in zip(x, g, m, v)])
+    opt.step(0.01, 1)
+    for a, a0, b in zip(x, x0, g):
+        ref = a0.double() - 0.01 * b.cpu().double() / (b.cpu().double().abs() + 1e-8)
+        assert float((a.cpu().double() - ref).abs().max()) <= 16 * EPS * (0.01 + float(a0.abs().max()))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_in_a_captured_graph(bits):
+    """Replays equal the same calls made one by one."""
+    a, b = (Rows(2, [700, 256], bits, seed=8) for _ in range(2))
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    oa, ob = a.optimizer([0.1], [1.0], stream=s), b.optimizer([0.1], [1.0], stream=s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        oa.step(step=5, **HYPER)
+    for _ in range(3):
+        with torch.cuda.stream(s):
+            graph.replay()
+        ob.step(step=5, **HYPER)
+        s.synchronize()
+        for k in ("x", "m", "v", "ms", "vs"):
+            assert torch.equal(getattr(a, k), getattr(b, k))
+
+
+def test_refusals():
+    f = lambda *s, dtype=torch.float32: torch.zeros(s, dtype=dtype, device=DEV)
+    T = L.AdamWTensor
+    with pytest.raises(ValueError, match="no tensors"):
+        L.AdamW([])
+    with pytest.raises(ValueError, match="shape"):
+        L.AdamW([T(f(2, 8), f(2, 7), f(2, 8), f(2, 8))])
+    with pytest.raises(ValueError, match="int8"):
+        L.AdamW([T(f(2, 8), f(2, 8), f(2, 8), f(2, 8))], bits=8)
+    with pytest.raises(ValueError, match="missing"):
+        L.AdamW([T(f(2, 8), f(2, 8), None, f(2, 8))])
+    with pytest.raises(L.LsgdError, match="m_scale"):
+        L.AdamW([T(f(2, 8), f(2, 8), f(2, 8, dtype=torch.int8), f(2, 8, dtype=torch.uint8))], bits=8)
+    with pytest.raises(ValueError, match=r"m_scale must be \[2, 2\]"):
+        L.AdamW([T(f(2, 300), f(2, 300), f(2, 300, dtype=torch.int8), f(2, 300, dtype=torch.uint8), m_scale=f(2, 1), v_scale=f(2, 1))], bits=8)
+    with pytest.raises(L.LsgdError, match="state_bits"):
+        L.AdamW([T(f(2, 8), f(2, 8), f(2, 8, dtype=torch.int8), f(2, 8, dtype=torch.uint8))], bits=16)
+    with pytest.raises(ValueError, match="must be torch.float32"):
+        L.AdamW([T(f(2, 8), f(2, 8), f(2, 8), f(2, 8)), T(f(2, 8), f(2, 8, dtype=torch.bfloat16), f(2, 8), f(2, 8))])
+    with pytest.raises(L.LsgdError, match="finite"):
+        L.AdamW([T(f(2, 8), f(2, 8), f(2, 8), f(2, 8), weight_decay=float("inf"))])
+    with pytest.raises(L.LsgdError, match="stride"):
+        L.AdamW([T(f(1, 8).expand(2, 8), f(2, 8), f(2, 8), f(2, 8))])
+    opt = L.AdamW([T(f(2, 8), f(2, 8), f(2, 8), f(2, 8))])
+    for bad in (dict(lr=float("nan"), step=1), dict(lr=0.1, step=0), dict(lr=0.1, step=1, beta1=1.0), dict(lr=0.1, step=1, beta2=-0.1),
+                dict(lr=0.1, step=1, eps=-1.0), dict(lr=0.1, step=1, grad_scale=float("inf"))):
+        with pytest.raises(L.LsgdError, match="INVALID_ARG"):
+            opt.step(**bad)
+    with pytest.raises(L.LsgdError, match="STATE"):
+        opt.moments()
+    torch.cuda.synchronize()

@@ -1,0 +1,332 @@
+"""Block norms (post-norm, gate, scaled residual sum, pre-norm) and their gradients against the formulas in 64 bits."""
+import pytest
+import torch
+
+import paper_1905_10395_amd as L
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+EPS = 2.0 ** -24
+UNIT = {torch.float32: EPS, torch.bfloat16: 2.0 ** -8}
+NORM_EPS = 1e-5
+SCALE = 0.5
+
+
+def rnd(*shape, seed, dtype=torch.float32, std=1.0, mean=0.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(shape, generator=g) * std + mean).to(dtype).to(DEV)
+
+
+def weights(W, D, seed, lead=0):
+    """Two weight vectors a worker, columns of wider rows."""
+    x = rnd(W, lead + 2 * D + 3, seed=seed, std=0.3, mean=1.0)
+    return x[:, lead:lead + D], x[:, lead + D:lead + 2 * D]
+
+
+def d(t):
+    return None if t is None else t.cpu().double()
+
+
+def slack(D, u=None):
+    """Relative error of a product that holds a norm's factor (a sum of D squares) and, with u, a sigmoid of u."""
+    return (D / 2 + 24 + (0 if u is None else 2 * u.abs())) * EPS
+
+
+def reference(r, y, u, wp, wn, post, scale=SCALE):
+    """r', n, q_post, q_pre in 64 bits, and bounds on what fp32 arithmetic makes of r' and n."""
+    D = r.shape[2]
+    r, y, u, wp, wn = d(r), d(y), d(u), d(wp), d(wn)
+    one = torch.ones((r.shape[0], D), dtype=torch.float64)
+    wp, wn = (one if wp is None else wp)[:, None], (one if wn is None else wn)[:, None]
+    br = torch.zeros_like(r)
+    qp = None
+    if y is not None:
+        qp = (y.pow(2).mean(2) + NORM_EPS).rsqrt() if post else torch.ones(y.shape[:2], dtype=torch.float64)
+        b = scale * y * qp[..., None] * wp * (1.0 if u is None else torch.sigmoid(u))
+        r = r + b
+        br = b.abs() * slack(D, u) + r.abs() * 2 * EPS
+    qn = (r.pow(2).mean(2) + NORM_EPS).rsqrt()
+    n = r * qn[..., None] * wn
+    # q moves with the whole row's error: at most by its 2-norm over the row's
+    dq = (br.norm(dim=2) / r.norm(dim=2).clamp(min=1e-30))[..., None]
+    bn = (br * qn[..., None] * wn.abs()) + n.abs() * (slack(D) + dq)
+    return r, n, qp, qn, br, bn
+
+
+SHAPES = [(1, 1, 1), (2, 3, 7), (3, 1, 64), (2, 5, 101), (2, 70, 512), (1, 9, 520), (2, 33, 1000), (1, 3, 1024), (2, 3, 2048), (1, 5, 2056),
+          (1, 2, 4097), (1, 2, 8192), (1, 3, 8200), (1, 2, 16384)]
+
+
+@pytest.mark.parametrize("W,T,D", SHAPES)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("gate", [False, True])
+def test_forward(W, T, D, dtype, gate):
+    r, y = rnd(W, T, D, seed=1, dtype=dtype), rnd(W, T, D, seed=2, dtype=dtype, std=3.0)
+    u = rnd(W, T, D, seed=3, dtype=dtype, std=2.0) if gate else None
+    wp, wn = weights(W, D, 4)
+    rr, n, stats = L.block_norm(r, y, gate=u, w_post=wp, w_pre=wn, scale=SCALE, eps=NORM_EPS)
+    R, N, qp, qn, br, bn = reference(r, y, u, wp, wn, True)
+    unit = UNIT[dtype]
+    assert bool(((d(rr) - R).abs() <= br + unit * R.abs() * 1.01).all())
+    assert bool(((d(n) - N).abs() <= bn + unit * N.abs() * 1.01).all())
+    assert bool(((d(stats[0]) - qp).abs() <= qp * slack(D)).all())
+    dq = br.norm(dim=2) / R.norm(dim=2)
+    assert bool(((d(stats[1]) - qn).abs() <= qn * (slack(D) + dq)).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_forward_parts_alone(dtype):
+    W, T, D = 2, 37, 72
+    r, y = rnd(W, T, D, seed=1, dtype=dtype), rnd(W, T, D, seed=2, dtype=dtype)
+    wp, wn = weights(W, D, 4, lead=1)
+    unit = UNIT[dtype]
+    # a model's first norm
+    same, n, stats = L.block_norm(r, w_pre=wn, eps=NORM_EPS)
+    R, N, _, qn, br, bn = reference(r, None, None, None, wn, True)
+    assert same is r and bool(((d(n) - N).abs() <= bn + unit * N.abs() * 1.01).all())
+    # its last sum, without a norm behind the block and without weights
+    rr, none, _ = L.block_norm(r, y, scale=SCALE, eps=NORM_EPS, post_norm=False, pre_norm=False)
+    R, _, _, _, br, _ = reference(r, y, None, None, None, False)
+    assert none is None and bool(((d(rr) - R).abs() <= br + unit * R.abs() * 1.01).all())
+    # channel weights without a norm
+    rr, _, _ = L.block_norm(r, y, w_post=wp, scale=SCALE, eps=NORM_EPS, post_norm=False, pre_norm=False)
+    R, _, _, _, br, _ = reference(r, y, None, wp, None, False)
+    assert bool(((d(rr) - R).abs() <= br + unit * R.abs() * 1.01).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("D", [64, 100, 333])
+def test_strides_and_places(dtype, D):
+    """The gate as half of a wider projection, activations with the token dimension outermost, results in the inputs' place."""
+    W, T = 3, 21
+    both = rnd(W, T, 2 * D, seed=5, dtype=dtype)
+    u = both[:, :, D:]
+    r, y = rnd(T, W, D, seed=6, dtype=dtype).transpose(0, 1), rnd(W, T, D, seed=7, dtype=dtype)
+    wp, wn = weights(W, D, 8)
+    want = L.block_norm(r.contiguous(), y, gate=u.contiguous(), w_post=wp, w_pre=wn, scale=SCALE)
+    got_r, got_n, got_s = L.block_norm(r, y, gate=u, w_post=wp, w_pre=wn, scale=SCALE, r_out=r, n=y)
+    assert got_r is r and got_n is y
+    assert torch.equal(r, want[0]) and torch.equal(y, want[1]) and torch.equal(got_s, want[2])
+    assert torch.equal(both[:, :, D:], u)
+
+
+def test_rows_do_not_reach_into_each_other():
+    W, T, D = 1, 6, 512
+    r, y = rnd(W, T, D, seed=1), rnd(W, T, D, seed=2)
+    clean = L.block_norm(r, y)
+    y[0, 2, 5], r[0, 4, 7] = float("nan"), float("inf")
+    y[0, 1], r[0, 1] = 0.0, 0.0                                       # a row of nothing
+    rr, n, stats = L.block_norm(r, y)
+    for t in (0, 3, 5):
+        assert torch.equal(rr[0, t], clean[0][0, t]) and torch.equal(n[0, t], clean[1][0, t])
+    assert bool(torch.isnan(n[0, 2]).all()) and bool((rr[0, 1] == 0).all()) and bool((n[0, 1] == 0).all())
+    assert bool(torch.isfinite(stats[:, 0, 1]).all())
+
+
+def gate_limits(dtype):
+    return torch.tensor([-float("inf"), -200.0, -90.0, -20.0, 0.0, 20.0, 200.0, float("inf")], dtype=dtype, device=DEV)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_gate_far_out(dtype):
+    u = gate_limits(dtype).view(1, 1, 8)
+    y, r = torch.ones((1, 1, 8), dtype=dtype, device=DEV), torch.zeros((1, 1, 8), dtype=dtype, device=DEV)
+    rr, _, _ = L.block_norm(r, y, gate=u, post_norm=False, pre_norm=False)
+    ref = torch.sigmoid(u.double())
+    assert bool(((rr.double() - ref).abs() <= ref * (UNIT[dtype] * 1.01 + 500 * EPS) + 1e-37).all())
+
+
+def reference_grad(dn, dR, r, y, u, wp, wn, q, post, scale=SCALE):
+    """Gradients in 64 bits and bounds on what fp32 arithmetic makes of them."""
+    D = r.shape[2]
+    dn, dR, r, y, u, wp, wn, q = d(dn), d(dR), d(r), d(y), d(u), d(wp), d(wn), d(q)
+    one = torch.ones((r.shape[0], D), dtype=torch.float64)
+    wp, wn = (one if wp is None else wp)[:, None], (one if wn is None else wn)[:, None]
+    out, bound = {}, {}
+    eps = slack(D) + D / 2 * EPS                                      # a sum of D products besides
+    dr = torch.zeros_like(r) if dR is None else dR
+    br = dr.abs() * 4 * EPS
+    if dn is not None:
+        qn = q[1][..., None]
+        h, t = r * qn, dn * wn
+        dr = dr + qn * (t - h * (t * h).mean(2, keepdim=True))
+        br = br + eps * qn * (t.abs() + h.abs() * (t * h).abs().mean(2, keepdim=True))
+        out["dw_pre"], bound["dw_pre"] = (dn * h).sum(1), (dn * h).abs().sum(1) * (r.shape[1] + 16) * EPS
+    out["dr"], bound["dr"] = dr, br
+    if y is not None:
+        qp = q[0][..., None] if post else 1.0
+        a = torch.ones_like(y) if u is None else torch.sigmoid(u)
+        su = 8 * EPS if u is None else (8 + 2 * u.abs()) * EPS
+        z, e = y * qp, scale * dr * a
+        be = scale * br * a + e.abs() * su
+        if u is not None:
+            out["dgate"] = scale * dr * z * wp * a * (1 - a)
+            # 1 - a carries a's absolute error
+            bound["dgate"] = (scale * br * z.abs() * wp.abs() * a * (1 - a)) + (scale * dr * z * wp).abs() * a * su * 2 + out["dgate"].abs() * 8 * EPS
+        out["dw_post"], bound["dw_post"] = (e * z).sum(1), (be * z.abs()).sum(1) + (e * z).abs().sum(1) * (r.shape[1] + 16) * EPS
+        t, bt = e * wp, be * wp.abs()
+        if post:
+            out["dy"] = qp * (t - z * (t * z).mean(2, keepdim=True))
+            bound["dy"] = qp * (bt + z.abs() * (bt * z.abs()).mean(2, keepdim=True)) + eps * qp * (t.abs() + z.abs() * (t * z).abs().mean(2, keepdim=True))
+        else:
+            out["dy"], bound["dy"] = t, bt + t.abs() * 4 * EPS
+    return out, bound
+
+
+def check(got, out, bound, dtype):
+    for k, ref in out.items():
+        g = d(got[k])
+        unit = EPS if k.startswith("dw") else UNIT[dtype]
+        bad = (g - ref).abs() > bound[k] + unit * ref.abs() * 1.01
+        assert not bool(bad.any()), (k, int(bad.sum()), float(((g - ref).abs() / (bound[k] + unit * ref.abs() + 1e-300)).max()))
+
+
+@pytest.mark.parametrize("W,T,D", SHAPES)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("gate", [False, True])
+def test_grad(W, T, D, dtype, gate):
+    r, y = rnd(W, T, D, seed=1, dtype=dtype), rnd(W, T, D, seed=2, dtype=dtype, std=3.0)
+    dn, dR = rnd(W, T, D, seed=3, dtype=dtype), rnd(W, T, D, seed=4, dtype=dtype)
+    u = rnd(W, T, D, seed=5, dtype=dtype, std=2.0) if gate else None
+    wp, wn = weights(W, D, 6)
+    q = torch.stack([(t.float().square().mean(2) + NORM_EPS).rsqrt() for t in (y, r)])
+    grads = torch.full((W, 2 * D + 4), 9.0, device=DEV)
+    dwp, dwn = grads[:, 1:1 + D], grads[:, 2 + D:2 + 2 * D]
+    dr, dy, du = L.block_norm_grad(dn, dR, r, q, y, gate=u, w_post=wp, w_pre=wn, scale=SCALE, dw_post=dwp, dw_pre=dwn)
+    out, bound = reference_grad(dn, dR, r, y, u, wp, wn, q, True)
+    check({"dr": dr, "dy": dy, "dgate": du, "dw_post": dwp, "dw_pre": dwn}, out, bound, dtype)
+    assert bool((grads[:, 0] == 9).all()) and bool((grads[:, 1 + D] == 9).all()) and bool((grads[:, 2 + 2 * D:] == 9).all())
+    assert (du is None) == (not gate)
+
+
+def test_grad_parts_alone_and_accumulated():
+    W, T, D = 3, 300, 80
+    r, y = rnd(W, T, D, seed=1), rnd(W, T, D, seed=2)
+    dn, dR = rnd(W, T, D, seed=3), rnd(W, T, D, seed=4)
+    wp, wn = weights(W, D, 6, lead=2)
+    q = torch.stack([(t.square().mean(2) + NORM_EPS).rsqrt() for t in (y, r)])
+    # only a norm before the block: nothing comes past it
+    dwn = torch.zeros((W, D), device=DEV)
+    dr, dy, _ = L.block_norm_grad(dn, None, r, q, w_pre=wn, dw_pre=dwn)
+    out, bound = reference_grad(dn, None, r, None, None, None, wn, q, True)
+    assert dy is None
+    check({"dr": dr, "dw_pre": dwn}, out, bound, torch.float32)
+    # only the sum, the block's output not normed
+    dwp = torch.zeros((W, D), device=DEV)
+    dr, dy, _ = L.block_norm_grad(None, dR, r, q, y, w_post=wp, scale=SCALE, post_norm=False, dw_post=dwp)
+    out, bound = reference_grad(None, dR, r, y, None, wp, None, q, False)
+    check({"dr": dr, "dy": dy, "dw_post": dwp}, out, bound, torch.float32)
+    # added to what is there
+    base = rnd(W, D, seed=9)
+    acc = base.clone()
+    L.block_norm_grad(None, dR, r, q, y, w_post=wp, scale=SCALE, post_norm=False, dw_post=acc, accumulate=True)
+    assert torch.equal(acc, base + dwp)
+    # without the weights' gradients
+    dr2, dy2, _ = L.block_norm_grad(None, dR, r, q, y, w_post=wp, scale=SCALE, post_norm=False)
+    assert torch.equal(dr, dr2) and torch.equal(dy, dy2)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("D", [64, 101])
+def test_grad_strides_and_places(dtype, D):
+    W, T = 2, 19
+    two = rnd(W, T, 2 * D, seed=1, dtype=dtype)
+    u = two[:, :, :D]
+    r, y, dn = (rnd(W, T, D, seed=k, dtype=dtype) for k in (2, 3, 4))
+    dR = rnd(T, W, D, seed=5, dtype=dtype).transpose(0, 1)
+    q = torch.stack([(t.float().square().mean(2) + NORM_EPS).rsqrt() for t in (y, r)])
+    want = L.block_norm_grad(dn, dR.contiguous(), r, q, y, gate=u.contiguous(), scale=SCALE)
+    got = L.block_norm_grad(dn, dR, r, q, y, gate=u, scale=SCALE, dr=dR, dy=y, dgate=u)
+    for a, b in zip(want, got):
+        assert torch.equal(a, b)
+
+
+def test_grad_equal_calls_give_equal_bits():
+    W, T, D = 2, 3000, 256
+    r, y, dn, dR = (rnd(W, T, D, seed=k, dtype=torch.bfloat16) for k in range(4))
+    q = torch.ones((2, W, T), device=DEV)
+    got = []
+    for _ in range(2):
+        dw = torch.empty((2, W, D), device=DEV)
+        L.block_norm_grad(dn, dR, r, q, y, dw_post=dw[0], dw_pre=dw[1])
+        got.append(dw)
+    assert torch.equal(*got)
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_no_tokens(accumulate):
+    e = torch.empty((2, 0, 40), device=DEV)
+    rr, n, stats = L.block_norm(e, e)
+    assert tuple(n.shape) == (2, 0, 40) and tuple(stats.shape) == (2, 2, 0)
+    dw = torch.full((2, 40), 3.0, device=DEV)
+    L.block_norm_grad(e, e, e, stats, e, dw_post=dw, dw_pre=dw.clone(), accumulate=accumulate)
+    assert bool((dw == (3.0 if accumulate else 0.0)).all())
+
+
+def test_gradients_by_differences():
+    """Each gradient along a direction against the difference quotient of the forward formula in 64 bits."""
+    W, T, D = 2, 3, 24
+    g = torch.Generator().manual_seed(3)
+    R = lambda *s: torch.randn(s, generator=g).double()
+    v = {"r": R(W, T, D), "y": R(W, T, D), "gate": R(W, T, D), "w_post": R(W, D), "w_pre": R(W, D)}
+    cr, cn = R(W, T, D), R(W, T, D)
+
+    def f(a):
+        z = a["y"] * (a["y"].pow(2).mean(2, keepdim=True) + NORM_EPS).rsqrt()
+        r = a["r"] + SCALE * torch.sigmoid(a["gate"]) * z * a["w_post"][:, None]
+        n = r * (r.pow(2).mean(2, keepdim=True) + NORM_EPS).rsqrt() * a["w_pre"][:, None]
+        return float((cr * r).sum() + (cn * n).sum())
+
+    dv = {k: t.float().to(DEV) for k, t in v.items()}
+    rr, n, stats = L.block_norm(dv["r"], dv["y"], gate=dv["gate"], w_post=dv["w_post"], w_pre=dv["w_pre"], scale=SCALE, eps=NORM_EPS)
+    dw = torch.empty((2, W, D), device=DEV)
+    dr, dy, du = L.block_norm_grad(cn.float().to(DEV), cr.float().to(DEV), rr, stats, dv["y"], gate=dv["gate"], w_post=dv["w_post"],
+                                   w_pre=dv["w_pre"], scale=SCALE, dw_post=dw[0], dw_pre=dw[1])
+    got = {"r": dr, "y": dy, "gate": du, "w_post": dw[0], "w_pre": dw[1]}
+    h = 1e-5
+    for k in v:
+        dirn = R(*v[k].shape)
+        quotient = (f({**v, k: v[k] + h * dirn}) - f({**v, k: v[k] - h * dirn})) / (2 * h)
+        have = float((got[k].cpu().double() * dirn).sum())
+        # fp32 gradients of order-one elements: 200 eps of the sum of magnitudes; the quotient's error is of order h^2
+        assert abs(have - quotient) <= 200 * EPS * float((got[k].cpu().double() * dirn).abs().sum()) + 1e-6, k
+
+
+def test_on_a_stream_of_its_own():
+    s = torch.cuda.Stream()
+    r, y = rnd(2, 50, 128, seed=1), rnd(2, 50, 128, seed=2)
+    want = L.block_norm(r, y)
+    s.wait_stream(torch.cuda.current_stream())
+    got = L.block_norm(r, y, stream=s)
+    s.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+def test_refusals():
+    r = torch.zeros((2, 4, 16), device=DEV)
+    with pytest.raises(ValueError, match="nothing to do"):
+        L.block_norm(r, pre_norm=False)
+    with pytest.raises(ValueError, match="need y"):
+        L.block_norm(r, gate=r)
+    with pytest.raises(ValueError, match="float32"):
+        L.block_norm(r, r.bfloat16())
+    with pytest.raises(ValueError, match="dense"):
+        L.block_norm(torch.zeros((2, 16, 4), device=DEV).transpose(1, 2), r)
+    with pytest.raises(ValueError, match="w_pre"):
+        L.block_norm(r, w_pre=torch.zeros(16, device=DEV))
+    with pytest.raises(L.LsgdError, match="eps"):
+        L.block_norm(r, eps=0.0)
+    with pytest.raises(L.LsgdError, match="overlap"):
+        L.block_norm(r, r, r_out=torch.zeros((2, 1, 16), device=DEV).expand(2, 4, 16))
+    with pytest.raises(L.LsgdError, match="UNSUPPORTED"):
+        L.block_norm(torch.zeros((1, 1, 16385), device=DEV))
+    q = torch.ones((2, 2, 4), device=DEV)
+    with pytest.raises(ValueError, match="neither"):
+        L.block_norm_grad(None, None, r, q)
+    with pytest.raises(L.LsgdError, match="dw_pre needs dn"):
+        L.block_norm_grad(None, r, r, q, dw_pre=torch.zeros((2, 16), device=DEV))
+    with pytest.raises(ValueError, match="dw_post"):
+        L.block_norm_grad(r, r, r, q, dw_post=torch.zeros((2, 16), device=DEV))
+    with pytest.raises(L.LsgdError, match="NOMEM"):
+        L.block_norm_grad(r, r, r, q, dw_pre=torch.zeros((2, 16), device=DEV), workspace=torch.zeros(16, dtype=torch.uint8, device=DEV))
+    torch.cuda.synchronize()

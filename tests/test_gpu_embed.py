@@ -1,0 +1,216 @@
+"""Embedding lookup and its gradient against the definition in 64 bits, at the sizes where tiles, spans, digits of the sort
+and vector widths end, with padding and with tables that are columns of a population's rows."""
+import numpy as np
+import pytest
+import torch
+
+import paper_1905_10395_amd as L
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+EPS = 2.0 ** -24                 # half a last place of fp32, relative
+EPS_BF16 = 2.0 ** -8
+CANARY = 123.0
+
+
+def table_in_rows(W, V, D, lead, dtype=torch.float32, seed=0):
+    """A table that is columns [lead, lead + V*D) of wider rows, and the rows."""
+    g = torch.Generator().manual_seed(seed)
+    ld = lead + V * D + 5
+    x = torch.full((W, ld), CANARY)
+    x[:, lead:lead + V * D] = torch.randn((W, V * D), generator=g)
+    x = x.to(dtype).to(DEV)
+    return x, x[:, lead:lead + V * D].unflatten(1, (V, D))
+
+
+def draw_tokens(W, T, V, seed, kind="zipf"):
+    g = np.random.default_rng(seed)
+    if kind == "same":
+        tok = np.full((W, T), V - 1)
+    elif kind == "padding":
+        tok = np.where(g.random((W, T)) < 0.5, -1, V)
+    elif kind == "sorted":
+        tok = np.sort(g.integers(0, V, (W, T)), axis=1)
+    else:
+        tok = np.minimum(np.exp(g.random((W, T)) * np.log(V + 1.0)).astype(np.int64) - 1, V - 1)
+        odd = g.random((W, T))
+        tok = np.where(odd < 0.05, -1, np.where(odd < 0.08, V, np.where(odd < 0.1, -2**31, np.where(odd < 0.12, 2**31 - 1, tok))))
+    return torch.from_numpy(tok.astype(np.int32)).to(DEV)
+
+
+@pytest.mark.parametrize("W,T,V,D", [(1, 1, 1, 1), (2, 3, 5, 7), (3, 65, 17, 100), (2, 130, 1003, 256), (1, 1029, 40, 12), (4, 1, 1003, 1024)])
+@pytest.mark.parametrize("src", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("dst", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("lead", [0, 3])
+def test_lookup(W, T, V, D, src, dst, lead):
+    _, table = table_in_rows(W, V, D, lead, src, seed=T)
+    tok = draw_tokens(W, T, V, seed=D)
+    scale = float(np.float32(D ** 0.5))
+    out = L.embed_lookup(table, tok, scale=scale, dtype=dst)
+    t = tok.cpu().long()
+    ref = torch.zeros((W, T, D), dtype=torch.float64)
+    for w in range(W):
+        ok = (t[w] >= 0) & (t[w] < V)
+        ref[w, ok] = table[w].cpu().double()[t[w, ok]] * scale
+    err = (out.cpu().double() - ref).abs()
+    bound = ref.abs() * (EPS + (EPS_BF16 if dst == torch.bfloat16 else 0.0)) * 1.01
+    assert out.dtype == dst and bool((err <= bound).all())
+    assert bool((out.cpu()[(t < 0) | (t >= V)] == 0).all())
+
+
+def test_lookup_one_table_for_all_workers_and_into_a_buffer():
+    one = torch.randn((1, 50, 24), device=DEV)
+    tok = draw_tokens(3, 9, 50, seed=4)
+    wide = torch.full((3, 9 * 24 + 8), CANARY, device=DEV)
+    out = wide[:, :9 * 24].unflatten(1, (9, 24))
+    got = L.embed_lookup(one.expand(3, 50, 24), tok, out=out)
+    assert got is out and bool((wide[:, 9 * 24:] == CANARY).all())
+    assert torch.equal(out, L.embed_lookup(one.repeat(3, 1, 1), tok))
+
+
+def test_lookup_of_no_tokens():
+    out = L.embed_lookup(torch.randn((2, 5, 8), device=DEV), torch.empty((2, 0), dtype=torch.int32, device=DEV))
+    assert tuple(out.shape) == (2, 0, 8)
+
+
+def reference_grad(dout, tok, V, scale, before=None):
+    """(sum, sum of magnitudes, tokens of the row) in 64 bits."""
+    W, T, D = dout.shape
+    d, t = dout.cpu().double() * scale, tok.cpu().long()
+    s, m, n = (torch.zeros((W, V, D), dtype=torch.float64), torch.zeros((W, V, D), dtype=torch.float64), torch.zeros((W, V, 1), dtype=torch.float64))
+    for w in range(W):
+        ok = (t[w] >= 0) & (t[w] < V)
+        s[w].index_add_(0, t[w, ok], d[w, ok])
+        m[w].index_add_(0, t[w, ok], d[w, ok].abs())
+        n[w].index_add_(0, t[w, ok], torch.ones((int(ok.sum()), 1), dtype=torch.float64))
+    if before is not None:
+        s += before
+        m += before.abs()
+    return s, m, n
+
+
+GRAD_SHAPES = [(1, 1, 1, 1), (2, 2, 2, 3), (1, 31, 5, 8), (3, 33, 7, 101), (2, 517, 131, 64), (1, 1000, 1023, 520), (1, 1000, 1024, 16),
+               (2, 4099, 300, 36), (1, 8192, 2000, 24), (1, 8193, 70000, 8), (2, 20000, 2500, 132), (1, 40000, 3, 40)]
+
+
+@pytest.mark.parametrize("W,T,V,D", GRAD_SHAPES)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_grad(W, T, V, D, dtype, accumulate):
+    lead = 0 if D % 4 == 0 else 3
+    rows, dtable = table_in_rows(W, V, D, lead, seed=1)
+    before = dtable.cpu().double() if accumulate else None
+    tok = draw_tokens(W, T, V, seed=T + V)
+    g = torch.Generator().manual_seed(7)
+    dout = torch.randn((W, T, D), generator=g).to(dtype).to(DEV)
+    scale = 1.75
+    ref, mag, n = reference_grad(dout, tok, V, scale, before)
+    L.embed_grad(dout, tok, dtable, scale=scale, accumulate=accumulate)
+    got = dtable.cpu().double()
+    # n additions in fp32 in some order, the product with the scale, the sum with what was there
+    assert bool(((got - ref).abs() <= mag * (n + 3) * EPS).all())
+    rows = rows.cpu()
+    assert bool((rows[:, :lead] == CANARY).all()) and bool((rows[:, lead + V * D:] == CANARY).all())
+    if accumulate:
+        assert torch.equal(got[(n == 0).expand_as(got)], before[(n == 0).expand_as(got)])
+    else:
+        assert bool((got[(n == 0).expand_as(got)] == 0).all())
+
+
+@pytest.mark.parametrize("kind", ["same", "padding", "sorted"])
+@pytest.mark.parametrize("W,T,V,D", [(2, 100, 9, 40), (1, 9000, 700, 72), (1, 30011, 5, 8)])
+def test_grad_of_lopsided_batches(kind, W, T, V, D):
+    tok = draw_tokens(W, T, V, seed=3, kind=kind)
+    dout = torch.randn((W, T, D), generator=torch.Generator().manual_seed(2)).to(torch.bfloat16).to(DEV)
+    dtable = torch.full((W, V, D), CANARY, device=DEV)
+    ref, mag, n = reference_grad(dout, tok, V, 1.0)
+    L.embed_grad(dout, tok, dtable)
+    assert bool(((dtable.cpu().double() - ref).abs() <= mag * (n + 3) * EPS).all())
+
+
+def test_grad_equal_calls_give_equal_bits():
+    tok = draw_tokens(2, 12000, 900, seed=5)
+    dout = torch.randn((2, 12000, 48), device=DEV)
+    a, b = torch.empty((2, 900, 48), device=DEV), torch.empty((2, 900, 48), device=DEV)
+    L.embed_grad(dout, tok, a)
+    L.embed_grad(dout, tok, b)
+    assert torch.equal(a, b)
+
+
+def test_grad_adds_what_is_not_finite_to_its_own_row_only():
+    tok = torch.tensor([[0, 1, 0, 2, -1]], dtype=torch.int32, device=DEV)
+    dout = torch.ones((1, 5, 16), device=DEV)
+    dout[0, 1, 3], dout[0, 2, 5], dout[0, 4] = float("nan"), float("inf"), float("nan")   # the last is padding's
+    dtable = torch.empty((1, 4, 16), device=DEV)
+    L.embed_grad(dout, tok, dtable)
+    ref = torch.zeros((4, 16))
+    ref[0], ref[1], ref[2] = 2.0, 1.0, 1.0
+    ref[0, 5], ref[1, 3] = float("inf"), float("nan")
+    assert torch.equal(torch.nan_to_num(dtable[0].cpu(), nan=-7.0), torch.nan_to_num(ref, nan=-7.0))
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_grad_of_no_tokens(accumulate):
+    dtable = torch.full((2, 300, 7), CANARY, device=DEV)
+    L.embed_grad(torch.empty((2, 0, 7), device=DEV), torch.empty((2, 0), dtype=torch.int32, device=DEV), dtable, accumulate=accumulate)
+    assert bool((dtable == (CANARY if accumulate else 0.0)).all())
+
+
+def test_grad_is_the_lookups_by_differences():
+    """<gradient of sum(c * lookup), direction> against the difference quotient of the lookup's definition."""
+    W, T, V, D, scale = 2, 40, 11, 12, 3.0
+    g = torch.Generator().manual_seed(9)
+    tok = draw_tokens(W, T, V, seed=1)
+    E, dirn, c = (torch.randn(s, generator=g, dtype=torch.float64) for s in ((W, V, D), (W, V, D), (W, T, D)))
+    c = c.float().double()
+    t = tok.cpu().long()
+    ok = (t >= 0) & (t < V)
+    f = lambda e: float((c * scale * e[torch.arange(W)[:, None], t.clamp(0, V - 1)] * ok[..., None]).sum())
+    h = 1e-4
+    quotient = (f(E + h * dirn) - f(E - h * dirn)) / (2 * h)
+    dtable = torch.empty((W, V, D), device=DEV)
+    L.embed_grad(c.float().to(DEV), tok, dtable, scale=scale)
+    got = float((dtable.cpu().double() * dirn).sum())
+    # f is linear: the quotient's own error is f's rounding over 2h; the gradient's is that of its elements
+    mag = float((c.abs() * scale).sum() * dirn.abs().max())
+    assert abs(got - quotient) <= 45 * EPS * mag + 1e-10 * mag
+
+
+def test_on_a_stream_of_its_own():
+    s = torch.cuda.Stream()
+    tok = draw_tokens(2, 700, 90, seed=6)
+    x, table = table_in_rows(2, 90, 64, 0)
+    dout = torch.randn((2, 700, 64), device=DEV)
+    want, dwant = L.embed_lookup(table, tok), torch.empty((2, 90, 64), device=DEV)
+    L.embed_grad(dout, tok, dwant)
+    s.wait_stream(torch.cuda.current_stream())
+    got = L.embed_lookup(table, tok, stream=s)
+    dgot = torch.empty((2, 90, 64), device=DEV)
+    s.wait_stream(torch.cuda.current_stream())
+    L.embed_grad(dout, tok, dgot, stream=s)
+    s.synchronize()
+    assert torch.equal(got, want) and torch.equal(dgot, dwant)
+
+
+def test_refusals():
+    f = lambda *s: torch.zeros(s, device=DEV)
+    tok = torch.zeros((2, 4), dtype=torch.int32, device=DEV)
+    with pytest.raises(ValueError, match="int32"):
+        L.embed_lookup(f(2, 5, 8), tok.long())
+    with pytest.raises(ValueError, match="workers"):
+        L.embed_lookup(f(3, 5, 8), tok)
+    with pytest.raises(ValueError, match="dense"):
+        L.embed_lookup(f(2, 5, 16)[:, :, :8], tok)
+    with pytest.raises(ValueError, match="not on a GPU"):
+        L.embed_lookup(f(2, 5, 8), tok.cpu())
+    with pytest.raises(L.LsgdError, match="INVALID_ARG.*scale"):
+        L.embed_lookup(f(2, 5, 8), tok, scale=float("nan"))
+    with pytest.raises(ValueError, match="dense"):
+        L.embed_grad(f(2, 1, 8).expand(2, 4, 8), tok, f(2, 5, 8))
+    with pytest.raises(ValueError, match="float32"):
+        L.embed_grad(f(2, 4, 8), tok, f(2, 5, 8).bfloat16())
+    with pytest.raises(L.LsgdError, match="overlap"):
+        L.embed_grad(f(2, 4, 8), tok, f(1, 5, 8).expand(2, 5, 8))
+    with pytest.raises(L.LsgdError, match="NOMEM"):
+        L.embed_grad(f(2, 4, 8), tok, f(2, 5, 8), workspace=torch.zeros(64, dtype=torch.uint8, device=DEV))
+    torch.cuda.synchronize()
