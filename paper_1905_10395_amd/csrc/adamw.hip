@@ -16,9 +16,11 @@
 // kept on average.  Between two codes v (not its root) is interpolated, or the second moment would be biased upwards.
 //
 // Bound by memory: 28 bytes an element (x, m, v read and written, g read) with 32-bit moments, 16 with 8-bit ones.
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 #include <new>
+#include <type_traits>
 #include <vector>
 
 #include "common.h"
@@ -28,13 +30,24 @@ using namespace lsgd;
 namespace {
 
 typedef float v4f __attribute__((ext_vector_type(4)));
+typedef float v2f __attribute__((ext_vector_type(2)));
 typedef uint32_t v2u __attribute__((ext_vector_type(2)));
 
-constexpr int kThreads = 256;
 constexpr int kBlock = LSGD_ADAMW_BLOCK;             // elements that share a scale: one wavefront, four each
 static_assert(kBlock == 4 * kWave, "a wavefront holds one block");
-constexpr int kChunk = 4096;                         // elements of one workgroup
+// Elements of one workgroup.  Short pieces in memory order keep what the chip has open in a few DRAM pages: 268 M parameters
+// of 30 bytes in 1.54 ms with 4096 elements a workgroup, 1.46 ms with 2048, 1.39 with 1024.
+constexpr int kChunk = 1024;
+constexpr int kThreads32 = kChunk / 2;               // 8-byte lanes: 1.33 ms, against 1.39 with 16-byte ones
+constexpr int kThreads = kChunk / 4;
 constexpr float kTopM = 127.0f * 127.0f, kTopV = 255.0f * 255.0f;
+
+// Every byte is touched once a step; accesses that do not stay in the caches are the faster ones only if reads and writes
+// both are such (1.50 to 1.52 ms with either alone).
+template <class V>
+__device__ __forceinline__ V load_once(const V* p) { return __builtin_nontemporal_load(p); }
+template <class V>
+__device__ __forceinline__ void store_once(V v, V* p) { __builtin_nontemporal_store(v, p); }
 
 // A tensor as the kernels see it.
 struct Tensor {
@@ -47,7 +60,7 @@ struct Tensor {
     int64_t ld_x, ld_g, ld_s, ld_scale, ld_b, ld_values;
     int64_t n;
     double wd, lr_mult;
-    int32_t wide, wide_values;                       // every row of every array starts on a four-element boundary
+    int32_t wide, wide_values;                       // every row of every array starts on a boundary of four elements (32-bit moments: two)
 };
 
 // What one workgroup does: elements [start, min(start + kChunk, n)) of one row.
@@ -95,20 +108,28 @@ __device__ __forceinline__ float grad1(const void* g, int64_t i)
 }
 
 template <class G>
+__device__ __forceinline__ v2f grad2(const void* g, int64_t i)
+{
+    if constexpr (sizeof(G) == 4) return load_once(reinterpret_cast<const v2f*>(static_cast<const float*>(g) + i));
+    else {
+        const uint32_t b = load_once(reinterpret_cast<const uint32_t*>(static_cast<const uint16_t*>(g) + i));
+        return v2f{__uint_as_float(b << 16), __uint_as_float(b & 0xFFFF0000u)};
+    }
+}
+
+template <class G>
 __device__ __forceinline__ v4f grad4(const void* g, int64_t i)
 {
-    if constexpr (sizeof(G) == 4) return *reinterpret_cast<const v4f*>(static_cast<const float*>(g) + i);
+    if constexpr (sizeof(G) == 4) return load_once(reinterpret_cast<const v4f*>(static_cast<const float*>(g) + i));
     else {
-        const v2u b = *reinterpret_cast<const v2u*>(static_cast<const uint16_t*>(g) + i);
+        const v2u b = load_once(reinterpret_cast<const v2u*>(static_cast<const uint16_t*>(g) + i));
         return v4f{__uint_as_float(b.x << 16), __uint_as_float(b.x & 0xFFFF0000u), __uint_as_float(b.y << 16), __uint_as_float(b.y & 0xFFFF0000u)};
     }
 }
 
-__device__ __forceinline__ v2u shadow4(v4f x) { return v2u{f32x2_to_bf16x2(x.x, x.y), f32x2_to_bf16x2(x.z, x.w)}; }
-
 // ---- 32-bit moments ----
 template <class G>
-__global__ __launch_bounds__(kThreads) void adamw32_kernel(const Tensor* __restrict__ tensors, const Work* __restrict__ works, Step p)
+__global__ __launch_bounds__(kThreads32) void adamw32_kernel(const Tensor* __restrict__ tensors, const Work* __restrict__ works, Step p)
 {
     const Work w = works[blockIdx.x];
     const Tensor t = tensors[w.tensor];
@@ -120,28 +141,27 @@ __global__ __launch_bounds__(kThreads) void adamw32_kernel(const Tensor* __restr
     const void* g = static_cast<const char*>(t.g) + w.row * t.ld_g * (int64_t)sizeof(G);
     uint16_t* xb = t.xb ? t.xb + w.row * t.ld_b : nullptr;
     float r;
-    int64_t i = w.start;
-    if (t.wide) {
-        const int64_t end4 = w.start + ((end - w.start) & ~(int64_t)3);
-        for (int64_t k = w.start + 4 * threadIdx.x; k < end4; k += 4 * kThreads) {
-            v4f xv = *reinterpret_cast<const v4f*>(x + k);
-            const v4f gv = grad4<G>(g, k);
-            v4f mv = *reinterpret_cast<const v4f*>(m + k);
-            v4f vv = *reinterpret_cast<const v4f*>(v + k);
+    int64_t i = w.start + 2 * threadIdx.x;
+    if (t.wide && i + 2 <= end) {
+        v2f xv = load_once(reinterpret_cast<const v2f*>(x + i));
+        const v2f gv = grad2<G>(g, i);
+        v2f mv = load_once(reinterpret_cast<const v2f*>(m + i));
+        v2f vv = load_once(reinterpret_cast<const v2f*>(v + i));
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                float xe = xv[e], me = mv[e], ve = vv[e];
-                update(xe, gv[e], me, ve, r, c, p);
-                xv[e] = xe; mv[e] = me; vv[e] = ve;
-            }
-            *reinterpret_cast<v4f*>(x + k) = xv;
-            *reinterpret_cast<v4f*>(m + k) = mv;
-            *reinterpret_cast<v4f*>(v + k) = vv;
-            if (xb) *reinterpret_cast<v2u*>(xb + k) = shadow4(xv);
+        for (int e = 0; e < 2; ++e) {
+            float xe = xv[e], me = mv[e], ve = vv[e];
+            update(xe, gv[e], me, ve, r, c, p);
+            xv[e] = xe; mv[e] = me; vv[e] = ve;
         }
-        i = end4;
+        store_once(xv, reinterpret_cast<v2f*>(x + i));
+        store_once(mv, reinterpret_cast<v2f*>(m + i));
+        store_once(vv, reinterpret_cast<v2f*>(v + i));
+        if (xb) store_once(f32x2_to_bf16x2(xv.x, xv.y), reinterpret_cast<uint32_t*>(xb + i));
+        return;
     }
-    for (i += threadIdx.x; i < end; i += kThreads) {
+    // not aligned: one element a lane at a time; aligned: what is left at the row's end is one element, of the lane it fell to
+    const int64_t step = t.wide ? 2 : kThreads32;
+    for (i = t.wide ? i : w.start + threadIdx.x; i < end; i += step) {
         float xe = x[i], me = m[i], ve = v[i];
         update(xe, grad1<G>(g, i), me, ve, r, c, p);
         x[i] = xe; m[i] = me; v[i] = ve;
@@ -150,53 +170,76 @@ __global__ __launch_bounds__(kThreads) void adamw32_kernel(const Tensor* __restr
 }
 
 // ---- 8-bit moments ----
+// The wavefront's largest value, in a scalar register (NaN counts as nothing).
 __device__ __forceinline__ float wave_max(float a)
 {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) a = fmaxf(a, __shfl_xor(a, o));
-    return a;
+    auto step = [&](auto ctrl) {
+        const int b = __builtin_amdgcn_update_dpp(__float_as_int(a), __float_as_int(a), decltype(ctrl)::value, 0xF, 0xF, false);
+        a = fmaxf(a, __int_as_float(b));
+    };
+    step(std::integral_constant<int, 0x111>{});      // the lane one to the left, in its row of 16
+    step(std::integral_constant<int, 0x112>{});
+    step(std::integral_constant<int, 0x114>{});
+    step(std::integral_constant<int, 0x118>{});      // the row's last lane has the row's largest
+    step(std::integral_constant<int, 0x142>{});      // to the next row, to the upper half
+    step(std::integral_constant<int, 0x143>{});
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(a), kWave - 1));
 }
 
 __device__ __forceinline__ bool finite(float a) { return fabsf(a) < __builtin_inff(); }
 
-// Scale of a block whose largest finite value is `big`, and its reciprocal; blocks of next to nothing are held as zero.
-__device__ __forceinline__ float scale_of(float big, float top, float& inv)
+__device__ __forceinline__ float largest(const float (&a)[4])
 {
-    float s = big * (1.0f / top);
+    const float big = wave_max(fmaxf(fmaxf(fabsf(a[0]), fabsf(a[1])), fmaxf(fabsf(a[2]), fabsf(a[3]))));
+    if (big < __builtin_inff()) return big;
+    float f = 0.0f;                                  // the largest finite one, then
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f = fmaxf(f, finite(a[e]) ? fabsf(a[e]) : 0.0f);
+    return wave_max(f);
+}
+
+struct Scales {
+    float m, v, inv_m, inv_v;
+};
+
+// Scales of a block whose largest finite moments are bm and bv, and their reciprocals; blocks of next to nothing are held
+// as zero.  One quotient for both: half of the wavefront divides for m, half for v.
+__device__ __forceinline__ Scales scales_of(float bm, float bv)
+{
+    const bool low = (threadIdx.x & (kWave - 1)) < kWave / 2;
+    float s = (low ? bm : bv) * (low ? 1.0f / kTopM : 1.0f / kTopV);
     if (!(s > 0x1p-100f)) s = 0.0f;
-    inv = s > 0.0f ? 1.0f / s : 0.0f;
-    return s;
+    const float inv = s > 0.0f ? 1.0f / s : 0.0f;
+    Scales q;
+    q.m = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(s), 0));
+    q.v = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(s), kWave - 1));
+    q.inv_m = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(inv), 0));
+    q.inv_v = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(inv), kWave - 1));
+    return q;
 }
 
-// The largest whole c with c*c <= y (0 <= y <= 65025): an approximate root is at most one off.
-__device__ __forceinline__ float floor_root(float y)
+// Codes.  c = floor(root of y) comes from an approximate root and may be one off where y is next to a square; the
+// threshold u lies far enough from 0 and 1 that the code taken is then the same: just below (c+1)^2 both choices end at c+1,
+// just above c^2 both at c.  All integers below are exact in fp32.  What is not finite gets the largest code (the parameter
+// it belongs to is not finite either).
+__device__ __forceinline__ int code_m(float m, float inv, float u)
 {
 #pragma clang fp contract(off)
-    float c = floorf(__builtin_amdgcn_sqrtf(y));
-    if (c * c > y) c -= 1.0f;
-    if ((c + 1.0f) * (c + 1.0f) <= y) c += 1.0f;
-    return c;
+    const float y = fminf(fabsf(m) * inv, kTopM);
+    const float c = floorf(__builtin_amdgcn_sqrtf(y));
+    const int q = (int)c + (__builtin_fmaf(-c, c, y) > u * __builtin_fmaf(2.0f, c, 1.0f) ? 1 : 0);
+    return m < 0.0f ? -q : q;
 }
 
-// A value that is not finite is held as the block's largest one (the parameter it belongs to is not finite either).
-__device__ __forceinline__ float code_m(float m, float s, float inv, float u)
+__device__ __forceinline__ int code_v(float r, float inv, float u, int least)
 {
 #pragma clang fp contract(off)
-    const float a = fabsf(m);
-    const float y = finite(a) ? fminf(a * inv, kTopM) : (s > 0.0f ? kTopM : 0.0f);
-    float c = floor_root(y);
-    if (y - c * c > u * (2.0f * c + 1.0f)) c += 1.0f;
-    return m < 0.0f ? -c : c;
-}
-
-__device__ __forceinline__ float code_v(float r, float s, float inv, float u)
-{
-#pragma clang fp contract(off)
-    const float y = finite(r) ? fminf(r * inv, kTopV) : (s > 0.0f ? kTopV : 0.0f);
-    float c = floor_root(y);
-    const float c2 = c * c, d2 = (c + 1.0f) * (c + 1.0f);
-    if ((y - c2) * (y + c2) > u * ((d2 - c2) * (d2 + c2))) c += 1.0f;
-    return r > 0.0f && s > 0.0f ? fmaxf(c, 1.0f) : c;        // a second moment that is not zero is not held as zero
+    const float y = fminf(r * inv, kTopV);
+    const float c = floorf(__builtin_amdgcn_sqrtf(y));
+    const float c2 = c * c, odd = __builtin_fmaf(2.0f, c, 1.0f);                 // (c+1)^2 - c^2
+    const float both = __builtin_fmaf(c, odd, c + 1.0f);                         // (c+1)^2 + c^2
+    const int q = (int)c + ((y - c2) * (y + c2) > u * (odd * both) ? 1 : 0);
+    return r > 0.0f && q < least ? least : q;                                    // a second moment that is not zero is not held as zero
 }
 
 __device__ __forceinline__ float value_m(int q, float s)
@@ -210,96 +253,89 @@ __device__ __forceinline__ float value_r(int q, float s)
     return c * c * s;
 }
 
-// A wavefront takes whole blocks: its lanes hold four elements each, adjacent ones where the arrays allow wide accesses.
+// A wavefront takes a block: its lanes hold four elements each, adjacent ones where the arrays allow wide accesses.
 template <class G>
 __global__ __launch_bounds__(kThreads) void adamw8_kernel(const Tensor* __restrict__ tensors, const Work* __restrict__ works, Step p)
 {
     const Work w = works[blockIdx.x];
     const Tensor t = tensors[w.tensor];
     const Coef c = coefficients(t, p);
-    const int64_t end = w.start + kChunk < t.n ? w.start + kChunk : t.n;
+    const int lane = threadIdx.x & (kWave - 1);
+    const int64_t b = w.start / kBlock + __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+    const int64_t first = b * kBlock;
+    if (first >= t.n) return;
     float* x = t.x + w.row * t.ld_x;
     int8_t* m = static_cast<int8_t*>(t.m) + w.row * t.ld_s;
     uint8_t* v = static_cast<uint8_t*>(t.v) + w.row * t.ld_s;
-    float* ms = t.m_scale + w.row * t.ld_scale;
-    float* vs = t.v_scale + w.row * t.ld_scale;
+    float* ms = t.m_scale + w.row * t.ld_scale + b;
+    float* vs = t.v_scale + w.row * t.ld_scale + b;
     const void* g = static_cast<const char*>(t.g) + w.row * t.ld_g * (int64_t)sizeof(G);
     uint16_t* xb = t.xb ? t.xb + w.row * t.ld_b : nullptr;
-    const int lane = threadIdx.x & (kWave - 1);
-    for (int64_t b = w.start / kBlock + threadIdx.x / kWave; b * kBlock < end; b += kThreads / kWave) {
-        const int64_t first = b * kBlock;
-        const float sm = ms[b], sv = vs[b];
-        float xe[4], me[4], re[4];
-        const bool wide = t.wide && first + kBlock <= end;
-        const int64_t k = first + 4 * lane;
-        if (wide) {
-            const v4f xv = *reinterpret_cast<const v4f*>(x + k);
-            const v4f gv = grad4<G>(g, k);
-            const uint32_t mq = *reinterpret_cast<const uint32_t*>(m + k), vq = *reinterpret_cast<const uint32_t*>(v + k);
+    const float sm = *ms, sv = *vs;
+    const bool wide = t.wide && first + kBlock <= t.n;
+    const int64_t k = first + 4 * lane;
+    float xe[4], me[4], re[4];
+    if (wide) {
+        const v4f xv = load_once(reinterpret_cast<const v4f*>(x + k));
+        const v4f gv = grad4<G>(g, k);
+        const uint32_t mq = load_once(reinterpret_cast<const uint32_t*>(m + k)), vq = load_once(reinterpret_cast<const uint32_t*>(v + k));
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                xe[e] = xv[e];
-                me[e] = value_m((int)(int8_t)(mq >> (8 * e)), sm);
-                const float rr = value_r((int)(vq >> (8 * e) & 255u), sv);
+        for (int e = 0; e < 4; ++e) {
+            xe[e] = xv[e];
+            me[e] = value_m((int)(int8_t)(mq >> (8 * e)), sm);
+            const float rr = value_r((int)(vq >> (8 * e) & 255u), sv);
+            float ve = rr * rr;
+            update(xe[e], gv[e], me[e], ve, re[e], c, p);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int64_t i = first + lane + e * kWave;
+            xe[e] = me[e] = re[e] = 0.0f;
+            if (i < t.n) {
+                xe[e] = x[i];
+                me[e] = value_m(m[i], sm);
+                const float rr = value_r(v[i], sv);
                 float ve = rr * rr;
-                update(xe[e], gv[e], me[e], ve, re[e], c, p);
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int64_t i = first + lane + e * kWave;
-                xe[e] = me[e] = re[e] = 0.0f;
-                if (i < end) {
-                    xe[e] = x[i];
-                    me[e] = value_m(m[i], sm);
-                    const float rr = value_r(v[i], sv);
-                    float ve = rr * rr;
-                    update(xe[e], grad1<G>(g, i), me[e], ve, re[e], c, p);
-                }
+                update(xe[e], grad1<G>(g, i), me[e], ve, re[e], c, p);
             }
         }
-        float bm = 0.0f, bv = 0.0f;
+    }
+    const Scales s = scales_of(largest(me), largest(re));
+    const int least = s.v > 0.0f ? 1 : 0;
+    int qm[4], qv[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        qm[e] = code_m(me[e], s.inv_m, p.um);
+        qv[e] = code_v(re[e], s.inv_v, p.uv, least);
+    }
+    if (wide) {
+        uint32_t mq = 0, vq = 0;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            if (finite(me[e])) bm = fmaxf(bm, fabsf(me[e]));
-            if (finite(re[e])) bv = fmaxf(bv, re[e]);
+            mq |= (uint32_t)(qm[e] & 255) << (8 * e);
+            vq |= (uint32_t)qv[e] << (8 * e);
         }
-        float im, iv;
-        const float nm = scale_of(wave_max(bm), kTopM, im), nv = scale_of(wave_max(bv), kTopV, iv);
-        int qm[4], qv[4];
+        const v4f xv = {xe[0], xe[1], xe[2], xe[3]};
+        store_once(xv, reinterpret_cast<v4f*>(x + k));
+        store_once(mq, reinterpret_cast<uint32_t*>(m + k));
+        store_once(vq, reinterpret_cast<uint32_t*>(v + k));
+        if (xb) store_once(v2u{f32x2_to_bf16x2(xv.x, xv.y), f32x2_to_bf16x2(xv.z, xv.w)}, reinterpret_cast<v2u*>(xb + k));
+    } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            qm[e] = (int)code_m(me[e], nm, im, p.um);
-            qv[e] = (int)code_v(re[e], nv, iv, p.uv);
-        }
-        if (wide) {
-            uint32_t mq = 0, vq = 0;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                mq |= (uint32_t)(qm[e] & 255) << (8 * e);
-                vq |= (uint32_t)qv[e] << (8 * e);
-            }
-            const v4f xv = {xe[0], xe[1], xe[2], xe[3]};
-            *reinterpret_cast<v4f*>(x + k) = xv;
-            *reinterpret_cast<uint32_t*>(m + k) = mq;
-            *reinterpret_cast<uint32_t*>(v + k) = vq;
-            if (xb) *reinterpret_cast<v2u*>(xb + k) = shadow4(xv);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int64_t i = first + lane + e * kWave;
-                if (i < end) {
-                    x[i] = xe[e];
-                    m[i] = (int8_t)qm[e];
-                    v[i] = (uint8_t)qv[e];
-                    if (xb) xb[i] = f32_to_bf16_rne(xe[e]);
-                }
+            const int64_t i = first + lane + e * kWave;
+            if (i < t.n) {
+                x[i] = xe[e];
+                m[i] = (int8_t)qm[e];
+                v[i] = (uint8_t)qv[e];
+                if (xb) xb[i] = f32_to_bf16_rne(xe[e]);
             }
         }
-        if (lane == 0) {
-            ms[b] = nm;
-            vs[b] = nv;
-        }
+    }
+    if (lane == 0) {
+        *ms = s.m;
+        *vs = s.v;
     }
 }
 
@@ -317,25 +353,23 @@ __global__ __launch_bounds__(kThreads) void adamw8_values_kernel(const Tensor* _
     const float* vs = t.v_scale + w.row * t.ld_scale;
     float* om = t.m_values + w.row * t.ld_values;
     float* ov = t.v_values + w.row * t.ld_values;
-    int64_t i = w.start;
-    if (t.wide_values) {
-        const int64_t end4 = w.start + ((end - w.start) & ~(int64_t)3);
-        for (int64_t k = w.start + 4 * threadIdx.x; k < end4; k += 4 * kThreads) {
-            const uint32_t mq = *reinterpret_cast<const uint32_t*>(m + k), vq = *reinterpret_cast<const uint32_t*>(v + k);
-            const float sm = ms[k / kBlock], sv = vs[k / kBlock];
-            v4f a, b;
+    const int64_t k = w.start + 4 * threadIdx.x;
+    if (t.wide_values && k + 4 <= end) {
+        const uint32_t mq = load_once(reinterpret_cast<const uint32_t*>(m + k)), vq = load_once(reinterpret_cast<const uint32_t*>(v + k));
+        const float sm = ms[k / kBlock], sv = vs[k / kBlock];
+        v4f a, b;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                a[e] = value_m((int)(int8_t)(mq >> (8 * e)), sm);
-                const float r = value_r((int)(vq >> (8 * e) & 255u), sv);
-                b[e] = r * r;
-            }
-            *reinterpret_cast<v4f*>(om + k) = a;
-            *reinterpret_cast<v4f*>(ov + k) = b;
+        for (int e = 0; e < 4; ++e) {
+            a[e] = value_m((int)(int8_t)(mq >> (8 * e)), sm);
+            const float r = value_r((int)(vq >> (8 * e) & 255u), sv);
+            b[e] = r * r;
         }
-        i = end4;
+        store_once(a, reinterpret_cast<v4f*>(om + k));
+        store_once(b, reinterpret_cast<v4f*>(ov + k));
+        return;
     }
-    for (i += threadIdx.x; i < end; i += kThreads) {
+    const int64_t step = t.wide_values ? 1 : kThreads;
+    for (int64_t i = t.wide_values ? k : w.start + threadIdx.x; i < end; i += step) {
         om[i] = value_m(m[i], ms[i / kBlock]);
         const float r = value_r(v[i], vs[i / kBlock]);
         ov[i] = r * r;
@@ -439,9 +473,9 @@ lsgd_status lsgd_adamw_create(const lsgd_adamw_tensor* tensors, int32_t n_tensor
             // one row: its stride is never multiplied by anything, so it does not matter to the alignment either
             auto ld = [&](int64_t v) { return a.rows > 1 ? v : (int64_t)0; };
             t.ld_x = ld(a.ld_x); t.ld_g = ld(a.ld_g); t.ld_s = ld(a.ld_state); t.ld_b = a.x_bf16 ? ld(a.ld_bf16) : 0;
-            const uintptr_t es = state_bits == 32 ? 16 : 4;
-            t.wide = on(t.x, 16) && on(t.g, g_is_bf16 ? 8 : 16) && on(t.m, es) && on(t.v, es) && on(t.xb, 8) &&
-                     (t.ld_x | t.ld_g | t.ld_s | t.ld_b) % 4 == 0;
+            const uintptr_t lanes = state_bits == 32 ? 2 : 4, es = state_bits == 32 ? 8 : 4;
+            t.wide = on(t.x, 4 * lanes) && on(t.g, (g_is_bf16 ? 2 : 4) * lanes) && on(t.m, es) && on(t.v, es) && on(t.xb, 2 * lanes) &&
+                     (t.ld_x | t.ld_g | t.ld_s | t.ld_b) % (int64_t)lanes == 0;
             if (state_bits == 8) {
                 t.m_scale = a.m_scale; t.v_scale = a.v_scale; t.ld_scale = ld(a.ld_scale);
                 t.m_values = a.m_values; t.v_values = a.v_values; t.ld_values = ld(a.ld_values);
@@ -506,9 +540,11 @@ lsgd_status lsgd_adamw_step(lsgd_adamw* opt, double lr, double beta1, double bet
     p.eps = (float)eps;
     p.gscale = (float)grad_scale;
     constexpr double kGolden = 0.6180339887498949;
-    p.uv = (float)std::fmod((double)step * kGolden, 1.0);
-    p.um = (float)std::fmod((double)step * kGolden + 0.5, 1.0);
-    const dim3 grid((unsigned)opt->n_works), block(kThreads);
+    // not nearer to 0 and 1 than 2^-12: see the codes
+    auto inside = [](double u) { return (float)std::min(std::max(u, 0x1p-12), 1.0 - 0x1p-12); };
+    p.uv = inside(std::fmod((double)step * kGolden, 1.0));
+    p.um = inside(std::fmod((double)step * kGolden + 0.5, 1.0));
+    const dim3 grid((unsigned)opt->n_works), block(opt->bits == 32 ? kThreads32 : kThreads);
     if (opt->bits == 32) {
         if (opt->g_is_bf16) hipLaunchKernelGGL((adamw32_kernel<uint16_t>), grid, block, 0, opt->stream, opt->tensors, opt->works, p);
         else hipLaunchKernelGGL((adamw32_kernel<float>), grid, block, 0, opt->stream, opt->tensors, opt->works, p);
