@@ -42,12 +42,21 @@ constexpr int kThreads32 = kChunk / 2;               // 8-byte lanes: 1.33 ms, a
 constexpr int kThreads = kChunk / 4;
 constexpr float kTopM = 127.0f * 127.0f, kTopV = 255.0f * 255.0f;
 
+// Pointers that come from a table in memory: told to be global memory's, or the compiler's generic accesses go by the LDS
+// path as well.
+template <class V>
+using Global = __attribute__((address_space(1))) V;
+
 // Every byte is touched once a step; accesses that do not stay in the caches are the faster ones only if reads and writes
 // both are such (1.50 to 1.52 ms with either alone).
 template <class V>
-__device__ __forceinline__ V load_once(const V* p) { return __builtin_nontemporal_load(p); }
+__device__ __forceinline__ V load_once(const V* p) { return __builtin_nontemporal_load((const Global<V>*)p); }
 template <class V>
-__device__ __forceinline__ void store_once(V v, V* p) { __builtin_nontemporal_store(v, p); }
+__device__ __forceinline__ void store_once(V v, V* p) { __builtin_nontemporal_store(v, (Global<V>*)p); }
+template <class V>
+__device__ __forceinline__ V load(const V* p) { return *(const Global<V>*)p; }
+template <class V, class U>
+__device__ __forceinline__ void store(U v, V* p) { *(Global<V>*)p = (V)v; }
 
 // A tensor as the kernels see it.
 struct Tensor {
@@ -103,8 +112,8 @@ __device__ __forceinline__ void update(float& x, float g, float& m, float& v, fl
 template <class G>
 __device__ __forceinline__ float grad1(const void* g, int64_t i)
 {
-    if constexpr (sizeof(G) == 4) return static_cast<const float*>(g)[i];
-    else return bf16_to_f32(static_cast<const uint16_t*>(g)[i]);
+    if constexpr (sizeof(G) == 4) return load(static_cast<const float*>(g) + i);
+    else return bf16_to_f32(load(static_cast<const uint16_t*>(g) + i));
 }
 
 template <class G>
@@ -162,10 +171,12 @@ __global__ __launch_bounds__(kThreads32) void adamw32_kernel(const Tensor* __res
     // not aligned: one element a lane at a time; aligned: what is left at the row's end is one element, of the lane it fell to
     const int64_t step = t.wide ? 2 : kThreads32;
     for (i = t.wide ? i : w.start + threadIdx.x; i < end; i += step) {
-        float xe = x[i], me = m[i], ve = v[i];
+        float xe = load(x + i), me = load(m + i), ve = load(v + i);
         update(xe, grad1<G>(g, i), me, ve, r, c, p);
-        x[i] = xe; m[i] = me; v[i] = ve;
-        if (xb) xb[i] = f32_to_bf16_rne(xe);
+        store(xe, x + i);
+        store(me, m + i);
+        store(ve, v + i);
+        if (xb) store(f32_to_bf16_rne(xe), xb + i);
     }
 }
 
@@ -271,7 +282,7 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(const Tensor* __restri
     float* vs = t.v_scale + w.row * t.ld_scale + b;
     const void* g = static_cast<const char*>(t.g) + w.row * t.ld_g * (int64_t)sizeof(G);
     uint16_t* xb = t.xb ? t.xb + w.row * t.ld_b : nullptr;
-    const float sm = *ms, sv = *vs;
+    const float sm = load(ms), sv = load(vs);
     const bool wide = t.wide && first + kBlock <= t.n;
     const int64_t k = first + 4 * lane;
     float xe[4], me[4], re[4];
@@ -293,9 +304,9 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(const Tensor* __restri
             const int64_t i = first + lane + e * kWave;
             xe[e] = me[e] = re[e] = 0.0f;
             if (i < t.n) {
-                xe[e] = x[i];
-                me[e] = value_m(m[i], sm);
-                const float rr = value_r(v[i], sv);
+                xe[e] = load(x + i);
+                me[e] = value_m(load(m + i), sm);
+                const float rr = value_r(load(v + i), sv);
                 float ve = rr * rr;
                 update(xe[e], grad1<G>(g, i), me[e], ve, re[e], c, p);
             }
@@ -326,16 +337,16 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(const Tensor* __restri
         for (int e = 0; e < 4; ++e) {
             const int64_t i = first + lane + e * kWave;
             if (i < t.n) {
-                x[i] = xe[e];
-                m[i] = (int8_t)qm[e];
-                v[i] = (uint8_t)qv[e];
-                if (xb) xb[i] = f32_to_bf16_rne(xe[e]);
+                store(xe[e], x + i);
+                store(qm[e], m + i);
+                store(qv[e], v + i);
+                if (xb) store(f32_to_bf16_rne(xe[e]), xb + i);
             }
         }
     }
     if (lane == 0) {
-        *ms = s.m;
-        *vs = s.v;
+        store(s.m, ms);
+        store(s.v, vs);
     }
 }
 
@@ -356,7 +367,7 @@ __global__ __launch_bounds__(kThreads) void adamw8_values_kernel(const Tensor* _
     const int64_t k = w.start + 4 * threadIdx.x;
     if (t.wide_values && k + 4 <= end) {
         const uint32_t mq = load_once(reinterpret_cast<const uint32_t*>(m + k)), vq = load_once(reinterpret_cast<const uint32_t*>(v + k));
-        const float sm = ms[k / kBlock], sv = vs[k / kBlock];
+        const float sm = load(ms + k / kBlock), sv = load(vs + k / kBlock);
         v4f a, b;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -370,9 +381,9 @@ __global__ __launch_bounds__(kThreads) void adamw8_values_kernel(const Tensor* _
     }
     const int64_t step = t.wide_values ? 1 : kThreads;
     for (int64_t i = t.wide_values ? k : w.start + threadIdx.x; i < end; i += step) {
-        om[i] = value_m(m[i], ms[i / kBlock]);
-        const float r = value_r(v[i], vs[i / kBlock]);
-        ov[i] = r * r;
+        store(value_m(load(m + i), load(ms + i / kBlock)), om + i);
+        const float r = value_r(load(v + i), load(vs + i / kBlock));
+        store(r * r, ov + i);
     }
 }
 

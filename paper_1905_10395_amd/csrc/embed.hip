@@ -4,11 +4,18 @@
 //
 // A token outside [0, V) is padding: zeros forward, nothing backward.
 //
-// The gradient.  Each worker's tokens are sorted (stable radix sort: equal tokens keep their order), so that the places
-// of a table row form one run, and the sorted list is cut into spans of equal length, whatever the runs: a token that
-// fills a tenth of the batch costs no team of lanes more than another.  A run inside a span is summed in registers and
-// written; of a run that crosses spans each span leaves a partial sum, and a second launch adds those up in order.  No
-// atomics touch a floating-point value: the order of every sum depends on the tokens alone, so equal calls give equal bits.
+// The gradient.  Each worker's tokens are sorted (stable radix sort: equal tokens keep their order), so that the places of
+// a table row form one run, and the sorted list is cut into spans of equal length, whatever the runs: a token that fills a
+// tenth of the batch costs no team of lanes more than another.  Frequencies that fall as 1/rank put two fifths of a batch
+// into the first 64 rows of a table; workgroups that own rows instead took seven times as long (2048 tokens, 65536 rows).
+//
+// Long lists: sorted in memory.  A run is summed in registers and written by the team of the span it begins in, also if
+// it ends in the next one; of a longer run each span leaves a partial sum, and another launch adds those up in order.
+//
+// Short ones take one launch: every workgroup sorts the whole list in LDS for itself, sums the runs that begin in its span
+// and writes zeros to its share of the rows without tokens; a run of many places is shared by its wavefronts.
+//
+// No atomics touch a floating-point value: the order of every sum depends on the tokens alone, so equal calls give equal bits.
 #include <algorithm>
 #include <cmath>
 
@@ -128,125 +135,85 @@ __global__ __launch_bounds__(kThreads) void lookup_kernel(const TI* __restrict__
 // ---- stable radix sort of each worker's tokens ----
 constexpr int kSortThreads = 1024;
 constexpr int kSortWaves = kSortThreads / kWave;
-constexpr int kSortEach = 8;
-constexpr int kSortTile = kSortThreads * kSortEach;                    // tokens of one workgroup
 constexpr int kMaxBits = 10;                                           // of a digit
 
 struct SortLds {
-    uint32_t key[kSortTile];
-    int32_t pos[kSortTile];
-    uint16_t count[kSortWaves][1 << kMaxBits];                         // of a wavefront's 512 tokens
+    alignas(16) uint16_t count[kSortWaves << kMaxBits];                // [wavefront][digit] of the wavefronts' tokens (at most 512)
     uint32_t base[1 << kMaxBits];
     uint32_t wave_sum[kSortWaves];
 };
 
 __device__ __forceinline__ uint32_t key_of(int tok, int V) { return (uint32_t)tok < (uint32_t)V ? (uint32_t)tok : (uint32_t)V; }
 
-// Rank of every token of the workgroup among those of its digit: in its wavefront (rank), the wavefronts before it
-// (count, turned into a sum over the earlier ones), and over the digits before it (base), which it returns in LDS.  `total`
-// adds where the workgroup's tokens of a digit begin, if that is not its own list's start.
-template <class F>
-__device__ __forceinline__ void rank_digits(SortLds& s, const uint32_t (&digit)[kSortEach], uint32_t (&rank)[kSortEach], int bits, F digit_base)
-{
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, bins = 1 << bits;
-    for (int i = threadIdx.x; i < kSortWaves * bins; i += kSortThreads) s.count[i >> bits][i & (bins - 1)] = 0;
-    __syncthreads();
-    const uint64_t below = (1ull << lane) - 1;
-#pragma unroll
-    for (int k = 0; k < kSortEach; ++k) {
-        uint64_t same = ~0ull;
-        for (int b = 0; b < bits; ++b) {
-            const uint64_t set = __ballot((digit[k] >> b) & 1u);
-            same &= (digit[k] >> b) & 1u ? set : ~set;
-        }
-        volatile uint16_t* cell = &s.count[wave][digit[k]];
-        const uint32_t before = *cell;
-        rank[k] = before + (uint32_t)__popcll(same & below);
-        __builtin_amdgcn_wave_barrier();
-        if ((same & below) == 0) *cell = (uint16_t)(before + (uint32_t)__popcll(same));     // its first lane
-        __builtin_amdgcn_wave_barrier();
-    }
-    __syncthreads();
-    // thread d: digit d's tokens of each wavefront to a sum over the wavefronts before it; then a scan over the digits
-    uint32_t mine = 0;
-    if ((int)threadIdx.x < bins) {
-#pragma unroll
-        for (int w = 0; w < kSortWaves; ++w) {
-            const uint32_t c = s.count[w][threadIdx.x];
-            s.count[w][threadIdx.x] = (uint16_t)mine;
-            mine += c;
-        }
-    }
-    digit_base(s, mine);
-    __syncthreads();
-}
-
-// Exclusive sum of v over the workgroup's threads.
+// Exclusive sum of v over the workgroup's threads (by lane shifts in the vector unit; LDS only between wavefronts).
 __device__ __forceinline__ uint32_t exclusive_scan(SortLds& s, uint32_t v)
 {
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    uint32_t x = v;
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-        const uint32_t y = __shfl_up(x, o);
-        if (lane >= o) x += y;
-    }
-    if (lane == kWave - 1) s.wave_sum[wave] = x;
+    int x = (int)v;
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, true);     // from the lane one to the left, in rows of 16
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);    // the row before's last lane, into rows 1 and 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);    // lane 31, into the upper half
+    if (lane == kWave - 1) s.wave_sum[wave] = (uint32_t)x;
     __syncthreads();
     uint32_t before = 0;
-    for (int w = 0; w < wave; ++w) before += s.wave_sum[w];
-    return before + x - v;
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) {
+        const uint32_t n = s.wave_sum[w];
+        before += w < wave ? n : 0;
+    }
+    return before + (uint32_t)x - v;
 }
 
-// A worker's whole list in one workgroup, all digits: no more than kSortTile tokens.
-__global__ __launch_bounds__(kSortThreads) void sort_small_kernel(const int32_t* __restrict__ tokens, int64_t ld_tokens, int T, int V,
-                                                                  int bits, int passes, uint32_t* __restrict__ keys, int32_t* __restrict__ pos)
+// Rank of every token of the workgroup among those of its digit: in its wavefront (rank) and over the wavefronts before it
+// (left in count); equal digits keep their order: wavefronts, rounds of a wavefront, lanes.  Thread d gets the number of
+// tokens of digit d.  The caller's next barrier makes count whole.
+template <int EACH>
+__device__ __forceinline__ uint32_t rank_tile(SortLds& s, const uint32_t (&digit)[EACH], uint32_t (&rank)[EACH], int bits)
 {
-    __shared__ SortLds s;
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    tokens += blockIdx.x * ld_tokens;
-    keys += (int64_t)blockIdx.x * T;
-    pos += (int64_t)blockIdx.x * T;
-    const int first = wave * (kWave * kSortEach) + lane;
-    uint32_t key[kSortEach], digit[kSortEach], rank[kSortEach];
-    int32_t at[kSortEach];
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, bins = 1 << bits;
+    for (int i = threadIdx.x; i < (kSortWaves << bits) / 2; i += kSortThreads) reinterpret_cast<uint32_t*>(s.count)[i] = 0;
+    __syncthreads();
+    const uint64_t below = (1ull << lane) - 1;
+    uint16_t* count = s.count + (wave << bits);
 #pragma unroll
-    for (int k = 0; k < kSortEach; ++k) {
-        at[k] = first + k * kWave;
-        key[k] = at[k] < T ? key_of(tokens[at[k]], V) : 0xFFFFFFFFu;   // past the end: last in every digit's order
-    }
-    for (int p = 0; p < passes; ++p) {
-        const uint32_t mask = (1u << bits) - 1;
+    for (int k = 0; k < EACH; ++k) {
+        uint32_t lo = ~0u, hi = ~0u;                                   // lanes of the same digit
 #pragma unroll
-        for (int k = 0; k < kSortEach; ++k) digit[k] = (key[k] >> (p * bits)) & mask;
-        rank_digits(s, digit, rank, bits, [&](SortLds& l, uint32_t mine) {
-            const uint32_t b = exclusive_scan(l, mine);
-            if ((int)threadIdx.x < (1 << bits)) l.base[threadIdx.x] = b;
-        });
-        const bool last = p + 1 == passes;
-#pragma unroll
-        for (int k = 0; k < kSortEach; ++k) {
-            const uint32_t to = s.base[digit[k]] + s.count[wave][digit[k]] + rank[k];
-            if (last) {
-                if ((int)to < T) { keys[to] = key[k]; pos[to] = at[k]; }
-            } else {
-                s.key[to] = key[k];
-                s.pos[to] = at[k];
+        for (int b = 0; b < kMaxBits; ++b) {
+            if (b < bits) {
+                const uint32_t mine = (uint32_t)((int32_t)(digit[k] << (31 - b)) >> 31);
+                const uint64_t set = __ballot(mine != 0);
+                lo &= ~((uint32_t)set ^ mine);
+                hi &= ~((uint32_t)(set >> 32) ^ mine);
             }
         }
-        __syncthreads();
-        if (!last) {
+        const uint64_t same = (uint64_t)hi << 32 | lo;
+        const uint32_t seen = count[digit[k]];
+        rank[k] = seen + (uint32_t)__popcll(same & below);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if ((same & below) == 0) count[digit[k]] = (uint16_t)(seen + (uint32_t)__popcll(same));       // its first lane
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+    __syncthreads();
+    uint32_t sum = 0;
+    if ((int)threadIdx.x < bins) {
+        uint32_t c[kSortWaves];
 #pragma unroll
-            for (int k = 0; k < kSortEach; ++k) {
-                key[k] = s.key[first + k * kWave];
-                at[k] = s.pos[first + k * kWave];
-            }
-            __syncthreads();
+        for (int w = 0; w < kSortWaves; ++w) c[w] = s.count[(w << bits) + threadIdx.x];
+#pragma unroll
+        for (int w = 0; w < kSortWaves; ++w) {
+            s.count[(w << bits) + threadIdx.x] = (uint16_t)sum;
+            sum += c[w];
         }
     }
+    return sum;
 }
 
-// Longer lists: how many tokens of each digit every tile has ...
+// A digit's turn: how many tokens of each digit every tile of EACH * kSortThreads has ...
+template <int EACH>
 __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const int32_t* __restrict__ tokens, int64_t ld_tokens,
                                                                   const uint32_t* __restrict__ keys_in, int T, int V, int bits, int shift,
                                                                   uint32_t* __restrict__ counts)
@@ -255,9 +222,9 @@ __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const int32_t*
     const int bins = 1 << bits;
     for (int i = threadIdx.x; i < bins; i += kSortThreads) bin[i] = 0;
     __syncthreads();
-    const int64_t first = (int64_t)blockIdx.x * kSortTile;
+    const int64_t first = (int64_t)blockIdx.x * (EACH * kSortThreads);
 #pragma unroll
-    for (int k = 0; k < kSortEach; ++k) {
+    for (int k = 0; k < EACH; ++k) {
         const int64_t i = first + k * kSortThreads + threadIdx.x;
         if (i < T) {
             const uint32_t key = keys_in ? keys_in[(int64_t)blockIdx.y * T + i] : key_of(tokens[blockIdx.y * ld_tokens + i], V);
@@ -270,6 +237,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const int32_t*
 }
 
 // ... and every tile's tokens to their places: after all smaller digits, and after the same digit's in earlier tiles.
+template <int EACH>
 __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const int32_t* __restrict__ tokens, int64_t ld_tokens,
                                                                   const uint32_t* __restrict__ keys_in, const int32_t* __restrict__ pos_in,
                                                                   int T, int V, int bits, int shift, const uint32_t* __restrict__ counts,
@@ -278,13 +246,13 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const int32_t*
     __shared__ SortLds s;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, bins = 1 << bits;
     const int64_t off = (int64_t)blockIdx.y * T;
-    const int64_t first = (int64_t)blockIdx.x * kSortTile + wave * (kWave * kSortEach) + lane;
-    uint32_t key[kSortEach], digit[kSortEach], rank[kSortEach];
-    int32_t at[kSortEach];
+    const int64_t first = (int64_t)blockIdx.x * (EACH * kSortThreads) + wave * (kWave * EACH) + lane;
+    uint32_t key[EACH], digit[EACH], rank[EACH];
+    int32_t at[EACH];
 #pragma unroll
-    for (int k = 0; k < kSortEach; ++k) {
+    for (int k = 0; k < EACH; ++k) {
         const int64_t i = first + k * kWave;
-        key[k] = 0xFFFFFFFFu;
+        key[k] = 0xFFFFFFFFu;                                          // past the end of the list: behind all others of its digit
         at[k] = -1;
         if (i < T) {
             key[k] = keys_in ? keys_in[off + i] : key_of(tokens[blockIdx.y * ld_tokens + i], V);
@@ -292,23 +260,25 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const int32_t*
         }
         digit[k] = (key[k] >> shift) & (uint32_t)(bins - 1);
     }
-    rank_digits(s, digit, rank, bits, [&](SortLds& l, uint32_t) {
-        uint32_t all = 0, before = 0;
-        if ((int)threadIdx.x < bins) {
-            const uint32_t* c = counts + (int64_t)blockIdx.y * gridDim.x * bins + threadIdx.x;
-            for (unsigned b = 0; b < gridDim.x; ++b) {
-                const uint32_t n = c[(int64_t)b * bins];
-                if (b < blockIdx.x) before += n;
-                all += n;
-            }
+    // where the tile's tokens of each digit begin (thread d: digit d)
+    uint32_t all = 0, before = 0;
+    if ((int)threadIdx.x < bins) {
+        const uint32_t* c = counts + (int64_t)blockIdx.y * gridDim.x * bins + threadIdx.x;
+#pragma unroll 8
+        for (unsigned b = 0; b < gridDim.x; ++b) {
+            const uint32_t n = c[(int64_t)b * bins];
+            before += b < blockIdx.x ? n : 0;
+            all += n;
         }
-        const uint32_t b = exclusive_scan(l, all);
-        if ((int)threadIdx.x < bins) l.base[threadIdx.x] = b + before;
-    });
+    }
+    const uint32_t smaller = exclusive_scan(s, all);
+    if ((int)threadIdx.x < bins) s.base[threadIdx.x] = smaller + before;
+    rank_tile<EACH>(s, digit, rank, bits);
+    __syncthreads();
 #pragma unroll
-    for (int k = 0; k < kSortEach; ++k) {
-        if (at[k] < 0) continue;                                       // past the end of the list
-        const int64_t to = off + s.base[digit[k]] + s.count[wave][digit[k]] + rank[k];
+    for (int k = 0; k < EACH; ++k) {
+        if (at[k] < 0) continue;
+        const int64_t to = off + s.base[digit[k]] + s.count[(wave << bits) + digit[k]] + rank[k];
         keys[to] = key[k];
         pos[to] = at[k];
     }
@@ -339,10 +309,10 @@ struct GradArgs {
     int64_t ld_dout;
     const uint32_t* keys;
     const int32_t* pos;
-    float* parts;            // [W][spans][2][Dp]: of the run that came into a span, of the one that began there and goes on
+    float* parts;            // [W][spans][2][Dp]: of the split run that came into a span, of the one that began there
     float* table;
     int64_t ld_table;
-    int T, V, D, Dp, L, spans, slices;
+    int T, V, D, Dp, spans, slices;
     int run_blocks;          // workgroups that sum runs; those after them write zeros to rows without tokens
     int zero_rows;           // table rows of such a workgroup
     float scale;
@@ -362,6 +332,21 @@ __device__ __forceinline__ void load_row(const T* p, int col, int D, float (&v)[
     }
 }
 
+template <int E, int TL, bool WIDE>
+__device__ __forceinline__ void store_row(float* p, int col, int D, const float (&v)[E])
+{
+    if constexpr (WIDE) {
+        if (col < D) store_adjacent<E>(p + col, v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (col + e * TL < D) p[col + e * TL] = v[e];
+    }
+}
+
+constexpr int kSpan = 16;              // sorted places of a team, and how far into the next span it may finish a run
+constexpr uint32_t kNone = 0xFFFFFFFFu;
+
 // TL lanes make a team: they own TL * E columns of one span.
 template <class T, int E, int TL, bool WIDE>
 __device__ __forceinline__ void sum_runs(const GradArgs& a, int64_t task)
@@ -376,24 +361,27 @@ __device__ __forceinline__ void sum_runs(const GradArgs& a, int64_t task)
     const int32_t* pos = a.pos + (int64_t)w * a.T;
     const T* dout = static_cast<const T*>(a.dout) + w * a.ld_dout;
     float* table = a.table + w * a.ld_table;
-    const int s0 = span * a.L, s1 = s0 + a.L < a.T ? s0 + a.L : a.T;
-    uint32_t cur = keys[s0];
-    bool head = s0 > 0 && keys[s0 - 1] == cur;
+    // A run is split if it goes on past the span after the one it begins in.  Of the run that comes into this span: it is if
+    // it goes on past this one, or if it came into the span before as well.  Else the team before has summed it.
+    const int s0 = span * kSpan, s1 = s0 + kSpan < a.T ? s0 + kSpan : a.T;
+    const uint32_t k0 = keys[s0], end = keys[s1 - 1], next = s1 < a.T ? keys[s1] : kNone;
+    const uint32_t after = s1 + kSpan < a.T ? keys[s1 + kSpan] : kNone;
+    const uint32_t before = s0 > 0 ? keys[s0 - 1] : kNone, start_before = s0 > 0 ? keys[s0 - kSpan] : kNone;
+    const uint32_t long_before = s0 > kSpan ? keys[s0 - kSpan - 1] : kNone;
+    const bool came_in = before == k0;
+    const bool head_split = came_in && ((end == k0 && next == k0) || (start_before == k0 && long_before == k0));
+    const bool tail_split = next == end && after == end;
+    const uint32_t skip = came_in && !head_split ? k0 : kNone;         // a run that is not this team's
+    uint32_t cur = k0;
+    bool head = head_split;
     float acc[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) acc[e] = 0.0f;
 
     auto flush = [&](bool tail) {
-        if (cur >= (uint32_t)a.V) return;                              // padding
+        if (cur >= (uint32_t)a.V || cur == skip) return;               // padding
         if (head || tail) {
-            float* p = a.parts + (((int64_t)w * a.spans + span) * 2 + (head ? 0 : 1)) * a.Dp;
-            if constexpr (WIDE) {
-                if (col < a.D) store_adjacent<E>(p + col, acc);
-            } else {
-#pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if (col + e * TL < a.D) p[col + e * TL] = acc[e];
-            }
+            store_row<E, TL, WIDE>(a.parts + (((int64_t)w * a.spans + span) * 2 + (head ? 0 : 1)) * a.Dp, col, a.D, acc);
         } else {
             float* p = table + (int64_t)cur * a.D;
             float old[E];
@@ -402,30 +390,29 @@ __device__ __forceinline__ void sum_runs(const GradArgs& a, int64_t task)
             if (a.accumulate) load_row<float, E, TL, WIDE>(p, col, a.D, old);
 #pragma unroll
             for (int e = 0; e < E; ++e) old[e] += a.scale * acc[e];
-            if constexpr (WIDE) {
-                if (col < a.D) store_adjacent<E>(p + col, old);
-            } else {
-#pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if (col + e * TL < a.D) p[col + e * TL] = old[e];
-            }
+            store_row<E, TL, WIDE>(p, col, a.D, old);
         }
     };
 
-    for (int i = s0; i < s1; i += U) {
+    // this span's places, and on into the next one as long as its last run goes on there (if it began here and is not split)
+    const bool finish = next == end && !tail_split && end != skip && !(head && end == k0);
+    const int s2 = !finish ? s1 : s1 + kSpan < a.T ? s1 + kSpan : a.T;
+    for (int i = s0; i < s2; i += U) {
         uint32_t key[U];
         int32_t at[U];
         float row[U][E];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            key[u] = i + u < s1 ? keys[i + u] : (uint32_t)a.V;
-            at[u] = i + u < s1 ? pos[i + u] : 0;
+            key[u] = i + u < s2 ? keys[i + u] : (uint32_t)a.V;
+            at[u] = i + u < s2 ? pos[i + u] : 0;
+            if (i + u >= s1 && key[u] != end) key[u] = (uint32_t)a.V;  // the next span's own
         }
+        if (i >= s1 && key[0] == (uint32_t)a.V) break;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
 #pragma unroll
             for (int e = 0; e < E; ++e) row[u][e] = 0.0f;
-            if (key[u] < (uint32_t)a.V) load_row<T, E, TL, WIDE>(dout + (int64_t)at[u] * a.D, col, a.D, row[u]);
+            if (key[u] < (uint32_t)a.V && key[u] != skip) load_row<T, E, TL, WIDE>(dout + (int64_t)at[u] * a.D, col, a.D, row[u]);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -440,7 +427,7 @@ __device__ __forceinline__ void sum_runs(const GradArgs& a, int64_t task)
             for (int e = 0; e < E; ++e) acc[e] += row[u][e];
         }
     }
-    flush(s1 < a.T && keys[s1] == cur);
+    flush(tail_split);
 }
 
 // Zeros to the rows of [v0, v0 + zero_rows) that no token names.
@@ -465,7 +452,7 @@ __device__ __forceinline__ void zero_rows(const GradArgs& a, int64_t v0, uint32_
         if (present[r >> 5] >> (r & 31) & 1u) continue;
         float* p = table + (v0 + r) * a.D;
         if constexpr (WIDE) {
-            for (int c = 4 * lane; c < a.D; c += 4 * kWave) *reinterpret_cast<v4f*>(p + c) = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int c = 4 * lane; c < a.D; c += 4 * kWave) __builtin_nontemporal_store(v4f{0.0f, 0.0f, 0.0f, 0.0f}, reinterpret_cast<v4f*>(p + c));
         } else {
             for (int c = lane; c < a.D; c += kWave) p[c] = 0.0f;
         }
@@ -482,41 +469,251 @@ __global__ __launch_bounds__(kThreads) void grad_runs_kernel(GradArgs a)
     else zero_rows<WIDE>(a, (int64_t)((int)blockIdx.x - a.run_blocks) * a.zero_rows, present);
 }
 
-// Runs that cross spans: the workgroup of the span where one begins adds up its parts, each wavefront a stretch of them.
-constexpr int kJoinCols = 4 * kWave;
+// Split runs.  A workgroup looks at the ends of kJoinSpans spans, a lane each, for such runs that began there (few are), for
+// kJoinCols columns; its wavefronts take those in turn and add up a run's parts, or share it if the parts are many.
+constexpr int kJoinSpans = 16, kJoinShared = 32, kJoinCols = 4 * kWave;
+static_assert(kJoinSpans <= kWave, "one wavefront looks");
 __global__ __launch_bounds__(kThreads) void grad_join_kernel(GradArgs a)
 {
-    __shared__ float sum[kThreads / kWave][kJoinCols];
-    const int w = blockIdx.y, span = blockIdx.x;
+    constexpr int waves = kThreads / kWave;
+    __shared__ float sum[waves][kJoinCols];
+    __shared__ int begun[kJoinSpans], shared_parts[kJoinSpans], runs;
+    const int w = blockIdx.y;
     const uint32_t* keys = a.keys + (int64_t)w * a.T;
-    const int s0 = span * a.L, s1 = s0 + a.L;
-    if (s1 >= a.T) return;
-    const uint32_t cur = keys[s1 - 1];
-    if (cur >= (uint32_t)a.V || keys[s1] != cur) return;               // nothing goes on into the next span
-    if (keys[s0] == cur && s0 > 0 && keys[s0 - 1] == cur) return;      // it began earlier
-    const int end = s1 + lower_bound(keys + s1, a.T - s1, cur + 1);
-    const int parts = (end - 1) / a.L - span + 1;                      // the tail of this span, then heads
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, waves = kThreads / kWave;
+    const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
     const int col0 = blockIdx.z * kJoinCols, col = col0 + 4 * lane;
-    const float* first = a.parts + ((int64_t)w * a.spans + span) * 2 * a.Dp;
-    const int per = (parts + waves - 1) / waves, p0 = wave * per, p1 = p0 + per < parts ? p0 + per : parts;
-    v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (col < a.Dp) {
+    float* table = a.table + w * a.ld_table;
+    if (wave == 0) {
+        const int span = blockIdx.x * kJoinSpans + lane;
+        const int64_t s0 = (int64_t)span * kSpan, s1 = s0 + kSpan;
+        bool split = false;
+        if (lane < kJoinSpans && s1 + kSpan < a.T) {
+            const uint32_t cur = keys[s1 - 1], next = keys[s1], after = keys[s1 + kSpan], start = keys[s0], before = s0 > 0 ? keys[s0 - 1] : ~0u;
+            split = next == cur && after == cur && cur < (uint32_t)a.V && !(start == cur && before == cur);
+        }
+        const uint64_t mask = __ballot(split);
+        if (split) begun[__popcll(mask & ((1ull << lane) - 1))] = span;
+        if (lane == 0) runs = __popcll(mask);
+    }
+    __syncthreads();
+    const int n_runs = runs;
+    auto add = [&](int span, int p0, int p1) {                         // part 0 began in the span, the others came into theirs
+        v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
+        const float* first = a.parts + ((int64_t)w * a.spans + span) * 2 * a.Dp + col;
+        if (col < a.Dp) {
 #pragma unroll 8
-        for (int p = p0; p < p1; ++p) {
-            const float* q = first + ((int64_t)p * 2 + (p == 0 ? 1 : 0)) * a.Dp + col;
-            acc += *reinterpret_cast<const v4f*>(q);
+            for (int p = p0; p < p1; ++p) acc += *reinterpret_cast<const v4f*>(first + (int64_t)(2 * p + (p == 0 ? 1 : 0)) * a.Dp);
+        }
+        return acc;
+    };
+    for (int k = wave; k < n_runs; k += waves) {
+        const int span = begun[k], s1 = (span + 1) * kSpan;
+        const uint32_t cur = keys[s1];
+        int n = 3;                                                     // parts: the spans after it that begin with its key
+        for (;;) {
+            const int64_t i = s1 + (int64_t)(n - 1 + lane) * kSpan;
+            const uint64_t goes_on = __ballot(i < a.T && keys[i] == cur);
+            if (goes_on != ~0ull) {
+                n += __builtin_ctzll(~goes_on);
+                break;
+            }
+            n += kWave;
+        }
+        if (lane == 0) shared_parts[k] = n > kJoinShared ? n : 0;
+        if (n > kJoinShared) continue;
+        float* row = table + (int64_t)cur * a.D;
+        const v4f acc = add(span, 0, n);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (col + e < a.D) row[col + e] = (a.accumulate ? row[col + e] : 0.0f) + a.scale * acc[e];
+    }
+    __syncthreads();
+    for (int k = 0; k < n_runs; ++k) {                                 // long ones, together
+        const int n = shared_parts[k];
+        if (n == 0) continue;
+        const int span = begun[k];
+        const int per = (n + waves - 1) / waves, p0 = wave * per, p1 = p0 + per < n ? p0 + per : n;
+        *reinterpret_cast<v4f*>(&sum[wave][4 * lane]) = add(span, p0, p1);
+        __syncthreads();
+        const int c = col0 + (int)threadIdx.x;
+        if (c < a.D) {
+            float t = 0.0f;
+#pragma unroll
+            for (int v = 0; v < waves; ++v) t += sum[v][threadIdx.x];
+            float* to = table + (int64_t)keys[(span + 1) * kSpan] * a.D + c;
+            *to = (a.accumulate ? *to : 0.0f) + a.scale * t;
+        }
+        __syncthreads();
+    }
+}
+
+// ---- the gradient in one launch ----
+constexpr int kSmallTokens = 8 * kSortThreads;     // tokens a worker may have for it
+constexpr int kSmallRows = 1 << 14;                // table rows whose zeros a workgroup may write
+constexpr int kSmallShared = 16;                   // places of a run from which on a workgroup's wavefronts share it
+
+struct SmallArgs {
+    const int32_t* tokens;
+    int64_t ld_tokens;
+    int bits, passes;
+    int span;                                      // sorted places whose runs a workgroup sums
+    int rows;                                      // table rows whose zeros it writes
+    int slices;                                    // of 64 * E columns, that it takes
+};
+
+template <class T, int E, bool WIDE, int EACH>
+__global__ __launch_bounds__(kSortThreads) void grad_small_kernel(GradArgs a, SmallArgs q)
+{
+    constexpr int TL = kWave, U = 8, cols = kWave * E;
+    __shared__ uint32_t key[EACH * kSortThreads];
+    __shared__ uint16_t pos[EACH * kSortThreads];
+    __shared__ union {
+        SortLds sort;
+        uint32_t present[kSmallRows / 32];
+        float sum[kSortWaves][cols];
+    } s;
+    __shared__ int shared_run[EACH * kSortThreads / kSmallShared], shared_places[EACH * kSortThreads / kSmallShared], shared_runs;
+    const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), w = blockIdx.y;
+    const int32_t* tokens = q.tokens + w * q.ld_tokens;
+    const int first = wave * (kWave * EACH) + lane;
+    {
+        uint32_t k0[EACH], digit[EACH], rank[EACH], p0[EACH];
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) {
+            p0[k] = first + k * kWave;
+            k0[k] = (int)p0[k] < a.T ? key_of(tokens[p0[k]], a.V) : 0xFFFFFFFFu;       // past the end: stays behind all others
+        }
+        for (int p = 0; p < q.passes; ++p) {
+#pragma unroll
+            for (int k = 0; k < EACH; ++k) digit[k] = (k0[k] >> (p * q.bits)) & ((1u << q.bits) - 1);
+            const uint32_t mine = rank_tile<EACH>(s.sort, digit, rank, q.bits);
+            const uint32_t smaller = exclusive_scan(s.sort, mine);
+            if ((int)threadIdx.x < 1 << q.bits) s.sort.base[threadIdx.x] = smaller;
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < EACH; ++k) {
+                const uint32_t to = s.sort.base[digit[k]] + s.sort.count[(wave << q.bits) + digit[k]] + rank[k];
+                key[to] = k0[k];
+                pos[to] = (uint16_t)p0[k];
+            }
+            __syncthreads();
+            if (p + 1 < q.passes) {
+#pragma unroll
+                for (int k = 0; k < EACH; ++k) {
+                    k0[k] = key[first + k * kWave];
+                    p0[k] = pos[first + k * kWave];
+                }
+                __syncthreads();
+            }
         }
     }
-    *reinterpret_cast<v4f*>(&sum[wave][4 * lane]) = acc;
-    __syncthreads();
-    const int c = col0 + (int)threadIdx.x;
-    if (c < a.D) {
-        float s = 0.0f;
+    const int slice0 = blockIdx.z * q.slices, col_end = (slice0 + q.slices) * cols < a.D ? (slice0 + q.slices) * cols : a.D;
+    const T* dout = static_cast<const T*>(a.dout) + w * a.ld_dout;
+    float* table = a.table + w * a.ld_table;
+    if (threadIdx.x == 0) shared_runs = 0;
+    if (!a.accumulate) {
+        const int64_t v0 = (int64_t)blockIdx.x * q.rows;
+        const int n = (int)(a.V - v0 < q.rows ? (a.V - v0 < 0 ? 0 : a.V - v0) : q.rows);
+        for (int i = threadIdx.x; i < (n + 31) / 32; i += kSortThreads) s.present[i] = 0;
+        __syncthreads();
 #pragma unroll
-        for (int v = 0; v < waves; ++v) s += sum[v][threadIdx.x];
-        float* p = a.table + w * a.ld_table + (int64_t)cur * a.D + c;
-        *p = (a.accumulate ? *p : 0.0f) + a.scale * s;
+        for (int k = 0; k < EACH; ++k) {
+            const uint32_t v = key[k * kSortThreads + threadIdx.x] - (uint32_t)v0;      // what is no row here wraps past n
+            if (v < (uint32_t)n) atomicOr(&s.present[v >> 5], 1u << (v & 31));
+        }
+        __syncthreads();
+        for (int r = wave; r < n; r += kSortWaves) {
+            if (s.present[r >> 5] >> (r & 31) & 1u) continue;
+            float* p = table + (v0 + r) * a.D;
+            if constexpr (WIDE) {
+                for (int c = slice0 * cols + 4 * lane; c < col_end; c += 4 * kWave) *reinterpret_cast<v4f*>(p + c) = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+            } else {
+                for (int c = slice0 * cols + lane; c < col_end; c += kWave) p[c] = 0.0f;
+            }
+        }
+    }
+    __syncthreads();
+
+    float acc[E];
+    auto add_places = [&](int p0, int p1, int col) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] = 0.0f;
+        for (int b = p0; b < p1; b += U) {
+            float row[U][E];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) row[u][e] = 0.0f;
+                if (b + u < p1) {
+                    const int at = __builtin_amdgcn_readfirstlane((int)pos[b + u]);
+                    load_row<T, E, TL, WIDE>(dout + (int64_t)at * a.D, col, a.D, row[u]);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int e = 0; e < E; ++e) acc[e] += row[u][e];
+        }
+    };
+    const int lo = blockIdx.x * q.span, hi = lo + q.span < a.T ? lo + q.span : a.T;
+    const int each = (q.span + kSortWaves - 1) / kSortWaves;
+    const int j1 = lo + (wave + 1) * each < hi ? lo + (wave + 1) * each : hi;
+    for (int j = lo + wave * each; j < j1; ++j) {
+        const uint32_t v = __builtin_amdgcn_readfirstlane(key[j]);
+        if (v >= (uint32_t)a.V) break;                                 // padding, behind all rows
+        if (j > 0 && __builtin_amdgcn_readfirstlane(key[j - 1]) == (int)v) continue;
+        int n = 0;
+        for (;;) {
+            const int i = j + n + lane;
+            const uint64_t same = __ballot(i < a.T && key[i] == v);
+            if (same != ~0ull) {
+                n += __builtin_ctzll(~same);
+                break;
+            }
+            n += kWave;
+        }
+        if (n > kSmallShared) {
+            if (lane == 0) {
+                const int k = atomicAdd(&shared_runs, 1);
+                shared_run[k] = j;
+                shared_places[k] = n;
+            }
+            continue;
+        }
+        for (int c = 0; c < q.slices; ++c) {
+            const int col0 = (slice0 + c) * cols, col = WIDE ? col0 + lane * E : col0 + lane;
+            if (col0 >= a.D) break;
+            float* p = table + (int64_t)v * a.D;
+            float old[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) old[e] = 0.0f;
+            if (a.accumulate) load_row<float, E, TL, WIDE>(p, col, a.D, old);
+            add_places(j, j + n, col);
+#pragma unroll
+            for (int e = 0; e < E; ++e) old[e] += a.scale * acc[e];
+            store_row<E, TL, WIDE>(p, col, a.D, old);
+        }
+    }
+    __syncthreads();
+    for (int k = 0; k < shared_runs; ++k) {
+        const int j = shared_run[k], n = shared_places[k];
+        float* p = table + (int64_t)key[j] * a.D;
+        for (int c = 0; c < q.slices; ++c) {
+            const int col0 = (slice0 + c) * cols, col = WIDE ? col0 + lane * E : col0 + lane;
+            if (col0 >= a.D) break;
+            add_places(j + n * wave / kSortWaves, j + n * (wave + 1) / kSortWaves, col);
+#pragma unroll
+            for (int e = 0; e < E; ++e) s.sum[wave][WIDE ? lane * E + e : e * kWave + lane] = acc[e];
+            __syncthreads();
+            if ((int)threadIdx.x < cols && col0 + (int)threadIdx.x < a.D) {
+                float t = 0.0f;
+#pragma unroll
+                for (int v = 0; v < kSortWaves; ++v) t += s.sum[v][threadIdx.x];
+                float* to = p + col0 + threadIdx.x;
+                *to = (a.accumulate ? *to : 0.0f) + a.scale * t;
+            }
+            __syncthreads();
+        }
     }
 }
 
@@ -545,34 +742,35 @@ lsgd_status check_shape(const char* who, int32_t W, int32_t T, int32_t V, int32_
 }
 
 struct Plan {
-    int bits, passes, tiles;     // of the sort
-    int L, spans, Dp;
+    int bits, passes, each, tiles;     // of the sort
+    int spans, Dp;
     size_t keys[2], pos[2], counts, parts, total;
 };
 
-// Spans of 32 places once those fill the chip; shorter batches are cut finer.
+// No memory for what takes one launch.  Sort tiles of 2048 tokens while a list has few of them (a tile adds up the counts of all
+// others), of 8192 then.
 Plan make_plan(int W, int T, int V, int D)
 {
-    Plan p;
+    Plan p{};
+    p.total = kAlign;
     int nb = 1;
     while (V >> nb) ++nb;                                              // keys are 0 .. V
     p.passes = (nb + kMaxBits - 1) / kMaxBits;
     p.bits = (nb + p.passes - 1) / p.passes;
-    p.tiles = T ? (T - 1) / kSortTile + 1 : 0;
-    p.L = 32;
-    while (p.L > 8 && (int64_t)W * T / p.L < 2048) p.L /= 2;
-    p.spans = T ? (T - 1) / p.L + 1 : 0;
+    if (T <= kSmallTokens) return p;
+    p.each = T <= 64 * 2 * kSortThreads ? 2 : 8;
+    p.tiles = (T - 1) / (p.each * kSortThreads) + 1;
+    p.spans = (T - 1) / kSpan + 1;
     p.Dp = (D + 7) / 8 * 8;
     const size_t list = align_up(sizeof(uint32_t) * (size_t)W * (size_t)T);
     size_t o = 0;
     for (int k = 0; k < 2; ++k) {
-        const bool used = k == 0 || (p.tiles > 1 && p.passes > 1);
-        p.keys[k] = o; o += used ? list : 0;
-        p.pos[k] = o;  o += used ? list : 0;
+        p.keys[k] = o; o += k == 0 || p.passes > 1 ? list : 0;
+        p.pos[k] = o;  o += k == 0 || p.passes > 1 ? list : 0;
     }
-    p.counts = o; o += p.tiles > 1 ? align_up(sizeof(uint32_t) * (size_t)W * (size_t)p.tiles << p.bits) : 0;
-    p.parts = o;  o += p.spans > 1 ? align_up(sizeof(float) * (size_t)W * (size_t)p.spans * 2 * (size_t)p.Dp) : 0;
-    p.total = o ? o : kAlign;
+    p.counts = o; o += align_up(sizeof(uint32_t) * ((size_t)W * (size_t)p.tiles << p.bits));
+    p.parts = o;  o += align_up(sizeof(float) * (size_t)W * (size_t)p.spans * 2 * (size_t)p.Dp);
+    p.total = o;
     return p;
 }
 
@@ -608,8 +806,31 @@ void launch_grad(GradArgs a, int W, hipStream_t s)
     a.zero_rows = kZeroRows;
     const int zero_blocks = a.accumulate ? 0 : (a.V - 1) / kZeroRows + 1;
     hipLaunchKernelGGL((grad_runs_kernel<T, E, TL, WIDE>), dim3((unsigned)(a.run_blocks + zero_blocks), (unsigned)W), dim3(kThreads), 0, s, a);
-    if (a.spans > 1)
-        hipLaunchKernelGGL(grad_join_kernel, dim3((unsigned)(a.spans - 1), (unsigned)W, (unsigned)((a.D - 1) / kJoinCols + 1)), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL(grad_join_kernel, dim3((unsigned)((a.spans - 1) / kJoinSpans + 1), (unsigned)W, (unsigned)((a.D - 1) / kJoinCols + 1)),
+                       dim3(kThreads), 0, s, a);
+}
+
+// A workgroup a compute unit (each sorts the list again; twice as many: 8.4 -> 12.1 us for 517 tokens, 15.6 -> 23.4 for 2048),
+// fewer columns each rather than fewer places.
+constexpr int kSmallGroups = 256;
+template <class T, int E, bool WIDE>
+void launch_grad_small(const GradArgs& a, int W, SmallArgs q, hipStream_t s)
+{
+    const int slices = (a.D - 1) / (kWave * E) + 1;
+    int z = 1;
+    while (z < slices && (int64_t)W * z * a.T < 256 * 16) ++z;
+    q.slices = (slices - 1) / z + 1;
+    z = (slices - 1) / q.slices + 1;
+    int n = std::max(1, kSmallGroups / (W * z));
+    if (a.accumulate) n = std::min(n, a.T);
+    else n = std::max(n, (a.V - 1) / kSmallRows + 1);
+    q.span = (a.T - 1) / n + 1;
+    q.rows = (a.V - 1) / n + 1;
+    const dim3 grid((unsigned)n, (unsigned)W, (unsigned)z), block(kSortThreads);
+    if (a.T <= kSortThreads) hipLaunchKernelGGL((grad_small_kernel<T, E, WIDE, 1>), grid, block, 0, s, a, q);
+    else if (a.T <= 2 * kSortThreads) hipLaunchKernelGGL((grad_small_kernel<T, E, WIDE, 2>), grid, block, 0, s, a, q);
+    else if (a.T <= 4 * kSortThreads) hipLaunchKernelGGL((grad_small_kernel<T, E, WIDE, 4>), grid, block, 0, s, a, q);
+    else hipLaunchKernelGGL((grad_small_kernel<T, E, WIDE, 8>), grid, block, 0, s, a, q);
 }
 
 template <class T, int E>
@@ -702,33 +923,43 @@ lsgd_status lsgd_embed_grad(int32_t W, int32_t T, int32_t V, int32_t D, const vo
     if ((int64_t)p.spans * ((D - 1) / 64 + 1) + V / kZeroRows >= 0x7fffffff)
         return set_error(LSGD_ERR_SHAPE, "embed_grad: T=%d of D=%d is too large for one launch", (int)T, (int)D);
 
-    char* base = static_cast<char*>(workspace);
-    uint32_t* keys[2] = {reinterpret_cast<uint32_t*>(base + p.keys[0]), reinterpret_cast<uint32_t*>(base + p.keys[1])};
-    int32_t* pos[2] = {reinterpret_cast<int32_t*>(base + p.pos[0]), reinterpret_cast<int32_t*>(base + p.pos[1])};
-    int at = 0;
-    if (p.tiles == 1) {
-        hipLaunchKernelGGL(sort_small_kernel, dim3((unsigned)W), dim3(kSortThreads), 0, s, tokens, ld_tokens, (int)T, (int)V, p.bits, p.passes, keys[0], pos[0]);
-    } else {
-        uint32_t* counts = reinterpret_cast<uint32_t*>(base + p.counts);
-        const dim3 grid((unsigned)p.tiles, (unsigned)W);
-        for (int k = 0; k < p.passes; ++k) {
-            const uint32_t* kin = k ? keys[at ^ 1] : nullptr;
-            const int32_t* pin = k ? pos[at ^ 1] : nullptr;
-            hipLaunchKernelGGL(sort_count_kernel, grid, dim3(kSortThreads), 0, s, tokens, ld_tokens, kin, (int)T, (int)V, p.bits, k * p.bits, counts);
-            hipLaunchKernelGGL(sort_place_kernel, grid, dim3(kSortThreads), 0, s, tokens, ld_tokens, kin, pin, (int)T, (int)V, p.bits, k * p.bits,
-                               counts, keys[at], pos[at]);
-            if (k + 1 < p.passes) at ^= 1;
-        }
-    }
     GradArgs a{};
     a.dout = dout; a.ld_dout = ld_dout;
-    a.keys = keys[at]; a.pos = pos[at];
-    a.parts = reinterpret_cast<float*>(base + p.parts);
     a.table = dtable; a.ld_table = ld_dtable;
-    a.T = T; a.V = V; a.D = D; a.Dp = p.Dp; a.L = p.L; a.spans = p.spans;
+    a.T = T; a.V = V; a.D = D;
     a.scale = scale; a.accumulate = accumulate;
     const int E = dout_is_bf16 ? 8 : 4;
     const bool wide = D % E == 0 && on(dout, 16) && on(dtable, 16) && (W == 1 || (ld_dout % E == 0 && ld_dtable % 4 == 0));
+    if (T <= kSmallTokens) {
+        SmallArgs q{};
+        q.tokens = tokens; q.ld_tokens = ld_tokens;
+        q.bits = p.bits; q.passes = p.passes;
+        if (dout_is_bf16) wide ? launch_grad_small<uint16_t, 8, true>(a, W, q, s) : launch_grad_small<uint16_t, 8, false>(a, W, q, s);
+        else wide ? launch_grad_small<float, 4, true>(a, W, q, s) : launch_grad_small<float, 4, false>(a, W, q, s);
+        e = hipGetLastError();
+        if (e != hipSuccess) return set_error(LSGD_ERR_HIP, "embed_grad: %s", hipGetErrorString(e));
+        return LSGD_OK;
+    }
+    char* base = static_cast<char*>(workspace);
+    uint32_t* keys[2] = {reinterpret_cast<uint32_t*>(base + p.keys[0]), reinterpret_cast<uint32_t*>(base + p.keys[1])};
+    int32_t* pos[2] = {reinterpret_cast<int32_t*>(base + p.pos[0]), reinterpret_cast<int32_t*>(base + p.pos[1])};
+    uint32_t* counts = reinterpret_cast<uint32_t*>(base + p.counts);
+    const dim3 grid((unsigned)p.tiles, (unsigned)W);
+    int at = 0;
+    for (int k = 0; k < p.passes; ++k) {
+        const uint32_t* kin = k ? keys[at] : nullptr;
+        const int32_t* pin = k ? pos[at] : nullptr;
+        if (k) at ^= 1;
+        auto go = [&](auto count, auto place) {
+            hipLaunchKernelGGL(count, grid, dim3(kSortThreads), 0, s, tokens, ld_tokens, kin, (int)T, (int)V, p.bits, k * p.bits, counts);
+            hipLaunchKernelGGL(place, grid, dim3(kSortThreads), 0, s, tokens, ld_tokens, kin, pin, (int)T, (int)V, p.bits, k * p.bits, counts, keys[at], pos[at]);
+        };
+        if (p.each == 2) go(sort_count_kernel<2>, sort_place_kernel<2>);
+        else go(sort_count_kernel<8>, sort_place_kernel<8>);
+    }
+    a.keys = keys[at]; a.pos = pos[at];
+    a.parts = reinterpret_cast<float*>(base + p.parts);
+    a.Dp = p.Dp; a.spans = p.spans;
     if (dout_is_bf16) launch_grad_team<uint16_t, 8>(a, W, wide, s);
     else launch_grad_team<float, 4>(a, W, wide, s);
     e = hipGetLastError();
