@@ -372,7 +372,9 @@ lsgd_status lsgd_embed_lookup(int32_t W, int32_t T, int32_t V, int32_t D, const 
  *              (tied weights, several batches a step) and rows that no token names are not touched
  *   dout       device, worker w's [T, D] at dout + w*ld_dout (fp32 or bf16)
  *   dtable     device fp32, worker w's [V, D] at dtable + w*ld_dtable, ld_dtable >= V*D; must not overlap the inputs
- *   workspace  device, >= lsgd_embed_grad_workspace_bytes, 256-byte aligned (may be NULL when T = 0); not kept      */
+ *   workspace  device, >= lsgd_embed_grad_workspace_bytes, 256-byte aligned; not kept; may be NULL up to
+ *              LSGD_EMBED_GRAD_ONE_LAUNCH tokens a worker, which take one launch and none                          */
+#define LSGD_EMBED_GRAD_ONE_LAUNCH 8192
 size_t lsgd_embed_grad_workspace_bytes(int32_t W, int32_t T, int32_t V, int32_t D); /* 0 on invalid arguments */
 lsgd_status lsgd_embed_grad(int32_t W, int32_t T, int32_t V, int32_t D, const void* dout, int64_t ld_dout, int32_t dout_is_bf16,
                             const int32_t* tokens, int64_t ld_tokens, float scale, int32_t accumulate, float* dtable, int64_t ld_dtable,

@@ -5,6 +5,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import torch
 
@@ -55,23 +56,9 @@ class _Batch(C.Structure):
     _fields_ = [("kind", C.c_int32), ("desc", C.c_void_p)]
 
 
-class _Rows(C.Structure):
-    _fields_ = [("data", C.c_void_p), ("worker_stride", C.c_int64), ("token_stride", C.c_int64)]
-
-
-class _BlockNorm(C.Structure):
-    _fields_ = [("W", C.c_int32), ("T", C.c_int32), ("D", C.c_int32), ("is_bf16", C.c_int32), ("post_norm", C.c_int32),
-                ("scale", C.c_float), ("eps", C.c_float), ("r", _Rows), ("y", _Rows), ("gate", _Rows), ("r_out", _Rows), ("n", _Rows),
-                ("w_post", C.c_void_p), ("w_pre", C.c_void_p), ("ld_w_post", C.c_int64), ("ld_w_pre", C.c_int64),
-                ("q_post", C.c_void_p), ("q_pre", C.c_void_p)]
-
-
-class _BlockNormGrad(C.Structure):
-    _fields_ = [("W", C.c_int32), ("T", C.c_int32), ("D", C.c_int32), ("is_bf16", C.c_int32), ("post_norm", C.c_int32),
-                ("accumulate", C.c_int32), ("scale", C.c_float), ("dn", _Rows), ("dr_out", _Rows), ("r_out", _Rows), ("y", _Rows),
-                ("gate", _Rows), ("dr", _Rows), ("dy", _Rows), ("dgate", _Rows), ("w_post", C.c_void_p), ("w_pre", C.c_void_p),
-                ("ld_w_post", C.c_int64), ("ld_w_pre", C.c_int64), ("q_post", C.c_void_p), ("q_pre", C.c_void_p),
-                ("dw_post", C.c_void_p), ("dw_pre", C.c_void_p), ("ld_dw_post", C.c_int64), ("ld_dw_pre", C.c_int64)]
+# lsgd_block_norm_args, lsgd_block_norm_grad_args (native layout): sizes and flags, factors, lsgd_rows triples, pointers and strides
+_BLOCK_NORM = struct.Struct("@5i2f" + "P2q" * 5 + "2P2q2P")
+_BLOCK_NORM_GRAD = struct.Struct("@6if" + "P2q" * 8 + "2P2q2P2P2q")
 
 
 class _AdamWTensor(C.Structure):
@@ -129,10 +116,10 @@ def lib():
         L.lsgd_embed_grad_workspace_bytes.argtypes = [C.c_int32] * 4
         L.lsgd_embed_grad.argtypes = [C.c_int32] * 4 + [C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_int64, C.c_float, C.c_int32,
                                                         C.c_void_p, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]
-        L.lsgd_block_norm.argtypes = [C.POINTER(_BlockNorm), C.c_void_p]
+        L.lsgd_block_norm.argtypes = [C.c_char_p, C.c_void_p]
         L.lsgd_block_norm_grad_workspace_bytes.restype = C.c_size_t
         L.lsgd_block_norm_grad_workspace_bytes.argtypes = [C.c_int32] * 3
-        L.lsgd_block_norm_grad.argtypes = [C.POINTER(_BlockNormGrad), C.c_void_p, C.c_size_t, C.c_void_p]
+        L.lsgd_block_norm_grad.argtypes = [C.c_char_p, C.c_void_p, C.c_size_t, C.c_void_p]
         L.lsgd_adamw_workspace_bytes.restype = C.c_size_t
         L.lsgd_adamw_workspace_bytes.argtypes = [C.POINTER(_AdamWTensor), C.c_int32, C.c_int32, C.c_int32]
         L.lsgd_adamw_create.argtypes = [C.POINTER(_AdamWTensor), C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p,
@@ -349,7 +336,12 @@ class Population:
 # ------------------------------------------------------------------------------------------------
 ADAMW_BLOCK = 256
 
-_FLOATS = (torch.float32, torch.bfloat16)
+EMBED_GRAD_ONE_LAUNCH = 8192
+
+_F32, _BF16, _I32 = torch.float32, torch.bfloat16, torch.int32
+_FLOATS = (_F32, _BF16)
+# the handle alone: a torch.cuda.Stream object takes longer to make than a small call
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
 
 
 def _need(ok, msg):
@@ -357,59 +349,54 @@ def _need(ok, msg):
         raise ValueError(msg)
 
 
-def _on_gpu(who, **tensors):
-    """All tensors that are given lie on one GPU; returns it."""
-    dev = None
-    for name, t in tensors.items():
-        if t is None:
-            continue
-        _need(t.is_cuda, f"{who}: {name} is not on a GPU")
-        _need(dev is None or t.device == dev, f"{who}: {name} is on {t.device}, other tensors on {dev}")
-        dev = t.device
-    return dev
+def _gpu(who, first, tensors):
+    """Index of the GPU that `first` and all given (name, tensor) pairs lie on."""
+    i = first.get_device()
+    for name, t in tensors:
+        if t is not None and t.get_device() != i or i < 0:
+            raise ValueError(f"{who}: {name} is not on {'a GPU' if t is None or t.get_device() < 0 or i < 0 else 'the GPU of the others'}")
+    return i
 
 
-def _launch_on(dev, stream):
-    return C.c_void_p((torch.cuda.current_stream(dev) if stream is None else stream).cuda_stream)
+def _call(index, stream, f, *args):
+    """f(*args, stream) with the tensors' GPU current."""
+    if torch.cuda.current_device() == index:
+        status = f(*args, _raw_stream(index) if stream is None else stream.cuda_stream)
+    else:
+        with torch.cuda.device(index):
+            status = f(*args, _raw_stream(index) if stream is None else stream.cuda_stream)
+    if status != 0:
+        _check(status)
 
 
-def _fresh(shape, dtype, dev, stream):
+def _fresh(like, shape, dtype, stream):
     """Memory of the stream that the call runs on, as under torch.cuda.stream(stream): whoever used it before, or will after it is
     freed, is ordered on that stream too."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=dev)
+        return like.new_empty(shape, dtype=dtype)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=dev)
+        return like.new_empty(shape, dtype=dtype)
 
 
-def _workspace(who, nbytes, dev, workspace, stream):
+def _workspace(who, nbytes, like, workspace, stream):
     """The caller's, or memory of this call's own."""
     if nbytes == 0:
         raise LsgdError(-1, lib().lsgd_last_error().decode())
     if workspace is None:
-        workspace = _fresh((nbytes,), torch.uint8, dev, stream)
-    _need(workspace.device == dev and workspace.is_contiguous(), f"{who}: workspace must be contiguous and on {dev}")
+        return _fresh(like, (nbytes,), torch.uint8, stream), nbytes
+    _need(workspace.device == like.device and workspace.is_contiguous(), f"{who}: workspace must be contiguous and on {like.device}")
     return workspace, workspace.numel() * workspace.element_size()
 
 
-def _stride0(t):
-    """Row stride of what the library reads by rows; of a single row any will do."""
-    return int(t.stride(0)) if t.shape[0] > 1 else int(t.numel())
-
-
-def _dense_after(t, k):
-    """Whether dimensions k.. of t lie in memory one after the other without gaps."""
+def _worker_stride(who, name, t, rule):
+    """Row stride of a tensor whose dimensions after the first lie in memory without gaps (of a single row any will do)."""
+    st, sh = t.stride(), t.shape
     want = 1
-    for d in range(t.dim() - 1, k - 1, -1):
-        if t.shape[d] > 1 and t.stride(d) != want:
-            return False
-        want *= t.shape[d]
-    return True
-
-
-def _tokens(who, tokens):
-    _need(tokens.dtype == torch.int32 and tokens.dim() == 2, f"{who}: tokens must be int32 [W, T]")
-    _need(tokens.numel() == 0 or _dense_after(tokens, 1), f"{who}: a worker's tokens must be dense")
+    for d in range(len(sh) - 1, 0, -1):
+        if sh[d] > 1 and st[d] != want and t.numel():
+            raise ValueError(f"{who}: {name} {rule}")
+        want *= sh[d]
+    return st[0] if sh[0] > 1 else want
 
 
 def embed_lookup(table, tokens, scale=1.0, dtype=None, out=None, stream=None):
@@ -417,24 +404,26 @@ def embed_lookup(table, tokens, scale=1.0, dtype=None, out=None, stream=None):
     table: float32 or bfloat16 [W, V, D], dense within a worker (columns of x: x[:, a:a + V * D].unflatten(1, (V, D)));
     tokens: int32 [W, T]; dtype: of the result (the table's if None); out: optional result buffer."""
     who = "embed_lookup"
-    dev = _on_gpu(who, table=table, tokens=tokens, out=out)
-    _tokens(who, tokens)
-    _need(table.dim() == 3 and table.dtype in _FLOATS, f"{who}: table must be float32 or bfloat16 [W, V, D]")
+    index = _gpu(who, table, (("table", table), ("tokens", tokens), ("out", out)))
+    _need(tokens.dtype is _I32 and tokens.dim() == 2, "embed_lookup: tokens must be int32 [W, T]")
+    _need(table.dim() == 3 and table.dtype in _FLOATS, "embed_lookup: table must be float32 or bfloat16 [W, V, D]")
     W, V, D = table.shape
-    T = tokens.shape[1]
-    _need(tokens.shape[0] == W, f"{who}: {tokens.shape[0]} rows of tokens for {W} workers")
-    _need(_dense_after(table, 1), f"{who}: a worker's table must be dense")
+    rows, T = tokens.shape
+    if rows != W:
+        raise ValueError(f"{who}: {rows} rows of tokens for {W} workers")
+    ld_table = _worker_stride(who, "table", table, "must be dense within a worker")
+    ld_tokens = _worker_stride(who, "tokens", tokens, "must be dense within a worker")
     if out is None:
         dtype = table.dtype if dtype is None else dtype
-        _need(dtype in _FLOATS, f"{who}: dtype must be float32 or bfloat16")
-        out = _fresh((W, T, D), dtype, dev, stream)
-    _need(out.shape == (W, T, D) and out.dtype in _FLOATS and (dtype is None or out.dtype == dtype), f"{who}: out must be [W, T, D] of dtype")
-    _need(out.numel() == 0 or _dense_after(out, 1), f"{who}: a worker's part of out must be dense")
-    if tokens.numel() == 0:
-        return out
-    with torch.cuda.device(dev):
-        _check(lib().lsgd_embed_lookup(W, T, V, D, _ptr(table), _stride0(table), int(table.dtype == torch.bfloat16), _ptr(tokens),
-                                       _stride0(tokens), scale, _ptr(out), _stride0(out), int(out.dtype == torch.bfloat16), _launch_on(dev, stream)))
+        _need(dtype in _FLOATS, "embed_lookup: dtype must be float32 or bfloat16")
+        out = _fresh(table, (W, T, D), dtype, stream)
+        ld_out = T * D
+    else:
+        _need(out.shape == (W, T, D) and out.dtype in _FLOATS and (dtype is None or out.dtype == dtype), "embed_lookup: out must be [W, T, D] of dtype")
+        ld_out = _worker_stride(who, "out", out, "must be dense within a worker")
+    if T:
+        _call(index, stream, lib().lsgd_embed_lookup, W, T, V, D, table.data_ptr(), ld_table, table.dtype is _BF16, tokens.data_ptr(), ld_tokens,
+              scale, out.data_ptr(), ld_out, out.dtype is _BF16)
     return out
 
 
@@ -442,38 +431,56 @@ def embed_grad(dout, tokens, dtable, scale=1.0, accumulate=False, workspace=None
     """lsgd_embed_grad: the table's gradient of embed_lookup, into dtable (float32 [W, V, D], dense within a worker).
     dout: float32 or bfloat16 [W, T, D], dense within a worker; accumulate: add to dtable instead of writing all of it."""
     who = "embed_grad"
-    dev = _on_gpu(who, dout=dout, tokens=tokens, dtable=dtable)
-    _tokens(who, tokens)
-    _need(dtable.dim() == 3 and dtable.dtype == torch.float32, f"{who}: dtable must be float32 [W, V, D]")
+    index = _gpu(who, dtable, (("dout", dout), ("tokens", tokens), ("dtable", dtable)))
+    _need(tokens.dtype is _I32 and tokens.dim() == 2, "embed_grad: tokens must be int32 [W, T]")
+    _need(dtable.dim() == 3 and dtable.dtype is _F32, "embed_grad: dtable must be float32 [W, V, D]")
     W, V, D = dtable.shape
-    T = tokens.shape[1]
-    _need(tokens.shape[0] == W and dout.shape == (W, T, D) and dout.dtype in _FLOATS, f"{who}: dout must be float32 or bfloat16 [W, T, D] and tokens [W, T]")
-    _need(_dense_after(dtable, 1), f"{who}: a worker's part of dtable must be dense")
-    _need(dout.numel() == 0 or _dense_after(dout, 1), f"{who}: a worker's part of dout must be dense (an expanded gradient needs .contiguous())")
-    with torch.cuda.device(dev):
-        nbytes = 0
-        if T > 0:
-            workspace, nbytes = _workspace(who, lib().lsgd_embed_grad_workspace_bytes(W, T, V, D), dev, workspace, stream)
-        _check(lib().lsgd_embed_grad(W, T, V, D, _ptr(dout), _stride0(dout) if T else 0, int(dout.dtype == torch.bfloat16), _ptr(tokens),
-                                     _stride0(tokens) if T else 0, scale, int(bool(accumulate)), _ptr(dtable), _stride0(dtable),
-                                     _ptr(workspace) if T else None, nbytes, _launch_on(dev, stream)))
+    rows, T = tokens.shape
+    _need(rows == W and dout.shape == (W, T, D) and dout.dtype in _FLOATS, "embed_grad: dout must be float32 or bfloat16 [W, T, D] and tokens [W, T]")
+    ld_table = _worker_stride(who, "dtable", dtable, "must be dense within a worker")
+    ld_dout = _worker_stride(who, "dout", dout, "must be dense within a worker (an expanded gradient needs .contiguous())")
+    ld_tokens = _worker_stride(who, "tokens", tokens, "must be dense within a worker")
+    L = lib()
+    ws, nbytes = None, 0
+    if T > EMBED_GRAD_ONE_LAUNCH or workspace is not None:
+        workspace, nbytes = _workspace(who, L.lsgd_embed_grad_workspace_bytes(W, T, V, D), dtable, workspace, stream)
+        ws = workspace.data_ptr()
+    _call(index, stream, L.lsgd_embed_grad, W, T, V, D, dout.data_ptr(), ld_dout, dout.dtype is _BF16, tokens.data_ptr(), ld_tokens, scale,
+          bool(accumulate), dtable.data_ptr(), ld_table, ws, nbytes)
 
 
-def _rows(who, name, t, shape, dtype):
+_NO_ROWS = (0, 0, 0)
+
+
+def _rows(who, name, t, shape, dtype, index):
+    """lsgd_rows of an activation tensor."""
     if t is None:
-        return _Rows(None, 0, 0)
-    _need(tuple(t.shape) == tuple(shape) and t.dtype == dtype, f"{who}: {name} must be {dtype} {list(shape)}")
-    _need(t.numel() == 0 or t.shape[2] == 1 or t.stride(2) == 1, f"{who}: rows of {name} must be dense")
+        return _NO_ROWS
+    if t.shape != shape or t.dtype is not dtype:
+        raise ValueError(f"{who}: {name} must be {dtype} {list(shape)}")
+    if t.get_device() != index:
+        raise ValueError(f"{who}: {name} is not on the GPU of the others")
     W, T, D = shape
+    sw, st, sd = t.stride()
+    if sd != 1 and D > 1 and t.numel():
+        raise ValueError(f"{who}: rows of {name} must be dense")
     # a dimension of one element has no stride that means anything
-    return _Rows(t.data_ptr() or None, t.stride(0) if W > 1 else T * D, t.stride(1) if T > 1 else D)
+    return t.data_ptr(), sw if W > 1 else T * D, st if T > 1 else D
 
 
-def _weights(who, name, w, W, D):
+def _weights(who, name, w, W, D, index):
     if w is None:
-        return None, 0
-    _need(w.dtype == torch.float32 and tuple(w.shape) == (W, D) and (D == 1 or w.stride(1) == 1), f"{who}: {name} must be float32 [W, D] with dense rows")
+        return 0, 0
+    if w.dtype is not _F32 or w.shape != (W, D) or w.get_device() != index or (D > 1 and w.stride(1) != 1):
+        raise ValueError(f"{who}: {name} must be float32 [W, D] with dense rows, on the GPU of the others")
     return w.data_ptr(), w.stride(0) if W > 1 else D
+
+
+def _stats(who, stats, W, T, index):
+    _need(stats.dtype is _F32 and stats.shape == (2, W, T) and stats.is_contiguous() and stats.get_device() == index,
+          f"{who}: stats must be contiguous float32 [2, W, T], on the GPU of the others")
+    p = stats.data_ptr()
+    return p, p + 4 * W * T if p else 0
 
 
 def block_norm(r, y=None, gate=None, w_post=None, w_pre=None, scale=1.0, eps=1e-6, post_norm=True, pre_norm=True, r_out=None, n=None,
@@ -484,27 +491,27 @@ def block_norm(r, y=None, gate=None, w_post=None, w_pre=None, scale=1.0, eps=1e-
     Returns (r_out, n, stats); stats: float32 [2, W, T], what block_norm_grad needs.  r_out, n, stats: optional buffers (r_out
     may be r)."""
     who = "block_norm"
-    dev = _on_gpu(who, r=r, y=y, gate=gate, w_post=w_post, w_pre=w_pre, r_out=r_out, n=n, stats=stats)
-    _need(r.dim() == 3 and r.dtype in _FLOATS, f"{who}: r must be float32 or bfloat16 [W, T, D]")
-    W, T, D = r.shape
-    _need(y is not None or pre_norm, f"{who}: neither y nor a norm after it: nothing to do")
-    _need(y is not None or (gate is None and r_out is None and w_post is None), f"{who}: gate, w_post and r_out need y")
-    _need(pre_norm or (n is None and w_pre is None), f"{who}: n and w_pre need pre_norm")
+    dt = r.dtype
+    _need(r.dim() == 3 and dt in _FLOATS, "block_norm: r must be float32 or bfloat16 [W, T, D]")
+    index = _gpu(who, r, (("r", r),))
+    shape = r.shape
+    W, T, D = shape
+    _need(y is not None or pre_norm, "block_norm: neither y nor a norm after it: nothing to do")
+    _need(y is not None or (gate is None and r_out is None and w_post is None), "block_norm: gate, w_post and r_out need y")
+    _need(pre_norm or (n is None and w_pre is None), "block_norm: n and w_pre need pre_norm")
     if y is not None and r_out is None:
-        r_out = _fresh((W, T, D), r.dtype, dev, stream)
+        r_out = _fresh(r, shape, dt, stream)
     if pre_norm and n is None:
-        n = _fresh((W, T, D), r.dtype, dev, stream)
+        n = _fresh(r, shape, dt, stream)
     if stats is None:
-        stats = _fresh((2, W, T), torch.float32, dev, stream)
-    _need(stats.dtype == torch.float32 and tuple(stats.shape) == (2, W, T) and stats.is_contiguous(), f"{who}: stats must be contiguous float32 [2, W, T]")
-    wp, lp = _weights(who, "w_post", w_post, W, D)
-    wn, ln = _weights(who, "w_pre", w_pre, W, D)
-    shape = (W, T, D)
-    a = _BlockNorm(W, T, D, int(r.dtype == torch.bfloat16), int(bool(post_norm)), scale, eps, _rows(who, "r", r, shape, r.dtype),
-                   _rows(who, "y", y, shape, r.dtype), _rows(who, "gate", gate, shape, r.dtype), _rows(who, "r_out", r_out, shape, r.dtype),
-                   _rows(who, "n", n, shape, r.dtype), wp, wn, lp, ln, stats[0].data_ptr() if y is not None else None, stats[1].data_ptr())
-    with torch.cuda.device(dev):
-        _check(lib().lsgd_block_norm(C.byref(a), _launch_on(dev, stream)))
+        stats = _fresh(r, (2, W, T), _F32, stream)
+    q_post, q_pre = _stats(who, stats, W, T, index)
+    wp, lp = _weights(who, "w_post", w_post, W, D, index)
+    wn, ln = _weights(who, "w_pre", w_pre, W, D, index)
+    a = _BLOCK_NORM.pack(W, T, D, dt is _BF16, bool(post_norm), scale, eps, *_rows(who, "r", r, shape, dt, index), *_rows(who, "y", y, shape, dt, index),
+                         *_rows(who, "gate", gate, shape, dt, index), *_rows(who, "r_out", r_out, shape, dt, index), *_rows(who, "n", n, shape, dt, index),
+                         wp, wn, lp, ln, q_post if y is not None else 0, q_pre)
+    _call(index, stream, lib().lsgd_block_norm, a)
     return (r if y is None else r_out), n, stats
 
 
@@ -514,34 +521,36 @@ def block_norm_grad(dn, dr_out, r_out, stats, y=None, gate=None, w_post=None, w_
     block, or None); r_out, stats: what block_norm returned; the rest as given to it.  dw_post, dw_pre: float32 [W, D]
     (columns of g) that receive the weights' gradients, added to what is there if accumulate; dr, dy, dgate: optional buffers."""
     who = "block_norm_grad"
-    dev = _on_gpu(who, dn=dn, dr_out=dr_out, r_out=r_out, stats=stats, y=y, gate=gate, w_post=w_post, w_pre=w_pre, dw_post=dw_post,
-                  dw_pre=dw_pre, dr=dr, dy=dy, dgate=dgate)
-    _need(r_out.dim() == 3 and r_out.dtype in _FLOATS, f"{who}: r_out must be float32 or bfloat16 [W, T, D]")
-    W, T, D = shape = tuple(r_out.shape)
     dt = r_out.dtype
-    _need(dn is not None or dr_out is not None, f"{who}: neither dn nor dr_out is given")
-    _need(y is not None or (gate is None and dw_post is None and dy is None and dgate is None), f"{who}: gate, dw_post, dy and dgate need y")
-    _need(gate is not None or dgate is None, f"{who}: dgate needs gate")
-    _need(stats.dtype == torch.float32 and tuple(stats.shape) == (2, W, T) and stats.is_contiguous(), f"{who}: stats must be contiguous float32 [2, W, T]")
+    _need(r_out.dim() == 3 and dt in _FLOATS, "block_norm_grad: r_out must be float32 or bfloat16 [W, T, D]")
+    index = _gpu(who, r_out, (("r_out", r_out),))
+    shape = r_out.shape
+    W, T, D = shape
+    _need(dn is not None or dr_out is not None, "block_norm_grad: neither dn nor dr_out is given")
+    _need(y is not None or (gate is None and dw_post is None and dy is None and dgate is None), "block_norm_grad: gate, dw_post, dy and dgate need y")
+    _need(gate is not None or dgate is None, "block_norm_grad: dgate needs gate")
     if dr is None:
-        dr = _fresh(shape, dt, dev, stream)
+        dr = _fresh(r_out, shape, dt, stream)
     if y is not None and dy is None:
-        dy = _fresh(shape, dt, dev, stream)
+        dy = _fresh(r_out, shape, dt, stream)
     if gate is not None and dgate is None:
-        dgate = _fresh(shape, dt, dev, stream)
-    wp, lp = _weights(who, "w_post", w_post, W, D)
-    wn, ln = _weights(who, "w_pre", w_pre, W, D)
-    dwp, ldp = _weights(who, "dw_post", dw_post, W, D)
-    dwn, ldn = _weights(who, "dw_pre", dw_pre, W, D)
-    R = lambda name, t: _rows(who, name, t, shape, dt)
-    a = _BlockNormGrad(W, T, D, int(dt == torch.bfloat16), int(bool(post_norm)), int(bool(accumulate)), scale, R("dn", dn), R("dr_out", dr_out),
-                       R("r_out", r_out), R("y", y), R("gate", gate), R("dr", dr), R("dy", dy), R("dgate", dgate), wp, wn, lp, ln,
-                       stats[0].data_ptr(), stats[1].data_ptr(), dwp, dwn, ldp, ldn)
-    with torch.cuda.device(dev):
-        nbytes = 0
-        if dwp or dwn:
-            workspace, nbytes = _workspace(who, lib().lsgd_block_norm_grad_workspace_bytes(W, T, D), dev, workspace, stream)
-        _check(lib().lsgd_block_norm_grad(C.byref(a), _ptr(workspace), nbytes, _launch_on(dev, stream)))
+        dgate = _fresh(r_out, shape, dt, stream)
+    q_post, q_pre = _stats(who, stats, W, T, index)
+    wp, lp = _weights(who, "w_post", w_post, W, D, index)
+    wn, ln = _weights(who, "w_pre", w_pre, W, D, index)
+    dwp, ldp = _weights(who, "dw_post", dw_post, W, D, index)
+    dwn, ldn = _weights(who, "dw_pre", dw_pre, W, D, index)
+    a = _BLOCK_NORM_GRAD.pack(W, T, D, dt is _BF16, bool(post_norm), bool(accumulate), scale, *_rows(who, "dn", dn, shape, dt, index),
+                              *_rows(who, "dr_out", dr_out, shape, dt, index), *_rows(who, "r_out", r_out, shape, dt, index),
+                              *_rows(who, "y", y, shape, dt, index), *_rows(who, "gate", gate, shape, dt, index), *_rows(who, "dr", dr, shape, dt, index),
+                              *_rows(who, "dy", dy, shape, dt, index), *_rows(who, "dgate", dgate, shape, dt, index), wp, wn, lp, ln, q_post, q_pre,
+                              dwp, dwn, ldp, ldn)
+    L = lib()
+    ws, nbytes = None, 0
+    if dwp or dwn:
+        workspace, nbytes = _workspace(who, L.lsgd_block_norm_grad_workspace_bytes(W, T, D), r_out, workspace, stream)
+        ws = workspace.data_ptr()
+    _call(index, stream, L.lsgd_block_norm_grad, a, ws, nbytes)
     return dr, dy, dgate
 
 
@@ -593,16 +602,16 @@ class AdamW:
     def __init__(self, tensors, bits=32, stream=None, workspace=None):
         self._h = None
         self.tensors = list(tensors)
-        _need(self.tensors, "AdamW: no tensors")
-        dev = _on_gpu("AdamW", **{f"{name} of tensor {k}": t for k, a in enumerate(self.tensors) for name, t in a.t.items()})
+        _need(len(self.tensors) > 0 and self.tensors[0].t["x"] is not None, "AdamW: no tensors")
+        self._index = _gpu("AdamW", self.tensors[0].t["x"], [(f"{name} of tensor {k}", t) for k, a in enumerate(self.tensors) for name, t in a.t.items()])
+        dev = self.tensors[0].t["x"].device
         g_dtype = self.tensors[0].t["g"].dtype
         _need(g_dtype in _FLOATS, "AdamW: g must be float32 or bfloat16")
         arr = (_AdamWTensor * len(self.tensors))(*[a._c(k, bits, g_dtype) for k, a in enumerate(self.tensors)])
         self.stream = torch.cuda.current_stream(dev) if stream is None else stream
-        self.device = dev
         bf = int(g_dtype == torch.bfloat16)
         with torch.cuda.device(dev):
-            self.workspace, nbytes = _workspace("AdamW", lib().lsgd_adamw_workspace_bytes(arr, len(arr), bits, bf), dev, workspace, stream)
+            self.workspace, nbytes = _workspace("AdamW", lib().lsgd_adamw_workspace_bytes(arr, len(arr), bits, bf), self.tensors[0].t["x"], workspace, stream)
             h = C.c_void_p()
             _check(lib().lsgd_adamw_create(arr, len(arr), bits, bf, _ptr(self.workspace), nbytes, C.c_void_p(self.stream.cuda_stream), C.byref(h)))
         self._h = h
@@ -620,10 +629,17 @@ class AdamW:
 
     def step(self, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=1.0):
         """One step; `step` counts from 1."""
-        with torch.cuda.device(self.device):
-            _check(lib().lsgd_adamw_step(self._h, lr, beta1, beta2, eps, int(step), grad_scale))
+        self._call(lib().lsgd_adamw_step, lr, beta1, beta2, eps, int(step), grad_scale)
 
     def moments(self):
         """8 bits: fills m_values and v_values of the tensors that have them."""
-        with torch.cuda.device(self.device):
-            _check(lib().lsgd_adamw_moments(self._h))
+        self._call(lib().lsgd_adamw_moments)
+
+    def _call(self, f, *args):
+        if torch.cuda.current_device() == self._index:
+            status = f(self._h, *args)
+        else:
+            with torch.cuda.device(self._index):
+                status = f(self._h, *args)
+        if status != 0:
+            _check(status)

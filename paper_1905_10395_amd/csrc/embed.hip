@@ -548,7 +548,8 @@ __global__ __launch_bounds__(kThreads) void grad_join_kernel(GradArgs a)
 }
 
 // ---- the gradient in one launch ----
-constexpr int kSmallTokens = 8 * kSortThreads;     // tokens a worker may have for it
+constexpr int kSmallTokens = LSGD_EMBED_GRAD_ONE_LAUNCH;
+static_assert(kSmallTokens == 8 * kSortThreads, "a workgroup sorts them, eight a thread");
 constexpr int kSmallRows = 1 << 14;                // table rows whose zeros a workgroup may write
 constexpr int kSmallShared = 16;                   // places of a run from which on a workgroup's wavefronts share it
 
@@ -916,10 +917,10 @@ lsgd_status lsgd_embed_grad(int32_t W, int32_t T, int32_t V, int32_t D, const vo
     if (W > 1 && (ld_tokens < T || ld_dout < (int64_t)T * D))
         return set_error(LSGD_ERR_SHAPE, "embed_grad: a worker stride is smaller than what a worker has (ld_tokens=%lld, ld_dout=%lld)",
                          (long long)ld_tokens, (long long)ld_dout);
-    if (!workspace) return set_error(LSGD_ERR_INVALID_ARG, "embed_grad: workspace is NULL");
-    if (!on(workspace, kAlign)) return set_error(LSGD_ERR_INVALID_ARG, "embed_grad: workspace must be 256-byte aligned");
     const Plan p = make_plan(W, T, V, D);
-    if (workspace_bytes < p.total) return set_error(LSGD_ERR_NOMEM, "embed_grad: workspace of %zu bytes < %zu needed", workspace_bytes, p.total);
+    if (!workspace && T > kSmallTokens) return set_error(LSGD_ERR_INVALID_ARG, "embed_grad: workspace is NULL");
+    if (!on(workspace, kAlign)) return set_error(LSGD_ERR_INVALID_ARG, "embed_grad: workspace must be 256-byte aligned");
+    if (workspace && workspace_bytes < p.total) return set_error(LSGD_ERR_NOMEM, "embed_grad: workspace of %zu bytes < %zu needed", workspace_bytes, p.total);
     if ((int64_t)p.spans * ((D - 1) / 64 + 1) + V / kZeroRows >= 0x7fffffff)
         return set_error(LSGD_ERR_SHAPE, "embed_grad: T=%d of D=%d is too large for one launch", (int)T, (int)D);
 
