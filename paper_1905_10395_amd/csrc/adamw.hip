@@ -20,7 +20,6 @@
 #include <cmath>
 #include <cstring>
 #include <new>
-#include <type_traits>
 #include <vector>
 
 #include "common.h"
@@ -181,32 +180,50 @@ __global__ __launch_bounds__(kThreads32) void adamw32_kernel(const Tensor* __res
 }
 
 // ---- 8-bit moments ----
-// The wavefront's largest value, in a scalar register (NaN counts as nothing).
-__device__ __forceinline__ float wave_max(float a)
+// Largest values over the wavefront, of two lists at once (the one's lane shifts fill the other's wait states), in scalar
+// registers.  Magnitudes are compared as bit patterns: NaN lies above infinity there.
+template <int CTRL>
+__device__ __forceinline__ uint32_t max_lanes(uint32_t a)
 {
-    auto step = [&](auto ctrl) {
-        const int b = __builtin_amdgcn_update_dpp(__float_as_int(a), __float_as_int(a), decltype(ctrl)::value, 0xF, 0xF, false);
-        a = fmaxf(a, __int_as_float(b));
-    };
-    step(std::integral_constant<int, 0x111>{});      // the lane one to the left, in its row of 16
-    step(std::integral_constant<int, 0x112>{});
-    step(std::integral_constant<int, 0x114>{});
-    step(std::integral_constant<int, 0x118>{});      // the row's last lane has the row's largest
-    step(std::integral_constant<int, 0x142>{});      // to the next row, to the upper half
-    step(std::integral_constant<int, 0x143>{});
-    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(a), kWave - 1));
+    const uint32_t b = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)a, CTRL, 0xF, 0xF, false);
+    return a > b ? a : b;
+}
+__device__ __forceinline__ void wave_max2(uint32_t& a, uint32_t& b)
+{
+    a = max_lanes<0x111>(a); b = max_lanes<0x111>(b);      // the lane one to the left, in its row of 16
+    a = max_lanes<0x112>(a); b = max_lanes<0x112>(b);
+    a = max_lanes<0x114>(a); b = max_lanes<0x114>(b);
+    a = max_lanes<0x118>(a); b = max_lanes<0x118>(b);      // the row's last lane has the row's largest
+    a = max_lanes<0x142>(a); b = max_lanes<0x142>(b);      // to the next row, to the upper half
+    a = max_lanes<0x143>(a); b = max_lanes<0x143>(b);
+    a = (uint32_t)__builtin_amdgcn_readlane((int)a, kWave - 1);
+    b = (uint32_t)__builtin_amdgcn_readlane((int)b, kWave - 1);
 }
 
-__device__ __forceinline__ bool finite(float a) { return fabsf(a) < __builtin_inff(); }
+constexpr uint32_t kInf = 0x7F800000u;
+__device__ __forceinline__ uint32_t magnitude(float a) { return __float_as_uint(a) & 0x7FFFFFFFu; }
 
-__device__ __forceinline__ float largest(const float (&a)[4])
+// The largest finite |m| and r of a block.
+__device__ __forceinline__ void largest(const float (&m)[4], const float (&r)[4], float& bm, float& bv)
 {
-    const float big = wave_max(fmaxf(fmaxf(fabsf(a[0]), fabsf(a[1])), fmaxf(fabsf(a[2]), fabsf(a[3]))));
-    if (big < __builtin_inff()) return big;
-    float f = 0.0f;                                  // the largest finite one, then
+    uint32_t a = 0, b = 0;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) f = fmaxf(f, finite(a[e]) ? fabsf(a[e]) : 0.0f);
-    return wave_max(f);
+    for (int e = 0; e < 4; ++e) {
+        a = max(a, magnitude(m[e]));
+        b = max(b, magnitude(r[e]));
+    }
+    wave_max2(a, b);
+    if (a >= kInf || b >= kInf) {                          // something is not: once more without it
+        a = b = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            a = max(a, magnitude(m[e]) < kInf ? magnitude(m[e]) : 0);
+            b = max(b, magnitude(r[e]) < kInf ? magnitude(r[e]) : 0);
+        }
+        wave_max2(a, b);
+    }
+    bm = __uint_as_float(a);
+    bv = __uint_as_float(b);
 }
 
 struct Scales {
@@ -312,7 +329,9 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(const Tensor* __restri
             }
         }
     }
-    const Scales s = scales_of(largest(me), largest(re));
+    float bm, bv;
+    largest(me, re, bm, bv);
+    const Scales s = scales_of(bm, bv);
     const int least = s.v > 0.0f ? 1 : 0;
     int qm[4], qv[4];
 #pragma unroll
