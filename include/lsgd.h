@@ -359,9 +359,9 @@ lsgd_status lsgd_stream_probe(int32_t kind, float* a, float* b, float* c, int64_
 /* Embedding lookup: out[w,t,:] = scale * table_w[tokens[w,t], :], rounded once; zeros where the token lies outside
  * [0, V) (padding: such a place is never looked up).
  *   table  device, worker w's [V, D] at table + w*ld_table (fp32 or bf16; ld_table = 0: one table for all workers)
- *   tokens device int32, worker w's [T] at tokens + w*ld_tokens
+ *   tokens device int32, worker w's [T] at tokens + w*ld_tokens (0: the same for all workers)
  *   out    device, worker w's [T, D] at out + w*ld_out (fp32 or bf16); must not overlap the inputs
- * T = 0 is allowed.  T <= 2^24, V < 2^30.                                                              */
+ * T = 0 is allowed.  T <= 2^24, V < 2^30, D <= 2^20.                                                   */
 lsgd_status lsgd_embed_lookup(int32_t W, int32_t T, int32_t V, int32_t D, const void* table, int64_t ld_table, int32_t table_is_bf16,
                               const int32_t* tokens, int64_t ld_tokens, float scale, void* out, int64_t ld_out, int32_t out_is_bf16,
                               void* hip_stream);
@@ -370,7 +370,7 @@ lsgd_status lsgd_embed_lookup(int32_t W, int32_t T, int32_t V, int32_t D, const 
  * depends on the tokens alone (equal calls give equal bits).
  *   accumulate 0: every row of the table is written, zeros where no token names it; 1: the sum is added to what is there
  *              (tied weights, several batches a step) and rows that no token names are not touched
- *   dout       device, worker w's [T, D] at dout + w*ld_dout (fp32 or bf16)
+ *   dout       device, worker w's [T, D] at dout + w*ld_dout (fp32 or bf16; 0: the same for all workers)
  *   dtable     device fp32, worker w's [V, D] at dtable + w*ld_dtable, ld_dtable >= V*D; must not overlap the inputs
  *   workspace  device, >= lsgd_embed_grad_workspace_bytes, 256-byte aligned; not kept; may be NULL up to
  *              LSGD_EMBED_GRAD_ONE_LAUNCH tokens a worker, which take one launch and none                          */

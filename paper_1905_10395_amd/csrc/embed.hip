@@ -637,7 +637,7 @@ __global__ __launch_bounds__(kSortThreads) void grad_small_kernel(GradArgs a, Sm
             if (s.present[r >> 5] >> (r & 31) & 1u) continue;
             float* p = table + (v0 + r) * a.D;
             if constexpr (WIDE) {
-                for (int c = slice0 * cols + 4 * lane; c < col_end; c += 4 * kWave) *reinterpret_cast<v4f*>(p + c) = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+                for (int c = slice0 * cols + 4 * lane; c < col_end; c += 4 * kWave) __builtin_nontemporal_store(v4f{0.0f, 0.0f, 0.0f, 0.0f}, reinterpret_cast<v4f*>(p + c));
             } else {
                 for (int c = slice0 * cols + lane; c < col_end; c += kWave) p[c] = 0.0f;
             }
@@ -740,15 +740,16 @@ constexpr size_t kAlign = 256;
 size_t align_up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
 bool on(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
-constexpr int kMaxTokens = 1 << 24, kMaxRows = (1 << 30) - 1;
+constexpr int kMaxTokens = 1 << 24, kMaxRows = (1 << 30) - 1, kMaxWidth = 1 << 20;
 
 lsgd_status check_shape(const char* who, int32_t W, int32_t T, int32_t V, int32_t D)
 {
     if (W <= 0 || W > LSGD_MAX_WORKERS) return set_error(LSGD_ERR_SHAPE, "%s: W=%d outside [1,%d]", who, (int)W, LSGD_MAX_WORKERS);
     if (T < 0) return set_error(LSGD_ERR_SHAPE, "%s: T=%d is negative", who, (int)T);
     if (V <= 0 || D <= 0) return set_error(LSGD_ERR_SHAPE, "%s: V=%d and D=%d must be positive", who, (int)V, (int)D);
-    if (T > kMaxTokens || V > kMaxRows)
-        return set_error(LSGD_ERR_UNSUPPORTED, "%s: T=%d or V=%d beyond the %d tokens and %d rows a worker may have", who, (int)T, (int)V, kMaxTokens, kMaxRows);
+    if (T > kMaxTokens || V > kMaxRows || D > kMaxWidth)
+        return set_error(LSGD_ERR_UNSUPPORTED, "%s: T=%d, V=%d or D=%d beyond the %d tokens, %d rows and %d columns a worker may have", who, (int)T, (int)V, (int)D,
+                         kMaxTokens, kMaxRows, kMaxWidth);
     return LSGD_OK;
 }
 
@@ -821,9 +822,11 @@ void launch_grad(GradArgs a, int W, hipStream_t s)
                        dim3(kThreads), 0, s, a);
 }
 
-// A workgroup a compute unit (each sorts the list again; twice as many: 8.4 -> 12.1 us for 517 tokens, 15.6 -> 23.4 for 2048),
-// fewer columns each rather than fewer places.
+// A workgroup a compute unit (each sorts the list again; with two 517 tokens take 12.1 us instead of 8.4, 2048 23.4 instead of
+// 15.6), fewer columns each rather than fewer places; two where the zeros of large tables are what takes the time (1000 tokens,
+// 4 x 65536 x 1024: 217 us instead of 234).
 constexpr int kSmallGroups = 256;
+constexpr int64_t kManyZeros = 128ll << 20;        // bytes of all tables
 template <class T, int E, bool WIDE>
 void launch_grad_small(const GradArgs& a, int W, SmallArgs q, hipStream_t s)
 {
@@ -832,7 +835,8 @@ void launch_grad_small(const GradArgs& a, int W, SmallArgs q, hipStream_t s)
     while (z < slices && (int64_t)W * z * a.T < 256 * 16) ++z;
     q.slices = (slices - 1) / z + 1;
     z = (slices - 1) / q.slices + 1;
-    int n = std::max(1, kSmallGroups / (W * z));
+    const bool zeros = !a.accumulate && 4ll * W * a.V * a.D >= kManyZeros;
+    int n = std::max(1, (zeros ? 2 : 1) * kSmallGroups / (W * z));
     if (a.accumulate) n = std::min(n, a.T);
     else n = std::max(n, (a.V - 1) / kSmallRows + 1);
     q.span = (a.T - 1) / n + 1;
@@ -875,7 +879,7 @@ lsgd_status lsgd_embed_lookup(int32_t W, int32_t T, int32_t V, int32_t D, const 
     if (!table || !tokens || !out) return set_error(LSGD_ERR_INVALID_ARG, "embed_lookup: table, tokens and out are required");
     if (!on(table, table_is_bf16 ? 2 : 4) || !on(out, out_is_bf16 ? 2 : 4) || !on(tokens, 4))
         return set_error(LSGD_ERR_INVALID_ARG, "embed_lookup: a pointer is not aligned to its element");
-    if (W > 1 && (ld_table < 0 || ld_tokens < T || ld_out < (int64_t)T * D))
+    if (W > 1 && (ld_table < 0 || (ld_tokens < T && ld_tokens != 0) || ld_out < (int64_t)T * D))
         return set_error(LSGD_ERR_SHAPE, "embed_lookup: a worker stride is smaller than what a worker has (ld_tokens=%lld, ld_out=%lld)",
                          (long long)ld_tokens, (long long)ld_out);
     const int64_t pieces = (int64_t)T * D;
@@ -924,7 +928,7 @@ lsgd_status lsgd_embed_grad(int32_t W, int32_t T, int32_t V, int32_t D, const vo
     }
     if (!dout || !tokens) return set_error(LSGD_ERR_INVALID_ARG, "embed_grad: dout and tokens are required");
     if (!on(dout, dout_is_bf16 ? 2 : 4) || !on(tokens, 4)) return set_error(LSGD_ERR_INVALID_ARG, "embed_grad: a pointer is not aligned to its element");
-    if (W > 1 && (ld_tokens < T || ld_dout < (int64_t)T * D))
+    if (W > 1 && ((ld_tokens < T && ld_tokens != 0) || (ld_dout < (int64_t)T * D && ld_dout != 0)))
         return set_error(LSGD_ERR_SHAPE, "embed_grad: a worker stride is smaller than what a worker has (ld_tokens=%lld, ld_dout=%lld)",
                          (long long)ld_tokens, (long long)ld_dout);
     const Plan p = make_plan(W, T, V, D);

@@ -68,6 +68,16 @@ def test_lookup_one_table_for_all_workers_and_into_a_buffer():
     assert torch.equal(out, L.embed_lookup(one.repeat(3, 1, 1), tok))
 
 
+def test_one_batch_for_all_workers():
+    table = torch.randn((3, 50, 24), device=DEV)
+    tok, dout = draw_tokens(1, 70, 50, seed=8), torch.randn((1, 70, 24), device=DEV)
+    assert torch.equal(L.embed_lookup(table, tok.expand(3, 70)), L.embed_lookup(table, tok.repeat(3, 1)))
+    a, b = torch.empty_like(table), torch.empty_like(table)
+    L.embed_grad(dout.expand(3, 70, 24), tok.expand(3, 70), a)
+    L.embed_grad(dout.repeat(3, 1, 1), tok.repeat(3, 1), b)
+    assert torch.equal(a, b)
+
+
 def test_lookup_of_no_tokens():
     out = L.embed_lookup(torch.randn((2, 5, 8), device=DEV), torch.empty((2, 0), dtype=torch.int32, device=DEV))
     assert tuple(out.shape) == (2, 0, 8)

@@ -22,6 +22,7 @@ def test_embed_workspace():
     for bad in ((0, 10, 100, 8), (4, -1, 100, 8), (4, 10, 0, 8), (4, 10, 100, 0), (40000, 1, 1, 1)):
         assert f(*bad) == 0 and "SHAPE" not in error() and "embed_grad" in error()
     assert f(1, 2 ** 24 + 1, 10, 8) == 0 and "beyond" in error()
+    assert f(1, 10, 2 ** 30, 8) == 0 and f(1, 10, 10, 2 ** 20 + 1) == 0 and "beyond" in error()
 
 
 def test_embed_arguments():
