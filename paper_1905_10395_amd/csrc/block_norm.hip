@@ -29,6 +29,9 @@ namespace {
 
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+// As they lie in rows of any width and stride: the chip's 16-byte accesses need no alignment.
+typedef v4f v4f_any __attribute__((aligned(4)));
+typedef v4u v4u_any __attribute__((aligned(2)));
 
 constexpr int E = 8;              // elements of a piece: 16 bytes of bf16, twice that of fp32
 
@@ -60,56 +63,72 @@ struct NormGradArgs {
 };
 
 // Activations are read once and written once; streaming accesses in both directions took 548 us where plain ones took 572,
-// either direction alone 557.
+// either direction alone 557.  Pieces that are not aligned go through the caches, which put their lines together.
+template <bool WIDE, class VA, class V, class P>
+__device__ __forceinline__ V load16(const P* p)
+{
+    if constexpr (WIDE) return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
+    else return *reinterpret_cast<const VA*>(p);
+}
+template <bool WIDE, class VA, class V, class P>
+__device__ __forceinline__ void store16(V v, P* p)
+{
+    if constexpr (WIDE) __builtin_nontemporal_store(v, reinterpret_cast<V*>(p));
+    else *reinterpret_cast<VA*>(p) = v;
+}
+template <bool WIDE>
 __device__ __forceinline__ void load8(const float* p, float (&v)[E])
 {
-    const v4f a = __builtin_nontemporal_load(reinterpret_cast<const v4f*>(p)), b = __builtin_nontemporal_load(reinterpret_cast<const v4f*>(p + 4));
+    const v4f a = load16<WIDE, v4f_any, v4f>(p), b = load16<WIDE, v4f_any, v4f>(p + 4);
 #pragma unroll
     for (int e = 0; e < 4; ++e) { v[e] = a[e]; v[e + 4] = b[e]; }
 }
+template <bool WIDE>
 __device__ __forceinline__ void load8(const uint16_t* p, float (&v)[E])
 {
-    const v4u a = __builtin_nontemporal_load(reinterpret_cast<const v4u*>(p));
+    const v4u a = load16<WIDE, v4u_any, v4u>(p);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         v[2 * e] = __uint_as_float(a[e] << 16);
         v[2 * e + 1] = __uint_as_float(a[e] & 0xFFFF0000u);
     }
 }
+template <bool WIDE>
 __device__ __forceinline__ void store8(float* p, const float (&v)[E])
 {
-    __builtin_nontemporal_store(v4f{v[0], v[1], v[2], v[3]}, reinterpret_cast<v4f*>(p));
-    __builtin_nontemporal_store(v4f{v[4], v[5], v[6], v[7]}, reinterpret_cast<v4f*>(p + 4));
+    store16<WIDE, v4f_any>(v4f{v[0], v[1], v[2], v[3]}, p);
+    store16<WIDE, v4f_any>(v4f{v[4], v[5], v[6], v[7]}, p + 4);
 }
+template <bool WIDE>
 __device__ __forceinline__ void store8(uint16_t* p, const float (&v)[E])
 {
     const v4u a = {f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]), f32x2_to_bf16x2(v[4], v[5]), f32x2_to_bf16x2(v[6], v[7])};
-    __builtin_nontemporal_store(a, reinterpret_cast<v4u*>(p));
+    store16<WIDE, v4u_any>(a, p);
 }
 __device__ __forceinline__ float get1(const float* p) { return *p; }
 __device__ __forceinline__ float get1(const uint16_t* p) { return bf16_to_f32(*p); }
 __device__ __forceinline__ void put1(float* p, float v) { *p = v; }
 __device__ __forceinline__ void put1(uint16_t* p, float v) { *p = f32_to_bf16_rne(v); }
 
-// A lane's N pieces of a row: adjacent elements where rows are aligned for 16-byte accesses (WIDE), else one element
-// every `ts` (the team's lanes) columns.  Elements past the row's end read zero and are not written.
+// A lane's N pieces of a row, of E adjacent elements each; WIDE: all of them whole and 16-byte aligned, else the row's last
+// piece may be shorter.  Elements past the row's end read zero and are not written.
 template <int N, bool WIDE>
 struct Piece {
-    static __device__ __forceinline__ int col(int lane, int ts, int n, int e) { return WIDE ? (n * ts + lane) * E + e : (n * E + e) * ts + lane; }
+    static __device__ __forceinline__ int col(int lane, int ts, int n) { return (n * ts + lane) * E; }
 
     template <class T>
     static __device__ __forceinline__ void load(const T* p, int lane, int ts, int D, float (&v)[N][E])
     {
 #pragma unroll
         for (int n = 0; n < N; ++n) {
+            const int c = col(lane, ts, n);
 #pragma unroll
             for (int e = 0; e < E; ++e) v[n][e] = 0.0f;
-            if constexpr (WIDE) {
-                if (col(lane, ts, n, 0) < D) load8(p + col(lane, ts, n, 0), v[n]);
-            } else {
+            if (WIDE ? c < D : c + E <= D) load8<WIDE>(p + c, v[n]);
+            else if constexpr (!WIDE) {
 #pragma unroll
                 for (int e = 0; e < E; ++e)
-                    if (col(lane, ts, n, e) < D) v[n][e] = get1(p + col(lane, ts, n, e));
+                    if (c + e < D) v[n][e] = get1(p + c + e);
             }
         }
     }
@@ -118,38 +137,34 @@ struct Piece {
     {
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            if constexpr (WIDE) {
-                if (col(lane, ts, n, 0) < D) store8(p + col(lane, ts, n, 0), v[n]);
-            } else {
+            const int c = col(lane, ts, n);
+            if (WIDE ? c < D : c + E <= D) store8<WIDE>(p + c, v[n]);
+            else if constexpr (!WIDE) {
 #pragma unroll
                 for (int e = 0; e < E; ++e)
-                    if (col(lane, ts, n, e) < D) put1(p + col(lane, ts, n, e), v[n][e]);
+                    if (c + e < D) put1(p + c + e, v[n][e]);
             }
         }
     }
     // per-column weights of a worker (a team reads them again and again: not streamed); absent: ones.  Past the row's end
     // zero, so that nothing there enters a sum.
-    static __device__ __forceinline__ void weights(const float* p, int lane, int ts, int D, bool wide, float (&v)[N][E])
+    static __device__ __forceinline__ void weights(const float* p, int lane, int ts, int D, float (&v)[N][E])
     {
 #pragma unroll
-        for (int n = 0; n < N; ++n)
+        for (int n = 0; n < N; ++n) {
+            const int c = col(lane, ts, n);
+            if (p && c + E <= D) {
+                const v4f_any* q = reinterpret_cast<const v4f_any*>(p + c);
+                const v4f a = q[0], b = q[1];
 #pragma unroll
-            for (int e = 0; e < E; ++e) v[n][e] = 0.0f;
-        if (WIDE && wide && p) {
+                for (int e = 0; e < 4; ++e) { v[n][e] = a[e]; v[n][e + 4] = b[e]; }
+            } else {
 #pragma unroll
-            for (int n = 0; n < N; ++n)
-                if (col(lane, ts, n, 0) < D) {
-                    const v4f* q = reinterpret_cast<const v4f*>(p + col(lane, ts, n, 0));
-                    const v4f a = q[0], b = q[1];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) { v[n][e] = a[e]; v[n][e + 4] = b[e]; }
+                for (int e = 0; e < E; ++e) {
+                    v[n][e] = 0.0f;
+                    if (c + e < D) v[n][e] = p ? p[c + e] : 1.0f;
                 }
-        } else {
-#pragma unroll
-            for (int n = 0; n < N; ++n)
-#pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if (col(lane, ts, n, e) < D) v[n][e] = p ? p[col(lane, ts, n, e)] : 1.0f;
+            }
         }
     }
 };
@@ -203,7 +218,7 @@ template <class T>
 __device__ __forceinline__ T* row_of(const Rows& a, int w, int64_t t) { return static_cast<T*>(a.p) + w * a.lw + t * a.lt; }
 
 template <class T, int N, bool WIDE, bool WAVE>
-__global__ __launch_bounds__(WAVE ? kWaveTeams * kWave : kMaxThreads) void block_norm_kernel(NormArgs a, int wide_w)
+__global__ __launch_bounds__(WAVE ? kWaveTeams * kWave : kMaxThreads) void block_norm_kernel(NormArgs a)
 {
     using P = Piece<N, WIDE>;
     __shared__ float buf[2][16];
@@ -211,8 +226,8 @@ __global__ __launch_bounds__(WAVE ? kWaveTeams * kWave : kMaxThreads) void block
     const int ts = WAVE ? kWave : (int)blockDim.x, teams = WAVE ? kWaveTeams : 1;
     const int lane = WAVE ? threadIdx.x % kWave : threadIdx.x, team = WAVE ? threadIdx.x / kWave : 0, w = blockIdx.y;
     float wp[N][E], wn[N][E];
-    if (a.y.p) P::weights(a.w_post ? a.w_post + w * a.ld_w_post : nullptr, lane, ts, a.D, wide_w & 1, wp);
-    if (a.n.p) P::weights(a.w_pre ? a.w_pre + w * a.ld_w_pre : nullptr, lane, ts, a.D, wide_w & 2, wn);
+    if (a.y.p) P::weights(a.w_post ? a.w_post + w * a.ld_w_post : nullptr, lane, ts, a.D, wp);
+    if (a.n.p) P::weights(a.w_pre ? a.w_pre + w * a.ld_w_pre : nullptr, lane, ts, a.D, wn);
     for (int64_t t = (int64_t)blockIdx.x * teams + team; t < a.T; t += (int64_t)gridDim.x * teams) {
         float r[N][E];
         P::load(row_of<T>(a.r, w, t), lane, ts, a.D, r);
@@ -259,7 +274,7 @@ __global__ __launch_bounds__(WAVE ? kWaveTeams * kWave : kMaxThreads) void block
 }
 
 template <class T, int N, bool WIDE, bool WAVE>
-__global__ __launch_bounds__(WAVE ? kWaveTeams * kWave : kMaxThreads) void block_norm_grad_kernel(NormGradArgs a, int wide_w)
+__global__ __launch_bounds__(WAVE ? kWaveTeams * kWave : kMaxThreads) void block_norm_grad_kernel(NormGradArgs a)
 {
     using P = Piece<N, WIDE>;
     __shared__ float buf[2][16];
@@ -267,8 +282,8 @@ __global__ __launch_bounds__(WAVE ? kWaveTeams * kWave : kMaxThreads) void block
     const int ts = WAVE ? kWave : (int)blockDim.x, teams = WAVE ? kWaveTeams : 1;
     const int lane = WAVE ? threadIdx.x % kWave : threadIdx.x, team = WAVE ? threadIdx.x / kWave : 0, w = blockIdx.y;
     float wp[N][E], wn[N][E], dwp[N][E], dwn[N][E];
-    if (a.y.p) P::weights(a.w_post ? a.w_post + w * a.ld_w_post : nullptr, lane, ts, a.D, wide_w & 1, wp);
-    if (a.dn.p) P::weights(a.w_pre ? a.w_pre + w * a.ld_w_pre : nullptr, lane, ts, a.D, wide_w & 2, wn);
+    if (a.y.p) P::weights(a.w_post ? a.w_post + w * a.ld_w_post : nullptr, lane, ts, a.D, wp);
+    if (a.dn.p) P::weights(a.w_pre ? a.w_pre + w * a.ld_w_pre : nullptr, lane, ts, a.D, wn);
 #pragma unroll
     for (int n = 0; n < N; ++n)
 #pragma unroll
@@ -355,14 +370,13 @@ __global__ __launch_bounds__(WAVE ? kWaveTeams * kWave : kMaxThreads) void block
 #pragma unroll
             for (int n = 0; n < N; ++n)
 #pragma unroll
-                for (int e = 0; e < E; ++e) sum[team][(n * E + e) * kWave + lane] = which ? dwn[n][e] : dwp[n][e];
+                for (int e = 0; e < E; ++e) sum[team][P::col(lane, kWave, n) + e] = which ? dwn[n][e] : dwp[n][e];
             __syncthreads();
             for (int i = threadIdx.x; i < kWave * N * E; i += kWaveTeams * kWave) {
                 float s = 0.0f;
 #pragma unroll
                 for (int k = 0; k < kWaveTeams; ++k) s += sum[k][i];
-                const int c = P::col(i % kWave, kWave, i / kWave / E, i / kWave % E);
-                if (c < a.D) part[which * a.Dp + c] = s;
+                if (i < a.D) part[which * a.Dp + i] = s;
             }
             __syncthreads();
         }
@@ -437,7 +451,6 @@ bool wide_rows(const lsgd_rows& a, int W, int T, int es)
     const int64_t per = 16 / es;
     return !a.data || (on(a.data, 16) && (W == 1 || a.worker_stride % per == 0) && (T <= 1 || a.token_stride % per == 0));
 }
-bool wide_weights(const float* w, int64_t ld, int W) { return on(w, 16) && (W == 1 || ld % 4 == 0); }
 
 Rows rows(const lsgd_rows& a) { return Rows{a.data, a.worker_stride, a.token_stride}; }
 
@@ -535,12 +548,11 @@ lsgd_status lsgd_block_norm(const lsgd_block_norm_args* p, void* hip_stream)
     a.post = p->post_norm;
     bool wide = D % E == 0;
     for (const lsgd_rows* q : {&p->r, &p->y, &p->gate, &p->r_out, &p->n}) wide = wide && wide_rows(*q, W, T, es);
-    const int wide_w = (wide_weights(p->w_post, p->ld_w_post, W) ? 1 : 0) | (wide_weights(p->w_pre, p->ld_w_pre, W) ? 2 : 0);
     const Shape sh = shape_of(D);
     const dim3 grid((unsigned)groups_of(W, T, sh, kLanes), (unsigned)W);
     dispatch(D, p->is_bf16, wide, [&](auto type, auto n, auto wide_rows, auto wave) {
         hipLaunchKernelGGL((block_norm_kernel<decltype(type), decltype(n)::value, decltype(wide_rows)::value, decltype(wave)::value>), grid,
-                           dim3((unsigned)sh.threads), 0, static_cast<hipStream_t>(hip_stream), a, wide_w);
+                           dim3((unsigned)sh.threads), 0, static_cast<hipStream_t>(hip_stream), a);
     });
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return set_error(LSGD_ERR_HIP, "%s: %s", who, hipGetErrorString(e));
@@ -611,10 +623,9 @@ lsgd_status lsgd_block_norm_grad(const lsgd_block_norm_grad_args* p, void* works
     a.post = p->post_norm;
     bool wide = D % E == 0;
     for (const lsgd_rows* q : {&p->dn, &p->dr_out, &p->r_out, &p->y, &p->gate, &p->dr, &p->dy, &p->dgate}) wide = wide && wide_rows(*q, W, T, es);
-    const int wide_w = (wide_weights(p->w_post, p->ld_w_post, W) ? 1 : 0) | (wide_weights(p->w_pre, p->ld_w_pre, W) ? 2 : 0);
     dispatch(D, p->is_bf16, wide, [&](auto type, auto n, auto wide_rows, auto wave) {
         hipLaunchKernelGGL((block_norm_grad_kernel<decltype(type), decltype(n)::value, decltype(wide_rows)::value, decltype(wave)::value>),
-                           dim3((unsigned)plan.groups, (unsigned)W), dim3((unsigned)shape_of(D).threads), 0, s, a, wide_w);
+                           dim3((unsigned)plan.groups, (unsigned)W), dim3((unsigned)shape_of(D).threads), 0, s, a);
     });
     if (sums)
         hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)((D - 1) / kWave + 1), (unsigned)W, 2), dim3(kJoinThreads), 0, s, a.parts, plan.groups, D,
