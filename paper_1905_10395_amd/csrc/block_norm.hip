@@ -224,7 +224,7 @@ __global__ __launch_bounds__(WAVE ? kWaveTeams * kWave : kMaxThreads) void block
     __shared__ float buf[2][16];
     TeamSum sums{buf, 0};
     const int ts = WAVE ? kWave : (int)blockDim.x, teams = WAVE ? kWaveTeams : 1;
-    const int lane = WAVE ? threadIdx.x % kWave : threadIdx.x, team = WAVE ? threadIdx.x / kWave : 0, w = blockIdx.y;
+    const int lane = WAVE ? threadIdx.x % kWave : threadIdx.x, team = WAVE ? __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave) : 0, w = blockIdx.y;
     float wp[N][E], wn[N][E];
     if (a.y.p) P::weights(a.w_post ? a.w_post + w * a.ld_w_post : nullptr, lane, ts, a.D, wp);
     if (a.n.p) P::weights(a.w_pre ? a.w_pre + w * a.ld_w_pre : nullptr, lane, ts, a.D, wn);
@@ -280,7 +280,7 @@ __global__ __launch_bounds__(WAVE ? kWaveTeams * kWave : kMaxThreads) void block
     __shared__ float buf[2][16];
     TeamSum sums{buf, 0};
     const int ts = WAVE ? kWave : (int)blockDim.x, teams = WAVE ? kWaveTeams : 1;
-    const int lane = WAVE ? threadIdx.x % kWave : threadIdx.x, team = WAVE ? threadIdx.x / kWave : 0, w = blockIdx.y;
+    const int lane = WAVE ? threadIdx.x % kWave : threadIdx.x, team = WAVE ? __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave) : 0, w = blockIdx.y;
     float wp[N][E], wn[N][E], dwp[N][E], dwn[N][E];
     if (a.y.p) P::weights(a.w_post ? a.w_post + w * a.ld_w_post : nullptr, lane, ts, a.D, wp);
     if (a.dn.p) P::weights(a.w_pre ? a.w_pre + w * a.ld_w_pre : nullptr, lane, ts, a.D, wn);
