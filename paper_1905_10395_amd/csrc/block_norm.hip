@@ -21,17 +21,11 @@
 #include <cmath>
 #include <type_traits>
 
-#include "common.h"
+#include "row_pieces.h"
 
 using namespace lsgd;
 
 namespace {
-
-typedef float v4f __attribute__((ext_vector_type(4)));
-typedef uint32_t v4u __attribute__((ext_vector_type(4)));
-// As they lie in rows of any width and stride: the chip's 16-byte accesses need no alignment.
-typedef v4f v4f_any __attribute__((aligned(4)));
-typedef v4u v4u_any __attribute__((aligned(2)));
 
 constexpr int E = 8;              // elements of a piece: 16 bytes of bf16, twice that of fp32
 
@@ -62,56 +56,9 @@ struct NormGradArgs {
     int post;
 };
 
-// Activations are read once and written once; streaming accesses in both directions took 548 us where plain ones took 572,
-// either direction alone 557.  Pieces that are not aligned go through the caches, which put their lines together.
-template <bool WIDE, class VA, class V, class P>
-__device__ __forceinline__ V load16(const P* p)
-{
-    if constexpr (WIDE) return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
-    else return *reinterpret_cast<const VA*>(p);
-}
-template <bool WIDE, class VA, class V, class P>
-__device__ __forceinline__ void store16(V v, P* p)
-{
-    if constexpr (WIDE) __builtin_nontemporal_store(v, reinterpret_cast<V*>(p));
-    else *reinterpret_cast<VA*>(p) = v;
-}
-template <bool WIDE>
-__device__ __forceinline__ void load8(const float* p, float (&v)[E])
-{
-    const v4f a = load16<WIDE, v4f_any, v4f>(p), b = load16<WIDE, v4f_any, v4f>(p + 4);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) { v[e] = a[e]; v[e + 4] = b[e]; }
-}
-template <bool WIDE>
-__device__ __forceinline__ void load8(const uint16_t* p, float (&v)[E])
-{
-    const v4u a = load16<WIDE, v4u_any, v4u>(p);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        v[2 * e] = __uint_as_float(a[e] << 16);
-        v[2 * e + 1] = __uint_as_float(a[e] & 0xFFFF0000u);
-    }
-}
-template <bool WIDE>
-__device__ __forceinline__ void store8(float* p, const float (&v)[E])
-{
-    store16<WIDE, v4f_any>(v4f{v[0], v[1], v[2], v[3]}, p);
-    store16<WIDE, v4f_any>(v4f{v[4], v[5], v[6], v[7]}, p + 4);
-}
-template <bool WIDE>
-__device__ __forceinline__ void store8(uint16_t* p, const float (&v)[E])
-{
-    const v4u a = {f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]), f32x2_to_bf16x2(v[4], v[5]), f32x2_to_bf16x2(v[6], v[7])};
-    store16<WIDE, v4u_any>(a, p);
-}
-__device__ __forceinline__ float get1(const float* p) { return *p; }
-__device__ __forceinline__ float get1(const uint16_t* p) { return bf16_to_f32(*p); }
-__device__ __forceinline__ void put1(float* p, float v) { *p = v; }
-__device__ __forceinline__ void put1(uint16_t* p, float v) { *p = f32_to_bf16_rne(v); }
-
-// A lane's N pieces of a row, of E adjacent elements each; WIDE: all of them whole and 16-byte aligned, else the row's last
-// piece may be shorter.  Elements past the row's end read zero and are not written.
+// A lane's N pieces of a row.  WIDE: all whole and 16-byte aligned; these are read once and written once, and streaming
+// accesses in both directions took 548 us where plain ones took 572, either direction alone 557.  Elements past the row's end
+// read zero and are not written.
 template <int N, bool WIDE>
 struct Piece {
     static __device__ __forceinline__ int col(int lane, int ts, int n) { return (n * ts + lane) * E; }
@@ -124,12 +71,8 @@ struct Piece {
             const int c = col(lane, ts, n);
 #pragma unroll
             for (int e = 0; e < E; ++e) v[n][e] = 0.0f;
-            if (WIDE ? c < D : c + E <= D) load8<WIDE>(p + c, v[n]);
-            else if constexpr (!WIDE) {
-#pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if (c + e < D) v[n][e] = get1(p + c + e);
-            }
+            if constexpr (!WIDE) load_piece(p, c, D, v[n]);
+            else if (c < D) load_whole<true>(p + c, v[n]);
         }
     }
     template <class T>
@@ -138,12 +81,8 @@ struct Piece {
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             const int c = col(lane, ts, n);
-            if (WIDE ? c < D : c + E <= D) store8<WIDE>(p + c, v[n]);
-            else if constexpr (!WIDE) {
-#pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if (c + e < D) put1(p + c + e, v[n][e]);
-            }
+            if constexpr (!WIDE) store_piece(p, c, D, v[n]);
+            else if (c < D) store_whole<true>(p + c, v[n]);
         }
     }
     // per-column weights of a worker (a team reads them again and again: not streamed); absent: ones.  Past the row's end
@@ -153,18 +92,9 @@ struct Piece {
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             const int c = col(lane, ts, n);
-            if (p && c + E <= D) {
-                const v4f_any* q = reinterpret_cast<const v4f_any*>(p + c);
-                const v4f a = q[0], b = q[1];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) { v[n][e] = a[e]; v[n][e + 4] = b[e]; }
-            } else {
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    v[n][e] = 0.0f;
-                    if (c + e < D) v[n][e] = p ? p[c + e] : 1.0f;
-                }
-            }
+            for (int e = 0; e < E; ++e) v[n][e] = !p && c + e < D ? 1.0f : 0.0f;
+            if (p) load_piece(p, c, D, v[n]);
         }
     }
 };

@@ -19,77 +19,13 @@
 #include <algorithm>
 #include <cmath>
 
-#include "common.h"
+#include "row_pieces.h"
 
 using namespace lsgd;
 
 namespace {
 
-typedef float v4f __attribute__((ext_vector_type(4)));
-typedef uint32_t v4u __attribute__((ext_vector_type(4)));
-typedef uint32_t v2u __attribute__((ext_vector_type(2)));
-
 constexpr int kThreads = 256;
-
-// ---- element access: E adjacent elements (E * size is 4, 8, 16 or 32 bytes), or one ----
-template <class T> struct Elem;
-template <> struct Elem<float> {
-    static __device__ __forceinline__ float get(const float* p) { return *p; }
-    static __device__ __forceinline__ void put(float* p, float v) { *p = v; }
-};
-template <> struct Elem<uint16_t> {
-    static __device__ __forceinline__ float get(const uint16_t* p) { return bf16_to_f32(*p); }
-    static __device__ __forceinline__ void put(uint16_t* p, float v) { *p = f32_to_bf16_rne(v); }
-};
-
-template <int E>
-__device__ __forceinline__ void load_adjacent(const float* p, float (&v)[E])
-{
-#pragma unroll
-    for (int e = 0; e < E; e += 4) {
-        const v4f a = *reinterpret_cast<const v4f*>(p + e);
-        v[e] = a.x; v[e + 1] = a.y; v[e + 2] = a.z; v[e + 3] = a.w;
-    }
-}
-template <int E>
-__device__ __forceinline__ void load_adjacent(const uint16_t* p, float (&v)[E])
-{
-    uint32_t q[E / 2];
-    if constexpr (E == 8) {
-        const v4u a = *reinterpret_cast<const v4u*>(p);
-        q[0] = a.x; q[1] = a.y; q[2] = a.z; q[3] = a.w;
-    } else {
-        const v2u a = *reinterpret_cast<const v2u*>(p);
-        q[0] = a.x; q[1] = a.y;
-    }
-#pragma unroll
-    for (int e = 0; e < E / 2; ++e) {
-        v[2 * e] = __uint_as_float(q[e] << 16);
-        v[2 * e + 1] = __uint_as_float(q[e] & 0xFFFF0000u);
-    }
-}
-template <int E>
-__device__ __forceinline__ void store_adjacent(float* p, const float (&v)[E])
-{
-#pragma unroll
-    for (int e = 0; e < E; e += 4) *reinterpret_cast<v4f*>(p + e) = v4f{v[e], v[e + 1], v[e + 2], v[e + 3]};
-}
-// The same past the caches, for what is written once.
-template <int E>
-__device__ __forceinline__ void stream_adjacent(float* p, const float (&v)[E])
-{
-#pragma unroll
-    for (int e = 0; e < E; e += 4) __builtin_nontemporal_store(v4f{v[e], v[e + 1], v[e + 2], v[e + 3]}, reinterpret_cast<v4f*>(p + e));
-}
-template <int E>
-__device__ __forceinline__ void stream_adjacent(uint16_t* p, const float (&v)[E])
-{
-    uint32_t q[E / 2];
-#pragma unroll
-    for (int e = 0; e < E / 2; ++e) q[e] = f32x2_to_bf16x2(v[2 * e], v[2 * e + 1]);
-    if constexpr (E == 8) __builtin_nontemporal_store(v4u{q[0], q[1], q[2], q[3]}, reinterpret_cast<v4u*>(p));
-    else __builtin_nontemporal_store(v2u{q[0], q[1]}, reinterpret_cast<v2u*>(p));
-}
 
 // ---- lookup ----
 constexpr int kLookupEach = 4;      // independent pieces of E elements a thread has in flight
@@ -97,12 +33,13 @@ constexpr int kLookupEach = 4;      // independent pieces of E elements a thread
 // A workgroup's pieces are adjacent in the output; which token and column a piece is follows from its number.  Bound by memory:
 // 16 x 8192 x 1024 bf16 from 32768 rows 73 us, 5.1 TB/s of the 375 MB that have to move (79 us with stores that stay in the
 // caches; 76 and 93 us with 2 and 8 pieces in flight).
-template <class TI, class TO, int E>
+template <class TI, class TO, bool ONCE>
 __global__ __launch_bounds__(kThreads) void lookup_kernel(const TI* __restrict__ table, int64_t ld_table, int V, int D,
                                                           const int32_t* __restrict__ tokens, int64_t ld_tokens, int T,
                                                           float scale, TO* __restrict__ out, int64_t ld_out)
 {
-    const int per = D / E;                                             // pieces of a token
+    constexpr int E = 8;
+    const int per = (D - 1) / E + 1;                                   // pieces of a token
     const int64_t base = (int64_t)blockIdx.x * (kThreads * kLookupEach);
     const int64_t t0 = base / per;
     const uint32_t c0 = (uint32_t)(base - t0 * per) + threadIdx.x;
@@ -110,14 +47,13 @@ __global__ __launch_bounds__(kThreads) void lookup_kernel(const TI* __restrict__
     tokens += blockIdx.y * ld_tokens;
     out += blockIdx.y * ld_out;
     int64_t t[kLookupEach];
-    uint32_t c[kLookupEach];
-    int tok[kLookupEach];
+    int c[kLookupEach], tok[kLookupEach];
 #pragma unroll
     for (int k = 0; k < kLookupEach; ++k) {
         const uint32_t q = c0 + k * kThreads;
         const uint32_t r = q / (uint32_t)per;
         t[k] = t0 + r;
-        c[k] = (q - r * (uint32_t)per) * E;
+        c[k] = (int)(q - r * (uint32_t)per) * E;
         tok[k] = t[k] < T ? tokens[t[k]] : -1;
     }
     float v[kLookupEach][E];
@@ -125,20 +61,17 @@ __global__ __launch_bounds__(kThreads) void lookup_kernel(const TI* __restrict__
     for (int k = 0; k < kLookupEach; ++k) {
 #pragma unroll
         for (int e = 0; e < E; ++e) v[k][e] = 0.0f;
-        if ((uint32_t)tok[k] < (uint32_t)V) {
-            const TI* p = table + (int64_t)tok[k] * D + c[k];
-            if constexpr (E == 1) v[k][0] = Elem<TI>::get(p);
-            else load_adjacent<E>(p, v[k]);
-        }
+        if ((uint32_t)tok[k] >= (uint32_t)V) continue;
+        if constexpr (ONCE) load_whole<false>(table + (int64_t)tok[k] * D + c[k], v[k]);
+        else load_piece(table + (int64_t)tok[k] * D, c[k], D, v[k]);
     }
 #pragma unroll
     for (int k = 0; k < kLookupEach; ++k) {
         if (t[k] >= T) continue;
-        TO* p = out + t[k] * D + c[k];
 #pragma unroll
         for (int e = 0; e < E; ++e) v[k][e] *= scale;
-        if constexpr (E == 1) Elem<TO>::put(p, v[k][0]);
-        else stream_adjacent<E>(p, v[k]);
+        if constexpr (ONCE) store_whole<true>(out + t[k] * D + c[k], v[k]);
+        else store_piece(out + t[k] * D, c[k], D, v[k]);
     }
 }
 
@@ -329,36 +262,11 @@ struct GradArgs {
     int accumulate;
 };
 
-// E elements of columns [col, D): adjacent ones, or one every TL columns where rows are not aligned for that.
-template <class T, int E, int TL, bool WIDE>
-__device__ __forceinline__ void load_row(const T* p, int col, int D, float (&v)[E])
-{
-    if constexpr (WIDE) {
-        if (col < D) load_adjacent<E>(p + col, v);
-    } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-            if (col + e * TL < D) v[e] = Elem<T>::get(p + col + e * TL);
-    }
-}
-
-template <int E, int TL, bool WIDE>
-__device__ __forceinline__ void store_row(float* p, int col, int D, const float (&v)[E])
-{
-    if constexpr (WIDE) {
-        if (col < D) store_adjacent<E>(p + col, v);
-    } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-            if (col + e * TL < D) p[col + e * TL] = v[e];
-    }
-}
-
 constexpr int kSpan = 16;              // sorted places of a team, and how far into the next span it may finish a run
 constexpr uint32_t kNone = 0xFFFFFFFFu;
 
 // TL lanes make a team: they own TL * E columns of one span.
-template <class T, int E, int TL, bool WIDE>
+template <class T, int E, int TL>
 __device__ __forceinline__ void sum_runs(const GradArgs& a, int64_t task)
 {
     constexpr int U = 4;                                               // rows in flight
@@ -366,7 +274,7 @@ __device__ __forceinline__ void sum_runs(const GradArgs& a, int64_t task)
     const int span = (int)(task / a.slices), slice = (int)(task - (int64_t)span * a.slices);
     if (span >= a.spans) return;
     const int lane = threadIdx.x % TL;
-    const int col = WIDE ? (slice * TL + lane) * E : slice * TL * E + lane;
+    const int col = (slice * TL + lane) * E;
     const uint32_t* keys = a.keys + (int64_t)w * a.T;
     const int32_t* pos = a.pos + (int64_t)w * a.T;
     const T* dout = static_cast<const T*>(a.dout) + w * a.ld_dout;
@@ -391,16 +299,16 @@ __device__ __forceinline__ void sum_runs(const GradArgs& a, int64_t task)
     auto flush = [&](bool tail) {
         if (cur >= (uint32_t)a.V || cur == skip) return;               // padding
         if (head || tail) {
-            store_row<E, TL, WIDE>(a.parts + (((int64_t)w * a.spans + span) * 2 + (head ? 0 : 1)) * a.Dp, col, a.D, acc);
+            store_piece(a.parts + (((int64_t)w * a.spans + span) * 2 + (head ? 0 : 1)) * a.Dp, col, a.D, acc);
         } else {
             float* p = table + (int64_t)cur * a.D;
             float old[E];
 #pragma unroll
             for (int e = 0; e < E; ++e) old[e] = 0.0f;
-            if (a.accumulate) load_row<float, E, TL, WIDE>(p, col, a.D, old);
+            if (a.accumulate) load_piece(p, col, a.D, old);
 #pragma unroll
             for (int e = 0; e < E; ++e) old[e] += a.scale * acc[e];
-            store_row<E, TL, WIDE>(p, col, a.D, old);
+            store_piece(p, col, a.D, old);
         }
     };
 
@@ -422,7 +330,7 @@ __device__ __forceinline__ void sum_runs(const GradArgs& a, int64_t task)
         for (int u = 0; u < U; ++u) {
 #pragma unroll
             for (int e = 0; e < E; ++e) row[u][e] = 0.0f;
-            if (key[u] < (uint32_t)a.V && key[u] != skip) load_row<T, E, TL, WIDE>(dout + (int64_t)at[u] * a.D, col, a.D, row[u]);
+            if (key[u] < (uint32_t)a.V && key[u] != skip) load_piece(dout + (int64_t)at[u] * a.D, col, a.D, row[u]);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -440,8 +348,22 @@ __device__ __forceinline__ void sum_runs(const GradArgs& a, int64_t task)
     flush(tail_split);
 }
 
+// Zeros to a wavefront's columns [c0, c1) of a row.
+template <bool ALIGNED>
+__device__ __forceinline__ void zero_columns(float* row, int c0, int c1)
+{
+    for (int c = c0 + 4 * (int)(threadIdx.x & (kWave - 1)); c < c1; c += 4 * kWave) {
+        const v4f zero = {0.0f, 0.0f, 0.0f, 0.0f};
+        if constexpr (ALIGNED) __builtin_nontemporal_store(zero, reinterpret_cast<v4f*>(row + c));
+        else if (c + 4 <= c1) *reinterpret_cast<v4f_any*>(row + c) = zero;
+        else {
+            for (int e = c; e < c1; ++e) row[e] = 0.0f;
+        }
+    }
+}
+
 // Zeros to the rows of [v0, v0 + zero_rows) that no token names.
-template <bool WIDE>
+template <bool ALIGNED>
 __device__ __forceinline__ void zero_rows(const GradArgs& a, int64_t v0, uint32_t* present)
 {
     const int w = blockIdx.y;
@@ -457,26 +379,20 @@ __device__ __forceinline__ void zero_rows(const GradArgs& a, int64_t v0, uint32_
     }
     __syncthreads();
     float* table = a.table + w * a.ld_table;
-    const int lane = threadIdx.x & (kWave - 1);
     for (int r = threadIdx.x / kWave; r < n; r += kThreads / kWave) {
         if (present[r >> 5] >> (r & 31) & 1u) continue;
-        float* p = table + (v0 + r) * a.D;
-        if constexpr (WIDE) {
-            for (int c = 4 * lane; c < a.D; c += 4 * kWave) __builtin_nontemporal_store(v4f{0.0f, 0.0f, 0.0f, 0.0f}, reinterpret_cast<v4f*>(p + c));
-        } else {
-            for (int c = lane; c < a.D; c += kWave) p[c] = 0.0f;
-        }
+        zero_columns<ALIGNED>(table + (v0 + r) * a.D, 0, a.D);
     }
 }
 
 constexpr int kZeroRows = 64;
 
-template <class T, int E, int TL, bool WIDE>
+template <class T, int E, int TL, bool ALIGNED>
 __global__ __launch_bounds__(kThreads) void grad_runs_kernel(GradArgs a)
 {
     __shared__ uint32_t present[(kZeroRows + 31) / 32];
-    if ((int)blockIdx.x < a.run_blocks) sum_runs<T, E, TL, WIDE>(a, (int64_t)blockIdx.x * (kThreads / TL) + threadIdx.x / TL);
-    else zero_rows<WIDE>(a, (int64_t)((int)blockIdx.x - a.run_blocks) * a.zero_rows, present);
+    if ((int)blockIdx.x < a.run_blocks) sum_runs<T, E, TL>(a, (int64_t)blockIdx.x * (kThreads / TL) + threadIdx.x / TL);
+    else zero_rows<ALIGNED>(a, (int64_t)((int)blockIdx.x - a.run_blocks) * a.zero_rows, present);
 }
 
 // Split runs.  A workgroup looks at the ends of kJoinSpans spans, a lane each, for such runs that began there (few are), for
@@ -533,9 +449,11 @@ __global__ __launch_bounds__(kThreads) void grad_join_kernel(GradArgs a)
         if (n > kJoinShared) continue;
         float* row = table + (int64_t)cur * a.D;
         const v4f acc = add(span, 0, n);
+        float old[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (a.accumulate) load_piece(row, col, a.D, old);
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (col + e < a.D) row[col + e] = (a.accumulate ? row[col + e] : 0.0f) + a.scale * acc[e];
+        for (int e = 0; e < 4; ++e) old[e] += a.scale * acc[e];
+        store_piece(row, col, a.D, old);
     }
     __syncthreads();
     for (int k = 0; k < n_runs; ++k) {                                 // long ones, together
@@ -572,10 +490,10 @@ struct SmallArgs {
     int slices;                                    // of 64 * E columns, that it takes
 };
 
-template <class T, int E, bool WIDE, int EACH>
+template <class T, int E, bool ALIGNED, int EACH>
 __global__ __launch_bounds__(kSortThreads) void grad_small_kernel(GradArgs a, SmallArgs q)
 {
-    constexpr int TL = kWave, U = 8, cols = kWave * E;
+    constexpr int U = 8, cols = kWave * E;
     __shared__ uint32_t key[EACH * kSortThreads];
     __shared__ uint16_t pos[EACH * kSortThreads];
     __shared__ union {
@@ -635,12 +553,7 @@ __global__ __launch_bounds__(kSortThreads) void grad_small_kernel(GradArgs a, Sm
         __syncthreads();
         for (int r = wave; r < n; r += kSortWaves) {
             if (s.present[r >> 5] >> (r & 31) & 1u) continue;
-            float* p = table + (v0 + r) * a.D;
-            if constexpr (WIDE) {
-                for (int c = slice0 * cols + 4 * lane; c < col_end; c += 4 * kWave) __builtin_nontemporal_store(v4f{0.0f, 0.0f, 0.0f, 0.0f}, reinterpret_cast<v4f*>(p + c));
-            } else {
-                for (int c = slice0 * cols + lane; c < col_end; c += kWave) p[c] = 0.0f;
-            }
+            zero_columns<ALIGNED>(table + (v0 + r) * a.D, slice0 * cols, col_end);
         }
     }
     __syncthreads();
@@ -657,7 +570,7 @@ __global__ __launch_bounds__(kSortThreads) void grad_small_kernel(GradArgs a, Sm
                 for (int e = 0; e < E; ++e) row[u][e] = 0.0f;
                 if (b + u < p1) {
                     const int at = __builtin_amdgcn_readfirstlane((int)pos[b + u]);
-                    load_row<T, E, TL, WIDE>(dout + (int64_t)at * a.D, col, a.D, row[u]);
+                    load_piece(dout + (int64_t)at * a.D, col, a.D, row[u]);
                 }
             }
 #pragma unroll
@@ -692,17 +605,17 @@ __global__ __launch_bounds__(kSortThreads) void grad_small_kernel(GradArgs a, Sm
             continue;
         }
         for (int c = 0; c < q.slices; ++c) {
-            const int col0 = (slice0 + c) * cols, col = WIDE ? col0 + lane * E : col0 + lane;
+            const int col0 = (slice0 + c) * cols, col = col0 + lane * E;
             if (col0 >= a.D) break;
             float* p = table + (int64_t)v * a.D;
             float old[E];
 #pragma unroll
             for (int e = 0; e < E; ++e) old[e] = 0.0f;
-            if (a.accumulate) load_row<float, E, TL, WIDE>(p, col, a.D, old);
+            if (a.accumulate) load_piece(p, col, a.D, old);
             add_places(j, j + n, col);
 #pragma unroll
             for (int e = 0; e < E; ++e) old[e] += a.scale * acc[e];
-            store_row<E, TL, WIDE>(p, col, a.D, old);
+            store_piece(p, col, a.D, old);
         }
     }
     __syncthreads();
@@ -710,11 +623,11 @@ __global__ __launch_bounds__(kSortThreads) void grad_small_kernel(GradArgs a, Sm
         const int j = shared_run[k], n = shared_places[k];
         float* p = table + (int64_t)key[j] * a.D;
         for (int c = 0; c < q.slices; ++c) {
-            const int col0 = (slice0 + c) * cols, col = WIDE ? col0 + lane * E : col0 + lane;
+            const int col0 = (slice0 + c) * cols, col = col0 + lane * E;
             if (col0 >= a.D) break;
             add_places(j + n * wave / kSortWaves, j + n * (wave + 1) / kSortWaves, col);
 #pragma unroll
-            for (int e = 0; e < E; ++e) s.sum[wave][WIDE ? lane * E + e : e * kWave + lane] = acc[e];
+            for (int e = 0; e < E; ++e) s.sum[wave][lane * E + e] = acc[e];
             __syncthreads();
             if ((int)threadIdx.x < cols && col0 + (int)threadIdx.x < a.D) {
                 float t = 0.0f;
@@ -790,26 +703,18 @@ template <class TI, class TO>
 void launch_lookup(int W, int T, int V, int D, const void* table, int64_t ld_table, const int32_t* tokens, int64_t ld_tokens, float scale,
                    void* out, int64_t ld_out, hipStream_t s)
 {
-    const TI* in = static_cast<const TI*>(table);
     TO* to = static_cast<TO*>(out);
-    auto ok = [&](int E) {
-        auto fits = [&](const void* p, int64_t ld, size_t es) {
-            const size_t a = std::min<size_t>(16, es * (size_t)E);
-            return on(p, a) && (W == 1 || (ld * (int64_t)es) % (int64_t)a == 0);
-        };
-        return D % E == 0 && fits(in, ld_table, sizeof(TI)) && fits(to, ld_out, sizeof(TO));
+    const int64_t pieces = (int64_t)T * ((D - 1) / 8 + 1);
+    const dim3 grid((unsigned)((pieces - 1) / (kThreads * kLookupEach) + 1), (unsigned)W);
+    const bool aligned = D % 8 == 0 && on(to, 16) && (W == 1 || ld_out % 8 == 0);
+    auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, s, static_cast<const TI*>(table), ld_table, V, D, tokens, ld_tokens, T, scale, to, ld_out);
     };
-    auto go = [&](auto kernel, int E) {
-        const int64_t pieces = (int64_t)T * (D / E);
-        const dim3 grid((unsigned)((pieces - 1) / (kThreads * kLookupEach) + 1), (unsigned)W);
-        hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, s, in, ld_table, V, D, tokens, ld_tokens, T, scale, to, ld_out);
-    };
-    if (ok(8)) go(lookup_kernel<TI, TO, 8>, 8);
-    else if (ok(4)) go(lookup_kernel<TI, TO, 4>, 4);
-    else go(lookup_kernel<TI, TO, 1>, 1);
+    if (aligned) go(lookup_kernel<TI, TO, true>);
+    else go(lookup_kernel<TI, TO, false>);
 }
 
-template <class T, int E, int TL, bool WIDE>
+template <class T, int E, int TL, bool ALIGNED>
 void launch_grad(GradArgs a, int W, hipStream_t s)
 {
     a.slices = (a.D - 1) / (TL * E) + 1;
@@ -817,7 +722,7 @@ void launch_grad(GradArgs a, int W, hipStream_t s)
     a.run_blocks = (int)(((int64_t)a.spans * a.slices - 1) / teams + 1);
     a.zero_rows = kZeroRows;
     const int zero_blocks = a.accumulate ? 0 : (a.V - 1) / kZeroRows + 1;
-    hipLaunchKernelGGL((grad_runs_kernel<T, E, TL, WIDE>), dim3((unsigned)(a.run_blocks + zero_blocks), (unsigned)W), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((grad_runs_kernel<T, E, TL, ALIGNED>), dim3((unsigned)(a.run_blocks + zero_blocks), (unsigned)W), dim3(kThreads), 0, s, a);
     hipLaunchKernelGGL(grad_join_kernel, dim3((unsigned)((a.spans - 1) / kJoinSpans + 1), (unsigned)W, (unsigned)((a.D - 1) / kJoinCols + 1)),
                        dim3(kThreads), 0, s, a);
 }
@@ -827,7 +732,7 @@ void launch_grad(GradArgs a, int W, hipStream_t s)
 // 4 x 65536 x 1024: 217 us instead of 234).
 constexpr int kSmallGroups = 256;
 constexpr int64_t kManyZeros = 128ll << 20;        // bytes of all tables
-template <class T, int E, bool WIDE>
+template <class T, int E, bool ALIGNED>
 void launch_grad_small(const GradArgs& a, int W, SmallArgs q, hipStream_t s)
 {
     const int slices = (a.D - 1) / (kWave * E) + 1;
@@ -842,17 +747,17 @@ void launch_grad_small(const GradArgs& a, int W, SmallArgs q, hipStream_t s)
     q.span = (a.T - 1) / n + 1;
     q.rows = (a.V - 1) / n + 1;
     const dim3 grid((unsigned)n, (unsigned)W, (unsigned)z), block(kSortThreads);
-    if (a.T <= kSortThreads) hipLaunchKernelGGL((grad_small_kernel<T, E, WIDE, 1>), grid, block, 0, s, a, q);
-    else if (a.T <= 2 * kSortThreads) hipLaunchKernelGGL((grad_small_kernel<T, E, WIDE, 2>), grid, block, 0, s, a, q);
-    else if (a.T <= 4 * kSortThreads) hipLaunchKernelGGL((grad_small_kernel<T, E, WIDE, 4>), grid, block, 0, s, a, q);
-    else hipLaunchKernelGGL((grad_small_kernel<T, E, WIDE, 8>), grid, block, 0, s, a, q);
+    if (a.T <= kSortThreads) hipLaunchKernelGGL((grad_small_kernel<T, E, ALIGNED, 1>), grid, block, 0, s, a, q);
+    else if (a.T <= 2 * kSortThreads) hipLaunchKernelGGL((grad_small_kernel<T, E, ALIGNED, 2>), grid, block, 0, s, a, q);
+    else if (a.T <= 4 * kSortThreads) hipLaunchKernelGGL((grad_small_kernel<T, E, ALIGNED, 4>), grid, block, 0, s, a, q);
+    else hipLaunchKernelGGL((grad_small_kernel<T, E, ALIGNED, 8>), grid, block, 0, s, a, q);
 }
 
 template <class T, int E>
-void launch_grad_team(const GradArgs& a, int W, bool wide, hipStream_t s)
+void launch_grad_team(const GradArgs& a, int W, bool aligned, hipStream_t s)
 {
     const int lanes = (a.D - 1) / E + 1;
-    if (wide) {
+    if (aligned) {
         if (lanes <= 16) launch_grad<T, E, 16, true>(a, W, s);
         else if (lanes <= 32) launch_grad<T, E, 32, true>(a, W, s);
         else launch_grad<T, E, 64, true>(a, W, s);
@@ -943,14 +848,13 @@ lsgd_status lsgd_embed_grad(int32_t W, int32_t T, int32_t V, int32_t D, const vo
     a.table = dtable; a.ld_table = ld_dtable;
     a.T = T; a.V = V; a.D = D;
     a.scale = scale; a.accumulate = accumulate;
-    const int E = dout_is_bf16 ? 8 : 4;
-    const bool wide = D % E == 0 && on(dout, 16) && on(dtable, 16) && (W == 1 || (ld_dout % E == 0 && ld_dtable % 4 == 0));
+    const bool aligned = D % 4 == 0 && on(dtable, 16) && (W == 1 || ld_dtable % 4 == 0);       // of the table's rows
     if (T <= kSmallTokens) {
         SmallArgs q{};
         q.tokens = tokens; q.ld_tokens = ld_tokens;
         q.bits = p.bits; q.passes = p.passes;
-        if (dout_is_bf16) wide ? launch_grad_small<uint16_t, 8, true>(a, W, q, s) : launch_grad_small<uint16_t, 8, false>(a, W, q, s);
-        else wide ? launch_grad_small<float, 4, true>(a, W, q, s) : launch_grad_small<float, 4, false>(a, W, q, s);
+        if (dout_is_bf16) aligned ? launch_grad_small<uint16_t, 8, true>(a, W, q, s) : launch_grad_small<uint16_t, 8, false>(a, W, q, s);
+        else aligned ? launch_grad_small<float, 4, true>(a, W, q, s) : launch_grad_small<float, 4, false>(a, W, q, s);
         e = hipGetLastError();
         if (e != hipSuccess) return set_error(LSGD_ERR_HIP, "embed_grad: %s", hipGetErrorString(e));
         return LSGD_OK;
@@ -975,8 +879,8 @@ lsgd_status lsgd_embed_grad(int32_t W, int32_t T, int32_t V, int32_t D, const vo
     a.keys = keys[at]; a.pos = pos[at];
     a.parts = reinterpret_cast<float*>(base + p.parts);
     a.Dp = p.Dp; a.spans = p.spans;
-    if (dout_is_bf16) launch_grad_team<uint16_t, 8>(a, W, wide, s);
-    else launch_grad_team<float, 4>(a, W, wide, s);
+    if (dout_is_bf16) launch_grad_team<uint16_t, 8>(a, W, aligned, s);
+    else launch_grad_team<float, 4>(a, W, aligned, s);
     e = hipGetLastError();
     if (e != hipSuccess) return set_error(LSGD_ERR_HIP, "embed_grad: %s", hipGetErrorString(e));
     return LSGD_OK;
