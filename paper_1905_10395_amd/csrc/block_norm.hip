@@ -99,10 +99,11 @@ struct Piece {
     }
 };
 
-// Teams: WAVE: a wavefront, four of them in a workgroup (rows of at most 512 columns); else the workgroup, of any whole
-// number of wavefronts.
-constexpr int kWaveTeams = 4;
+// Teams: LANES of a wavefront (8 to 64, as many as rows of at most 512 columns need) in workgroups of 256; or, LANES = 0, the
+// workgroup, of any whole number of wavefronts.
+constexpr int kTeamThreads = 256;
 constexpr int kMaxThreads = 1024;
+constexpr int threads_limit(int lanes) { return lanes ? kTeamThreads : kMaxThreads; }
 
 // Sums over rows of 16 lanes and over a wavefront by lane shifts in the vector unit.
 template <int CTRL>
@@ -128,16 +129,24 @@ struct TeamSum {
     float (*buf)[16];
     int turn;
 };
-template <bool WAVE>
+template <int LANES>
 __device__ __forceinline__ float team_sum(float a, TeamSum& s)
 {
-    a = wave_sum(a);
-    if constexpr (!WAVE) {
-        const int lane = threadIdx.x & (kWave - 1), waves = blockDim.x / kWave;
-        if (lane == 0) s.buf[s.turn][threadIdx.x / kWave] = a;
-        __syncthreads();
-        a = row_sum((lane & 15) < waves ? s.buf[s.turn][lane & 15] : 0.0f);
-        s.turn ^= 1;
+    if constexpr (LANES == 8 || LANES == 16 || LANES == 32) {
+        a = add_lanes<0xB1>(a);                            // the other lane of a pair, the other pair, the other four, ...
+        a = add_lanes<0x4E>(a);
+        a = add_lanes<0x141>(a);
+        if constexpr (LANES >= 16) a = add_lanes<0x140>(a);
+        if constexpr (LANES == 32) a += __shfl_xor(a, 16);
+    } else {
+        a = wave_sum(a);
+        if constexpr (LANES == 0) {
+            const int lane = threadIdx.x & (kWave - 1), waves = blockDim.x / kWave;
+            if (lane == 0) s.buf[s.turn][threadIdx.x / kWave] = a;
+            __syncthreads();
+            a = row_sum((lane & 15) < waves ? s.buf[s.turn][lane & 15] : 0.0f);
+            s.turn ^= 1;
+        }
     }
     return a;
 }
@@ -147,14 +156,16 @@ __device__ __forceinline__ float sigmoid(float u) { return __builtin_amdgcn_rcpf
 template <class T>
 __device__ __forceinline__ T* row_of(const Rows& a, int w, int64_t t) { return static_cast<T*>(a.p) + w * a.lw + t * a.lt; }
 
-template <class T, int N, bool WIDE, bool WAVE>
-__global__ __launch_bounds__(WAVE ? kWaveTeams * kWave : kMaxThreads) void block_norm_kernel(NormArgs a)
+template <class T, int N, bool WIDE, int LANES>
+__global__ __launch_bounds__(threads_limit(LANES)) void block_norm_kernel(NormArgs a)
 {
     using P = Piece<N, WIDE>;
     __shared__ float buf[2][16];
     TeamSum sums{buf, 0};
-    const int ts = WAVE ? kWave : (int)blockDim.x, teams = WAVE ? kWaveTeams : 1;
-    const int lane = WAVE ? threadIdx.x % kWave : threadIdx.x, team = WAVE ? __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave) : 0, w = blockIdx.y;
+    constexpr int teams = LANES ? kTeamThreads / (LANES ? LANES : 1) : 1;
+    const int ts = LANES ? LANES : (int)blockDim.x, lane = threadIdx.x % (unsigned)ts, w = blockIdx.y;
+    int team = LANES ? (int)threadIdx.x / ts : 0;
+    if constexpr (LANES == kWave) team = __builtin_amdgcn_readfirstlane(team);
     float wp[N][E], wn[N][E];
     if (a.y.p) P::weights(a.w_post ? a.w_post + w * a.ld_w_post : nullptr, lane, ts, a.D, wp);
     if (a.n.p) P::weights(a.w_pre ? a.w_pre + w * a.ld_w_pre : nullptr, lane, ts, a.D, wn);
@@ -172,7 +183,7 @@ __global__ __launch_bounds__(WAVE ? kWaveTeams * kWave : kMaxThreads) void block
                 for (int n = 0; n < N; ++n)
 #pragma unroll
                     for (int e = 0; e < E; ++e) s += y[n][e] * y[n][e];
-                q = 1.0f / sqrtf(team_sum<WAVE>(s, sums) * a.inv_d + a.eps);
+                q = 1.0f / sqrtf(team_sum<LANES>(s, sums) * a.inv_d + a.eps);
                 if (a.q_post && lane == 0) a.q_post[(int64_t)w * a.T + t] = q;
             }
             const float sq = a.scale * q;
@@ -192,7 +203,7 @@ __global__ __launch_bounds__(WAVE ? kWaveTeams * kWave : kMaxThreads) void block
             for (int n = 0; n < N; ++n)
 #pragma unroll
                 for (int e = 0; e < E; ++e) s += r[n][e] * r[n][e];
-            const float q = 1.0f / sqrtf(team_sum<WAVE>(s, sums) * a.inv_d + a.eps);
+            const float q = 1.0f / sqrtf(team_sum<LANES>(s, sums) * a.inv_d + a.eps);
             if (a.q_pre && lane == 0) a.q_pre[(int64_t)w * a.T + t] = q;
 #pragma unroll
             for (int n = 0; n < N; ++n)
@@ -203,14 +214,16 @@ __global__ __launch_bounds__(WAVE ? kWaveTeams * kWave : kMaxThreads) void block
     }
 }
 
-template <class T, int N, bool WIDE, bool WAVE>
-__global__ __launch_bounds__(WAVE ? kWaveTeams * kWave : kMaxThreads) void block_norm_grad_kernel(NormGradArgs a)
+template <class T, int N, bool WIDE, int LANES>
+__global__ __launch_bounds__(threads_limit(LANES)) void block_norm_grad_kernel(NormGradArgs a)
 {
     using P = Piece<N, WIDE>;
     __shared__ float buf[2][16];
     TeamSum sums{buf, 0};
-    const int ts = WAVE ? kWave : (int)blockDim.x, teams = WAVE ? kWaveTeams : 1;
-    const int lane = WAVE ? threadIdx.x % kWave : threadIdx.x, team = WAVE ? __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave) : 0, w = blockIdx.y;
+    constexpr int teams = LANES ? kTeamThreads / (LANES ? LANES : 1) : 1;
+    const int ts = LANES ? LANES : (int)blockDim.x, lane = threadIdx.x % (unsigned)ts, w = blockIdx.y;
+    int team = LANES ? (int)threadIdx.x / ts : 0;
+    if constexpr (LANES == kWave) team = __builtin_amdgcn_readfirstlane(team);
     float wp[N][E], wn[N][E], dwp[N][E], dwn[N][E];
     if (a.y.p) P::weights(a.w_post ? a.w_post + w * a.ld_w_post : nullptr, lane, ts, a.D, wp);
     if (a.dn.p) P::weights(a.w_pre ? a.w_pre + w * a.ld_w_pre : nullptr, lane, ts, a.D, wn);
@@ -247,7 +260,7 @@ __global__ __launch_bounds__(WAVE ? kWaveTeams * kWave : kMaxThreads) void block
                     dn[n][e] *= wn[n][e];
                     s += dn[n][e] * h[n][e];
                 }
-            s = team_sum<WAVE>(s, sums) * a.inv_d;
+            s = team_sum<LANES>(s, sums) * a.inv_d;
 #pragma unroll
             for (int n = 0; n < N; ++n)
 #pragma unroll
@@ -278,7 +291,7 @@ __global__ __launch_bounds__(WAVE ? kWaveTeams * kWave : kMaxThreads) void block
                 }
             if (a.u.p) P::store(row_of<T>(a.du, w, t), lane, ts, a.D, u);
             if (a.post) {
-                s = team_sum<WAVE>(s, sums) * a.inv_d;
+                s = team_sum<LANES>(s, sums) * a.inv_d;
 #pragma unroll
                 for (int n = 0; n < N; ++n)
 #pragma unroll
@@ -289,24 +302,22 @@ __global__ __launch_bounds__(WAVE ? kWaveTeams * kWave : kMaxThreads) void block
     }
     if (!a.parts) return;
     float* part = a.parts + ((int64_t)w * gridDim.x + blockIdx.x) * 2 * a.Dp;
-    if constexpr (!WAVE) {
+    if constexpr (LANES == 0) {
         P::store(part, lane, ts, a.D, dwp);
         P::store(part + a.Dp, lane, ts, a.D, dwn);
     } else {
         // the workgroup's teams add up theirs in order
-        __shared__ float sum[kWaveTeams][kWave * N * E];
+        __shared__ float sum[teams][LANES * E];
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
 #pragma unroll
-            for (int n = 0; n < N; ++n)
-#pragma unroll
-                for (int e = 0; e < E; ++e) sum[team][P::col(lane, kWave, n) + e] = which ? dwn[n][e] : dwp[n][e];
+            for (int e = 0; e < E; ++e) sum[team][lane * E + e] = which ? dwn[0][e] : dwp[0][e];
             __syncthreads();
-            for (int i = threadIdx.x; i < kWave * N * E; i += kWaveTeams * kWave) {
+            for (int i = threadIdx.x; i < LANES * E && i < a.D; i += kTeamThreads) {
                 float s = 0.0f;
 #pragma unroll
-                for (int k = 0; k < kWaveTeams; ++k) s += sum[k][i];
-                if (i < a.D) part[which * a.Dp + i] = s;
+                for (int k = 0; k < teams; ++k) s += sum[k][i];
+                part[which * a.Dp + i] = s;
             }
             __syncthreads();
         }
@@ -384,13 +395,22 @@ bool wide_rows(const lsgd_rows& a, int W, int T, int es)
 
 Rows rows(const lsgd_rows& a) { return Rows{a.data, a.worker_stride, a.token_stride}; }
 
+// Lanes of a team within a wavefront for rows of at most 512 columns; whole wavefronts for all of those took 72 us instead of
+// 20 for 12 x 11864 x 64 bf16.
+int lanes_of(int D)
+{
+    int lanes = 8;
+    while (lanes * E < D) lanes *= 2;
+    return lanes;
+}
+
 // Lanes and pieces for rows of D columns.
 struct Shape {
     int n, teams, threads;
 };
 Shape shape_of(int D)
 {
-    if (D <= kWave * E) return {1, kWaveTeams, kWaveTeams * kWave};
+    if (D <= kWave * E) return {1, kTeamThreads / lanes_of(D), kTeamThreads};
     if (D <= kMaxThreads * E) return {1, 1, (D - 1) / (kWave * E) * kWave + kWave};
     return {2, 1, kMaxThreads};
 }
@@ -422,9 +442,13 @@ template <class F>
 void dispatch(int D, bool bf16, bool wide, F launch)
 {
     auto shaped = [&](auto type, auto wide_rows) {
-        if (D <= kWave * E) launch(type, std::integral_constant<int, 1>{}, wide_rows, std::true_type{});
-        else if (D <= kMaxThreads * E) launch(type, std::integral_constant<int, 1>{}, wide_rows, std::false_type{});
-        else launch(type, std::integral_constant<int, 2>{}, wide_rows, std::false_type{});
+        const std::integral_constant<int, 1> one{};
+        if (D <= 8 * E) launch(type, one, wide_rows, std::integral_constant<int, 8>{});
+        else if (D <= 16 * E) launch(type, one, wide_rows, std::integral_constant<int, 16>{});
+        else if (D <= 32 * E) launch(type, one, wide_rows, std::integral_constant<int, 32>{});
+        else if (D <= 64 * E) launch(type, one, wide_rows, std::integral_constant<int, 64>{});
+        else if (D <= kMaxThreads * E) launch(type, one, wide_rows, std::integral_constant<int, 0>{});
+        else launch(type, std::integral_constant<int, 2>{}, wide_rows, std::integral_constant<int, 0>{});
     };
     if (bf16) wide ? shaped(uint16_t{}, std::true_type{}) : shaped(uint16_t{}, std::false_type{});
     else wide ? shaped(float{}, std::true_type{}) : shaped(float{}, std::false_type{});
@@ -480,8 +504,8 @@ lsgd_status lsgd_block_norm(const lsgd_block_norm_args* p, void* hip_stream)
     for (const lsgd_rows* q : {&p->r, &p->y, &p->gate, &p->r_out, &p->n}) wide = wide && wide_rows(*q, W, T, es);
     const Shape sh = shape_of(D);
     const dim3 grid((unsigned)groups_of(W, T, sh, kLanes), (unsigned)W);
-    dispatch(D, p->is_bf16, wide, [&](auto type, auto n, auto wide_rows, auto wave) {
-        hipLaunchKernelGGL((block_norm_kernel<decltype(type), decltype(n)::value, decltype(wide_rows)::value, decltype(wave)::value>), grid,
+    dispatch(D, p->is_bf16, wide, [&](auto type, auto n, auto wide_rows, auto lanes) {
+        hipLaunchKernelGGL((block_norm_kernel<decltype(type), decltype(n)::value, decltype(wide_rows)::value, decltype(lanes)::value>), grid,
                            dim3((unsigned)sh.threads), 0, static_cast<hipStream_t>(hip_stream), a);
     });
     const hipError_t e = hipGetLastError();
@@ -553,8 +577,8 @@ lsgd_status lsgd_block_norm_grad(const lsgd_block_norm_grad_args* p, void* works
     a.post = p->post_norm;
     bool wide = D % E == 0;
     for (const lsgd_rows* q : {&p->dn, &p->dr_out, &p->r_out, &p->y, &p->gate, &p->dr, &p->dy, &p->dgate}) wide = wide && wide_rows(*q, W, T, es);
-    dispatch(D, p->is_bf16, wide, [&](auto type, auto n, auto wide_rows, auto wave) {
-        hipLaunchKernelGGL((block_norm_grad_kernel<decltype(type), decltype(n)::value, decltype(wide_rows)::value, decltype(wave)::value>),
+    dispatch(D, p->is_bf16, wide, [&](auto type, auto n, auto wide_rows, auto lanes) {
+        hipLaunchKernelGGL((block_norm_grad_kernel<decltype(type), decltype(n)::value, decltype(wide_rows)::value, decltype(lanes)::value>),
                            dim3((unsigned)plan.groups, (unsigned)W), dim3((unsigned)shape_of(D).threads), 0, s, a);
     });
     if (sums)

@@ -53,7 +53,7 @@ def reference(r, y, u, wp, wn, post, scale=SCALE):
     return r, n, qp, qn, br, bn
 
 
-SHAPES = [(1, 1, 1), (2, 3, 7), (3, 1, 64), (2, 5, 101), (2, 70, 512), (1, 9, 520), (2, 33, 1000), (1, 3, 1024), (2, 3, 2048), (1, 5, 2056),
+SHAPES = [(1, 1, 1), (2, 3, 7), (3, 1, 64), (2, 75, 65), (2, 5, 101), (1, 40, 128), (3, 39, 130), (2, 33, 256), (1, 17, 257), (2, 70, 512), (1, 9, 520), (2, 33, 1000), (1, 3, 1024), (2, 3, 2048), (1, 5, 2056),
           (1, 2, 4097), (1, 2, 8192), (1, 3, 8200), (1, 2, 16384)]
 
 
