@@ -265,27 +265,45 @@ struct GradArgs {
 constexpr int kSpan = 16;              // sorted places of a team, and how far into the next span it may finish a run
 constexpr uint32_t kNone = 0xFFFFFFFFu;
 
-// TL lanes make a team: they own TL * E columns of one span.
-template <class T, int E, int TL>
+// Lane i's value to all lanes of a team of TL (i the same for all of a wavefront's teams).
+template <int TL>
+__device__ __forceinline__ uint32_t from_lane(uint32_t v, int i)
+{
+    if constexpr (TL == kWave) return (uint32_t)__builtin_amdgcn_readlane((int)v, i);
+    else return (uint32_t)__shfl((int)v, i, TL);
+}
+
+// TL lanes make a team: they own TL * E columns of one span.  All it goes by - the keys and places of its span and of the next
+// one, a lane each, and four keys around - is on its way at once.
+template <class T, int E, int TL, bool ALIGNED>
 __device__ __forceinline__ void sum_runs(const GradArgs& a, int64_t task)
 {
-    constexpr int U = 4;                                               // rows in flight
+    // Rows in flight.  Fewer where pieces are not whole and aligned, as those take registers (16 x 40462 x 350 bf16: 206 us, 256 with
+    // eight; but 8 x 32768 x 1024: 473 with eight, 487 with four).
+    constexpr int U = ALIGNED ? 8 : 4;
+    static_assert(TL >= kSpan && kSpan % U == 0, "a lane a place, whole batches");
     const int w = blockIdx.y;
-    const int span = (int)(task / a.slices), slice = (int)(task - (int64_t)span * a.slices);
+    int span = (int)(task / a.slices), slice = (int)(task - (int64_t)span * a.slices);
     if (span >= a.spans) return;
+    if constexpr (TL == kWave) {
+        span = __builtin_amdgcn_readfirstlane(span);
+        slice = __builtin_amdgcn_readfirstlane(slice);
+    }
     const int lane = threadIdx.x % TL;
     const int col = (slice * TL + lane) * E;
     const uint32_t* keys = a.keys + (int64_t)w * a.T;
     const int32_t* pos = a.pos + (int64_t)w * a.T;
     const T* dout = static_cast<const T*>(a.dout) + w * a.ld_dout;
     float* table = a.table + w * a.ld_table;
+    const int s0 = span * kSpan, m = a.T - s0 < kSpan ? a.T - s0 : kSpan;
+    auto key_at = [&](int i) { return i >= 0 && i < a.T ? keys[i] : kNone; };
+    const int mine = s0 + lane % kSpan;
+    const uint32_t own_keys = key_at(mine), next_keys = key_at(mine + kSpan);
+    const uint32_t own_places = mine < a.T ? (uint32_t)pos[mine] : 0, next_places = mine + kSpan < a.T ? (uint32_t)pos[mine + kSpan] : 0;
+    const uint32_t before = key_at(s0 - 1), start_before = key_at(s0 - kSpan), long_before = key_at(s0 - kSpan - 1), after = key_at(s0 + m + kSpan);
     // A run is split if it goes on past the span after the one it begins in.  Of the run that comes into this span: it is if
     // it goes on past this one, or if it came into the span before as well.  Else the team before has summed it.
-    const int s0 = span * kSpan, s1 = s0 + kSpan < a.T ? s0 + kSpan : a.T;
-    const uint32_t k0 = keys[s0], end = keys[s1 - 1], next = s1 < a.T ? keys[s1] : kNone;
-    const uint32_t after = s1 + kSpan < a.T ? keys[s1 + kSpan] : kNone;
-    const uint32_t before = s0 > 0 ? keys[s0 - 1] : kNone, start_before = s0 > 0 ? keys[s0 - kSpan] : kNone;
-    const uint32_t long_before = s0 > kSpan ? keys[s0 - kSpan - 1] : kNone;
+    const uint32_t k0 = from_lane<TL>(own_keys, 0), end = from_lane<TL>(own_keys, m - 1), next = m == kSpan ? from_lane<TL>(next_keys, 0) : kNone;
     const bool came_in = before == k0;
     const bool head_split = came_in && ((end == k0 && next == k0) || (start_before == k0 && long_before == k0));
     const bool tail_split = next == end && after == end;
@@ -311,30 +329,23 @@ __device__ __forceinline__ void sum_runs(const GradArgs& a, int64_t task)
             store_piece(p, col, a.D, old);
         }
     };
-
-    // this span's places, and on into the next one as long as its last run goes on there (if it began here and is not split)
-    const bool finish = next == end && !tail_split && end != skip && !(head && end == k0);
-    const int s2 = !finish ? s1 : s1 + kSpan < a.T ? s1 + kSpan : a.T;
-    for (int i = s0; i < s2; i += U) {
+    // a batch of places of this span (first = 0 .. kSpan - U) or, where only `end` counts, of the next one
+    auto batch = [&](uint32_t lane_keys, uint32_t lane_places, int first, bool own) {
         uint32_t key[U];
-        int32_t at[U];
         float row[U][E];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            key[u] = i + u < s2 ? keys[i + u] : (uint32_t)a.V;
-            at[u] = i + u < s2 ? pos[i + u] : 0;
-            if (i + u >= s1 && key[u] != end) key[u] = (uint32_t)a.V;  // the next span's own
-        }
-        if (i >= s1 && key[0] == (uint32_t)a.V) break;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
+            const int at = (int)from_lane<TL>(lane_places, first + u);
+            key[u] = from_lane<TL>(lane_keys, first + u);
+            const bool mine = own ? first + u < m : key[u] == end;
+            if (!mine) key[u] = (uint32_t)a.V;
 #pragma unroll
             for (int e = 0; e < E; ++e) row[u][e] = 0.0f;
-            if (key[u] < (uint32_t)a.V && key[u] != skip) load_piece(dout + (int64_t)at[u] * a.D, col, a.D, row[u]);
+            if (key[u] < (uint32_t)a.V && key[u] != skip) load_piece(dout + (int64_t)at * a.D, col, a.D, row[u]);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (i + u < s1 && key[u] != cur) {
+            if (own && first + u < m && key[u] != cur) {
                 flush(false);
                 cur = key[u];
                 head = false;
@@ -344,7 +355,12 @@ __device__ __forceinline__ void sum_runs(const GradArgs& a, int64_t task)
 #pragma unroll
             for (int e = 0; e < E; ++e) acc[e] += row[u][e];
         }
-    }
+    };
+    for (int i = 0; i < m; i += U) batch(own_keys, own_places, i, true);
+    // on into the next span as long as the last run goes on there, if it began here and is not split
+    const bool finish = next == end && !tail_split && end != skip && !(head && end == k0);
+    if (finish)
+        for (int i = 0; i < kSpan && from_lane<TL>(next_keys, i) == end; i += U) batch(next_keys, next_places, i, false);
     flush(tail_split);
 }
 
@@ -391,7 +407,7 @@ template <class T, int E, int TL, bool ALIGNED>
 __global__ __launch_bounds__(kThreads) void grad_runs_kernel(GradArgs a)
 {
     __shared__ uint32_t present[(kZeroRows + 31) / 32];
-    if ((int)blockIdx.x < a.run_blocks) sum_runs<T, E, TL>(a, (int64_t)blockIdx.x * (kThreads / TL) + threadIdx.x / TL);
+    if ((int)blockIdx.x < a.run_blocks) sum_runs<T, E, TL, ALIGNED>(a, (int64_t)blockIdx.x * (kThreads / TL) + threadIdx.x / TL);
     else zero_rows<ALIGNED>(a, (int64_t)((int)blockIdx.x - a.run_blocks) * a.zero_rows, present);
 }
 
