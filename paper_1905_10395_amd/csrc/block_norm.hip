@@ -12,7 +12,8 @@
 //
 // Bound by memory.  Workers' weights are columns of fp32 rows; a team keeps them in registers over the tokens it takes,
 // as it does its part of the sums over tokens, which go to the workspace once a workgroup and are added up in order by a
-// second launch: no atomics, equal calls give equal bits.
+// second launch: no atomics, equal calls give equal bits.  Forward 8 x 8192 x 4096 bf16 480 us, 5.6 TB/s of the 2.7 GB that have to
+// move; backward 8 x 4096 x 2048 205 us, 5.2 TB/s of 1.07 GB, with the join.
 //
 // A lane holds eight columns, so a team is as wide as its row (16 columns a lane and half the lanes: 536 instead of 487 us
 // forward at 8 x 8192 x 4096 bf16, 339 instead of 230 backward at 4 x 4096 x 4096).  Teams take every grid-th token, so that
@@ -27,7 +28,8 @@ using namespace lsgd;
 
 namespace {
 
-constexpr int E = 8;              // elements of a piece: 16 bytes of bf16, twice that of fp32
+constexpr int kColumns = 8;       // of a row that a lane holds, or twice as many
+constexpr int kTeamThreads = 256, kMaxThreads = 1024;
 
 // [W, T, D] with dense rows
 struct Rows {
@@ -56,53 +58,86 @@ struct NormGradArgs {
     int post;
 };
 
-// A lane's N pieces of a row.  WIDE: all whole and 16-byte aligned; these are read once and written once, and streaming
-// accesses in both directions took 548 us where plain ones took 572, either direction alone 557.  Elements past the row's end
-// read zero and are not written.
-template <int N, bool WIDE>
+// A lane's columns of a row: pieces of 16 bytes, adjacent lanes' adjacent, so that an access of a wavefront covers whole lines
+// (of fp32, 32 bytes a lane took 272 instead of 220 us forward at 8 x 4096 x 2048).  WIDE: all pieces whole and 16-byte aligned; these are
+// read once and written once, and streaming accesses in both directions took 548 us where plain ones took 572 (8 x 8192 x 4096
+// bf16), either direction alone 557.  Elements past the row's end read zero and are not written.  SHORT: rows may be shorter than
+// a piece.
+template <class T, int N, bool WIDE, bool SHORT>
 struct Piece {
-    static __device__ __forceinline__ int col(int lane, int ts, int n) { return (n * ts + lane) * E; }
+    static constexpr int E = 16 / (int)sizeof(T), PIECES = N * kColumns / E;
+    using Row = Raw<T, E>[PIECES];                                     // as in memory
+    using Values = float[PIECES][E];
 
-    template <class T>
-    static __device__ __forceinline__ void load(const T* p, int lane, int ts, int D, float (&v)[N][E])
+    static __device__ __forceinline__ int col(int lane, int ts, int n) { return (n * ts + lane) * E; }
+    static __device__ __forceinline__ void load(const T* p, int lane, int ts, int D, Row& v)
     {
 #pragma unroll
-        for (int n = 0; n < N; ++n) {
+        for (int n = 0; n < PIECES; ++n) {
             const int c = col(lane, ts, n);
-#pragma unroll
-            for (int e = 0; e < E; ++e) v[n][e] = 0.0f;
-            if constexpr (!WIDE) load_piece(p, c, D, v[n]);
-            else if (c < D) load_whole<true>(p + c, v[n]);
+            clear(v[n]);
+            if constexpr (!WIDE) load_piece<SHORT>(p, c, D, v[n]);
+            else if (c < D) load_whole<true>(column(p, c), v[n]);
         }
     }
-    template <class T>
-    static __device__ __forceinline__ void store(T* p, int lane, int ts, int D, const float (&v)[N][E])
+    static __device__ __forceinline__ void none(Row& v)
     {
 #pragma unroll
-        for (int n = 0; n < N; ++n) {
+        for (int n = 0; n < PIECES; ++n) clear(v[n]);
+    }
+    static __device__ __forceinline__ void get(const Row& v, int lane, int ts, int D, Values& f)
+    {
+#pragma unroll
+        for (int n = 0; n < PIECES; ++n) {
+            unpack(v[n], f[n]);
+            if constexpr (!WIDE) keep_own(col(lane, ts, n), D, f[n]);
+        }
+    }
+    template <class TO>
+    static __device__ __forceinline__ void store(TO* p, int lane, int ts, int D, const Values& v)
+    {
+#pragma unroll
+        for (int n = 0; n < PIECES; ++n) {
             const int c = col(lane, ts, n);
-            if constexpr (!WIDE) store_piece(p, c, D, v[n]);
-            else if (c < D) store_whole<true>(p + c, v[n]);
+            if constexpr (!WIDE) store_piece<SHORT>(p, c, D, v[n]);
+            else if (c < D) store_whole<true>(column(p, c), v[n]);
         }
     }
     // per-column weights of a worker (a team reads them again and again: not streamed); absent: ones.  Past the row's end
     // zero, so that nothing there enters a sum.
-    static __device__ __forceinline__ void weights(const float* p, int lane, int ts, int D, float (&v)[N][E])
+    static __device__ __forceinline__ void weights(const float* p, int lane, int ts, int D, Values& v)
     {
 #pragma unroll
-        for (int n = 0; n < N; ++n) {
+        for (int n = 0; n < PIECES; ++n) {
             const int c = col(lane, ts, n);
 #pragma unroll
-            for (int e = 0; e < E; ++e) v[n][e] = !p && c + e < D ? 1.0f : 0.0f;
-            if (p) load_piece(p, c, D, v[n]);
+            for (int e = 0; e < E; ++e) v[n][e] = c < D ? 1.0f : 0.0f;
+            if (p) load_piece<SHORT>(p, c, D, v[n]);
+            keep_own(c, D, v[n]);
         }
     }
 };
 
+// Whether a team holds the weights and its sums for their gradients in registers over its tokens.  With twice the columns a lane
+// they do not fit, and it reads the weights again for each token and keeps the sums in LDS (2 x 2048 x 16384 bf16 backward 228 us,
+// 316 with spilled registers; fp32 468 and 777).
+template <int N>
+constexpr bool kHold = N == 1;
+
+// A lane's part of a weight's gradient, over its tokens: in registers, or where those are short in the lane's own LDS.
+template <int N, bool LDS>
+struct Grad {
+    v4f v[N * kColumns / 4];
+    __device__ __forceinline__ v4f& at(int k) { return v[k]; }
+};
+template <int N>
+struct Grad<N, true> {
+    v4f* v;
+    __device__ __forceinline__ v4f& at(int k) { return v[k * kMaxThreads]; }
+};
+
 // Teams: LANES of a wavefront (8 to 64, as many as rows of at most 512 columns need) in workgroups of 256; or, LANES = 0, the
 // workgroup, of any whole number of wavefronts.
-constexpr int kTeamThreads = 256;
-constexpr int kMaxThreads = 1024;
 constexpr int threads_limit(int lanes) { return lanes ? kTeamThreads : kMaxThreads; }
 
 // Sums over rows of 16 lanes and over a wavefront by lane shifts in the vector unit.
@@ -159,36 +194,44 @@ __device__ __forceinline__ T* row_of(const Rows& a, int w, int64_t t) { return s
 template <class T, int N, bool WIDE, int LANES>
 __global__ __launch_bounds__(threads_limit(LANES)) void block_norm_kernel(NormArgs a)
 {
-    using P = Piece<N, WIDE>;
+    using P = Piece<T, N, WIDE, LANES == 8>;
+    constexpr int E = P::E, PIECES = P::PIECES;
     __shared__ float buf[2][16];
     TeamSum sums{buf, 0};
     constexpr int teams = LANES ? kTeamThreads / (LANES ? LANES : 1) : 1;
     const int ts = LANES ? LANES : (int)blockDim.x, lane = threadIdx.x % (unsigned)ts, w = blockIdx.y;
     int team = LANES ? (int)threadIdx.x / ts : 0;
     if constexpr (LANES == kWave) team = __builtin_amdgcn_readfirstlane(team);
-    float wp[N][E], wn[N][E];
-    if (a.y.p) P::weights(a.w_post ? a.w_post + w * a.ld_w_post : nullptr, lane, ts, a.D, wp);
-    if (a.n.p) P::weights(a.w_pre ? a.w_pre + w * a.ld_w_pre : nullptr, lane, ts, a.D, wn);
+    typename P::Values wp, wn;
+    auto post_weights = [&] { P::weights(a.w_post ? a.w_post + w * a.ld_w_post : nullptr, lane, ts, a.D, wp); };
+    auto pre_weights = [&] { P::weights(a.w_pre ? a.w_pre + w * a.ld_w_pre : nullptr, lane, ts, a.D, wn); };
+    if (kHold<N> && a.y.p) post_weights();
+    if (kHold<N> && a.n.p) pre_weights();
     for (int64_t t = (int64_t)blockIdx.x * teams + team; t < a.T; t += (int64_t)gridDim.x * teams) {
-        float r[N][E];
-        P::load(row_of<T>(a.r, w, t), lane, ts, a.D, r);
+        typename P::Row rr, ry, ru;
+        typename P::Values r;
+        P::load(row_of<T>(a.r, w, t), lane, ts, a.D, rr);
         if (a.y.p) {
-            float y[N][E], u[N][E];
-            P::load(row_of<T>(a.y, w, t), lane, ts, a.D, y);
-            if (a.u.p) P::load(row_of<T>(a.u, w, t), lane, ts, a.D, u);
+            typename P::Values y, u;
+            P::load(row_of<T>(a.y, w, t), lane, ts, a.D, ry);
+            if (a.u.p) P::load(row_of<T>(a.u, w, t), lane, ts, a.D, ru);
+            P::get(ry, lane, ts, a.D, y);
             float q = 1.0f;
             if (a.post) {
                 float s = 0.0f;
 #pragma unroll
-                for (int n = 0; n < N; ++n)
+                for (int n = 0; n < PIECES; ++n)
 #pragma unroll
                     for (int e = 0; e < E; ++e) s += y[n][e] * y[n][e];
                 q = 1.0f / sqrtf(team_sum<LANES>(s, sums) * a.inv_d + a.eps);
                 if (a.q_post && lane == 0) a.q_post[(int64_t)w * a.T + t] = q;
             }
             const float sq = a.scale * q;
+            if (!kHold<N>) post_weights();
+            P::get(rr, lane, ts, a.D, r);
+            if (a.u.p) P::get(ru, lane, ts, a.D, u);
 #pragma unroll
-            for (int n = 0; n < N; ++n)
+            for (int n = 0; n < PIECES; ++n)
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
                     float b = y[n][e] * sq * wp[n][e];
@@ -196,17 +239,20 @@ __global__ __launch_bounds__(threads_limit(LANES)) void block_norm_kernel(NormAr
                     r[n][e] += b;
                 }
             P::store(row_of<T>(a.r_out, w, t), lane, ts, a.D, r);
+        } else {
+            P::get(rr, lane, ts, a.D, r);
         }
         if (a.n.p) {
             float s = 0.0f;
 #pragma unroll
-            for (int n = 0; n < N; ++n)
+            for (int n = 0; n < PIECES; ++n)
 #pragma unroll
                 for (int e = 0; e < E; ++e) s += r[n][e] * r[n][e];
             const float q = 1.0f / sqrtf(team_sum<LANES>(s, sums) * a.inv_d + a.eps);
             if (a.q_pre && lane == 0) a.q_pre[(int64_t)w * a.T + t] = q;
+            if (!kHold<N>) pre_weights();
 #pragma unroll
-            for (int n = 0; n < N; ++n)
+            for (int n = 0; n < PIECES; ++n)
 #pragma unroll
                 for (int e = 0; e < E; ++e) r[n][e] *= q * wn[n][e];
             P::store(row_of<T>(a.n, w, t), lane, ts, a.D, r);
@@ -214,86 +260,117 @@ __global__ __launch_bounds__(threads_limit(LANES)) void block_norm_kernel(NormAr
     }
 }
 
+// Four wavefronts a SIMD have to fit (8 x 16384 x 201 bf16 115 us, 145 where registers decide), but for fp32 in unaligned pieces,
+// which would spill (182 us so, 295 with four).
 template <class T, int N, bool WIDE, int LANES>
-__global__ __launch_bounds__(threads_limit(LANES)) void block_norm_grad_kernel(NormGradArgs a)
+__global__ __launch_bounds__(threads_limit(LANES), sizeof(T) == 2 || WIDE ? 4 : 1) void block_norm_grad_kernel(NormGradArgs a)
 {
-    using P = Piece<N, WIDE>;
+    using P = Piece<T, N, WIDE, LANES == 8>;
+    constexpr int E = P::E, PIECES = P::PIECES;
     __shared__ float buf[2][16];
     TeamSum sums{buf, 0};
     constexpr int teams = LANES ? kTeamThreads / (LANES ? LANES : 1) : 1;
     const int ts = LANES ? LANES : (int)blockDim.x, lane = threadIdx.x % (unsigned)ts, w = blockIdx.y;
     int team = LANES ? (int)threadIdx.x / ts : 0;
     if constexpr (LANES == kWave) team = __builtin_amdgcn_readfirstlane(team);
-    float wp[N][E], wn[N][E], dwp[N][E], dwn[N][E];
-    if (a.y.p) P::weights(a.w_post ? a.w_post + w * a.ld_w_post : nullptr, lane, ts, a.D, wp);
-    if (a.dn.p) P::weights(a.w_pre ? a.w_pre + w * a.ld_w_pre : nullptr, lane, ts, a.D, wn);
+    typename P::Values wp, wn;
+    Grad<N, !kHold<N>> dwp, dwn;
+    if constexpr (!kHold<N>) {
+        __shared__ v4f held[2 * N * kColumns / 4 * kMaxThreads];
+        dwp.v = held + threadIdx.x;
+        dwn.v = dwp.v + N * kColumns / 4 * kMaxThreads;
+    }
+    auto post_weights = [&] { P::weights(a.w_post ? a.w_post + w * a.ld_w_post : nullptr, lane, ts, a.D, wp); };
+    auto pre_weights = [&] { P::weights(a.w_pre ? a.w_pre + w * a.ld_w_pre : nullptr, lane, ts, a.D, wn); };
+    if (kHold<N> && a.y.p) post_weights();
+    if (kHold<N> && a.dn.p) pre_weights();
 #pragma unroll
-    for (int n = 0; n < N; ++n)
-#pragma unroll
-        for (int e = 0; e < E; ++e) dwp[n][e] = dwn[n][e] = 0.0f;
+    for (int k = 0; k < N * kColumns / 4; ++k) dwp.at(k) = dwn.at(k) = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     for (int64_t t = (int64_t)blockIdx.x * teams + team; t < a.T; t += (int64_t)gridDim.x * teams) {
-        float dr[N][E], z[N][E], u[N][E];
+        typename P::Row rz, ru, rdr, rdn, rh;
+        typename P::Values dr, z, u;
         constexpr bool kEarly = N == 1;                                 // in flight while the first sum is made, if registers are left
-        if (kEarly && a.y.p) {                                          // (two pieces: 316 us late, 569 early, 2 x 2048 x 16384 bf16)
-            P::load(row_of<T>(a.y, w, t), lane, ts, a.D, z);
-            if (a.u.p) P::load(row_of<T>(a.u, w, t), lane, ts, a.D, u);
-        }
-        if (a.dr_out.p) P::load(row_of<T>(a.dr_out, w, t), lane, ts, a.D, dr);
-        else {
-#pragma unroll
-            for (int n = 0; n < N; ++n)
-#pragma unroll
-                for (int e = 0; e < E; ++e) dr[n][e] = 0.0f;
+        if (kEarly && a.y.p) {                                          // (two pieces a lane: 228 us late, 255 early, 2 x 2048 x 16384 bf16)
+            P::load(row_of<T>(a.y, w, t), lane, ts, a.D, rz);
+            if (a.u.p) P::load(row_of<T>(a.u, w, t), lane, ts, a.D, ru);
         }
         if (a.dn.p) {
-            float dn[N][E], h[N][E];
-            P::load(row_of<T>(a.dn, w, t), lane, ts, a.D, dn);
-            P::load(row_of<T>(a.r, w, t), lane, ts, a.D, h);
+            P::load(row_of<T>(a.dn, w, t), lane, ts, a.D, rdn);
+            P::load(row_of<T>(a.r, w, t), lane, ts, a.D, rh);
+        }
+        auto load_dr = [&] {
+            if (a.dr_out.p) P::load(row_of<T>(a.dr_out, w, t), lane, ts, a.D, rdr);
+            else P::none(rdr);
+        };
+        if (kEarly) load_dr();
+        if (a.dn.p) {
+            typename P::Values dn, h;
+            P::get(rdn, lane, ts, a.D, dn);
+            P::get(rh, lane, ts, a.D, h);
+            if (!kHold<N>) pre_weights();
             const float q = a.q_pre[(int64_t)w * a.T + t];
             float s = 0.0f;
 #pragma unroll
-            for (int n = 0; n < N; ++n)
+            for (int n = 0; n < PIECES; ++n)
 #pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    h[n][e] *= q;
-                    dwn[n][e] += dn[n][e] * h[n][e];
-                    dn[n][e] *= wn[n][e];
-                    s += dn[n][e] * h[n][e];
+                for (int e = 0; e < E; e += 4) {
+                    v4f dw = dwn.at((n * E + e) / 4);
+#pragma unroll
+                    for (int k = e; k < e + 4; ++k) {
+                        h[n][k] *= q;
+                        dw[k - e] += dn[n][k] * h[n][k];
+                        dn[n][k] *= wn[n][k];
+                        s += dn[n][k] * h[n][k];
+                    }
+                    dwn.at((n * E + e) / 4) = dw;
                 }
             s = team_sum<LANES>(s, sums) * a.inv_d;
+            if (!kEarly) load_dr();
+            P::get(rdr, lane, ts, a.D, dr);
 #pragma unroll
-            for (int n = 0; n < N; ++n)
+            for (int n = 0; n < PIECES; ++n)
 #pragma unroll
                 for (int e = 0; e < E; ++e) dr[n][e] += q * (dn[n][e] - h[n][e] * s);
+        } else {
+            if (!kEarly) load_dr();
+            P::get(rdr, lane, ts, a.D, dr);
         }
         P::store(row_of<T>(a.dr, w, t), lane, ts, a.D, dr);
         if (a.y.p) {
             if (!kEarly) {
-                P::load(row_of<T>(a.y, w, t), lane, ts, a.D, z);
-                if (a.u.p) P::load(row_of<T>(a.u, w, t), lane, ts, a.D, u);
+                P::load(row_of<T>(a.y, w, t), lane, ts, a.D, rz);
+                if (a.u.p) P::load(row_of<T>(a.u, w, t), lane, ts, a.D, ru);
             }
+            P::get(rz, lane, ts, a.D, z);
+            if (a.u.p) P::get(ru, lane, ts, a.D, u);
+            if (!kHold<N>) post_weights();
             const float q = a.post ? a.q_post[(int64_t)w * a.T + t] : 1.0f;
             float s = 0.0f;
 #pragma unroll
-            for (int n = 0; n < N; ++n)
+            for (int n = 0; n < PIECES; ++n)
 #pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    z[n][e] *= q;
-                    float d = a.scale * dr[n][e];                       // e of the formula, gate still missing
-                    if (a.u.p) {
-                        const float g = sigmoid(u[n][e]);
-                        u[n][e] = d * z[n][e] * wp[n][e] * (g * (1.0f - g));
-                        d *= g;
+                for (int e = 0; e < E; e += 4) {
+                    v4f dw = dwp.at((n * E + e) / 4);
+#pragma unroll
+                    for (int k = e; k < e + 4; ++k) {
+                        z[n][k] *= q;
+                        float d = a.scale * dr[n][k];                   // e of the formula, gate still missing
+                        if (a.u.p) {
+                            const float g = sigmoid(u[n][k]);
+                            u[n][k] = d * z[n][k] * wp[n][k] * (g * (1.0f - g));
+                            d *= g;
+                        }
+                        dw[k - e] += d * z[n][k];
+                        dr[n][k] = d * wp[n][k];
+                        s += dr[n][k] * z[n][k];
                     }
-                    dwp[n][e] += d * z[n][e];
-                    dr[n][e] = d * wp[n][e];
-                    s += dr[n][e] * z[n][e];
+                    dwp.at((n * E + e) / 4) = dw;
                 }
             if (a.u.p) P::store(row_of<T>(a.du, w, t), lane, ts, a.D, u);
             if (a.post) {
                 s = team_sum<LANES>(s, sums) * a.inv_d;
 #pragma unroll
-                for (int n = 0; n < N; ++n)
+                for (int n = 0; n < PIECES; ++n)
 #pragma unroll
                     for (int e = 0; e < E; ++e) dr[n][e] = q * (dr[n][e] - z[n][e] * s);
             }
@@ -303,17 +380,25 @@ __global__ __launch_bounds__(threads_limit(LANES)) void block_norm_grad_kernel(N
     if (!a.parts) return;
     float* part = a.parts + ((int64_t)w * gridDim.x + blockIdx.x) * 2 * a.Dp;
     if constexpr (LANES == 0) {
-        P::store(part, lane, ts, a.D, dwp);
-        P::store(part + a.Dp, lane, ts, a.D, dwn);
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            typename P::Values f;
+#pragma unroll
+            for (int k = 0; k < PIECES * E; ++k) f[k / E][k % E] = (which ? dwn : dwp).at(k / 4)[k % 4];
+            P::store(part + which * a.Dp, lane, ts, a.D, f);
+        }
     } else {
         // the workgroup's teams add up theirs in order
-        __shared__ float sum[teams][LANES * E];
+        __shared__ float sum[teams][LANES * kColumns];
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) sum[team][lane * E + e] = which ? dwn[0][e] : dwp[0][e];
+            for (int k = 0; k < PIECES * E; ++k) {
+                const int first = P::col(lane, ts, k / E), c = (WIDE ? first : piece_start<E>(first, a.D)) + k % E;
+                if (c >= first) sum[team][c] = (which ? dwn : dwp).at(k / 4)[k % 4];
+            }
             __syncthreads();
-            for (int i = threadIdx.x; i < LANES * E && i < a.D; i += kTeamThreads) {
+            for (int i = threadIdx.x; i < LANES * kColumns && i < a.D; i += kTeamThreads) {
                 float s = 0.0f;
 #pragma unroll
                 for (int k = 0; k < teams; ++k) s += sum[k][i];
@@ -360,7 +445,7 @@ __global__ __launch_bounds__(256) void norm_zero_kernel(float* dw, int64_t ld, i
 
 // ---- host ----
 constexpr size_t kAlign = 256;
-constexpr int kMaxWidth = kMaxThreads * 2 * E;
+constexpr int kMaxWidth = kMaxThreads * 2 * kColumns;
 bool on(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
 lsgd_status check_shape(const char* who, int32_t W, int32_t T, int32_t D)
@@ -400,7 +485,7 @@ Rows rows(const lsgd_rows& a) { return Rows{a.data, a.worker_stride, a.token_str
 int lanes_of(int D)
 {
     int lanes = 8;
-    while (lanes * E < D) lanes *= 2;
+    while (lanes * kColumns < D) lanes *= 2;
     return lanes;
 }
 
@@ -410,18 +495,20 @@ struct Shape {
 };
 Shape shape_of(int D)
 {
-    if (D <= kWave * E) return {1, kTeamThreads / lanes_of(D), kTeamThreads};
-    if (D <= kMaxThreads * E) return {1, 1, (D - 1) / (kWave * E) * kWave + kWave};
+    if (D <= kWave * kColumns) return {1, kTeamThreads / lanes_of(D), kTeamThreads};
+    if (D <= kMaxThreads * kColumns) return {1, 1, (D - 1) / (kWave * kColumns) * kWave + kWave};
     return {2, 1, kMaxThreads};
 }
 
-// Workgroups of a worker: by lanes in all.  Forward many: a team's only gain from further tokens is the weights it holds
-// (8 x 8192 x 4096: 470 us with 2^22 lanes, 488 with 2^20; x 1024: 113 and 126).  Backward each leaves partial sums, and
-// enough have to be left over to even out (8 x 4096 x 2048: 214 us with 2^19, 222 with 2^18, 224 with 2^20).
-constexpr int kLanes = 1 << 22, kLanesGrad = 1 << 19;
-int groups_of(int W, int T, const Shape& s, int lanes)
+// Workgroups of a worker.  Forward many, by lanes in all: a team's only gain from further tokens is the weights it holds
+// (8 x 8192 x 4096: 470 us with 2^22 lanes, 488 with 2^20; x 1024: 113 and 126).  Backward each leaves partial sums; twice what
+// the chip holds at a time, which is 1024 lanes a compute unit by their registers: enough to even out (8 x 4096 x 2048 bf16 208 us,
+// 222 with once as many, 216 with four times), and whole rounds (6 x 4064 x 4496, nine wavefronts a team: 400 us, 430 with 2^19
+// lanes in all; 12 x 990 x 7384 298 and 372).
+constexpr int kLanes = 1 << 22, kRoundsGrad = 2, kComputeUnits = 256;
+int groups_of(int W, int T, const Shape& s, int all)
 {
-    return (int)std::min<int64_t>((T - 1) / s.teams + 1, std::max(1, lanes / s.threads / W));
+    return (int)std::min<int64_t>((T - 1) / s.teams + 1, std::max(1, all / W));
 }
 
 struct GradPlan {
@@ -431,8 +518,9 @@ struct GradPlan {
 GradPlan grad_plan(int W, int T, int D)
 {
     GradPlan p;
-    p.groups = T ? groups_of(W, T, shape_of(D), kLanesGrad) : 0;
-    p.Dp = (D + E - 1) / E * E;
+    const Shape sh = shape_of(D);
+    p.groups = T ? groups_of(W, T, sh, kRoundsGrad * kComputeUnits * (kMaxThreads / sh.threads)) : 0;
+    p.Dp = (D + kColumns - 1) / kColumns * kColumns;
     p.bytes = std::max<size_t>(kAlign, sizeof(float) * (size_t)W * (size_t)p.groups * 2 * (size_t)p.Dp);
     return p;
 }
@@ -443,11 +531,11 @@ void dispatch(int D, bool bf16, bool wide, F launch)
 {
     auto shaped = [&](auto type, auto wide_rows) {
         const std::integral_constant<int, 1> one{};
-        if (D <= 8 * E) launch(type, one, wide_rows, std::integral_constant<int, 8>{});
-        else if (D <= 16 * E) launch(type, one, wide_rows, std::integral_constant<int, 16>{});
-        else if (D <= 32 * E) launch(type, one, wide_rows, std::integral_constant<int, 32>{});
-        else if (D <= 64 * E) launch(type, one, wide_rows, std::integral_constant<int, 64>{});
-        else if (D <= kMaxThreads * E) launch(type, one, wide_rows, std::integral_constant<int, 0>{});
+        if (D <= 8 * kColumns) launch(type, one, wide_rows, std::integral_constant<int, 8>{});
+        else if (D <= 16 * kColumns) launch(type, one, wide_rows, std::integral_constant<int, 16>{});
+        else if (D <= 32 * kColumns) launch(type, one, wide_rows, std::integral_constant<int, 32>{});
+        else if (D <= 64 * kColumns) launch(type, one, wide_rows, std::integral_constant<int, 64>{});
+        else if (D <= kMaxThreads * kColumns) launch(type, one, wide_rows, std::integral_constant<int, 0>{});
         else launch(type, std::integral_constant<int, 2>{}, wide_rows, std::integral_constant<int, 0>{});
     };
     if (bf16) wide ? shaped(uint16_t{}, std::true_type{}) : shaped(uint16_t{}, std::false_type{});
@@ -500,10 +588,10 @@ lsgd_status lsgd_block_norm(const lsgd_block_norm_args* p, void* hip_stream)
     a.T = T; a.D = D;
     a.scale = p->scale; a.eps = p->eps; a.inv_d = 1.0f / (float)D;
     a.post = p->post_norm;
-    bool wide = D % E == 0;
+    bool wide = D % (16 / es) == 0;
     for (const lsgd_rows* q : {&p->r, &p->y, &p->gate, &p->r_out, &p->n}) wide = wide && wide_rows(*q, W, T, es);
     const Shape sh = shape_of(D);
-    const dim3 grid((unsigned)groups_of(W, T, sh, kLanes), (unsigned)W);
+    const dim3 grid((unsigned)groups_of(W, T, sh, kLanes / sh.threads), (unsigned)W);
     dispatch(D, p->is_bf16, wide, [&](auto type, auto n, auto wide_rows, auto lanes) {
         hipLaunchKernelGGL((block_norm_kernel<decltype(type), decltype(n)::value, decltype(wide_rows)::value, decltype(lanes)::value>), grid,
                            dim3((unsigned)sh.threads), 0, static_cast<hipStream_t>(hip_stream), a);
@@ -575,7 +663,7 @@ lsgd_status lsgd_block_norm_grad(const lsgd_block_norm_grad_args* p, void* works
     a.T = T; a.D = D; a.Dp = plan.Dp;
     a.scale = p->scale; a.inv_d = 1.0f / (float)D;
     a.post = p->post_norm;
-    bool wide = D % E == 0;
+    bool wide = D % (16 / es) == 0;
     for (const lsgd_rows* q : {&p->dn, &p->dr_out, &p->r_out, &p->y, &p->gate, &p->dr, &p->dy, &p->dgate}) wide = wide && wide_rows(*q, W, T, es);
     dispatch(D, p->is_bf16, wide, [&](auto type, auto n, auto wide_rows, auto lanes) {
         hipLaunchKernelGGL((block_norm_grad_kernel<decltype(type), decltype(n)::value, decltype(wide_rows)::value, decltype(lanes)::value>),

@@ -56,22 +56,23 @@ __global__ __launch_bounds__(kThreads) void lookup_kernel(const TI* __restrict__
         c[k] = (int)(q - r * (uint32_t)per) * E;
         tok[k] = t[k] < T ? tokens[t[k]] : -1;
     }
-    float v[kLookupEach][E];
+    Raw<TI, E> row[kLookupEach];
 #pragma unroll
     for (int k = 0; k < kLookupEach; ++k) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) v[k][e] = 0.0f;
+        clear(row[k]);
         if ((uint32_t)tok[k] >= (uint32_t)V) continue;
-        if constexpr (ONCE) load_whole<false>(table + (int64_t)tok[k] * D + c[k], v[k]);
-        else load_piece(table + (int64_t)tok[k] * D, c[k], D, v[k]);
+        if constexpr (ONCE) load_whole<false>(table + (int64_t)tok[k] * D + c[k], row[k]);
+        else load_piece(table + (int64_t)tok[k] * D, c[k], D, row[k]);
     }
 #pragma unroll
     for (int k = 0; k < kLookupEach; ++k) {
         if (t[k] >= T) continue;
+        float v[E];
+        unpack(row[k], v);
 #pragma unroll
-        for (int e = 0; e < E; ++e) v[k][e] *= scale;
-        if constexpr (ONCE) store_whole<true>(out + t[k] * D + c[k], v[k]);
-        else store_piece(out + t[k] * D, c[k], D, v[k]);
+        for (int e = 0; e < E; ++e) v[e] *= scale;
+        if constexpr (ONCE) store_whole<true>(out + t[k] * D + c[k], v);
+        else store_piece(out + t[k] * D, c[k], D, v);
     }
 }
 
@@ -320,9 +321,7 @@ __device__ __forceinline__ void sum_runs(const GradArgs& a, int64_t task)
             store_piece(a.parts + (((int64_t)w * a.spans + span) * 2 + (head ? 0 : 1)) * a.Dp, col, a.D, acc);
         } else {
             float* p = table + (int64_t)cur * a.D;
-            float old[E];
-#pragma unroll
-            for (int e = 0; e < E; ++e) old[e] = 0.0f;
+            float old[E] = {};
             if (a.accumulate) load_piece(p, col, a.D, old);
 #pragma unroll
             for (int e = 0; e < E; ++e) old[e] += a.scale * acc[e];
@@ -332,15 +331,14 @@ __device__ __forceinline__ void sum_runs(const GradArgs& a, int64_t task)
     // a batch of places of this span (first = 0 .. kSpan - U) or, where only `end` counts, of the next one
     auto batch = [&](uint32_t lane_keys, uint32_t lane_places, int first, bool own) {
         uint32_t key[U];
-        float row[U][E];
+        Raw<T, E> row[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int at = (int)from_lane<TL>(lane_places, first + u);
             key[u] = from_lane<TL>(lane_keys, first + u);
             const bool mine = own ? first + u < m : key[u] == end;
             if (!mine) key[u] = (uint32_t)a.V;
-#pragma unroll
-            for (int e = 0; e < E; ++e) row[u][e] = 0.0f;
+            clear(row[u]);
             if (key[u] < (uint32_t)a.V && key[u] != skip) load_piece(dout + (int64_t)at * a.D, col, a.D, row[u]);
         }
 #pragma unroll
@@ -352,8 +350,10 @@ __device__ __forceinline__ void sum_runs(const GradArgs& a, int64_t task)
 #pragma unroll
                 for (int e = 0; e < E; ++e) acc[e] = 0.0f;
             }
+            float v[E];
+            unpack(row[u], v);
 #pragma unroll
-            for (int e = 0; e < E; ++e) acc[e] += row[u][e];
+            for (int e = 0; e < E; ++e) acc[e] += v[e];
         }
     };
     for (int i = 0; i < m; i += U) batch(own_keys, own_places, i, true);
@@ -465,11 +465,9 @@ __global__ __launch_bounds__(kThreads) void grad_join_kernel(GradArgs a)
         if (n > kJoinShared) continue;
         float* row = table + (int64_t)cur * a.D;
         const v4f acc = add(span, 0, n);
-        float old[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (a.accumulate) load_piece(row, col, a.D, old);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) old[e] += a.scale * acc[e];
-        store_piece(row, col, a.D, old);
+        for (int e = 0; e < 4; ++e)
+            if (col + e < a.D) row[col + e] = (a.accumulate ? row[col + e] : 0.0f) + a.scale * acc[e];
     }
     __syncthreads();
     for (int k = 0; k < n_runs; ++k) {                                 // long ones, together
@@ -579,20 +577,22 @@ __global__ __launch_bounds__(kSortThreads) void grad_small_kernel(GradArgs a, Sm
 #pragma unroll
         for (int e = 0; e < E; ++e) acc[e] = 0.0f;
         for (int b = p0; b < p1; b += U) {
-            float row[U][E];
+            Raw<T, E> row[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-#pragma unroll
-                for (int e = 0; e < E; ++e) row[u][e] = 0.0f;
+                clear(row[u]);
                 if (b + u < p1) {
                     const int at = __builtin_amdgcn_readfirstlane((int)pos[b + u]);
                     load_piece(dout + (int64_t)at * a.D, col, a.D, row[u]);
                 }
             }
 #pragma unroll
-            for (int u = 0; u < U; ++u)
+            for (int u = 0; u < U; ++u) {
+                float v[E];
+                unpack(row[u], v);
 #pragma unroll
-                for (int e = 0; e < E; ++e) acc[e] += row[u][e];
+                for (int e = 0; e < E; ++e) acc[e] += v[e];
+            }
         }
     };
     const int lo = blockIdx.x * q.span, hi = lo + q.span < a.T ? lo + q.span : a.T;
@@ -624,9 +624,7 @@ __global__ __launch_bounds__(kSortThreads) void grad_small_kernel(GradArgs a, Sm
             const int col0 = (slice0 + c) * cols, col = col0 + lane * E;
             if (col0 >= a.D) break;
             float* p = table + (int64_t)v * a.D;
-            float old[E];
-#pragma unroll
-            for (int e = 0; e < E; ++e) old[e] = 0.0f;
+            float old[E] = {};
             if (a.accumulate) load_piece(p, col, a.D, old);
             add_places(j, j + n, col);
 #pragma unroll
@@ -642,8 +640,10 @@ __global__ __launch_bounds__(kSortThreads) void grad_small_kernel(GradArgs a, Sm
             const int col0 = (slice0 + c) * cols, col = col0 + lane * E;
             if (col0 >= a.D) break;
             add_places(j + n * wave / kSortWaves, j + n * (wave + 1) / kSortWaves, col);
+            const int at = piece_start<E>(col, a.D) - col0;
 #pragma unroll
-            for (int e = 0; e < E; ++e) s.sum[wave][lane * E + e] = acc[e];
+            for (int e = 0; e < E; ++e)
+                if (at + e >= lane * E) s.sum[wave][at + e] = acc[e];
             __syncthreads();
             if ((int)threadIdx.x < cols && col0 + (int)threadIdx.x < a.D) {
                 float t = 0.0f;
