@@ -28,7 +28,11 @@ namespace {
 constexpr int kThreads = 256;
 
 // ---- lookup ----
-constexpr int kLookupEach = 4;      // independent pieces of E elements a thread has in flight
+constexpr int kLookupEach = 4;      // independent pieces a thread has in flight
+// Elements of a piece: 16 bytes of it are adjacent to the next lane's, so that streaming stores fill lines (16 x 8192 x 1024 fp32
+// 182 us, 196 with 32).
+template <class TI, class TO>
+constexpr int kLookupPiece = sizeof(TI) == 4 && sizeof(TO) == 4 ? 4 : 8;
 
 // A workgroup's pieces are adjacent in the output; which token and column a piece is follows from its number.  Bound by memory:
 // 16 x 8192 x 1024 bf16 from 32768 rows 73 us, 5.1 TB/s of the 375 MB that have to move (79 us with stores that stay in the
@@ -38,7 +42,7 @@ __global__ __launch_bounds__(kThreads) void lookup_kernel(const TI* __restrict__
                                                           const int32_t* __restrict__ tokens, int64_t ld_tokens, int T,
                                                           float scale, TO* __restrict__ out, int64_t ld_out)
 {
-    constexpr int E = 8;
+    constexpr int E = kLookupPiece<TI, TO>;
     const int per = (D - 1) / E + 1;                                   // pieces of a token
     const int64_t base = (int64_t)blockIdx.x * (kThreads * kLookupEach);
     const int64_t t0 = base / per;
@@ -276,12 +280,10 @@ __device__ __forceinline__ uint32_t from_lane(uint32_t v, int i)
 
 // TL lanes make a team: they own TL * E columns of one span.  All it goes by - the keys and places of its span and of the next
 // one, a lane each, and four keys around - is on its way at once.
-template <class T, int E, int TL, bool ALIGNED>
+template <class T, int E, int TL>
 __device__ __forceinline__ void sum_runs(const GradArgs& a, int64_t task)
 {
-    // Rows in flight.  Fewer where pieces are not whole and aligned, as those take registers (16 x 40462 x 350 bf16: 206 us, 256 with
-    // eight; but 8 x 32768 x 1024: 473 with eight, 487 with four).
-    constexpr int U = ALIGNED ? 8 : 4;
+    constexpr int U = 8;                                               // rows in flight (8 x 32768 x 1024: 473 us, 487 with four)
     static_assert(TL >= kSpan && kSpan % U == 0, "a lane a place, whole batches");
     const int w = blockIdx.y;
     int span = (int)(task / a.slices), slice = (int)(task - (int64_t)span * a.slices);
@@ -407,7 +409,7 @@ template <class T, int E, int TL, bool ALIGNED>
 __global__ __launch_bounds__(kThreads) void grad_runs_kernel(GradArgs a)
 {
     __shared__ uint32_t present[(kZeroRows + 31) / 32];
-    if ((int)blockIdx.x < a.run_blocks) sum_runs<T, E, TL, ALIGNED>(a, (int64_t)blockIdx.x * (kThreads / TL) + threadIdx.x / TL);
+    if ((int)blockIdx.x < a.run_blocks) sum_runs<T, E, TL>(a, (int64_t)blockIdx.x * (kThreads / TL) + threadIdx.x / TL);
     else zero_rows<ALIGNED>(a, (int64_t)((int)blockIdx.x - a.run_blocks) * a.zero_rows, present);
 }
 
@@ -720,9 +722,10 @@ void launch_lookup(int W, int T, int V, int D, const void* table, int64_t ld_tab
                    void* out, int64_t ld_out, hipStream_t s)
 {
     TO* to = static_cast<TO*>(out);
-    const int64_t pieces = (int64_t)T * ((D - 1) / 8 + 1);
+    constexpr int E = kLookupPiece<TI, TO>;
+    const int64_t pieces = (int64_t)T * ((D - 1) / E + 1);
     const dim3 grid((unsigned)((pieces - 1) / (kThreads * kLookupEach) + 1), (unsigned)W);
-    const bool aligned = D % 8 == 0 && on(to, 16) && (W == 1 || ld_out % 8 == 0);
+    const bool aligned = D % E == 0 && on(to, 16) && (W == 1 || ld_out % E == 0);
     auto go = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, s, static_cast<const TI*>(table), ld_table, V, D, tokens, ld_tokens, T, scale, to, ld_out);
     };
