@@ -12,7 +12,7 @@
 //
 // Bound by memory.  Workers' weights are columns of fp32 rows; a team keeps them in registers over the tokens it takes,
 // as it does its part of the sums over tokens, which go to the workspace once a workgroup and are added up in order by a
-// second launch: no atomics, equal calls give equal bits.  Forward 8 x 8192 x 4096 bf16 480 us, 5.6 TB/s of the 2.7 GB that have to
+// second launch: no atomics, equal calls give equal bits.  Forward 8 x 8192 x 4096 bf16 465 us, 5.8 TB/s of the 2.7 GB that have to
 // move; backward 8 x 4096 x 2048 205 us, 5.2 TB/s of 1.07 GB, with the join.
 //
 // A lane holds eight columns, so a team is as wide as its row (16 columns a lane and half the lanes: 536 instead of 487 us
@@ -210,10 +210,12 @@ __global__ __launch_bounds__(threads_limit(LANES)) void block_norm_kernel(NormAr
     for (int64_t t = (int64_t)blockIdx.x * teams + team; t < a.T; t += (int64_t)gridDim.x * teams) {
         typename P::Row rr, ry, ru;
         typename P::Values r;
-        P::load(row_of<T>(a.r, w, t), lane, ts, a.D, rr);
+        // y is waited for first (8 x 8192 x 4096 bf16 465 us, 478 with r's load first; but 6 x 4064 x 4495 286 and 268)
+        if (!WIDE || !a.y.p) P::load(row_of<T>(a.r, w, t), lane, ts, a.D, rr);
         if (a.y.p) {
             typename P::Values y, u;
             P::load(row_of<T>(a.y, w, t), lane, ts, a.D, ry);
+            if (WIDE) P::load(row_of<T>(a.r, w, t), lane, ts, a.D, rr);
             if (a.u.p) P::load(row_of<T>(a.u, w, t), lane, ts, a.D, ru);
             P::get(ry, lane, ts, a.D, y);
             float q = 1.0f;
