@@ -330,3 +330,32 @@ def test_refusals():
     with pytest.raises(L.LsgdError, match="NOMEM"):
         L.block_norm_grad(r, r, r, q, dw_pre=torch.zeros((2, 16), device=DEV), workspace=torch.zeros(16, dtype=torch.uint8, device=DEV))
     torch.cuda.synchronize()
+
+
+def in_gaps(W, T, D, gap, seed, dtype):
+    """[W, T, D] whose rows stand `gap` elements apart, and the buffer."""
+    buf = rnd(W, T, D + gap, seed=seed, dtype=dtype)
+    return buf, buf[:, :, :D]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("W,T,D,gap", [(2, 19, 5, 2), (2, 19, 203, 1), (2, 19, 515, 3), (2, 19, 1003, 0), (2, 5, 4495, 1), (1, 5, 8195, 2), (1, 5, 16381, 3),
+                                       (2, 19, 516, 0), (2, 19, 1004, 4)])
+def test_odd_rows_in_place(dtype, W, T, D, gap):
+    """Rows that end inside a piece, their last piece shared with the lane before; results in the inputs' place."""
+    (rb, r), (yb, y), (ub, u) = (in_gaps(W, T, D, gap, seed, dtype) for seed in (1, 2, 3))
+    gaps = [t[:, :, D:].clone() for t in (rb, yb, ub)]
+    wp, wn = weights(W, D, 4, lead=1)
+    unit = UNIT[dtype]
+    R, N, qp, qn, br, bn = reference(r, y, u, wp, wn, True)
+    y0, u0 = y.clone(), u.clone()
+    _, _, stats = L.block_norm(r, y, gate=u, w_post=wp, w_pre=wn, scale=SCALE, eps=NORM_EPS, r_out=r, n=y)
+    assert bool(((d(r) - R).abs() <= br + unit * R.abs() * 1.01).all())
+    assert bool(((d(y) - N).abs() <= bn + unit * N.abs() * 1.01).all())
+    y.copy_(y0)
+    (nb, dn), (db, dR) = (in_gaps(W, T, D, gap, seed, dtype) for seed in (5, 6))
+    out, bound = reference_grad(dn, dR, r, y, u, wp, wn, stats, True)
+    dwp, dwn = torch.empty((W, D), device=DEV), torch.empty((W, D), device=DEV)
+    L.block_norm_grad(dn, dR, r, stats, y, gate=u, w_post=wp, w_pre=wn, scale=SCALE, dw_post=dwp, dw_pre=dwn, dr=dR, dy=y, dgate=u)
+    check({"dr": dR, "dy": y, "dgate": u, "dw_post": dwp, "dw_pre": dwn}, out, bound, dtype)
+    assert all(torch.equal(t[:, :, D:], g) for t, g in zip((rb, yb, ub), gaps))

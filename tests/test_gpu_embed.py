@@ -224,3 +224,37 @@ def test_refusals():
     with pytest.raises(L.LsgdError, match="NOMEM"):
         L.embed_grad(f(2, 4, 8), tok, f(2, 5, 8), workspace=torch.zeros(64, dtype=torch.uint8, device=DEV))
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("W,T,V,D", [(2, 9001, 301, 5), (2, 9001, 301, 77), (1, 9001, 301, 515), (1, 9001, 97, 1023), (1, 3001, 97, 515), (2, 301, 97, 1021)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_grad_of_odd_rows(W, T, V, D, dtype, accumulate):
+    """Rows that end inside a piece, their last piece shared with the lane before."""
+    rows, dtable = table_in_rows(W, V, D, 1, seed=2)
+    before = dtable.cpu().double() if accumulate else None
+    tok = draw_tokens(W, T, V, seed=T + D)
+    dout = torch.randn((W, T, D), generator=torch.Generator().manual_seed(8)).to(dtype).to(DEV)
+    ref, mag, n = reference_grad(dout, tok, V, 1.25, before)
+    L.embed_grad(dout, tok, dtable, scale=1.25, accumulate=accumulate)
+    assert bool(((dtable.cpu().double() - ref).abs() <= mag * (n + 3) * EPS).all())
+    rows = rows.cpu()
+    assert bool((rows[:, :1] == CANARY).all()) and bool((rows[:, 1 + V * D:] == CANARY).all())
+
+
+@pytest.mark.parametrize("D", [4, 5, 515, 516, 1023])
+@pytest.mark.parametrize("src", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("dst", [torch.float32, torch.bfloat16])
+def test_lookup_of_odd_rows(D, src, dst):
+    W, T, V = 2, 203, 61
+    _, table = table_in_rows(W, V, D, 1, src, seed=4)
+    tok = draw_tokens(W, T, V, seed=D)
+    want = torch.zeros((W, T, D))
+    for w in range(W):
+        t = tok[w].cpu().long()
+        ok = (t >= 0) & (t < V)
+        want[w, ok] = table[w].cpu().float()[t[ok]] * 1.5
+    buf = torch.full((W, T * D + 3), CANARY, dtype=dst, device=DEV)
+    out = buf[:, :T * D].unflatten(1, (T, D))
+    L.embed_lookup(table, tok, scale=1.5, dtype=dst, out=out)
+    assert torch.equal(out.cpu(), want.to(dst)) and bool((buf[:, T * D:] == CANARY).all())
