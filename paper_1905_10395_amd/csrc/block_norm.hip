@@ -60,8 +60,8 @@ struct NormGradArgs {
 
 // A lane's columns of a row: pieces of 16 bytes, adjacent lanes' adjacent, so that an access of a wavefront covers whole lines
 // (of fp32, 32 bytes a lane took 272 instead of 220 us forward at 8 x 4096 x 2048).  WIDE: all pieces whole and 16-byte aligned; these are
-// read once and written once, and streaming accesses in both directions took 548 us where plain ones took 572 (8 x 8192 x 4096
-// bf16), either direction alone 557.  Elements past the row's end read zero and are not written.  SHORT: rows may be shorter than
+// read once and written once, and streaming accesses in both directions took 478 us where plain ones took 518 (8 x 8192 x 4096
+// bf16).  Elements past the row's end read zero and are not written.  SHORT: rows may be shorter than
 // a piece.
 template <class T, int N, bool WIDE, bool SHORT>
 struct Piece {
