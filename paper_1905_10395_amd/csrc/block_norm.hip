@@ -186,7 +186,16 @@ __device__ __forceinline__ float team_sum(float a, TeamSum& s)
     return a;
 }
 
+// The gate, to 2 |u| + 5 roundings: the quick exponential takes a rounded multiple of u, the quick reciprocal is one last bit off.
 __device__ __forceinline__ float sigmoid(float u) { return __builtin_amdgcn_rcpf(1.0f + __expf(-u)); }
+// The same value, and 1 - a as exp(-u) a: the difference itself would keep only a's absolute error, and nothing from u = 17 on.
+// Where the exponential overflows a is zero, and so is the product of the two.
+__device__ __forceinline__ float sigmoid(float u, float& rest)
+{
+    const float t = __expf(-u), a = __builtin_amdgcn_rcpf(1.0f + t);
+    rest = fminf(t, 0x1.fffffep127f) * a;
+    return a;
+}
 
 template <class T>
 __device__ __forceinline__ T* row_of(const Rows& a, int w, int64_t t) { return static_cast<T*>(a.p) + w * a.lw + t * a.lt; }
@@ -358,8 +367,9 @@ __global__ __launch_bounds__(threads_limit(LANES), sizeof(T) == 2 || WIDE ? 4 : 
                         z[n][k] *= q;
                         float d = a.scale * dr[n][k];                   // e of the formula, gate still missing
                         if (a.u.p) {
-                            const float g = sigmoid(u[n][k]);
-                            u[n][k] = d * z[n][k] * wp[n][k] * (g * (1.0f - g));
+                            float rest;
+                            const float g = sigmoid(u[n][k], rest);
+                            u[n][k] = d * z[n][k] * wp[n][k] * (g * rest);
                             d *= g;
                         }
                         dw[k - e] += d * z[n][k];

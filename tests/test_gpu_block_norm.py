@@ -359,3 +359,21 @@ def test_odd_rows_in_place(dtype, W, T, D, gap):
     L.block_norm_grad(dn, dR, r, stats, y, gate=u, w_post=wp, w_pre=wn, scale=SCALE, dw_post=dwp, dw_pre=dwn, dr=dR, dy=y, dgate=u)
     check({"dr": dR, "dy": y, "dgate": u, "dw_post": dwp, "dw_pre": dwn}, out, bound, dtype)
     assert all(torch.equal(t[:, :, D:], g) for t, g in zip((rb, yb, ub), gaps))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("D", [8, 13])
+def test_gate_gradient_far_out(dtype, D):
+    """a(1-a) of gates that are nearly shut or open keeps its relative accuracy on both sides."""
+    inf = float("inf")
+    far = torch.tensor([-inf, -200.0, -80.0, -20.0, -16.0, -12.0, -8.0, -1.0, 0.0, 1.0, 8.0, 12.0, 16.0, 20.0, 80.0, 200.0, inf], dtype=dtype, device=DEV)
+    T = len(far)
+    u = far.view(1, T, 1).expand(2, T, D).contiguous()
+    y, dR = rnd(2, T, D, seed=1, dtype=dtype), rnd(2, T, D, seed=2, dtype=dtype)
+    wp, _ = weights(2, D, 3)
+    _, _, du = L.block_norm_grad(None, dR, y, torch.ones((2, 2, T), device=DEV), y, gate=u, w_post=wp, scale=SCALE, post_norm=False)
+    a = torch.sigmoid(d(u)) * torch.sigmoid(-d(u))
+    ref = SCALE * d(dR) * d(y) * d(wp)[:, None] * a
+    # exp(-u): 2 |u| + 2 roundings; a: 3 more; 1 - a = exp(-u) a and the product with a: 6 |u| + 14 in all, and 4 of the other factors
+    rel = (6 * d(u).abs().clamp(max=200.0) + 20) * EPS + UNIT[dtype] * 1.01
+    assert bool(((d(du) - ref).abs() <= ref.abs() * rel + 1e-37).all())
