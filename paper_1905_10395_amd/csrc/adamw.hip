@@ -442,9 +442,9 @@ lsgd_status check_tensors(const lsgd_adamw_tensor* t, int32_t count, int32_t bit
             if (a.m_values && a.rows > 1 && a.ld_values < a.n) return set_error(LSGD_ERR_SHAPE, "adamw: tensor %d: ld_values is smaller than n", k);
         }
         const int64_t per = (a.n - 1) / kChunk + 1;
-        if (per > (int64_t)0x7fffffff / a.rows) return set_error(LSGD_ERR_SHAPE, "adamw: tensor %d is too large for one launch", k);
+        if (per > (int64_t)0x7fffffff / a.rows) return set_error(LSGD_ERR_SHAPE, "adamw: tensor %d is too large for one call", k);
         total += per * a.rows;
-        if (total > 0x7fffffff) return set_error(LSGD_ERR_SHAPE, "adamw: the tensors are too large for one launch");
+        if (total > 0x7fffffff) return set_error(LSGD_ERR_SHAPE, "adamw: the tensors are too large for one call");
     }
     *works = total;
     return LSGD_OK;
@@ -465,6 +465,19 @@ struct lsgd_adamw {
     bool values;             // some tensor has room for its moments' values
     hipStream_t stream;
 };
+
+namespace {
+
+// All of a handle's workgroups: one launch, but that a launch has fewer than 2^32 threads (8.6 G parameters with 32-bit moments).
+template <class... A, class... B>
+void launch_all(const lsgd_adamw& h, int threads, void (*kernel)(const Tensor*, const Work*, A...), B... args)
+{
+    const int64_t most = 0xFFFFFFFFll / threads;
+    for (int64_t first = 0; first < h.n_works; first += most)
+        hipLaunchKernelGGL(kernel, dim3((unsigned)std::min(most, h.n_works - first)), dim3((unsigned)threads), 0, h.stream, h.tensors, h.works + first, args...);
+}
+
+} // namespace
 
 extern "C" {
 
@@ -576,14 +589,9 @@ lsgd_status lsgd_adamw_step(lsgd_adamw* opt, double lr, double beta1, double bet
     auto inside = [](double u) { return (float)std::min(std::max(u, 0x1p-12), 1.0 - 0x1p-12); };
     p.uv = inside(std::fmod((double)step * kGolden, 1.0));
     p.um = inside(std::fmod((double)step * kGolden + 0.5, 1.0));
-    const dim3 grid((unsigned)opt->n_works), block(opt->bits == 32 ? kThreads32 : kThreads);
-    if (opt->bits == 32) {
-        if (opt->g_is_bf16) hipLaunchKernelGGL((adamw32_kernel<uint16_t>), grid, block, 0, opt->stream, opt->tensors, opt->works, p);
-        else hipLaunchKernelGGL((adamw32_kernel<float>), grid, block, 0, opt->stream, opt->tensors, opt->works, p);
-    } else {
-        if (opt->g_is_bf16) hipLaunchKernelGGL((adamw8_kernel<uint16_t>), grid, block, 0, opt->stream, opt->tensors, opt->works, p);
-        else hipLaunchKernelGGL((adamw8_kernel<float>), grid, block, 0, opt->stream, opt->tensors, opt->works, p);
-    }
+    auto go = [&](auto kernel, int threads) { launch_all(*opt, threads, kernel, p); };
+    if (opt->bits == 32) opt->g_is_bf16 ? go(adamw32_kernel<uint16_t>, kThreads32) : go(adamw32_kernel<float>, kThreads32);
+    else opt->g_is_bf16 ? go(adamw8_kernel<uint16_t>, kThreads) : go(adamw8_kernel<float>, kThreads);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return set_error(LSGD_ERR_HIP, "adamw: %s", hipGetErrorString(e));
     return LSGD_OK;
@@ -594,7 +602,7 @@ lsgd_status lsgd_adamw_moments(lsgd_adamw* opt)
     if (!opt) return set_error(LSGD_ERR_INVALID_ARG, "adamw: handle is NULL");
     if (opt->bits != 8) return set_error(LSGD_ERR_STATE, "adamw: 32-bit moments are their own values");
     if (!opt->values) return set_error(LSGD_ERR_STATE, "adamw: no tensor was given m_values and v_values");
-    hipLaunchKernelGGL(adamw8_values_kernel, dim3((unsigned)opt->n_works), dim3(kThreads), 0, opt->stream, opt->tensors, opt->works);
+    launch_all(*opt, kThreads, adamw8_values_kernel);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return set_error(LSGD_ERR_HIP, "adamw: moments: %s", hipGetErrorString(e));
     return LSGD_OK;

@@ -347,3 +347,26 @@ def test_refusals():
     with pytest.raises(L.LsgdError, match="STATE"):
         opt.moments()
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_more_workgroups_than_a_launch_has(bits):
+    """A workgroup a row: of 512 threads (32 bits) 2^23 - 1 make a launch, of 256 (8 bits) 2^24 - 1."""
+    rows = (1 << (23 if bits == 32 else 24)) + 5
+    f = lambda dtype=torch.float32: torch.zeros((rows, 1), dtype=dtype, device=DEV)
+    x, g = f(), f().normal_(generator=torch.Generator(device=DEV).manual_seed(1))
+    if bits == 32:
+        t = L.AdamWTensor(x, g, f(), f())
+    else:
+        t = L.AdamWTensor(x, g, f(torch.int8), f(torch.uint8), m_scale=f(), v_scale=f(), m_values=f(), v_values=f())
+    opt = L.AdamW([t], bits=bits)
+    opt.step(0.25, 1, beta1=0.5, beta2=0.75)
+    ref, g = -0.25 * g.double() / (g.double().abs() + 1e-8), g.double()
+    # the first step from nothing: a dozen roundings, and of an element alone in its block the moments' code is the largest
+    assert bool(((x.double() - ref).abs() <= 16 * EPS * ref.abs()).all())
+    if bits == 8:
+        opt.moments()
+        # g of at least 2^-40, as all drawn but zeros are, or the block is held as zeros
+        ok = g.abs() > 2.0 ** -40
+        within = lambda got, want: bool(((got.double() - want).abs() <= 16 * EPS * want)[ok].all())
+        assert within(t.t["m_values"].abs(), 0.5 * g.abs()) and within(t.t["v_values"], 0.25 * g * g)
