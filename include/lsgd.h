@@ -361,7 +361,7 @@ lsgd_status lsgd_stream_probe(int32_t kind, float* a, float* b, float* c, int64_
  *   table  device, worker w's [V, D] at table + w*ld_table (fp32 or bf16; ld_table = 0: one table for all workers)
  *   tokens device int32, worker w's [T] at tokens + w*ld_tokens (0: the same for all workers)
  *   out    device, worker w's [T, D] at out + w*ld_out (fp32 or bf16); must not overlap the inputs
- * T = 0 is allowed.  T <= 2^24, V < 2^30, D <= 2^20.                                                   */
+ * T = 0 is allowed.  T <= 2^24, V < 2^30, D <= 2^20, and T * ceil(D/8) below 2^34 (T * ceil(D/4) from fp32 to fp32). */
 lsgd_status lsgd_embed_lookup(int32_t W, int32_t T, int32_t V, int32_t D, const void* table, int64_t ld_table, int32_t table_is_bf16,
                               const int32_t* tokens, int64_t ld_tokens, float scale, void* out, int64_t ld_out, int32_t out_is_bf16,
                               void* hip_stream);

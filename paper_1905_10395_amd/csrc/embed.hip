@@ -404,12 +404,14 @@ __device__ __forceinline__ void zero_rows(const GradArgs& a, int64_t v0, uint32_
     }
 }
 
-constexpr int kZeroRows = 64;
+// Rows to a workgroup; of tables from 2^28 rows on more, so that their workgroups fit one launch.
+constexpr int kZeroRows = 64, kMoreZeroRows = 1024;
+constexpr int kManyRows = 1 << 28;
 
 template <class T, int E, int TL, bool ALIGNED>
 __global__ __launch_bounds__(kThreads) void grad_runs_kernel(GradArgs a)
 {
-    __shared__ uint32_t present[(kZeroRows + 31) / 32];
+    __shared__ uint32_t present[kMoreZeroRows / 32];
     if ((int)blockIdx.x < a.run_blocks) sum_runs<T, E, TL>(a, (int64_t)blockIdx.x * (kThreads / TL) + threadIdx.x / TL);
     else zero_rows<ALIGNED>(a, (int64_t)((int)blockIdx.x - a.run_blocks) * a.zero_rows, present);
 }
@@ -721,6 +723,25 @@ Plan make_plan(int W, int T, int V, int D)
     return p;
 }
 
+constexpr int64_t kLaunchThreads = 1ll << 32;                          // a launch has fewer
+
+// Workgroups that sum runs, of teams of `lanes`, and that write zeros.
+struct RunPlan {
+    int lanes, slices, zero_rows;
+    int64_t run_blocks, zero_blocks;
+};
+RunPlan run_plan(const Plan& p, int V, int D, int elements, int accumulate)
+{
+    RunPlan r;
+    const int lanes = (D - 1) / elements + 1;
+    r.lanes = lanes <= 16 ? 16 : lanes <= 32 ? 32 : 64;
+    r.slices = (D - 1) / (r.lanes * elements) + 1;
+    r.zero_rows = V < kManyRows ? kZeroRows : kMoreZeroRows;
+    r.run_blocks = ((int64_t)p.spans * r.slices - 1) / (kThreads / r.lanes) + 1;
+    r.zero_blocks = accumulate ? 0 : (V - 1) / r.zero_rows + 1;
+    return r;
+}
+
 template <class TI, class TO>
 void launch_lookup(int W, int T, int V, int D, const void* table, int64_t ld_table, const int32_t* tokens, int64_t ld_tokens, float scale,
                    void* out, int64_t ld_out, hipStream_t s)
@@ -738,16 +759,17 @@ void launch_lookup(int W, int T, int V, int D, const void* table, int64_t ld_tab
 }
 
 template <class T, int E, int TL, bool ALIGNED>
-void launch_grad(GradArgs a, int W, hipStream_t s)
+hipError_t launch_grad(GradArgs a, int W, const RunPlan& p, hipStream_t s)
 {
-    a.slices = (a.D - 1) / (TL * E) + 1;
-    const int teams = kThreads / TL;
-    a.run_blocks = (int)(((int64_t)a.spans * a.slices - 1) / teams + 1);
-    a.zero_rows = kZeroRows;
-    const int zero_blocks = a.accumulate ? 0 : (a.V - 1) / kZeroRows + 1;
-    hipLaunchKernelGGL((grad_runs_kernel<T, E, TL, ALIGNED>), dim3((unsigned)(a.run_blocks + zero_blocks), (unsigned)W), dim3(kThreads), 0, s, a);
+    a.slices = p.slices;
+    a.run_blocks = (int)p.run_blocks;
+    a.zero_rows = p.zero_rows;
+    hipLaunchKernelGGL((grad_runs_kernel<T, E, TL, ALIGNED>), dim3((unsigned)(p.run_blocks + p.zero_blocks), (unsigned)W), dim3(kThreads), 0, s, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;                                     // there are no partial sums to join
     hipLaunchKernelGGL(grad_join_kernel, dim3((unsigned)((a.spans - 1) / kJoinSpans + 1), (unsigned)W, (unsigned)((a.D - 1) / kJoinCols + 1)),
                        dim3(kThreads), 0, s, a);
+    return hipGetLastError();
 }
 
 // A workgroup a compute unit (each sorts the list again; with two 517 tokens take 12.1 us instead of 8.4, 2048 23.4 instead of
@@ -777,18 +799,16 @@ void launch_grad_small(const GradArgs& a, int W, SmallArgs q, hipStream_t s)
 }
 
 template <class T, int E>
-void launch_grad_team(const GradArgs& a, int W, bool aligned, hipStream_t s)
+hipError_t launch_grad_team(const GradArgs& a, int W, const RunPlan& p, bool aligned, hipStream_t s)
 {
-    const int lanes = (a.D - 1) / E + 1;
     if (aligned) {
-        if (lanes <= 16) launch_grad<T, E, 16, true>(a, W, s);
-        else if (lanes <= 32) launch_grad<T, E, 32, true>(a, W, s);
-        else launch_grad<T, E, 64, true>(a, W, s);
-    } else {
-        if (lanes <= 16) launch_grad<T, E, 16, false>(a, W, s);
-        else if (lanes <= 32) launch_grad<T, E, 32, false>(a, W, s);
-        else launch_grad<T, E, 64, false>(a, W, s);
+        if (p.lanes == 16) return launch_grad<T, E, 16, true>(a, W, p, s);
+        if (p.lanes == 32) return launch_grad<T, E, 32, true>(a, W, p, s);
+        return launch_grad<T, E, 64, true>(a, W, p, s);
     }
+    if (p.lanes == 16) return launch_grad<T, E, 16, false>(a, W, p, s);
+    if (p.lanes == 32) return launch_grad<T, E, 32, false>(a, W, p, s);
+    return launch_grad<T, E, 64, false>(a, W, p, s);
 }
 
 } // namespace
@@ -810,8 +830,9 @@ lsgd_status lsgd_embed_lookup(int32_t W, int32_t T, int32_t V, int32_t D, const 
     if (W > 1 && (ld_table < 0 || (ld_tokens < T && ld_tokens != 0) || ld_out < (int64_t)T * D))
         return set_error(LSGD_ERR_SHAPE, "embed_lookup: a worker stride is smaller than what a worker has (ld_tokens=%lld, ld_out=%lld)",
                          (long long)ld_tokens, (long long)ld_out);
-    const int64_t pieces = (int64_t)T * D;
-    if (pieces / (kThreads * kLookupEach) >= 0x7fffffff) return set_error(LSGD_ERR_SHAPE, "embed_lookup: T*D=%lld is too large for one launch", (long long)pieces);
+    const int64_t pieces = (int64_t)T * ((D - 1) / (table_is_bf16 | out_is_bf16 ? kLookupPiece<uint16_t, uint16_t> : kLookupPiece<float, float>) + 1);
+    if (((pieces - 1) / (kThreads * kLookupEach) + 1) * kThreads >= kLaunchThreads)
+        return set_error(LSGD_ERR_SHAPE, "embed_lookup: T=%d of D=%d is too large for one launch", (int)T, (int)D);
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     if (table_is_bf16) {
         if (out_is_bf16) launch_lookup<uint16_t, uint16_t>(W, T, V, D, table, ld_table, tokens, ld_tokens, scale, out, ld_out, s);
@@ -863,8 +884,6 @@ lsgd_status lsgd_embed_grad(int32_t W, int32_t T, int32_t V, int32_t D, const vo
     if (!workspace && T > kSmallTokens) return set_error(LSGD_ERR_INVALID_ARG, "embed_grad: workspace is NULL");
     if (!on(workspace, kAlign)) return set_error(LSGD_ERR_INVALID_ARG, "embed_grad: workspace must be 256-byte aligned");
     if (workspace && workspace_bytes < p.total) return set_error(LSGD_ERR_NOMEM, "embed_grad: workspace of %zu bytes < %zu needed", workspace_bytes, p.total);
-    if ((int64_t)p.spans * ((D - 1) / 64 + 1) + V / kZeroRows >= 0x7fffffff)
-        return set_error(LSGD_ERR_SHAPE, "embed_grad: T=%d of D=%d is too large for one launch", (int)T, (int)D);
 
     GradArgs a{};
     a.dout = dout; a.ld_dout = ld_dout;
@@ -882,6 +901,9 @@ lsgd_status lsgd_embed_grad(int32_t W, int32_t T, int32_t V, int32_t D, const vo
         if (e != hipSuccess) return set_error(LSGD_ERR_HIP, "embed_grad: %s", hipGetErrorString(e));
         return LSGD_OK;
     }
+    const RunPlan runs = run_plan(p, V, D, dout_is_bf16 ? 8 : 4, accumulate);
+    if ((runs.run_blocks + runs.zero_blocks) * kThreads >= kLaunchThreads)
+        return set_error(LSGD_ERR_SHAPE, "embed_grad: T=%d of D=%d is too large for one launch", (int)T, (int)D);
     char* base = static_cast<char*>(workspace);
     uint32_t* keys[2] = {reinterpret_cast<uint32_t*>(base + p.keys[0]), reinterpret_cast<uint32_t*>(base + p.keys[1])};
     int32_t* pos[2] = {reinterpret_cast<int32_t*>(base + p.pos[0]), reinterpret_cast<int32_t*>(base + p.pos[1])};
@@ -902,9 +924,9 @@ lsgd_status lsgd_embed_grad(int32_t W, int32_t T, int32_t V, int32_t D, const vo
     a.keys = keys[at]; a.pos = pos[at];
     a.parts = reinterpret_cast<float*>(base + p.parts);
     a.Dp = p.Dp; a.spans = p.spans;
-    if (dout_is_bf16) launch_grad_team<uint16_t, 8>(a, W, aligned, s);
-    else launch_grad_team<float, 4>(a, W, aligned, s);
     e = hipGetLastError();
+    if (e == hipSuccess)
+        e = dout_is_bf16 ? launch_grad_team<uint16_t, 8>(a, W, runs, aligned, s) : launch_grad_team<float, 4>(a, W, runs, aligned, s);
     if (e != hipSuccess) return set_error(LSGD_ERR_HIP, "embed_grad: %s", hipGetErrorString(e));
     return LSGD_OK;
 }

@@ -209,3 +209,19 @@ def test_in_a_captured_graph(T):
         torch.cuda.synchronize()
         for a, b in zip(want, [*held, dtable, dw]):
             assert torch.equal(a, b)
+
+
+def test_embedding_gradient_of_the_most_rows():
+    V, T = (1 << 30) - 1, 9001
+    tok, dout = draw_tokens(1, T, V, seed=5), rnd(1, T, 1, seed=6)
+    tok[0, 7], tok[0, 8] = V - 1, V                                    # the last row, and one past it: padding
+    dtable = torch.full((1, V, 1), 7.0, device=DEV)
+    L.embed_grad(dout, tok, dtable)
+    ok = (tok[0] >= 0) & (tok[0] < V)
+    rows, at = tok[0, ok].long().unique(return_inverse=True)
+    f = lambda: torch.zeros(len(rows), dtype=torch.float64, device=DEV)
+    d = dout[0, ok, 0].double()
+    ref, mag, n = f().index_add_(0, at, d), f().index_add_(0, at, d.abs()), f().index_add_(0, at, torch.ones_like(d))
+    within(dtable[0, rows, 0], ref, mag * (n + 3) * EPS)
+    dtable[0, rows] = 0.0
+    assert int(dtable.count_nonzero()) == 0

@@ -103,3 +103,12 @@ def test_tensors_on_the_cpu_are_refused():
                  lambda: L.block_norm_grad(t, None, t, torch.zeros((2, 2, 5))), lambda: L.AdamW([L.AdamWTensor(t, t, t, t)])):
         with pytest.raises(ValueError, match="not on a GPU"):
             call()
+
+
+def test_embed_launches_are_of_fewer_than_2_to_the_32_threads():
+    f, g, p = b.lib().lsgd_embed_lookup, b.lib().lsgd_embed_grad, 4096          # never followed
+    T = 1 << 24
+    for D, table, out in ((1 << 12, 0, 0), (1 << 13, 1, 1), (1 << 13, 0, 1), (1 << 16, 1, 0)):
+        assert f(1, T, 5, D, p, 5 * D, table, p, T, 1.0, p, T * D, out, None) == SHAPE and "too large" in error()
+    for D, bf16 in ((1 << 14, 0), (1 << 15, 1)):                                # 2^20 spans of 64 teams of 64 lanes
+        assert g(1, T, 5, D, p, T * D, bf16, p, T, 1.0, 0, p, 5 * D, p, 1 << 60, None) == SHAPE and "too large" in error()
