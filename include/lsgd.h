@@ -453,10 +453,13 @@ typedef struct lsgd_adamw lsgd_adamw; /* opaque host object */
 /* Bytes of the tables a handle keeps in its workspace; 0 on invalid arguments. */
 size_t lsgd_adamw_workspace_bytes(const lsgd_adamw_tensor* tensors, int32_t n_tensors, int32_t state_bits, int32_t g_is_bf16);
 /* Binds caller-owned buffers into a handle; workspace is device memory, 256-byte aligned, owned by the caller for the
- * life of the handle.  Copies the tables there and synchronises the stream, which all later calls use.            */
+ * life of the handle.  Copies the tables there and synchronises the stream, which later calls use until
+ * lsgd_adamw_set_stream names another.                                                                            */
 lsgd_status lsgd_adamw_create(const lsgd_adamw_tensor* tensors, int32_t n_tensors, int32_t state_bits, int32_t g_is_bf16, void* workspace,
                               size_t workspace_bytes, void* hip_stream, lsgd_adamw** out);
 lsgd_status lsgd_adamw_destroy(lsgd_adamw* opt); /* frees the host object only */
+/* Later calls run on this stream; the caller orders it behind what earlier ones left on another. */
+lsgd_status lsgd_adamw_set_stream(lsgd_adamw* opt, void* hip_stream);
 /* step counts from 1; grad_scale is the c above.  All are values of this call: a captured call repeats them. */
 lsgd_status lsgd_adamw_step(lsgd_adamw* opt, double lr, double beta1, double beta2, double eps, int64_t step, double grad_scale);
 /* 8 bits: writes what the stored codes stand for to m_values and v_values of the tensors that have them. */

@@ -125,6 +125,7 @@ def lib():
         L.lsgd_adamw_create.argtypes = [C.POINTER(_AdamWTensor), C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p,
                                         C.POINTER(C.c_void_p)]
         L.lsgd_adamw_destroy.argtypes = [C.c_void_p]
+        L.lsgd_adamw_set_stream.argtypes = [C.c_void_p, C.c_void_p]
         L.lsgd_adamw_step.argtypes = [C.c_void_p, C.c_double, C.c_double, C.c_double, C.c_double, C.c_int64, C.c_double]
         L.lsgd_adamw_moments.argtypes = [C.c_void_p]
         _lib = L
@@ -597,7 +598,8 @@ class AdamWTensor:
 
 
 class AdamW:
-    """lsgd_adamw_create over a list of AdamWTensor; bits: 32 or 8, how the moments are held.  Keeps the tensors alive."""
+    """lsgd_adamw_create over a list of AdamWTensor; bits: 32 or 8, how the moments are held.  Keeps the tensors alive.
+    Calls run on `stream`, or where none is given on the stream that is current at each call, as the other operators do."""
 
     def __init__(self, tensors, bits=32, stream=None, workspace=None):
         self._h = None
@@ -608,7 +610,10 @@ class AdamW:
         g_dtype = self.tensors[0].t["g"].dtype
         _need(g_dtype in _FLOATS, "AdamW: g must be float32 or bfloat16")
         arr = (_AdamWTensor * len(self.tensors))(*[a._c(k, bits, g_dtype) for k, a in enumerate(self.tensors)])
+        self._follows = stream is None
         self.stream = torch.cuda.current_stream(dev) if stream is None else stream
+        self._raw = self.stream.cuda_stream
+        self._step = lib().lsgd_adamw_step
         bf = int(g_dtype == torch.bfloat16)
         with torch.cuda.device(dev):
             self.workspace, nbytes = _workspace("AdamW", lib().lsgd_adamw_workspace_bytes(arr, len(arr), bits, bf), self.tensors[0].t["x"], workspace, stream)
@@ -628,14 +633,19 @@ class AdamW:
             pass
 
     def step(self, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=1.0):
-        """One step; `step` counts from 1."""
-        self._call(lib().lsgd_adamw_step, lr, beta1, beta2, eps, int(step), grad_scale)
+        """One step; `step` counts from 1.  Captured in a graph, it is replayed with the rates and the step number of its call."""
+        self._call(self._step, lr, beta1, beta2, eps, int(step), grad_scale)
 
     def moments(self):
         """8 bits: fills m_values and v_values of the tensors that have them."""
         self._call(lib().lsgd_adamw_moments)
 
     def _call(self, f, *args):
+        if self._follows and _raw_stream(self._index) != self._raw:
+            self.stream = torch.cuda.current_stream(self._index)
+            self._raw = self.stream.cuda_stream
+            _check(lib().lsgd_adamw_set_stream(self._h, self._raw))
+            self.workspace.record_stream(self.stream)        # its memory is another stream's
         if torch.cuda.current_device() == self._index:
             status = f(self._h, *args)
         else:

@@ -568,6 +568,13 @@ lsgd_status lsgd_adamw_destroy(lsgd_adamw* opt)
     return LSGD_OK;
 }
 
+lsgd_status lsgd_adamw_set_stream(lsgd_adamw* opt, void* hip_stream)
+{
+    if (!opt) return set_error(LSGD_ERR_INVALID_ARG, "adamw: handle is NULL");
+    opt->stream = static_cast<hipStream_t>(hip_stream);
+    return LSGD_OK;
+}
+
 lsgd_status lsgd_adamw_step(lsgd_adamw* opt, double lr, double beta1, double beta2, double eps, int64_t step, double grad_scale)
 {
     if (!opt) return set_error(LSGD_ERR_INVALID_ARG, "adamw: handle is NULL");

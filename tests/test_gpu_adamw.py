@@ -370,3 +370,32 @@ def test_more_workgroups_than_a_launch_has(bits):
         ok = g.abs() > 2.0 ** -40
         within = lambda got, want: bool(((got.double() - want).abs() <= 16 * EPS * want)[ok].all())
         assert within(t.t["m_values"].abs(), 0.5 * g.abs()) and within(t.t["v_values"], 0.25 * g * g)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_steps_run_on_the_current_stream(bits):
+    """A handle made without a stream: a step in a captured graph is the graph's, one under another stream that stream's."""
+    a, b = (Rows(2, [700, 256], bits, seed=8) for _ in range(2))
+    oa, ob = a.optimizer([0.1], [1.0]), b.optimizer([0.1], [1.0])
+    same_state = lambda: all(torch.equal(getattr(a, k), getattr(b, k)) for k in ("x", "m", "v", "ms", "vs"))
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        oa.step(step=5, **HYPER)
+    torch.cuda.synchronize()
+    assert same_state()                                              # captured, not run
+    for _ in range(3):
+        graph.replay()
+        ob.step(step=5, **HYPER)
+        torch.cuda.synchronize()
+        assert same_state()
+    with torch.cuda.stream(s):
+        oa.step(step=6, **HYPER)
+        if bits == 8:
+            oa.moments()
+    s.synchronize()
+    assert oa.stream == s
+    ob.step(step=6, **HYPER)
+    torch.cuda.synchronize()
+    assert same_state()

@@ -112,3 +112,7 @@ def test_embed_launches_are_of_fewer_than_2_to_the_32_threads():
         assert f(1, T, 5, D, p, 5 * D, table, p, T, 1.0, p, T * D, out, None) == SHAPE and "too large" in error()
     for D, bf16 in ((1 << 14, 0), (1 << 15, 1)):                                # 2^20 spans of 64 teams of 64 lanes
         assert g(1, T, 5, D, p, T * D, bf16, p, T, 1.0, 0, p, 5 * D, p, 1 << 60, None) == SHAPE and "too large" in error()
+
+
+def test_adamw_stream_needs_a_handle():
+    assert b.lib().lsgd_adamw_set_stream(None, None) == INVALID and "NULL" in error()
