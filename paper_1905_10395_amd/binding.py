@@ -582,7 +582,9 @@ class AdamWTensor:
             _need(t.dtype == types[name], f"{who}: {name} must be {types[name]}, is {t.dtype}")
             if name in ("m_scale", "v_scale"):
                 nb = -(-n // ADAMW_BLOCK)
-                t = t if t.dim() == 2 else t.reshape(1, -1)
+                if t.dim() != 2:
+                    _need(t.is_contiguous(), f"{who}: {name} must be contiguous or [{rows}, {nb}]")
+                    t = t.view(1, -1)
                 _need(tuple(t.shape) == (rows, nb), f"{who}: {name} must be [{rows}, {nb}]")
             else:
                 _need(t.shape == x.shape, f"{who}: {name} has shape {list(t.shape)}, x has {list(x.shape)}")

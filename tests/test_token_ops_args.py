@@ -116,3 +116,15 @@ def test_embed_launches_are_of_fewer_than_2_to_the_32_threads():
 
 def test_adamw_stream_needs_a_handle():
     assert b.lib().lsgd_adamw_set_stream(None, None) == INVALID and "NULL" in error()
+
+
+def test_adamw_scales_without_a_copy():
+    """Scales of any shape but [rows, blocks] have to lie in memory as one row: a copy's memory would be gone before the first step."""
+    f = lambda *s, dtype=torch.float32: torch.zeros(s, dtype=dtype)
+    x, sm = f(2, 5, 100), f(2, 2)                                     # 1000 elements: 4 blocks
+    make = lambda a, v: L.AdamWTensor(x, x, f(2, 5, 100, dtype=torch.int8), f(2, 5, 100, dtype=torch.uint8), m_scale=a, v_scale=v)._c(0, 8, torch.float32)
+    assert make(f(4), f(4)).ld_scale == 4
+    c = make(sm[None], sm[None])
+    assert c.m_scale == c.v_scale == sm.data_ptr()
+    with pytest.raises(ValueError, match="m_scale must be contiguous"):
+        make(sm.t()[None], sm[None])
