@@ -570,8 +570,6 @@ class AdamWTensor:
         x = self.t["x"]
         types = {"x": torch.float32, "g": g_dtype, "m": torch.float32 if bits == 32 else torch.int8, "v": torch.float32 if bits == 32 else torch.uint8,
                  "m_scale": torch.float32, "v_scale": torch.float32, "m_values": torch.float32, "v_values": torch.float32, "x_bf16": torch.bfloat16}
-        for name in ("x", "g", "m", "v"):
-            _need(self.t[name] is not None, f"{who}: {name} is missing")
         two = x.dim() == 2
         rows, n = (x.shape if two else (1, x.numel()))
         got, ld = {}, {}
@@ -606,7 +604,10 @@ class AdamW:
     def __init__(self, tensors, bits=32, stream=None, workspace=None):
         self._h = None
         self.tensors = list(tensors)
-        _need(len(self.tensors) > 0 and self.tensors[0].t["x"] is not None, "AdamW: no tensors")
+        _need(len(self.tensors) > 0, "AdamW: no tensors")
+        for k, a in enumerate(self.tensors):
+            for name in ("x", "g", "m", "v"):
+                _need(a.t[name] is not None, f"AdamW: tensor {k}: {name} is missing")
         self._index = _gpu("AdamW", self.tensors[0].t["x"], [(f"{name} of tensor {k}", t) for k, a in enumerate(self.tensors) for name, t in a.t.items()])
         dev = self.tensors[0].t["x"].device
         g_dtype = self.tensors[0].t["g"].dtype

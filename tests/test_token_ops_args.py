@@ -128,3 +128,13 @@ def test_adamw_scales_without_a_copy():
     assert c.m_scale == c.v_scale == sm.data_ptr()
     with pytest.raises(ValueError, match="m_scale must be contiguous"):
         make(sm.t()[None], sm[None])
+
+
+def test_adamw_names_what_is_missing(monkeypatch):
+    monkeypatch.setattr(b, "_gpu", lambda who, first, tensors: 0)     # as if the others were on a GPU
+    t = torch.zeros((2, 8))
+    for name in ("x", "g", "m", "v"):
+        with pytest.raises(ValueError, match=f"tensor 0: {name} is missing"):
+            L.AdamW([L.AdamWTensor(**{k: None if k == name else t for k in ("x", "g", "m", "v")})])
+    with pytest.raises(ValueError, match="no tensors"):
+        L.AdamW([])
