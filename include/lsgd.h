@@ -431,6 +431,9 @@ lsgd_status lsgd_block_norm_grad(const lsgd_block_norm_grad_args* args, void* wo
  *   x <- x (1 - lr lr_mult wd) - lr lr_mult/(1-b1^t) * m / (sqrt(v)/sqrt(1-b2^t) + eps)
  * A tensor is a [rows, n] part of matrices (for a population: rows = W, n = the tensor's elements in a worker's row, the
  * strides those of x and g); one row stands for any dense tensor.  Tensors must not overlap.
+ * x_bf16 is what the step leaves: whoever changes x afterwards leaves the copy behind.  With a population over the same x
+ * and x_bf16, its updates and pulls write the copy too under LSGD_WRITE_BF16_SHADOW, else lsgd_sync_shadow brings it up to date
+ * (as it does for the population after a step of tensors without x_bf16).
  * state_bits 32: m, v fp32.  8: m int8 and v uint8 codes with one fp32 scale for every LSGD_ADAMW_BLOCK elements of a
  * row (the last block may be shorter): m = sign(q) q^2 m_scale, v = (q^2 v_scale)^2; all zeros is the state before the
  * first step.  Which of the two codes around a value is stored follows from a threshold that the step number sets, so

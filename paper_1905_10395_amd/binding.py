@@ -559,7 +559,9 @@ class AdamWTensor:
     """One tensor of an AdamW step: float32 x and its gradient g (float32 or bfloat16), both [rows, n] with dense rows (columns of a
     population's x and g, or any dense tensor, which counts as one row).  Moments m, v of the same shape: float32 for 32 bits;
     int8 and uint8 for 8 bits with float32 scales m_scale, v_scale [rows, ceil(n / ADAMW_BLOCK)].  x_bf16: optional bfloat16 copy
-    of x that the step keeps current.  m_values, v_values: optional float32 tensors that AdamW.moments() fills."""
+    of x that the step keeps current (a Population over the same x does so at its updates and pulls if it has x_bf16 and
+    WRITE_BF16_SHADOW; else Population.sync_shadow before the copy is read).  m_values, v_values: optional float32 tensors that
+    AdamW.moments() fills."""
 
     def __init__(self, x, g, m, v, weight_decay=0.0, lr_mult=1.0, x_bf16=None, m_scale=None, v_scale=None, m_values=None, v_values=None):
         self.t = dict(x=x, g=g, m=m, v=v, m_scale=m_scale, v_scale=v_scale, m_values=m_values, v_values=v_values, x_bf16=x_bf16)

@@ -399,3 +399,22 @@ def test_steps_run_on_the_current_stream(bits):
     ob.step(step=6, **HYPER)
     torch.cuda.synchronize()
     assert same_state()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_the_bf16_copy_beside_a_population(bits):
+    """A population over the same x and copy writes the copy at a pull if told to; else it is brought up to date when asked."""
+    W, n = 4, 600
+    for flags in (L.WRITE_BF16_SHADOW, 0):
+        r = Rows(W, [n], bits, shadow=True, seed=3)
+        x, xb, g = (t[:, :n].contiguous() for t in (r.x, r.xb, r.g))
+        r.x, r.xb, r.g = x, xb, g
+        opt = r.optimizer([0.1], [1.0])
+        pop = L.Population(x, g, 2, z_snapshot=torch.zeros((3, n), device=DEV), x_bf16=xb, flags=flags)
+        opt.step(step=1, **HYPER)
+        assert torch.equal(xb, x.bfloat16())
+        pop.select_leaders(torch.arange(W, dtype=torch.float32, device=DEV))
+        pop.leader_pull(0.25, 0.125)
+        assert torch.equal(xb, x.bfloat16()) == bool(flags)
+        pop.sync_shadow()
+        assert torch.equal(xb, x.bfloat16())
