@@ -356,8 +356,8 @@ lsgd_status lsgd_stream_probe(int32_t kind, float* a, float* b, float* c, int64_
  * device pointers and workspace from the caller, allocates nothing on the device and does not synchronise (except
  * lsgd_adamw_create).  Strides count elements.  bf16 data are bit patterns; sums, norms and moments' arithmetic are fp32. */
 
-/* Embedding lookup: out[w,t,:] = scale * table_w[tokens[w,t], :], rounded once; zeros where the token lies outside
- * [0, V) (padding: such a place is never looked up).
+/* Embedding lookup: out[w,t,:] = scale * table_w[tokens[w,t], :], the fp32 product, rounded again to bf16 if out is; zeros
+ * where the token lies outside [0, V) (padding: such a place is never looked up).
  *   table  device, worker w's [V, D] at table + w*ld_table (fp32 or bf16; ld_table = 0: one table for all workers)
  *   tokens device int32, worker w's [T] at tokens + w*ld_tokens (0: the same for all workers)
  *   out    device, worker w's [T, D] at out + w*ld_out (fp32 or bf16); must not overlap the inputs
