@@ -333,7 +333,8 @@ class Population:
 
 
 # ------------------------------------------------------------------------------------------------
-# operators of token models
+# operators of token models: plain functions over memory.  Results carry no autograd graph, whatever the inputs require:
+# embed_grad and block_norm_grad are how gradients come about (in the backward of a torch.autograd.Function, say).
 # ------------------------------------------------------------------------------------------------
 ADAMW_BLOCK = 256
 
@@ -401,7 +402,8 @@ def _worker_stride(who, name, t, rule):
 
 
 def embed_lookup(table, tokens, scale=1.0, dtype=None, out=None, stream=None):
-    """lsgd_embed_lookup: scale * table[w, tokens[w, t]] as [W, T, D]; zeros where a token lies outside [0, V).
+    """lsgd_embed_lookup: scale * table[w, tokens[w, t]] as [W, T, D]; zeros where a token lies outside [0, V).  Not recorded by
+    autograd: embed_grad is its gradient.
     table: float32 or bfloat16 [W, V, D], dense within a worker (columns of x: x[:, a:a + V * D].unflatten(1, (V, D)));
     tokens: int32 [W, T]; dtype: of the result (the table's if None); out: optional result buffer."""
     who = "embed_lookup"
@@ -486,7 +488,8 @@ def _stats(who, stats, W, T, index):
 
 def block_norm(r, y=None, gate=None, w_post=None, w_pre=None, scale=1.0, eps=1e-6, post_norm=True, pre_norm=True, r_out=None, n=None,
                stats=None, stream=None):
-    """lsgd_block_norm: r_out = r + scale * sigmoid(gate) * norm(y) * w_post, n = norm(r_out) * w_pre.
+    """lsgd_block_norm: r_out = r + scale * sigmoid(gate) * norm(y) * w_post, n = norm(r_out) * w_pre.  Not recorded by autograd:
+    block_norm_grad is its gradient.
     r, y, gate: float32 or bfloat16 [W, T, D] with dense rows; w_post, w_pre: float32 [W, D] (columns of x) or None (ones).
     y None: only n = norm(r) * w_pre.  post_norm False: y itself instead of norm(y).  pre_norm False: no n.
     Returns (r_out, n, stats); stats: float32 [2, W, T], what block_norm_grad needs.  r_out, n, stats: optional buffers (r_out
