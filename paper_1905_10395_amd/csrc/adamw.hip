@@ -34,10 +34,10 @@ typedef uint32_t v2u __attribute__((ext_vector_type(2)));
 
 constexpr int kBlock = LSGD_ADAMW_BLOCK;             // elements that share a scale: one wavefront, four each
 static_assert(kBlock == 4 * kWave, "a wavefront holds one block");
-// Elements of one workgroup.  Short pieces in memory order keep what the chip has open in a few DRAM pages: 268 M parameters
-// of 30 bytes in 1.54 ms with 4096 elements a workgroup, 1.46 ms with 2048, 1.39 with 1024.
+// Elements of one workgroup: short pieces in memory order keep what the chip has open in a few DRAM pages (268 M parameters of 30
+// bytes 1.32 ms, with 2048 elements 1.31; before accesses were streaming and lanes short, 1.39 and 1.46, and 1.54 with 4096).
 constexpr int kChunk = 1024;
-constexpr int kThreads32 = kChunk / 2;               // 8-byte lanes: 1.33 ms, against 1.39 with 16-byte ones
+constexpr int kThreads32 = kChunk / 2;               // 8-byte lanes: 1.32 ms, against 1.37 with 16-byte ones
 constexpr int kThreads = kChunk / 4;
 constexpr float kTopM = 127.0f * 127.0f, kTopV = 255.0f * 255.0f;
 
@@ -47,7 +47,7 @@ template <class V>
 using Global = __attribute__((address_space(1))) V;
 
 // Every byte is touched once a step; accesses that do not stay in the caches are the faster ones only if reads and writes
-// both are such (1.50 to 1.52 ms with either alone).
+// both are such (1.32 ms; 1.52 with streaming reads alone, 1.48 with such writes alone).
 template <class V>
 __device__ __forceinline__ V load_once(const V* p) { return __builtin_nontemporal_load((const Global<V>*)p); }
 template <class V>
@@ -136,7 +136,8 @@ __device__ __forceinline__ v4f grad4(const void* g, int64_t i)
 }
 
 // ---- 32-bit moments ----
-// Bound by memory: 268 M parameters with a bf16 copy in 1.33 ms, 6.05 TB/s of 8.1 GB; 5 us a call for a few hundred.
+// Bound by memory: 268 M parameters with a bf16 copy in 1.29 to 1.37 ms, by where their arrays lie, 5.9 to 6.25 TB/s of 8.1 GB; half
+// of them off alignment 1.50.  5 us a call for a few hundred.
 template <class G>
 __global__ __launch_bounds__(kThreads32) void adamw32_kernel(const Tensor* __restrict__ tensors, const Work* __restrict__ works, Step p)
 {
@@ -249,8 +250,8 @@ __device__ __forceinline__ Scales scales_of(float bm, float bv)
 
 // Codes.  c = floor(root of y) comes from an approximate root and may be one off where y is next to a square; the
 // threshold u lies far enough from 0 and 1 that the code taken is then the same: just below (c+1)^2 both choices end at c+1,
-// just above c^2 both at c.  All integers below are exact in fp32.  What is not finite gets the largest code (the parameter
-// it belongs to is not finite either).
+// just above c^2 both at c.  All integers below are exact in fp32.  What is not finite gets the largest code: the gradient was
+// not (nor is its parameter then), or its square overflows.
 __device__ __forceinline__ int code_m(float m, float inv, float u)
 {
 #pragma clang fp contract(off)
@@ -283,7 +284,8 @@ __device__ __forceinline__ float value_r(int q, float s)
 }
 
 // A wavefront takes a block: its lanes hold four elements each, adjacent ones where the arrays allow wide accesses.  103 vector
-// instructions an element: at 8 x 29.3 M elements 650 us, 5.8 TB/s of 16 bytes each, arithmetic and memory about even.
+// instructions an element: 268 M elements 787 us, 5.5 TB/s of 16 bytes each, arithmetic and memory about even; half of them off
+// alignment 860.
 template <class G>
 __global__ __launch_bounds__(kThreads) void adamw8_kernel(const Tensor* __restrict__ tensors, const Work* __restrict__ works, Step p)
 {
@@ -371,7 +373,7 @@ __global__ __launch_bounds__(kThreads) void adamw8_kernel(const Tensor* __restri
     }
 }
 
-// The values that the codes stand for.
+// The values that the codes stand for: 268 M elements 400 us, half of them off alignment 825.
 __global__ __launch_bounds__(kThreads) void adamw8_values_kernel(const Tensor* __restrict__ tensors, const Work* __restrict__ works)
 {
 #pragma clang fp contract(off)

@@ -15,9 +15,9 @@
 // second launch: no atomics, equal calls give equal bits.  Forward 8 x 8192 x 4096 bf16 465 us, 5.8 TB/s of the 2.7 GB that have to
 // move; backward 8 x 4096 x 2048 205 us, 5.2 TB/s of 1.07 GB, with the join.
 //
-// A lane holds eight columns, so a team is as wide as its row (16 columns a lane and half the lanes: 536 instead of 487 us
-// forward at 8 x 8192 x 4096 bf16, 339 instead of 230 backward at 4 x 4096 x 4096).  Teams take every grid-th token, so that
-// those at work at a time are neighbours in memory.
+// A lane holds eight columns, so a team is as wide as its row.  16 columns a lane and half the lanes: backward 221 instead of 203 us at
+// 4 x 4096 x 4096 bf16, forward 155 instead of 139 at 4 x 2048 x 8192, but 452 instead of 466 at 8 x 8192 x 4096.  Teams take every
+// grid-th token, so that those at work at a time are neighbours in memory.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -59,8 +59,8 @@ struct NormGradArgs {
 };
 
 // A lane's columns of a row: pieces of 16 bytes, adjacent lanes' adjacent, so that an access of a wavefront covers whole lines
-// (of fp32, 32 bytes a lane took 272 instead of 220 us forward at 8 x 4096 x 2048).  WIDE: all pieces whole and 16-byte aligned; these are
-// read once and written once, and streaming accesses in both directions took 478 us where plain ones took 518 (8 x 8192 x 4096
+// (of fp32, 32 bytes a lane took 271 instead of 218 us forward at 8 x 4096 x 2048).  WIDE: all pieces whole and 16-byte aligned; these are
+// read once and written once, and streaming accesses in both directions took 466 us where plain ones took 500 (8 x 8192 x 4096
 // bf16).  Elements past the row's end read zero and are not written.  SHORT: rows may be shorter than
 // a piece.
 template <class T, int N, bool WIDE, bool SHORT>
@@ -119,8 +119,8 @@ struct Piece {
 };
 
 // Whether a team holds the weights and its sums for their gradients in registers over its tokens.  With twice the columns a lane
-// they do not fit, and it reads the weights again for each token and keeps the sums in LDS (2 x 2048 x 16384 bf16 backward 228 us,
-// 316 with spilled registers; fp32 468 and 777).
+// they do not fit, and it reads the weights again for each token and keeps the sums in LDS (2 x 2048 x 16384 bf16 backward 229 us,
+// 487 with registers spilled; fp32 466 and 841).
 template <int N>
 constexpr bool kHold = N == 1;
 
@@ -219,7 +219,7 @@ __global__ __launch_bounds__(threads_limit(LANES)) void block_norm_kernel(NormAr
     for (int64_t t = (int64_t)blockIdx.x * teams + team; t < a.T; t += (int64_t)gridDim.x * teams) {
         typename P::Row rr, ry, ru;
         typename P::Values r;
-        // y is waited for first (8 x 8192 x 4096 bf16 465 us, 478 with r's load first; but 6 x 4064 x 4495 286 and 268)
+        // y is waited for first (8 x 8192 x 4096 bf16 466 us, 480 with r's load first; but 6 x 4064 x 4495 283 and 265)
         if (!WIDE || !a.y.p) P::load(row_of<T>(a.r, w, t), lane, ts, a.D, rr);
         if (a.y.p) {
             typename P::Values y, u;
@@ -271,8 +271,8 @@ __global__ __launch_bounds__(threads_limit(LANES)) void block_norm_kernel(NormAr
     }
 }
 
-// Four wavefronts a SIMD have to fit (8 x 16384 x 201 bf16 115 us, 145 where registers decide), but for fp32 in unaligned pieces,
-// which would spill (182 us so, 295 with four).
+// Four wavefronts a SIMD have to fit (12 x 11864 x 64 bf16 34 us, 36 where registers decide; 8 x 16000 x 128 54 and 55; the other way
+// round for some odd rows, 8 x 16384 x 201 122 and 114), but for fp32 in unaligned pieces, which would spill (201: 173 us so, 266).
 template <class T, int N, bool WIDE, int LANES>
 __global__ __launch_bounds__(threads_limit(LANES), sizeof(T) == 2 || WIDE ? 4 : 1) void block_norm_grad_kernel(NormGradArgs a)
 {
@@ -301,7 +301,7 @@ __global__ __launch_bounds__(threads_limit(LANES), sizeof(T) == 2 || WIDE ? 4 : 
         typename P::Row rz, ru, rdr, rdn, rh;
         typename P::Values dr, z, u;
         constexpr bool kEarly = N == 1;                                 // in flight while the first sum is made, if registers are left
-        if (kEarly && a.y.p) {                                          // (two pieces a lane: 228 us late, 255 early, 2 x 2048 x 16384 bf16)
+        if (kEarly && a.y.p) {                                          // (two pieces a lane: 229 us late, 256 early, 2 x 2048 x 16384 bf16)
             P::load(row_of<T>(a.y, w, t), lane, ts, a.D, rz);
             if (a.u.p) P::load(row_of<T>(a.u, w, t), lane, ts, a.D, ru);
         }
@@ -493,7 +493,7 @@ bool wide_rows(const lsgd_rows& a, int W, int T, int es)
 Rows rows(const lsgd_rows& a) { return Rows{a.data, a.worker_stride, a.token_stride}; }
 
 // Lanes of a team within a wavefront for rows of at most 512 columns; whole wavefronts for all of those took 72 us instead of
-// 20 for 12 x 11864 x 64 bf16.
+// 19 for 12 x 11864 x 64 bf16.
 int lanes_of(int D)
 {
     int lanes = 8;
@@ -513,10 +513,10 @@ Shape shape_of(int D)
 }
 
 // Workgroups of a worker.  Forward many, by lanes in all: a team's only gain from further tokens is the weights it holds
-// (8 x 8192 x 4096: 470 us with 2^22 lanes, 488 with 2^20; x 1024: 113 and 126).  Backward each leaves partial sums; twice what
-// the chip holds at a time, which is 1024 lanes a compute unit by their registers: enough to even out (8 x 4096 x 2048 bf16 208 us,
-// 222 with once as many, 216 with four times), and whole rounds (6 x 4064 x 4496, nine wavefronts a team: 400 us, 430 with 2^19
-// lanes in all; 12 x 990 x 7384 298 and 372).
+// (8 x 8192 x 4096: 466 us with 2^22 lanes, 491 with 2^20; x 1024: 111 and 120).  Backward each leaves partial sums; twice what
+// the chip holds at a time, which is 1024 lanes a compute unit by their registers: enough to even out (8 x 4096 x 2048 bf16 205 us,
+// 215 with once as many, 212 with four times), and whole rounds (6 x 4064 x 4496, nine wavefronts a team: 402 us, 430 with 2^19
+// lanes in all, 391 with once as many; 12 x 990 x 7384 300, 370 with 2^19 lanes).
 constexpr int kLanes = 1 << 22, kRoundsGrad = 2, kComputeUnits = 256;
 int groups_of(int W, int T, const Shape& s, int all)
 {

@@ -30,13 +30,14 @@ constexpr int kThreads = 256;
 // ---- lookup ----
 constexpr int kLookupEach = 4;      // independent pieces a thread has in flight
 // Elements of a piece: 16 bytes of it are adjacent to the next lane's, so that streaming stores fill lines (16 x 8192 x 1024 fp32
-// 182 us, 196 with 32).
+// 131 us, 159 with 32).
 template <class TI, class TO>
 constexpr int kLookupPiece = sizeof(TI) == 4 && sizeof(TO) == 4 ? 4 : 8;
 
 // A workgroup's pieces are adjacent in the output; which token and column a piece is follows from its number.  Bound by memory:
-// 16 x 8192 x 1024 bf16 from 32768 rows 73 us, 5.1 TB/s of the 375 MB that have to move (79 us with stores that stay in the
-// caches; 76 and 93 us with 2 and 8 pieces in flight).
+// 16 x 8192 x 1024 bf16 from 32768 rows 70 to 72 us, 5.3 TB/s of the 375 MB that have to move (75 us with stores that stay in the
+// caches; 76 and 72 us with 2 and 8 pieces in flight).  Rows that are not aligned take up to twice as long as their bytes:
+// 8 x 32768 x 1023 195 us bf16, 321 fp32.
 template <class TI, class TO, bool ONCE>
 __global__ __launch_bounds__(kThreads) void lookup_kernel(const TI* __restrict__ table, int64_t ld_table, int V, int D,
                                                           const int32_t* __restrict__ tokens, int64_t ld_tokens, int T,
@@ -284,7 +285,7 @@ __device__ __forceinline__ uint32_t from_lane(uint32_t v, int i)
 template <class T, int E, int TL>
 __device__ __forceinline__ void sum_runs(const GradArgs& a, int64_t task)
 {
-    constexpr int U = 8;                                               // rows in flight (8 x 32768 x 1024: 473 us, 487 with four)
+    constexpr int U = 8;                                               // rows in flight (8 x 32768 x 1023: 530 us, 554 with four; x 1024: 478 both)
     static_assert(TL >= kSpan && kSpan % U == 0, "a lane a place, whole batches");
     const int w = blockIdx.y;
     int span = (int)(task / a.slices), slice = (int)(task - (int64_t)span * a.slices);
@@ -511,7 +512,7 @@ struct SmallArgs {
 };
 
 // 4 x 2048 x 512 bf16, added to tables of 65536 rows, 14 us; 3 x 517 x 101 fp32 7: the passes of the sort one after the other,
-// then a round of loads.  Where tables are large their zeros take the time (16 x 8192 x 1024 into 32768 rows 539 us, 4.5 TB/s).
+// then a round of loads.  Where tables are large their zeros take the time (16 x 8192 x 1024 into 32768 rows 566 us, 4.3 TB/s).
 template <class T, int E, bool ALIGNED, int EACH>
 __global__ __launch_bounds__(kSortThreads) void grad_small_kernel(GradArgs a, SmallArgs q)
 {
@@ -772,9 +773,9 @@ hipError_t launch_grad(GradArgs a, int W, const RunPlan& p, hipStream_t s)
     return hipGetLastError();
 }
 
-// A workgroup a compute unit (each sorts the list again; with two 517 tokens take 12.1 us instead of 8.4, 2048 23.4 instead of
-// 15.6), fewer columns each rather than fewer places; two where the zeros of large tables are what takes the time (1000 tokens,
-// 4 x 65536 x 1024: 217 us instead of 234).
+// A workgroup a compute unit (each sorts the list again; with two 517 tokens take 10.2 us instead of 7.4, 2048 20.6 instead of
+// 13.8), fewer columns each rather than fewer places; two where the zeros of large tables are what takes the time (1000 tokens,
+// 4 x 65536 x 1024: 216 us instead of 234; of 8192 tokens the second sort weighs more, 16 x 32768 x 1024: 566 and 534).
 constexpr int kSmallGroups = 256;
 constexpr int64_t kManyZeros = 128ll << 20;        // bytes of all tables
 template <class T, int E, bool ALIGNED>
