@@ -426,6 +426,101 @@ typedef struct {
 size_t lsgd_block_norm_grad_workspace_bytes(int32_t W, int32_t T, int32_t D); /* 0 on invalid arguments */
 lsgd_status lsgd_block_norm_grad(const lsgd_block_norm_grad_args* args, void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* Activations [B, T, H, D] of attention with dense columns: head h of token t of entry b (a worker, or one of its sequences) at
+ * data + b*batch_stride + t*token_stride + h*head_stride.  Parts of one projection's columns are such tensors.        */
+typedef struct {
+    void* data; /* device; NULL: absent */
+    int64_t batch_stride, token_stride, head_stride;
+} lsgd_heads;
+
+/* Queries and keys before attention: each head's norm and its rotation by the token's position, D <= 256:
+ *   z = x o w / sqrt(mean_d x^2 + eps)       (norm = 0: z = x o w)
+ *   out = z with pair i of its first R columns turned by 2 pi * position * turns[i] and multiplied by magnitude; pairs are columns
+ *         (i, i + R/2), or, interleaved = 1, (2i, 2i + 1); columns from R on are z's
+ * The entries are workers; q [W, T, Hq, D], k [W, T, Hk, D] (Hk = 0: no keys; keys alone are passed as q).
+ *   turns      device fp64 [R/2]: turns per position of each pair; a context is stretched by making them smaller.  The product with
+ *              the position is made in 64 bits.  R = 0: no rotation.
+ *   positions  device int32, worker w's [T] at positions + w*ld_positions (0: the same for all workers); any values; NULL: 0 .. T-1
+ *   w_q, w_k   device fp32, worker w's [D] at w + w*ld (0: the same for all workers), shared by its heads; NULL: ones
+ *   stats      device fp32 [W, T, Hq + Hk]: the norms' factors, which the gradient needs; NULL: not wanted
+ * q_out may be q and k_out may be k, element for element; no other overlaps.  T <= 2^24, Hq and Hk <= 1024.               */
+typedef struct {
+    int32_t W, T, Hq, Hk, D, R;
+    int32_t is_bf16;              /* type of q, k and the results: 0 fp32, 1 bf16 */
+    int32_t norm, interleaved;
+    float eps, magnitude;         /* eps > 0                                     */
+    lsgd_heads q, k, q_out, k_out;
+    const int32_t* positions;
+    int64_t ld_positions;
+    const double* turns;
+    const float *w_q, *w_k;
+    int64_t ld_w_q, ld_w_k;
+    float* stats;
+} lsgd_qk_rotary_args;
+lsgd_status lsgd_qk_rotary(const lsgd_qk_rotary_args* args, void* hip_stream);
+
+/* Its gradients from dq_out, dk_out (of the results), given what the forward call read and gave:
+ *   dq, dk      of q and k; dq may be dq_out or q, dk may be dk_out or k, element for element
+ *   dw_q, dw_k  device fp32, worker w's [D] at dw + w*ld; NULL: not wanted; accumulate = 1 adds to them
+ * q, k may be absent where there is no norm and their dw is not wanted.  Sums over tokens and heads are made in an order that depends
+ * on the sizes and alignment alone.
+ *   workspace  device, >= lsgd_qk_rotary_grad_workspace_bytes, 256-byte aligned; may be NULL when no dw is wanted          */
+typedef struct {
+    int32_t W, T, Hq, Hk, D, R;
+    int32_t is_bf16, norm, interleaved, accumulate;
+    float magnitude;
+    lsgd_heads dq_out, dk_out, q, k, dq, dk;
+    const int32_t* positions;
+    int64_t ld_positions;
+    const double* turns;
+    const float *w_q, *w_k;
+    int64_t ld_w_q, ld_w_k;
+    const float* stats;
+    float *dw_q, *dw_k;
+    int64_t ld_dw_q, ld_dw_k;
+} lsgd_qk_rotary_grad_args;
+size_t lsgd_qk_rotary_grad_workspace_bytes(int32_t W, int32_t T, int32_t Hq, int32_t Hk, int32_t D, int32_t R, int32_t is_bf16); /* 0 on invalid arguments */
+lsgd_status lsgd_qk_rotary_grad(const lsgd_qk_rotary_grad_args* args, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Attention, D <= 128: out[b,t,h,:] = sum_j p_j v[b,j,h',:], p = softmax over the seen keys j of scale * q[b,t,h,:] . k[b,j,h',:]
+ * with h' = h / (Hq / Hk) (Hk divides Hq: query heads that share a key head are adjacent).
+ *   seen        j < k_lens[b]; causal = 1: and j <= t + k_lens[b] - q_lens[b], that is both sequences end together (a new token sees
+ *               its whole cache)
+ *   q_lens, k_lens  device int32 [B], read on the device and taken as within [0, Tq], [0, Tk]; NULL: all Tq, all Tk
+ *   lse         device fp32 [B, Hq, Tq]: log of the sum of exp(scale q.k), which the gradient needs; NULL: not wanted
+ * A query that sees no key, or behind q_lens[b], has out = 0 and lse = -inf.  What lies in memory at keys from k_lens[b] and queries from
+ * q_lens[b] on does not matter (NaN neither); a key that is merely not seen yet must be finite.  Scores, softmax and sums are
+ * fp32; with bf16 data p is rounded to bf16 before the product with v.  out must not overlap the inputs.
+ *   workspace  device, >= lsgd_attention_workspace_bytes, 256-byte aligned, not kept; may be NULL where that says 256.
+ *              Few queries and long keys are split over the keys, and the parts joined from there.                          */
+typedef struct {
+    int32_t B, Tq, Tk, Hq, Hk, D;
+    int32_t is_bf16;              /* type of q, k, v, out: 0 fp32, 1 bf16 */
+    int32_t causal;
+    float scale;                  /* positive                            */
+    lsgd_heads q, k, v, out;
+    const int32_t *q_lens, *k_lens;
+    float* lse;
+} lsgd_attention_args;
+size_t lsgd_attention_workspace_bytes(int32_t B, int32_t Tq, int32_t Tk, int32_t Hq, int32_t Hk, int32_t D, int32_t is_bf16); /* 0 on invalid arguments */
+lsgd_status lsgd_attention(const lsgd_attention_args* args, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Its gradients dq, dk, dv from dout, given what the forward call read and gave (out, lse): sums over queries, and over the heads that
+ * share a key head, in an order that depends on the sizes and lengths alone.  Zeros at queries that see nothing, at queries from q_lens
+ * and keys from k_lens on.  With bf16 data p and its gradient are rounded to bf16 before their products.  dq, dk, dv must not overlap
+ * the inputs or each other.
+ *   workspace  device, >= lsgd_attention_grad_workspace_bytes, 256-byte aligned, not kept                                  */
+typedef struct {
+    int32_t B, Tq, Tk, Hq, Hk, D;
+    int32_t is_bf16, causal;
+    float scale;
+    lsgd_heads dout, q, k, v, out, dq, dk, dv;
+    const int32_t *q_lens, *k_lens;
+    const float* lse;
+} lsgd_attention_grad_args;
+size_t lsgd_attention_grad_workspace_bytes(int32_t B, int32_t Tq, int32_t Tk, int32_t Hq, int32_t Hk, int32_t D, int32_t is_bf16); /* 0 on invalid arguments */
+lsgd_status lsgd_attention_grad(const lsgd_attention_grad_args* args, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* AdamW over a list of tensors, one launch a step.
  *   m <- b1 m + (1-b1) c g;  v <- b2 v + (1-b2) (c g)^2
  *   x <- x (1 - lr lr_mult wd) - lr lr_mult/(1-b1^t) * m / (sqrt(v)/sqrt(1-b2^t) + eps)

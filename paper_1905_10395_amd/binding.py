@@ -4,6 +4,7 @@ lsgd_step (+ helpers).  No arithmetic of the method happens in Python."""
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 import struct
 
@@ -59,6 +60,12 @@ class _Batch(C.Structure):
 # lsgd_block_norm_args, lsgd_block_norm_grad_args (native layout): sizes and flags, factors, lsgd_rows triples, pointers and strides
 _BLOCK_NORM = struct.Struct("@5i2f" + "P2q" * 5 + "2P2q2P")
 _BLOCK_NORM_GRAD = struct.Struct("@6if" + "P2q" * 8 + "2P2q2P2P2q")
+
+# lsgd_qk_rotary_args, lsgd_qk_rotary_grad_args, lsgd_attention_args, lsgd_attention_grad_args; lsgd_heads are a pointer and three strides
+_QK_ROTARY = struct.Struct("@9i2f" + "P3q" * 4 + "PqP2P2qP")
+_QK_ROTARY_GRAD = struct.Struct("@10if" + "P3q" * 6 + "PqP2P2qP2P2q")
+_ATTENTION = struct.Struct("@8if" + "P3q" * 4 + "3P")
+_ATTENTION_GRAD = struct.Struct("@8if" + "P3q" * 8 + "3P")
 
 
 class _AdamWTensor(C.Structure):
@@ -120,6 +127,14 @@ def lib():
         L.lsgd_block_norm_grad_workspace_bytes.restype = C.c_size_t
         L.lsgd_block_norm_grad_workspace_bytes.argtypes = [C.c_int32] * 3
         L.lsgd_block_norm_grad.argtypes = [C.c_char_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.lsgd_qk_rotary.argtypes = [C.c_char_p, C.c_void_p]
+        L.lsgd_qk_rotary_grad_workspace_bytes.restype = C.c_size_t
+        L.lsgd_qk_rotary_grad_workspace_bytes.argtypes = [C.c_int32] * 7
+        L.lsgd_qk_rotary_grad.argtypes = [C.c_char_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        for f in ("attention", "attention_grad"):
+            size, call = getattr(L, f"lsgd_{f}_workspace_bytes"), getattr(L, f"lsgd_{f}")
+            size.restype, size.argtypes = C.c_size_t, [C.c_int32] * 7
+            call.argtypes = [C.c_char_p, C.c_void_p, C.c_size_t, C.c_void_p]
         L.lsgd_adamw_workspace_bytes.restype = C.c_size_t
         L.lsgd_adamw_workspace_bytes.argtypes = [C.POINTER(_AdamWTensor), C.c_int32, C.c_int32, C.c_int32]
         L.lsgd_adamw_create.argtypes = [C.POINTER(_AdamWTensor), C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p,
@@ -556,6 +571,215 @@ def block_norm_grad(dn, dr_out, r_out, stats, y=None, gate=None, w_post=None, w_
         ws = workspace.data_ptr()
     _call(index, stream, L.lsgd_block_norm_grad, a, ws, nbytes)
     return dr, dy, dgate
+
+
+_NO_HEADS = (0, 0, 0, 0)
+
+
+def _heads(who, name, t, shape, dtype, index):
+    """lsgd_heads of an activation tensor [B, T, H, D]."""
+    if t is None:
+        return _NO_HEADS
+    if t.shape != shape or t.dtype is not dtype:
+        raise ValueError(f"{who}: {name} must be {dtype} {list(shape)}")
+    if t.get_device() != index:
+        raise ValueError(f"{who}: {name} is not on the GPU of the others")
+    B, T, H, D = shape
+    sb, st, sh, sd = t.stride()
+    if sd != 1 and D > 1 and t.numel():
+        raise ValueError(f"{who}: columns of {name} must be dense")
+    # a dimension of one element has no stride that means anything
+    return t.data_ptr(), sb if B > 1 else 0, st if T > 1 else 0, sh if H > 1 else 0
+
+
+def _vector(who, name, t, dtype, n, index):
+    """Address of a dense vector, or of n things in any shape."""
+    if t is None:
+        return 0
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous() or t.get_device() != index:
+        raise ValueError(f"{who}: {name} must be {n} contiguous {dtype}, on the GPU of the others")
+    return t.data_ptr()
+
+
+def _positions(who, positions, W, T, index):
+    if positions is None:
+        return 0, 0
+    if positions.dtype is not _I32 or positions.shape not in ((W, T), (1, T)) or positions.get_device() != index:
+        raise ValueError(f"{who}: positions must be int32 [W, T] or [1, T], on the GPU of the others")
+    ld = _worker_stride(who, "positions", positions, "must be dense within a worker")
+    return positions.data_ptr(), ld if positions.shape[0] > 1 else 0
+
+
+def _head_weights(who, name, w, W, D, index):
+    """[W, D], or [1, D] for all workers."""
+    if w is not None and w.dim() == 2 and w.shape[0] == 1 < W:
+        return _weights(who, name, w, 1, D, index)[0], 0
+    return _weights(who, name, w, W, D, index)
+
+
+def rotary_turns(columns, base=10000.0, stretch=1.0, keep=None, device="cuda"):
+    """Turns per position of the pairs of `columns` rotated columns, float64 [columns / 2] on device, for qk_rotary: pair i makes
+    base^(-2 i / columns) / (2 pi).
+    stretch > 1 serves contexts that much longer than those trained on.  keep None: every pair turns that much slower.  keep =
+    (length, low, high): a pair that makes at least `high` turns over the trained length keeps its pace, one that makes at most `low` is
+    slowed by the whole factor, between them a share in proportion."""
+    _need(columns >= 0 and columns % 2 == 0, "rotary_turns: columns must be even")
+    _need(base > 0 and stretch > 0, "rotary_turns: base and stretch must be positive")
+    turns = torch.tensor([base ** (-2.0 * i / columns) / (2.0 * math.pi) for i in range(columns // 2)], dtype=torch.float64)
+    if keep is None:
+        turns = turns / stretch
+    else:
+        length, low, high = keep
+        _need(length > 0 and 0 <= low < high, "rotary_turns: keep must be (length, low, high) with 0 <= low < high")
+        share = ((turns * length - low) / (high - low)).clamp(0.0, 1.0)
+        turns = share * turns + (1.0 - share) * (turns / stretch)
+    return turns.to(device)
+
+
+def qk_rotary(q, k=None, positions=None, turns=None, w_q=None, w_k=None, norm=True, eps=1e-6, interleaved=False, magnitude=1.0, q_out=None,
+              k_out=None, stats=None, stream=None):
+    """lsgd_qk_rotary: each head's norm and its rotation by the token's position, of queries and keys in one pass.  Not recorded by
+    autograd: qk_rotary_grad is its gradient.
+    q, k: float32 or bfloat16 [W, T, Hq, D], [W, T, Hk, D] with dense columns (views of one projection will do); positions: int32 [W, T] or
+    [1, T], None: 0 .. T-1; turns: float64 [R / 2] on the GPU (rotary_turns), None: no rotation; w_q, w_k: float32 [W, D] (columns of x)
+    or [1, D], None: ones; norm False: no norm; interleaved: pairs are neighbours, not a half apart; magnitude: of the rotated columns.
+    Returns (q_out, k_out, stats); stats: float32 [W, T, Hq + Hk], what the gradient needs, None without a norm.  q_out, k_out, stats:
+    optional buffers (q_out may be q, k_out may be k; a slice of a cache)."""
+    who = "qk_rotary"
+    dt = q.dtype
+    _need(q.dim() == 4 and dt in _FLOATS, "qk_rotary: q must be float32 or bfloat16 [W, T, H, D]")
+    index = _gpu(who, q, (("q", q),))
+    W, T, Hq, D = shape = q.shape
+    _need(k is None or k.dim() == 4, "qk_rotary: k must be [W, T, H, D]")
+    _need(k is not None or (w_k is None and k_out is None), "qk_rotary: w_k and k_out need k")
+    _need(norm or stats is None, "qk_rotary: stats need a norm")
+    Hk = 0 if k is None else k.shape[2]
+    kshape = (W, T, Hk, D)
+    half = 0 if turns is None else turns.numel()
+    _need(half * 2 <= D, "qk_rotary: more turns than pairs of columns")
+    if q_out is None:
+        q_out = _fresh(q, shape, dt, stream)
+    if Hk and k_out is None:
+        k_out = _fresh(q, kshape, dt, stream)
+    if norm and stats is None:
+        stats = _fresh(q, (W, T, Hq + Hk), _F32, stream)
+    wq, lq = _head_weights(who, "w_q", w_q, W, D, index)
+    wk, lk = _head_weights(who, "w_k", w_k, W, D, index)
+    if T:
+        a = _QK_ROTARY.pack(W, T, Hq, Hk, D, 2 * half, dt is _BF16, bool(norm), bool(interleaved), eps, magnitude, *_heads(who, "q", q, shape, dt, index),
+                            *_heads(who, "k", k, kshape, dt, index), *_heads(who, "q_out", q_out, shape, dt, index),
+                            *_heads(who, "k_out", k_out, kshape, dt, index), *_positions(who, positions, W, T, index),
+                            _vector(who, "turns", turns, torch.float64, half, index), wq, wk, lq, lk,
+                            _vector(who, "stats", stats, _F32, W * T * (Hq + Hk), index))
+        _call(index, stream, lib().lsgd_qk_rotary, a)
+    return q_out, k_out, stats
+
+
+def qk_rotary_grad(dq_out, dk_out=None, q=None, k=None, stats=None, positions=None, turns=None, w_q=None, w_k=None, norm=True, interleaved=False,
+                   magnitude=1.0, dw_q=None, dw_k=None, accumulate=False, dq=None, dk=None, workspace=None, stream=None):
+    """lsgd_qk_rotary_grad: (dq, dk) from dq_out, dk_out (gradients of qk_rotary's results); q, k, stats and the rest as it had or gave
+    them (q, k None: neither a norm nor dw_q, dw_k).  dw_q, dw_k: float32 [W, D] (columns of g) that receive the weights' gradients, added to
+    what is there if accumulate; weights shared by workers have theirs worker by worker.  dq, dk: optional buffers."""
+    who = "qk_rotary_grad"
+    dt = dq_out.dtype
+    _need(dq_out.dim() == 4 and dt in _FLOATS, "qk_rotary_grad: dq_out must be float32 or bfloat16 [W, T, H, D]")
+    index = _gpu(who, dq_out, (("dq_out", dq_out),))
+    W, T, Hq, D = shape = dq_out.shape
+    _need(dk_out is None or dk_out.dim() == 4, "qk_rotary_grad: dk_out must be [W, T, H, D]")
+    _need(dk_out is not None or (k is None and w_k is None and dw_k is None and dk is None), "qk_rotary_grad: k, w_k, dw_k and dk need dk_out")
+    _need(not norm or stats is not None, "qk_rotary_grad: a norm's gradient needs stats")
+    Hk = 0 if dk_out is None else dk_out.shape[2]
+    kshape = (W, T, Hk, D)
+    half = 0 if turns is None else turns.numel()
+    _need(half * 2 <= D, "qk_rotary_grad: more turns than pairs of columns")
+    if dq is None:
+        dq = _fresh(dq_out, shape, dt, stream)
+    if Hk and dk is None:
+        dk = _fresh(dq_out, kshape, dt, stream)
+    wq, lq = _head_weights(who, "w_q", w_q, W, D, index)
+    wk, lk = _head_weights(who, "w_k", w_k, W, D, index)
+    dwq, ldq = _weights(who, "dw_q", dw_q, W, D, index)
+    dwk, ldk = _weights(who, "dw_k", dw_k, W, D, index)
+    a = _QK_ROTARY_GRAD.pack(W, T, Hq, Hk, D, 2 * half, dt is _BF16, bool(norm), bool(interleaved), bool(accumulate), magnitude,
+                             *_heads(who, "dq_out", dq_out, shape, dt, index), *_heads(who, "dk_out", dk_out, kshape, dt, index),
+                             *_heads(who, "q", q, shape, dt, index), *_heads(who, "k", k, kshape, dt, index), *_heads(who, "dq", dq, shape, dt, index),
+                             *_heads(who, "dk", dk, kshape, dt, index), *_positions(who, positions, W, T, index),
+                             _vector(who, "turns", turns, torch.float64, half, index), wq, wk, lq, lk,
+                             _vector(who, "stats", stats, _F32, W * T * (Hq + Hk), index) if norm else 0, dwq, dwk, ldq, ldk)
+    L = lib()
+    ws, nbytes = None, 0
+    if T and (dwq or dwk):
+        workspace, nbytes = _workspace(who, L.lsgd_qk_rotary_grad_workspace_bytes(W, T, Hq, Hk, D, 2 * half, dt is _BF16), dq_out, workspace, stream)
+        ws = workspace.data_ptr()
+    _call(index, stream, L.lsgd_qk_rotary_grad, a, ws, nbytes)
+    return dq, dk
+
+
+def _attention_shapes(who, q, k, v):
+    _need(q.dim() == 4 and q.dtype in _FLOATS, f"{who}: q must be float32 or bfloat16 [B, Tq, Hq, D]")
+    B, Tq, Hq, D = q.shape
+    _need(k.dim() == 4 and k.shape[0] == B and k.shape[3] == D, f"{who}: k must be [B, Tk, Hk, D] beside q")
+    return B, Tq, k.shape[1], Hq, k.shape[2], D
+
+
+def attention(q, k, v, causal=False, scale=None, q_lens=None, k_lens=None, with_lse=True, out=None, lse=None, workspace=None, stream=None):
+    """lsgd_attention: softmax(scale q k') v.  Not recorded by autograd: attention_grad is its gradient.
+    q: float32 or bfloat16 [B, Tq, Hq, D], k, v: [B, Tk, Hk, D] with dense columns, Hk a divisor of Hq (query heads that share a key head are
+    adjacent); an entry is a worker, or one of its sequences.  q_lens, k_lens: int32 [B] on the GPU, lengths of the entries' sequences
+    (None: full); causal: a query sees the keys up to its own place, both sequences ending together; scale: 1 / sqrt(D) if None.
+    Returns (out, lse): out like q, lse float32 [B, Hq, Tq], which the gradient needs (None if not with_lse).  Queries that see nothing have zeros
+    and -inf.  out, lse: optional buffers."""
+    who = "attention"
+    B, Tq, Tk, Hq, Hk, D = _attention_shapes(who, q, k, v)
+    dt = q.dtype
+    index = _gpu(who, q, (("q", q),))
+    shape, kshape = (B, Tq, Hq, D), (B, Tk, Hk, D)
+    if scale is None:
+        scale = D ** -0.5
+    if out is None:
+        out = _fresh(q, shape, dt, stream)
+    if lse is None and with_lse:
+        lse = _fresh(q, (B, Hq, Tq), _F32, stream)
+    a = _ATTENTION.pack(B, Tq, Tk, Hq, Hk, D, dt is _BF16, bool(causal), scale, *_heads(who, "q", q, shape, dt, index),
+                        *_heads(who, "k", k, kshape, dt, index), *_heads(who, "v", v, kshape, dt, index), *_heads(who, "out", out, shape, dt, index),
+                        _vector(who, "q_lens", q_lens, _I32, B, index), _vector(who, "k_lens", k_lens, _I32, B, index),
+                        _vector(who, "lse", lse, _F32, B * Hq * Tq, index))
+    L = lib()
+    ws, nbytes = None, 0
+    need = L.lsgd_attention_workspace_bytes(B, Tq, Tk, Hq, Hk, D, dt is _BF16)
+    if need != _ATTENTION_NO_WORKSPACE:
+        workspace, nbytes = _workspace(who, need, q, workspace, stream)
+        ws = workspace.data_ptr()
+    _call(index, stream, L.lsgd_attention, a, ws, nbytes)
+    return out, lse
+
+
+_ATTENTION_NO_WORKSPACE = 256
+
+
+def attention_grad(dout, q, k, v, out, lse, causal=False, scale=None, q_lens=None, k_lens=None, dq=None, dk=None, dv=None, workspace=None, stream=None):
+    """lsgd_attention_grad: (dq, dk, dv) from dout; out, lse: what attention returned; the rest as given to it.  dq, dk, dv: optional
+    buffers (parts of one projection's gradient will do)."""
+    who = "attention_grad"
+    B, Tq, Tk, Hq, Hk, D = _attention_shapes(who, q, k, v)
+    dt = q.dtype
+    index = _gpu(who, q, (("q", q),))
+    shape, kshape = (B, Tq, Hq, D), (B, Tk, Hk, D)
+    if scale is None:
+        scale = D ** -0.5
+    dq = _fresh(q, shape, dt, stream) if dq is None else dq
+    dk = _fresh(q, kshape, dt, stream) if dk is None else dk
+    dv = _fresh(q, kshape, dt, stream) if dv is None else dv
+    a = _ATTENTION_GRAD.pack(B, Tq, Tk, Hq, Hk, D, dt is _BF16, bool(causal), scale, *_heads(who, "dout", dout, shape, dt, index),
+                             *_heads(who, "q", q, shape, dt, index), *_heads(who, "k", k, kshape, dt, index), *_heads(who, "v", v, kshape, dt, index),
+                             *_heads(who, "out", out, shape, dt, index), *_heads(who, "dq", dq, shape, dt, index),
+                             *_heads(who, "dk", dk, kshape, dt, index), *_heads(who, "dv", dv, kshape, dt, index),
+                             _vector(who, "q_lens", q_lens, _I32, B, index), _vector(who, "k_lens", k_lens, _I32, B, index),
+                             _vector(who, "lse", lse, _F32, B * Hq * Tq, index))
+    L = lib()
+    workspace, nbytes = _workspace(who, L.lsgd_attention_grad_workspace_bytes(B, Tq, Tk, Hq, Hk, D, dt is _BF16), q, workspace, stream)
+    _call(index, stream, L.lsgd_attention_grad, a, workspace.data_ptr(), nbytes)
+    return dq, dk, dv
 
 
 class AdamWTensor:

@@ -1,0 +1,426 @@
+// Attention forward: softmax(scale q k') v of the keys that each query sees.
+//
+//   s = q . k,  c = scale log2 e,  p = 2^(c (s - m)),  l = sum p,  out = (sum p v) / l,  lse = scale m + log l
+//
+// One pass over the keys.  m is a running reference of the scores, not always their maximum: sums are rescaled only when a score
+// exceeds it by 8 or more powers of two, so most tiles need no rescaling, and p stays below 2^8.  s^T = K Q^T and out^T = V^T P^T:
+// a lane's result column is one query, so its maximum and sum need one exchange between two lanes, and p goes from result to operand
+// without leaving the registers (attention_common.h).
+//
+// Two kernels.  By rows: a workgroup takes 128 rows (query, head of the key head's), 32 a wavefront, and all pass over the keys
+// together; K and V tiles are read by all four from LDS, the next ones are on their way meanwhile.  By keys: where there are few rows,
+// a workgroup takes 32 of them, and its wavefronts and further workgroups split the keys; each wavefront has tiles of its own
+// and waits for nobody, and the parts are joined at the end.
+#include <algorithm>
+#include <cmath>
+
+#include "attention_common.h"
+
+namespace lsgd {
+namespace attention {
+namespace {
+
+struct Args : Shape {
+    Heads q, k, v, out;
+    float* lse;                      // [B][Hq][Tq], or NULL
+    float* parts;                    // by keys: parts of splits, NULL: one split
+    int tiles;                       // of rows
+    int splits, chunk;               // by keys: workgroups a tile of rows, and the keys of one
+    float scale, c;                  // c: scale log2 e
+};
+
+// What a wavefront holds of 32 rows: their sums so far, relative to m.
+template <int PARTS>
+struct State {
+    f32x16 o[PARTS];
+    float m, l;                      // l: of this lane's keys
+    __device__ __forceinline__ State() : m(-INFINITY), l(0.0f)
+    {
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[p][i] = 0.0f;
+    }
+};
+
+constexpr float kSlack = 8.0f;       // powers of two
+
+// KEYS keys of tiles kt and vt.  masked: some row does not see some of them.
+template <class T, int PARTS, int KEYS>
+__device__ __forceinline__ void pass_tile(const T* kt, const T* vt, int lane, int key0, int sees, bool masked, float c, const Frag<T> (&qf)[2 * PARTS],
+                                          State<PARTS>& st)
+{
+    constexpr int NS = KEYS / 32;
+    const int h = lane >> 5;
+    f32x16 s[NS];
+#pragma unroll
+    for (int n = 0; n < NS; ++n) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[n][i] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 2 * PARTS; ++k) {
+            Frag<T> f;
+            read_row(kt, KEYS, 32 * n + (lane & 31), h, k, f);
+            multiply(s[n], f, qf[k]);
+        }
+    }
+    if (masked) {
+#pragma unroll
+        for (int n = 0; n < NS; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[n][i] = key0 + 32 * n + 8 * (i >> 2) + 4 * h + (i & 3) < sees ? s[n][i] : -INFINITY;
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int n = 0; n < NS; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[n][i]);
+    top = fmaxf(top, other_half(top));
+    if (__any((top - st.m) * c > kSlack)) {
+        const float m = fmaxf(st.m, top), a = m == st.m ? 1.0f : __builtin_amdgcn_exp2f((st.m - m) * c);
+        st.m = m;
+        st.l *= a;
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) st.o[p][i] *= a;
+    }
+    const float mc = st.m == -INFINITY ? 0.0f : st.m * c;
+#pragma unroll
+    for (int n = 0; n < NS; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            s[n][i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], c, -mc));
+            st.l += s[n][i];
+        }
+#pragma unroll
+    for (int k = 0; k < KEYS / 16; ++k) {
+        Frag<T> p;
+        from_result(s[k / 2], k % 2, p);
+#pragma unroll
+        for (int part = 0; part < PARTS; ++part) {
+            Frag<T> f;
+            read_column(vt, KEYS, 16 * k, lane, part, f);
+            multiply(st.o[part], f, p);
+        }
+    }
+}
+
+template <class T, int PARTS>
+__device__ __forceinline__ void load_queries(const Args& g, const Rows& rows, const Row& row, int h, Frag<T> (&qf)[2 * PARTS])
+{
+    const T* q = static_cast<const T*>(g.q.p) + rows.b * g.q.lb + row.t * g.q.lt + row.head * g.q.lh;
+#pragma unroll
+    for (int k = 0; k < 2 * PARTS; ++k) {
+        if (row.sees) load_frag(q, 16 * k + 8 * h, g.D, qf[k]);
+        else no_frag(qf[k]);
+    }
+}
+
+constexpr int kWaves = 4, kThreads = 64 * kWaves;
+constexpr int kRowsByRows = 32 * kWaves;
+template <class T>
+constexpr int kKeysByRows = sizeof(T) == 2 ? 64 : 32;     // two buffers of K and V tiles leave two workgroups a compute unit
+
+template <class T, int PARTS, bool ALIGNED>
+__global__ __launch_bounds__(kThreads, 2) void attention_rows_kernel(Args g)
+{
+    constexpr int KEYS = kKeysByRows<T>;
+    // separate objects, so that the compiler sees that a read of one does not wait for loads into another
+    __shared__ __attribute__((aligned(16))) T k0[tile_elements<T>(KEYS, PARTS)], k1[tile_elements<T>(KEYS, PARTS)];
+    __shared__ __attribute__((aligned(16))) T v0[tile_elements<T>(KEYS, PARTS)], v1[tile_elements<T>(KEYS, PARTS)];
+    const int lane = threadIdx.x & 63, h = lane >> 5, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Place at = place_of(g);
+    const int unit = at.unit, tile = g.tiles - 1 - (int)at.at;             // late rows see most keys: first
+    if (unit >= g.units) return;
+    const Rows rows = rows_of(g, unit, tile * kRowsByRows, kRowsByRows);
+    const Row row = row_of(g, rows, tile * kRowsByRows + wid * 32 + (lane & 31));
+    const int least = wave_min(row.sees), most = wave_max(row.sees);
+    Frag<T> qf[2 * PARTS];
+    load_queries<T, PARTS>(g, rows, row, h, qf);
+    State<PARTS> st;
+    const T* k = static_cast<const T*>(g.k.p) + rows.b * g.k.lb + rows.hk * g.k.lh;
+    const T* v = static_cast<const T*>(g.v.p) + rows.b * g.v.lb + rows.hk * g.v.lh;
+    auto issue = [&](int key0, T* kb, T* vb) {
+        auto key = [&](int r) { return key0 + r < rows.nk ? key0 + r : rows.nk - 1; };
+        load_tile<T, KEYS, PARTS, kWaves, ALIGNED>(kb, wid, lane, g.D, [&](int r) { return k + key(r) * g.k.lt; });
+        load_tile<T, KEYS, PARTS, kWaves, ALIGNED>(vb, wid, lane, g.D, [&](int r) { return v + key(r) * g.v.lt; });
+    };
+    auto step = [&](int key0, T* kb, T* vb, T* next_k, T* next_v) {
+        tiles_barrier();
+        if (key0 + KEYS < rows.end) issue(key0 + KEYS, next_k, next_v);
+        if (key0 < most) pass_tile<T, PARTS, KEYS>(kb, vb, lane, key0, row.sees, key0 + KEYS > least, g.c, qf, st);
+    };
+    if (rows.end > 0) issue(0, k0, v0);
+    for (int key0 = 0; key0 < rows.end; key0 += 2 * KEYS) {
+        step(key0, k0, v0, k1, v1);
+        if (key0 + KEYS < rows.end) step(key0 + KEYS, k1, v1, k0, v0);
+    }
+    if (!row.there) return;
+    const float l = st.l + other_half(st.l), inv = l > 0.0f ? 1.0f / l : 0.0f;
+    T* out = static_cast<T*>(g.out.p) + rows.b * g.out.lb + row.t * g.out.lt + row.head * g.out.lh;
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            const float o[4] = {st.o[p][i] * inv, st.o[p][i + 1] * inv, st.o[p][i + 2] * inv, st.o[p][i + 3] * inv};
+            store4(out, p * kPart + 2 * i + 4 * h, g.D, o);
+        }
+    if (g.lse && h == 0) g.lse[((int64_t)rows.b * g.Hq + row.head) * g.Tq + row.t] = l > 0.0f ? st.m * g.scale + logf(l) : -INFINITY;
+}
+
+// ---- by keys ----
+template <class T, int PARTS>
+constexpr int kWavesByKeys = sizeof(T) == 4 && PARTS > 2 ? 2 : 4;   // as many as their tiles leave room for
+constexpr int kRowsByKeys = 32, kKeysByKeys = 32;
+
+// A split's part: sums relative to m, [32][parts of 32], then m and l of each row.
+__host__ __device__ constexpr int part_floats(int parts) { return kRowsByKeys * (parts * kPart + 2); }
+
+template <class T, int PARTS, bool ALIGNED>
+__global__ __launch_bounds__((64 * kWavesByKeys<T, PARTS>), 1) void attention_keys_kernel(Args g)
+{
+    constexpr int W = kWavesByKeys<T, PARTS>, KEYS = kKeysByKeys, N = tile_elements<T>(KEYS, PARTS);
+    __shared__ __attribute__((aligned(16))) T k0[W][N], k1[W][N];
+    __shared__ __attribute__((aligned(16))) T v0[W][N], v1[W][N];
+    __shared__ float sums[W][kRowsByKeys][kPart + 1], tops[W][kRowsByKeys], ls[W][kRowsByKeys];
+    const int lane = threadIdx.x & 63, h = lane >> 5, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int64_t id = blockIdx.x;
+    const int split = (int)(id % g.splits);
+    id /= g.splits;
+    const int tile = g.tiles - 1 - (int)(id % g.tiles), unit = (int)(id / g.tiles);
+    const Rows rows = rows_of(g, unit, tile * kRowsByKeys, kRowsByKeys);
+    const Row row = row_of(g, rows, tile * kRowsByKeys + (lane & 31));
+    const int begin = split * g.chunk, end = min(begin + g.chunk, rows.end);
+    const int least = wave_min(row.sees);
+    State<PARTS> st;
+    if (begin + wid * KEYS < end) {
+        Frag<T> qf[2 * PARTS];
+        load_queries<T, PARTS>(g, rows, row, h, qf);
+        const T* k = static_cast<const T*>(g.k.p) + rows.b * g.k.lb + rows.hk * g.k.lh;
+        const T* v = static_cast<const T*>(g.v.p) + rows.b * g.v.lb + rows.hk * g.v.lh;
+        auto issue = [&](int key0, T* kb, T* vb) {
+            auto key = [&](int r) { return key0 + r < rows.nk ? key0 + r : rows.nk - 1; };
+            load_tile<T, KEYS, PARTS, 1, ALIGNED>(kb, 0, lane, g.D, [&](int r) { return k + key(r) * g.k.lt; });
+            load_tile<T, KEYS, PARTS, 1, ALIGNED>(vb, 0, lane, g.D, [&](int r) { return v + key(r) * g.v.lt; });
+        };
+        auto step = [&](int key0, T* kb, T* vb, T* next_k, T* next_v) {
+            __builtin_amdgcn_s_waitcnt(0xC07F);                    // lgkmcnt 0: the next buffers have been read
+            asm volatile("" ::: "memory");
+            if (key0 + W * KEYS < end) {
+                issue(key0 + W * KEYS, next_k, next_v);
+                constexpr int later = 2 * TileLoad<T, KEYS, PARTS, 1>::kLoads;
+                if constexpr (ALIGNED) __builtin_amdgcn_s_waitcnt((later & 15) | ((later >> 4) << 14) | 0x0F70);    // this tile is there
+            } else {
+                __builtin_amdgcn_s_waitcnt(0x0F70);
+            }
+            asm volatile("" ::: "memory");
+            pass_tile<T, PARTS, KEYS>(kb, vb, lane, key0, row.sees, key0 + KEYS > least, g.c, qf, st);
+        };
+        const int first = begin + wid * KEYS;
+        issue(first, k0[wid], v0[wid]);
+        for (int key0 = first; key0 < end; key0 += 2 * W * KEYS) {
+            step(key0, k0[wid], v0[wid], k1[wid], v1[wid]);
+            if (key0 + W * KEYS < end) step(key0 + W * KEYS, k1[wid], v1[wid], k0[wid], v0[wid]);
+        }
+    }
+    // the wavefronts' sums, 32 columns at a time
+    const float l = st.l + other_half(st.l);
+    if (h == 0) {
+        tops[wid][lane] = st.m;
+        ls[wid][lane] = l;
+    }
+    float* const part = g.parts ? g.parts + (((int64_t)unit * g.tiles + tile) * g.splits + split) * part_floats(PARTS) : nullptr;
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sums[wid][lane & 31][8 * (i >> 2) + 4 * h + (i & 3)] = st.o[p][i];
+        __syncthreads();
+#pragma unroll
+        for (int i = threadIdx.x; i < kRowsByKeys * kPart; i += 64 * W) {
+            const int r = i / kPart, c = i % kPart;
+            float m = tops[0][r], o = 0.0f, n = 0.0f;
+#pragma unroll
+            for (int w = 1; w < W; ++w) m = fmaxf(m, tops[w][r]);
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                const float a = tops[w][r] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((tops[w][r] - m) * g.c);
+                o += a * sums[w][r][c];
+                n += a * ls[w][r];
+            }
+            const Row to = row_of(g, rows, tile * kRowsByKeys + r);
+            if (!to.there) continue;
+            if (part) {
+                if (n > 0.0f) part[r * (PARTS * kPart) + p * kPart + c] = o;
+                if (p == 0 && c < 2) part[kRowsByKeys * PARTS * kPart + 2 * r + c] = c ? n : m;
+            } else {
+                if (p * kPart + c < g.D)
+                    put1(static_cast<T*>(g.out.p) + rows.b * g.out.lb + to.t * g.out.lt + to.head * g.out.lh + p * kPart + c, n > 0.0f ? o / n : 0.0f);
+                if (p == 0 && c == 0 && g.lse)
+                    g.lse[((int64_t)rows.b * g.Hq + to.head) * g.Tq + to.t] = n > 0.0f ? m * g.scale + logf(n) : -INFINITY;
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// The splits' parts of a tile of rows, a wavefront a row.
+template <class T, int PARTS>
+__global__ __launch_bounds__(kThreads) void attention_join_kernel(Args g)
+{
+    const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
+    const int64_t id = blockIdx.x;
+    const int tile = (int)(id % g.tiles), unit = (int)(id / g.tiles);
+    const Rows rows = rows_of(g, unit, tile * kRowsByKeys, kRowsByKeys);
+    const float* parts = g.parts + id * g.splits * part_floats(PARTS);
+    constexpr int COLS = (PARTS * kPart + 63) / 64;
+    for (int r = wid; r < kRowsByKeys; r += kWaves) {
+        const Row to = row_of(g, rows, tile * kRowsByKeys + r);
+        if (!to.there) break;
+        const float* ml = parts + kRowsByKeys * PARTS * kPart + 2 * r;
+        float m = -INFINITY;
+        for (int s = 0; s < g.splits; ++s) m = fmaxf(m, ml[(int64_t)s * part_floats(PARTS)]);
+        float o[COLS], n = 0.0f;
+#pragma unroll
+        for (int k = 0; k < COLS; ++k) o[k] = 0.0f;
+        for (int s = 0; s < g.splits; ++s) {
+            const float* p = parts + (int64_t)s * part_floats(PARTS);
+            const float ms = p[kRowsByKeys * PARTS * kPart + 2 * r], l = p[kRowsByKeys * PARTS * kPart + 2 * r + 1];
+            if (l == 0.0f) continue;
+            const float a = __builtin_amdgcn_exp2f((ms - m) * g.c);
+            n += a * l;
+#pragma unroll
+            for (int k = 0; k < COLS; ++k)
+                if (lane + 64 * k < PARTS * kPart) o[k] += a * p[r * (PARTS * kPart) + lane + 64 * k];
+        }
+        T* out = static_cast<T*>(g.out.p) + rows.b * g.out.lb + to.t * g.out.lt + to.head * g.out.lh;
+#pragma unroll
+        for (int k = 0; k < COLS; ++k)
+            if (lane + 64 * k < g.D) put1(out + lane + 64 * k, n > 0.0f ? o[k] / n : 0.0f);
+        if (g.lse && lane == 0) g.lse[((int64_t)rows.b * g.Hq + to.head) * g.Tq + to.t] = n > 0.0f ? m * g.scale + logf(n) : -INFINITY;
+    }
+}
+
+// ---- host ----
+struct Plan {
+    bool by_keys;
+    int tiles, splits, chunk;
+    size_t bytes;
+};
+constexpr int kComputeUnits = 256;
+Plan plan_of(int B, int Tq, int Tk, int Hq, int Hk, int D)
+{
+    Plan p{};
+    const int64_t rows = (int64_t)Tq * (Hq / Hk), units = (int64_t)B * Hk;
+    const int64_t by_rows = units * ((rows + kRowsByRows - 1) / kRowsByRows);
+    p.by_keys = rows <= kRowsByKeys || by_rows < kComputeUnits / 2;
+    p.splits = 1;
+    p.chunk = std::max(Tk, 1);
+    p.bytes = kAlign;
+    if (!p.by_keys) {
+        p.tiles = (int)((rows + kRowsByRows - 1) / kRowsByRows);
+        return p;
+    }
+    p.tiles = (int)((rows + kRowsByKeys - 1) / kRowsByKeys);
+    const int64_t groups = units * p.tiles, wanted = std::max<int64_t>(1, 8 * kComputeUnits / std::max<int64_t>(1, groups));
+    const int least = 1024, step = 128;
+    const int64_t splits = std::min<int64_t>(wanted, (Tk + least - 1) / least);
+    if (splits > 1) {
+        p.chunk = (int)(((Tk + splits - 1) / splits + step - 1) / step * step);
+        p.splits = (Tk + p.chunk - 1) / p.chunk;
+        p.bytes = sizeof(float) * (size_t)groups * (size_t)p.splits * (size_t)part_floats(parts_of(D));
+    }
+    return p;
+}
+
+template <class T, int PARTS>
+void launch(const Args& g, const Plan& p, bool aligned, hipStream_t s)
+{
+    if (!p.by_keys) {
+        const dim3 grid((unsigned)workgroups(g, g.tiles));
+        if (aligned) hipLaunchKernelGGL((attention_rows_kernel<T, PARTS, true>), grid, dim3(kThreads), 0, s, g);
+        else hipLaunchKernelGGL((attention_rows_kernel<T, PARTS, false>), grid, dim3(kThreads), 0, s, g);
+        return;
+    }
+    const dim3 grid((unsigned)((int64_t)g.units * g.tiles * g.splits)), threads(64 * kWavesByKeys<T, PARTS>);
+    if (aligned) hipLaunchKernelGGL((attention_keys_kernel<T, PARTS, true>), grid, threads, 0, s, g);
+    else hipLaunchKernelGGL((attention_keys_kernel<T, PARTS, false>), grid, threads, 0, s, g);
+    if (g.splits > 1) hipLaunchKernelGGL((attention_join_kernel<T, PARTS>), dim3((unsigned)((int64_t)g.units * g.tiles)), dim3(kThreads), 0, s, g);
+}
+
+// Launches of at most 2^31 workgroups and fewer than 2^32 threads.
+bool fits(int B, int Tq, int Tk, int Hq, int Hk, int D)
+{
+    const Plan p = plan_of(B, Tq, Tk, Hq, Hk, D);
+    return (double)((int64_t)B * Hk + 7) * 1.2 * p.tiles * p.splits * kThreads < 4294967296.0;
+}
+
+} // namespace
+
+lsgd_status check_attention_shape(const char* who, int64_t B, int64_t Tq, int64_t Tk, int64_t Hq, int64_t Hk, int64_t D)
+{
+    if (B <= 0 || B > kMaxEntries) return set_error(LSGD_ERR_SHAPE, "%s: B=%lld outside [1,%d]", who, (long long)B, kMaxEntries);
+    if (Tq < 0 || Tk < 0 || Tq > kMaxTokens || Tk > kMaxTokens)
+        return set_error(LSGD_ERR_SHAPE, "%s: Tq=%lld or Tk=%lld outside [0,%d]", who, (long long)Tq, (long long)Tk, kMaxTokens);
+    if (Hk <= 0 || Hq <= 0 || Hq > kMaxHeads || Hq % Hk) return set_error(LSGD_ERR_SHAPE, "%s: Hq=%lld must be a multiple of Hk=%lld and within [1,%d]", who, (long long)Hq, (long long)Hk, kMaxHeads);
+    if (D <= 0) return set_error(LSGD_ERR_SHAPE, "%s: D=%lld must be positive", who, (long long)D);
+    if (D > kMaxColumns) return set_error(LSGD_ERR_UNSUPPORTED, "%s: D=%lld beyond %d columns", who, (long long)D, kMaxColumns);
+    if (Tq * (Hq / Hk) >= INT64_C(1) << 30) return set_error(LSGD_ERR_SHAPE, "%s: Tq * (Hq / Hk) = %lld is too large", who, (long long)(Tq * (Hq / Hk)));
+    return LSGD_OK;
+}
+
+} // namespace attention
+} // namespace lsgd
+
+using namespace lsgd;
+using namespace lsgd::attention;
+
+extern "C" {
+
+size_t lsgd_attention_workspace_bytes(int32_t B, int32_t Tq, int32_t Tk, int32_t Hq, int32_t Hk, int32_t D, int32_t is_bf16)
+{
+    (void)is_bf16;
+    if (check_attention_shape("attention", B, Tq, Tk, Hq, Hk, D) != LSGD_OK) return 0;
+    return plan_of(B, Tq, Tk, Hq, Hk, D).bytes;
+}
+
+lsgd_status lsgd_attention(const lsgd_attention_args* p, void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+    const char* who = "attention";
+    if (!p) return set_error(LSGD_ERR_INVALID_ARG, "%s: arguments are NULL", who);
+    const int B = p->B, Tq = p->Tq, Tk = p->Tk, Hq = p->Hq, Hk = p->Hk, D = p->D, es = p->is_bf16 ? 2 : 4;
+    LSGD_TRY(check_attention_shape(who, B, Tq, Tk, Hq, Hk, D));
+    if (p->is_bf16 & ~1 || p->causal & ~1) return set_error(LSGD_ERR_INVALID_ARG, "%s: is_bf16 and causal must be 0 or 1", who);
+    if (!std::isfinite(p->scale) || p->scale <= 0.0f) return set_error(LSGD_ERR_INVALID_ARG, "%s: scale must be finite and positive", who);
+    if (Tq == 0) return LSGD_OK;
+    if ((int64_t)B * Hk > INT64_C(1) << 30 || !fits(B, Tq, Tk, Hq, Hk, D)) return set_error(LSGD_ERR_SHAPE, "%s: B=%d, Tq=%d, Hk=%d are too large for one launch", who, B, Tq, Hk);
+    LSGD_TRY(check_heads(who, "q", p->q, B, Tq, Hq, D, es, true, false));
+    LSGD_TRY(check_heads(who, "k", p->k, B, Tk, Hk, D, es, Tk > 0 || p->k.data, false));
+    LSGD_TRY(check_heads(who, "v", p->v, B, Tk, Hk, D, es, Tk > 0 || p->v.data, false));
+    LSGD_TRY(check_heads(who, "out", p->out, B, Tq, Hq, D, es, true, true));
+    if (!on(p->q_lens, 4) || !on(p->k_lens, 4) || !on(p->lse, 4)) return set_error(LSGD_ERR_INVALID_ARG, "%s: q_lens, k_lens or lse is not aligned to its element", who);
+    const Plan plan = plan_of(B, Tq, Tk, Hq, Hk, D);
+    if (plan.splits > 1) {
+        if (!workspace) return set_error(LSGD_ERR_INVALID_ARG, "%s: workspace is NULL", who);
+        if (!on(workspace, kAlign)) return set_error(LSGD_ERR_INVALID_ARG, "%s: workspace must be 256-byte aligned", who);
+        if (workspace_bytes < plan.bytes) return set_error(LSGD_ERR_NOMEM, "%s: workspace of %zu bytes < %zu needed", who, workspace_bytes, plan.bytes);
+    }
+    Args g{};
+    g.q = heads(p->q); g.k = heads(p->k); g.v = heads(p->v); g.out = heads(p->out);
+    set_shape(g, *p);
+    g.lse = p->lse;
+    g.parts = plan.splits > 1 ? static_cast<float*>(workspace) : nullptr;
+    g.tiles = plan.tiles;
+    g.splits = plan.splits; g.chunk = plan.chunk;
+    g.scale = p->scale; g.c = p->scale * kLog2e;
+    // what is read by 16 bytes straight to LDS has to lie on them
+    const bool aligned = D % (16 / es) == 0 && wide_heads(p->k, B, Tk, Hk, es) && wide_heads(p->v, B, Tk, Hk, es);
+    by_type_and_parts(p->is_bf16, parts_of(D), [&](auto type, auto parts) {
+        launch<decltype(type), decltype(parts)::value>(g, plan, aligned, static_cast<hipStream_t>(hip_stream));
+    });
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return set_error(LSGD_ERR_HIP, "%s: %s", who, hipGetErrorString(e));
+    return LSGD_OK;
+}
+
+} // extern "C"

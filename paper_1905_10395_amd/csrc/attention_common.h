@@ -1,0 +1,347 @@
+// What the attention kernels share: fragments of the matrix instructions, tiles of rows in LDS, numbering of rows.
+//
+// Rows.  The query heads that share a key head see the same keys, so their queries are one list of rows: row r = t G + g is
+// query t of the head g of the G = Hq / Hk heads of a key head.  A unit is an entry and a key head.
+//
+// Matrix instructions take 32 x 32 results: A gives rows, B columns, both 8 elements a lane of a contraction of 16 (lane % 32: the row
+// or column; lane / 32 = h: contraction places 8 h .. 8 h + 7).  A lane holds of the result column lane % 32, rows
+// 8 (i / 4) + 4 h + i % 4, i = 0 .. 15.  So a product's result, rows becoming the contraction, is the next product's B as it lies in the
+// registers, if the other operand's contraction places are taken in the same order: 4 h .. 4 h + 3, then 8 + 4 h .. 8 + 4 h + 3 (of
+// 16).  One operand of every product stays in registers that way, the other passes through LDS.
+//
+// Tiles.  R rows of a tile lie in LDS as parts of 32 columns, [part][row][32], in pieces of 16 bytes; loads straight to LDS write
+// consecutive pieces, so rows cannot be padded: a row's pieces are stored in another order (exclusive or with part of the row's
+// number), such that the reads along rows and those along columns both spread over all banks.
+#pragma once
+
+#include <type_traits>
+
+#include "heads.h"
+#include "row_pieces.h"
+
+namespace lsgd {
+namespace attention {
+
+constexpr int kPart = 32;                   // columns of a part of a tile
+constexpr int kMaxColumns = 128;            // of a head
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) void* lds_ptr;
+typedef const __attribute__((address_space(1))) void* global_ptr;
+
+// Eight elements of an operand.
+template <class T> struct Frag;
+template <> struct Frag<uint16_t> { bf16x8 v; };
+template <> struct Frag<float> { v4f lo, hi; };
+
+__device__ __forceinline__ void multiply(f32x16& c, const Frag<uint16_t>& a, const Frag<uint16_t>& b)
+{
+    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, b.v, c, 0, 0, 0);
+}
+// fp32: instructions of a contraction of two, element e of both halves in each
+__device__ __forceinline__ void multiply(f32x16& c, const Frag<float>& a, const Frag<float>& b)
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.lo[e], b.lo[e], c, 0, 0, 0);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.hi[e], b.hi[e], c, 0, 0, 0);
+}
+
+// Half of a result's column as an operand: registers 8 k .. 8 k + 7.
+__device__ __forceinline__ void from_result(const f32x16& r, int k, Frag<uint16_t>& f)
+{
+    v4u q;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) q[e] = f32x2_to_bf16x2(r[8 * k + 2 * e], r[8 * k + 2 * e + 1]);
+    f.v = __builtin_bit_cast(bf16x8, q);
+}
+__device__ __forceinline__ void from_result(const f32x16& r, int k, Frag<float>& f)
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        f.lo[e] = r[8 * k + e];
+        f.hi[e] = r[8 * k + 4 + e];
+    }
+}
+
+// 16 bytes of a row of D columns from column c on, zeros past its end; any alignment.
+template <class T>
+__device__ __forceinline__ v4u load16(const T* row, int c, int D)
+{
+    constexpr int per = 16 / (int)sizeof(T);
+    if (c + per <= D) return *reinterpret_cast<const v4u_any*>(row + c);
+    v4u q = {0, 0, 0, 0};
+    if (c < D) {
+#pragma unroll
+        for (int e = 0; e < per - 1; ++e)
+            if (c + e < D) {
+                if constexpr (sizeof(T) == 4) q[e] = __float_as_uint(row[c + e]);
+                else q[e / 2] |= (uint32_t)row[c + e] << (16 * (e & 1));
+            }
+    }
+    return q;
+}
+// An operand's eight elements from memory.
+__device__ __forceinline__ void load_frag(const uint16_t* row, int c, int D, Frag<uint16_t>& f) { f.v = __builtin_bit_cast(bf16x8, load16(row, c, D)); }
+__device__ __forceinline__ void load_frag(const float* row, int c, int D, Frag<float>& f)
+{
+    f.lo = __builtin_bit_cast(v4f, load16(row, c, D));
+    f.hi = __builtin_bit_cast(v4f, load16(row, c + 4, D));
+}
+template <class T>
+__device__ __forceinline__ void no_frag(Frag<T>& f) { __builtin_memset(&f, 0, sizeof(f)); }
+
+// ---- tiles in LDS ----
+template <class T>
+struct Tile {
+    static constexpr int kPer = 16 / (int)sizeof(T);              // elements a piece
+    static constexpr int kPieces = kPart / kPer;                  // pieces of a part's row: 4, or 8 of fp32
+    static __device__ __forceinline__ int order(int row) { return sizeof(T) == 2 ? (row >> 2) & 3 : (row >> 1) & 7; }
+};
+template <class T>
+constexpr int tile_elements(int rows, int parts) { return rows * parts * kPart; }
+
+// Rows as an operand whose contraction are the columns: columns 16 s + 8 h .. + 7 of row `row`.
+__device__ __forceinline__ void read_row(const uint16_t* tile, int rows, int row, int h, int s, Frag<uint16_t>& f)
+{
+    const int piece = ((s & 1) * 2 + h) ^ Tile<uint16_t>::order(row);
+    f.v = *reinterpret_cast<const bf16x8*>(tile + ((s >> 1) * rows * kPart + row * kPart + piece * 8));
+}
+__device__ __forceinline__ void read_row(const float* tile, int rows, int row, int h, int s, Frag<float>& f)
+{
+    const int o = Tile<float>::order(row), p = (s & 1) * 4 + h * 2;
+    const int at = (s >> 1) * rows * kPart + row * kPart;
+    f.lo = *reinterpret_cast<const v4f*>(tile + (at + (p ^ o) * 4));
+    f.hi = *reinterpret_cast<const v4f*>(tile + (at + ((p + 1) ^ o) * 4));
+}
+// Columns as an operand whose contraction are the rows r0 .. r0 + 15 (a multiple of 16), in the order of a result's registers: column
+// 32 part + lane % 32.  bf16: the LDS transposing read (in every group of 16 lanes, lanes 4 k .. 4 k + 3 point at 16 elements of row k, and
+// lane i receives column i of the four rows).
+__device__ __forceinline__ void read_column(const uint16_t* tile, int rows, int r0, int lane, int part, Frag<uint16_t>& f)
+{
+    const int h = lane >> 5, i = lane & 15, row = r0 + 4 * h + (i >> 2), piece = ((lane & 16) >> 3) + ((i & 3) >> 1);
+    const uint16_t* base = tile + part * rows * kPart;
+    const int lo = row * kPart + (piece ^ Tile<uint16_t>::order(4 * h)) * 8 + (i & 1) * 4;
+    const int hi = (row + 8) * kPart + (piece ^ Tile<uint16_t>::order(8 + 4 * h)) * 8 + (i & 1) * 4;
+    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(base + lo));
+    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(base + hi));
+    const s16x8 v = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    f.v = __builtin_bit_cast(bf16x8, v);
+}
+__device__ __forceinline__ void read_column(const float* tile, int rows, int r0, int lane, int part, Frag<float>& f)
+{
+    const int h = lane >> 5, c = lane & 31;
+    const float* base = tile + part * rows * kPart;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int row = r0 + (e & 3) + 4 * h + 8 * (e >> 2);
+        const float x = base[row * kPart + ((c >> 2) ^ Tile<float>::order(row)) * 4 + (c & 3)];
+        if (e < 4) f.lo[e] = x;
+        else f.hi[e - 4] = x;
+    }
+}
+
+// Where the threads' pieces of a tile of R rows and PARTS parts come from.  A wavefront's load writes 64 consecutive pieces; wavefront
+// `wid` of `WAVES` takes every WAVES-th 64.
+template <class T, int R, int PARTS, int WAVES>
+struct TileLoad {
+    static constexpr int kPer = Tile<T>::kPer, kPieces = Tile<T>::kPieces;
+    static constexpr int kLoads = R * PARTS * kPieces / (64 * WAVES);
+    static_assert(kLoads * 64 * WAVES == R * PARTS * kPieces && R * kPieces % 64 == 0, "whole wavefronts' loads");
+
+    // f(load, first element of the wavefront's 64 pieces, row, column) for each of the thread's pieces
+    template <class F>
+    static __device__ __forceinline__ void each(int wid, int lane, F f)
+    {
+#pragma unroll
+        for (int c = 0; c < kLoads; ++c) {
+            const int first = (c * WAVES + wid) * 64, part = first / (R * kPieces);
+            const int row = (first % (R * kPieces) + lane) / kPieces, piece = (lane % kPieces) ^ Tile<T>::order(row);
+            f(c, first * kPer, row, part * kPart + piece * kPer);
+        }
+    }
+};
+
+// Straight to LDS (16-byte aligned rows, a whole number of pieces: one past the row's end becomes its last one; what that multiplies is
+// zero, or is not stored), or through registers.  src(row): the row's address.
+template <class T, int R, int PARTS, int WAVES, bool ALIGNED, class F>
+__device__ __forceinline__ void load_tile(T* tile, int wid, int lane, int D, F src)
+{
+    using L = TileLoad<T, R, PARTS, WAVES>;
+    if constexpr (ALIGNED) {
+        L::each(wid, lane, [&](int, int first, int row, int c) {
+            const int last = D - L::kPer;
+            __builtin_amdgcn_global_load_lds((global_ptr)(src(row) + (c < last ? c : last)), (lds_ptr)(tile + first), 16, 0, 0);
+        });
+    } else {
+        v4u q[L::kLoads];
+        L::each(wid, lane, [&](int i, int, int row, int c) { q[i] = load16(src(row), c, D); });
+        L::each(wid, lane, [&](int i, int first, int, int) { *reinterpret_cast<v4u*>(tile + (first + lane * L::kPer)) = q[i]; });
+    }
+}
+
+// The tile handed over: this wavefront's loads have arrived, everyone's part is there, and nobody reads the buffer that is filled next.
+__device__ __forceinline__ void tiles_barrier()
+{
+    __builtin_amdgcn_s_waitcnt(0x0070);                           // vmcnt 0, lgkmcnt 0
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// ---- rows ----
+// x / d for x < 2^31
+struct Divide {
+    uint32_t mul;
+    int shift;
+};
+inline Divide divide_by(int d)
+{
+    int l = 0;
+    while ((INT64_C(1) << l) < d) ++l;
+    return Divide{(uint32_t)(((UINT64_C(1) << (31 + l)) + (uint64_t)d - 1) / (uint64_t)d), 31 + l};
+}
+__device__ __forceinline__ int over(int x, const Divide& d) { return (int)(((uint64_t)(uint32_t)x * d.mul) >> d.shift); }
+
+// The value that the lane of the other half (lane exclusive or 32) holds.
+__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
+
+// Units a die, if all dies get (about) as many.
+inline int units_a_die(int units)
+{
+    const int each = (units + 7) / 8;
+    return 8 * each * 9 <= units * 10 ? each : 0;
+}
+// What a call is about; its entries' lengths are read on the device.
+struct Shape {
+    const int32_t *q_lens, *k_lens;
+    int Tq, Tk, Hq, Hk, D, G, rows;  // rows: Tq G
+    int units, causal;               // units: entries x key heads
+    int per_die;                     // units a die takes for itself, 0: any takes any
+    Divide by_g;
+};
+template <class A>
+void set_shape(Shape& g, const A& p)
+{
+    g.q_lens = p.q_lens; g.k_lens = p.k_lens;
+    g.Tq = p.Tq; g.Tk = p.Tk; g.Hq = p.Hq; g.Hk = p.Hk; g.D = p.D;
+    g.G = p.Hq / p.Hk; g.rows = p.Tq * g.G;
+    g.units = p.B * p.Hk; g.causal = p.causal;
+    g.by_g = divide_by(g.G);
+    g.per_die = units_a_die(g.units);
+}
+
+// A workgroup's unit, and its number among the unit's.  Workgroups go to the eight dies in turn, and each die has a cache of its own:
+// where units come out even, a die takes units of its own.
+struct Place {
+    int unit;
+    int64_t at;
+};
+__device__ __forceinline__ Place place_of(const Shape& g)
+{
+    if (g.per_die == 0) return Place{(int)(blockIdx.x % g.units), blockIdx.x / g.units};
+    const int at = blockIdx.x >> 3;
+    return Place{(int)(blockIdx.x & 7) * g.per_die + at % g.per_die, at / g.per_die};
+}
+inline int64_t workgroups(const Shape& g, int64_t each) { return each * (g.per_die ? 8 * g.per_die : g.units); }
+__device__ __forceinline__ int length_of(const int32_t* lens, int b, int most)
+{
+    const int n = lens ? lens[b] : most;
+    return n < 0 ? 0 : n > most ? most : n;
+}
+
+// Which queries and keys a tile of rows is about.
+struct Rows {
+    int b, hk, nq, nk;
+    int end;                         // keys from there on are seen by none of its rows
+};
+__device__ __forceinline__ Rows rows_of(const Shape& g, int unit, int r0, int n)
+{
+    Rows t;
+    t.b = unit / g.Hk;
+    t.hk = unit % g.Hk;
+    t.nq = length_of(g.q_lens, t.b, g.Tq);
+    t.nk = length_of(g.k_lens, t.b, g.Tk);
+    const int first = over(r0, g.by_g), r1 = r0 + n - 1 < g.rows ? r0 + n - 1 : g.rows - 1;
+    int last = over(r1, g.by_g);
+    if (last > t.nq - 1) last = t.nq - 1;
+    t.end = t.nk;
+    if (g.causal && last + t.nk - t.nq + 1 < t.nk) t.end = last + t.nk - t.nq + 1;
+    if (first > last || t.end < 0) t.end = 0;
+    return t;
+}
+
+// A lane's row: its query and head, and how many keys it sees.
+struct Row {
+    int t, head, sees;
+    bool there;
+};
+__device__ __forceinline__ Row row_of(const Shape& g, const Rows& rows, int r)
+{
+    Row q;
+    q.there = r < g.rows;
+    if (!q.there) r = g.rows - 1;
+    q.t = over(r, g.by_g);
+    q.head = rows.hk * g.G + r - q.t * g.G;
+    q.sees = rows.nk;
+    if (g.causal && q.t + rows.nk - rows.nq + 1 < q.sees) q.sees = q.t + rows.nk - rows.nq + 1;
+    if (q.t >= rows.nq || q.sees < 0) q.sees = 0;
+    return q;
+}
+
+__device__ __forceinline__ int wave_min(int x)
+{
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) x = min(x, __shfl_xor(x, d));
+    return __builtin_amdgcn_readfirstlane(x);
+}
+__device__ __forceinline__ int wave_max(int x)
+{
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) x = max(x, __shfl_xor(x, d));
+    return __builtin_amdgcn_readfirstlane(x);
+}
+
+// Four columns of a row, as many of them as it has.
+template <class T>
+__device__ __forceinline__ void store4(T* row, int c, int D, const float (&v)[4])
+{
+    if (c + 4 <= D) put4(row + c, v);
+    else
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+            if (c + e < D) put1(row + c + e, v[e]);
+}
+
+// ---- host ----
+constexpr size_t kAlign = 256;
+constexpr int kMaxEntries = 1 << 20, kMaxTokens = 1 << 24, kMaxHeads = 1024;
+
+#define LSGD_TRY(x)                         \
+    do {                                    \
+        const lsgd_status st_ = (x);        \
+        if (st_ != LSGD_OK) return st_;     \
+    } while (0)
+
+lsgd_status check_attention_shape(const char* who, int64_t B, int64_t Tq, int64_t Tk, int64_t Hq, int64_t Hk, int64_t D);
+inline int parts_of(int D) { return (D + kPart - 1) / kPart; }
+
+template <class F>
+void by_type_and_parts(bool bf16, int parts, F f)
+{
+    auto typed = [&](auto type) {
+        if (parts == 1) f(type, std::integral_constant<int, 1>{});
+        else if (parts == 2) f(type, std::integral_constant<int, 2>{});
+        else if (parts == 3) f(type, std::integral_constant<int, 3>{});
+        else f(type, std::integral_constant<int, 4>{});
+    };
+    if (bf16) typed(uint16_t{});
+    else typed(float{});
+}
+
+} // namespace attention
+} // namespace lsgd
