@@ -145,25 +145,16 @@ __device__ __forceinline__ void read_column(const float* tile, int rows, int r0,
     }
 }
 
-// Where the threads' pieces of a tile of R rows and PARTS parts come from.  A wavefront's load writes 64 consecutive pieces; wavefront
-// `wid` of `WAVES` takes every WAVES-th 64.
+// Where the threads' pieces of a tile of R rows and PARTS parts come from.  A wavefront's load writes 64 consecutive pieces, all of one
+// part; wavefront `wid` of `WAVES` takes every WAVES-th 64, so a thread has the same GROUPS rows and the same piece of them in every part.
 template <class T, int R, int PARTS, int WAVES>
 struct TileLoad {
     static constexpr int kPer = Tile<T>::kPer, kPieces = Tile<T>::kPieces;
-    static constexpr int kLoads = R * PARTS * kPieces / (64 * WAVES);
-    static_assert(kLoads * 64 * WAVES == R * PARTS * kPieces && R * kPieces % 64 == 0, "whole wavefronts' loads");
-
-    // f(load, first element of the wavefront's 64 pieces, row, column) for each of the thread's pieces
-    template <class F>
-    static __device__ __forceinline__ void each(int wid, int lane, F f)
-    {
-#pragma unroll
-        for (int c = 0; c < kLoads; ++c) {
-            const int first = (c * WAVES + wid) * 64, part = first / (R * kPieces);
-            const int row = (first % (R * kPieces) + lane) / kPieces, piece = (lane % kPieces) ^ Tile<T>::order(row);
-            f(c, first * kPer, row, part * kPart + piece * kPer);
-        }
-    }
+    static constexpr int kGroups = R * kPieces / (64 * WAVES), kLoads = kGroups * PARTS;
+    static_assert(kGroups * 64 * WAVES == R * kPieces, "whole wavefronts' loads");
+    static __device__ __forceinline__ int row(int group, int wid, int lane) { return ((group * WAVES + wid) * 64 + lane) / kPieces; }
+    static __device__ __forceinline__ int column(int group, int wid, int lane) { return ((lane % kPieces) ^ Tile<T>::order(row(group, wid, lane))) * kPer; }
+    static __device__ __forceinline__ int first(int group, int part, int wid) { return part * R * kPart + (group * WAVES + wid) * 64 * kPer; }
 };
 
 // Straight to LDS (16-byte aligned rows, a whole number of pieces: one past the row's end becomes its last one; what that multiplies is
@@ -173,14 +164,28 @@ __device__ __forceinline__ void load_tile(T* tile, int wid, int lane, int D, F s
 {
     using L = TileLoad<T, R, PARTS, WAVES>;
     if constexpr (ALIGNED) {
-        L::each(wid, lane, [&](int, int first, int row, int c) {
-            const int last = D - L::kPer;
-            __builtin_amdgcn_global_load_lds((global_ptr)(src(row) + (c < last ? c : last)), (lds_ptr)(tile + first), 16, 0, 0);
-        });
+#pragma unroll
+        for (int g = 0; g < L::kGroups; ++g) {
+            const int c = L::column(g, wid, lane), end = D - L::kPer - (PARTS - 1) * kPart;
+            const T* p = src(L::row(g, wid, lane)) + c;
+#pragma unroll
+            for (int part = 0; part < PARTS; ++part) {
+                if (part == PARTS - 1) p -= c > end ? c - end : 0;
+                __builtin_amdgcn_global_load_lds((global_ptr)(p + part * kPart), (lds_ptr)(tile + L::first(g, part, wid)), 16, 0, 0);
+            }
+        }
     } else {
         v4u q[L::kLoads];
-        L::each(wid, lane, [&](int i, int, int row, int c) { q[i] = load16(src(row), c, D); });
-        L::each(wid, lane, [&](int i, int first, int, int) { *reinterpret_cast<v4u*>(tile + (first + lane * L::kPer)) = q[i]; });
+#pragma unroll
+        for (int g = 0; g < L::kGroups; ++g) {
+            const T* p = src(L::row(g, wid, lane));
+#pragma unroll
+            for (int part = 0; part < PARTS; ++part) q[g * PARTS + part] = load16(p, part * kPart + L::column(g, wid, lane), D);
+        }
+#pragma unroll
+        for (int g = 0; g < L::kGroups; ++g)
+#pragma unroll
+            for (int part = 0; part < PARTS; ++part) *reinterpret_cast<v4u*>(tile + (L::first(g, part, wid) + lane * L::kPer)) = q[g * PARTS + part];
     }
 }
 

@@ -2,6 +2,9 @@
 //
 //   p = 2^(c s - z),  s = q . k;   dv = p' dout;   dp = dout . v;   ds = p (dp - delta);   dq = scale ds k;   dk = scale ds' q
 //
+// z / c and delta are taken off where the products begin: their negatives are what the accumulators hold first.  (fp32's s begins with
+// zero: its chain of D / 2 sums would round at the size of z / c each time, which the 8 of bf16 can bear.)
+//
 // Two passes over the pairs, so that every sum has one owner and an order of its own: no atomics, equal calls give equal bits.  By
 // rows: 32 rows a wavefront keep q, dout and the sums for dq in registers while K and V tiles pass through LDS; it makes delta on the way and
 // leaves z and delta to the other.  By keys: 32 keys a wavefront keep k, v and the sums for dk and dv while tiles of q and dout
@@ -22,18 +25,20 @@ namespace {
 struct Args : Shape {
     Heads dout, q, k, v, out, dq, dk, dv;
     const float* lse;                // [B][Hq][Tq]
-    float *z, *delta;                // [units][row_tiles 128]; z: +inf for rows that see nothing
+    float *z, *delta;                // [units][row_tiles 128]: -z / c (fp32: -z), -inf for rows that see nothing, and -delta
     float *dq_parts, *dkv_parts;     // of splits, NULL: one
     int row_tiles, key_tiles;
     int row_splits, row_chunk;       // by rows: workgroups a tile, and the keys of one
     int key_splits, key_chunk;       // by keys: workgroups a tile, and the rows of one
-    float scale, c;
+    float scale, inv_scale, c;
 };
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr int kMine = 32 * kWaves;                       // rows, or keys, that a workgroup owns
 template <class T>
 constexpr int kPass = sizeof(T) == 2 ? 64 : 32;          // keys, or rows, of the tiles that pass
+template <class T>
+constexpr bool kFromZ = sizeof(T) == 2;                  // s begins with -z / c
 
 template <class T, int PARTS>
 __device__ __forceinline__ void load_frags(const T* row, bool live, int h, int D, Frag<T> (&f)[2 * PARTS])
@@ -58,12 +63,10 @@ __device__ __forceinline__ float dot(const Frag<float>& a, const Frag<float>& b)
     for (int e = 0; e < 4; ++e) s += a.lo[e] * b.lo[e] + a.hi[e] * b.hi[e];
     return s;
 }
-// A product of 32 rows of a tile, from row r0 on, with an operand in registers.
+// c += the product of 32 rows of a tile, from row r0 on, with an operand in registers.
 template <class T, int PARTS>
 __device__ __forceinline__ void rows_times(const T* tile, int rows, int r0, int lane, const Frag<T> (&b)[2 * PARTS], f32x16& c)
 {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) c[i] = 0.0f;
 #pragma unroll
     for (int k = 0; k < 2 * PARTS; ++k) {
         Frag<T> f;
@@ -123,7 +126,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(Args g)
     const Row row = row_of(g, rows, r);
     const int least = wave_min(row.sees), most = wave_max(row.sees);
     Frag<T> qf[2 * PARTS], df[2 * PARTS];
-    float z = INFINITY, delta = 0.0f;
+    float z = -INFINITY, delta = 0.0f;                                     // negative, as the accumulators begin
     {
         const T* q = static_cast<const T*>(g.q.p) + rows.b * g.q.lb + row.t * g.q.lt + row.head * g.q.lh;
         const T* d = static_cast<const T*>(g.dout.p) + rows.b * g.dout.lb + row.t * g.dout.lt + row.head * g.dout.lh;
@@ -135,14 +138,14 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(Args g)
             for (int k = 0; k < 2 * PARTS; ++k) {
                 Frag<T> f;
                 load_frag(o, 16 * k + 8 * h, g.D, f);
-                delta += dot(f, df[k]);
+                delta -= dot(f, df[k]);
             }
-            z = g.lse[((int64_t)rows.b * g.Hq + row.head) * g.Tq + row.t] * kLog2e;
+            z = -g.lse[((int64_t)rows.b * g.Hq + row.head) * g.Tq + row.t] * (kFromZ<T> ? g.inv_scale : kLog2e);
         }
         delta += other_half(delta);
         if (split == 0 && h == 0) {
             const int64_t to = (int64_t)at.unit * g.row_tiles * kMine + r;
-            g.z[to] = row.there ? z : INFINITY;
+            g.z[to] = row.there ? z : -INFINITY;
             g.delta[to] = row.there ? delta : 0.0f;
         }
     }
@@ -164,13 +167,15 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(Args g)
 #pragma unroll
         for (int n = 0; n < KEYS / 32; ++n) {
             f32x16 s, dp;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[i] = kFromZ<T> ? z : 0.0f;
+                dp[i] = delta;
+            }
             rows_times<T, PARTS>(kb, KEYS, 32 * n, lane, qf, s);
             rows_times<T, PARTS>(vb, KEYS, 32 * n, lane, df, dp);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float p = __builtin_amdgcn_exp2f(fmaf(s[i], g.c, -z));
-                dp[i] = p * (dp[i] - delta);
-            }
+            for (int i = 0; i < 16; ++i) dp[i] *= __builtin_amdgcn_exp2f(kFromZ<T> ? s[i] * g.c : fmaf(s[i], g.c, z));
             if (masked) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) dp[i] = key0 + 32 * n + 8 * (i >> 2) + 4 * h + (i & 3) < row.sees ? dp[i] : 0.0f;
@@ -245,28 +250,39 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dkv_kernel(Args g)
         if (r0 + ROWS < end) issue(r0 + ROWS, next_q, next_d, next_z, next_e);
         if (r0 + ROWS <= least) return;
         const bool masked = r0 < most;
-#pragma unroll
+#pragma unroll 1
         for (int n = 0; n < ROWS / 32; ++n) {
             f32x16 s, dp;
-            rows_times<T, PARTS>(qb, ROWS, 32 * n, lane, kf, s);
+            auto begin_with = [&](const float* first, f32x16& c) {
 #pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-                const v4f zr = *reinterpret_cast<const v4f*>(zb + 32 * n + 2 * i + 4 * h);
+                for (int i = 0; i < 16; i += 4) {
+                    const v4f x = *reinterpret_cast<const v4f*>(first + 32 * n + 2 * i + 4 * h);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[i + e] = __builtin_amdgcn_exp2f(fmaf(s[i + e], g.c, -zr[e]));
+                    for (int e = 0; e < 4; ++e) c[i + e] = x[e];
+                }
+            };
+            if constexpr (kFromZ<T>) {
+                begin_with(zb, s);
+                rows_times<T, PARTS>(qb, ROWS, 32 * n, lane, kf, s);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i] * g.c);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+                rows_times<T, PARTS>(qb, ROWS, 32 * n, lane, kf, s);
+                begin_with(zb, dp);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], g.c, dp[i]));
             }
             if (masked) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[i] = r0 + 32 * n + 8 * (i >> 2) + 4 * h + (i & 3) >= from ? s[i] : 0.0f;
             }
             columns_times<T, PARTS>(db, ROWS, 32 * n, lane, s, dv);
+            begin_with(eb, dp);
             rows_times<T, PARTS>(db, ROWS, 32 * n, lane, vf, dp);
 #pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-                const v4f er = *reinterpret_cast<const v4f*>(eb + 32 * n + 2 * i + 4 * h);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) dp[i + e] = s[i + e] * (dp[i + e] - er[e]);
-            }
+            for (int i = 0; i < 16; ++i) dp[i] *= s[i];
             columns_times<T, PARTS>(qb, ROWS, 32 * n, lane, dp, dk);
         }
     };
@@ -427,7 +443,7 @@ lsgd_status lsgd_attention_grad(const lsgd_attention_grad_args* p, void* workspa
     g.row_tiles = plan.row_tiles; g.key_tiles = plan.key_tiles;
     g.row_splits = plan.row_splits; g.row_chunk = plan.row_chunk;
     g.key_splits = plan.key_splits; g.key_chunk = plan.key_chunk;
-    g.scale = p->scale; g.c = p->scale * kLog2e;
+    g.scale = p->scale; g.inv_scale = 1.0f / p->scale; g.c = p->scale * kLog2e;
     // what is read by 16 bytes straight to LDS has to lie on them
     const bool whole = D % (16 / es) == 0;
     const bool aligned_rows = whole && wide_heads(p->q, B, Tq, Hq, es) && wide_heads(p->dout, B, Tq, Hq, es);
