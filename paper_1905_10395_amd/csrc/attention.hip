@@ -9,8 +9,8 @@
 //
 // Two kernels.  By rows: a workgroup takes 128 rows (query, head of the key head's), 32 a wavefront, and all pass over the keys
 // together; K and V tiles are read by all four from LDS, the next ones are on their way meanwhile.  By keys: where there are few rows,
-// a workgroup takes 32 of them, and its wavefronts and further workgroups split the keys; each wavefront has tiles of its own
-// and waits for nobody, and the parts are joined at the end.
+// a workgroup takes 32 of them, and its wavefronts and further workgroups split the keys; each wavefront has tiles of its own and waits
+// for nobody, and the parts are joined at the end.
 #include <algorithm>
 #include <cmath>
 
@@ -45,25 +45,27 @@ struct State {
 
 constexpr float kSlack = 8.0f;       // powers of two
 
-// KEYS keys of tiles kt and vt.  masked: some row does not see some of them.
-template <class T, int PARTS, int KEYS>
-__device__ __forceinline__ void pass_tile(const T* kt, const T* vt, int lane, int key0, int sees, bool masked, float c, const Frag<T> (&qf)[2 * PARTS],
-                                          State<PARTS>& st)
+// How far operands are read ahead; fp32's instructions take long enough without.
+template <class T>
+constexpr int kAhead = sizeof(T) == 2 ? 4 : 1;
+
+// KEYS keys of a tile: their p of the lane's row, and the state's reference moved if need be.  masked: some row does not see some of
+// them.  then() is called when the products are on their way.
+template <class T, int PARTS, int KEYS, class F>
+__device__ __forceinline__ void pass_keys(const T* kt, int lane, int key0, int sees, bool masked, float c, const Frag<T> (&qf)[2 * PARTS], State<PARTS>& st,
+                                          f32x16 (&s)[KEYS / 32], F then)
 {
     constexpr int NS = KEYS / 32;
     const int h = lane >> 5;
-    f32x16 s[NS];
 #pragma unroll
-    for (int n = 0; n < NS; ++n) {
+    for (int n = 0; n < NS; ++n)
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[n][i] = 0.0f;
-#pragma unroll
-        for (int k = 0; k < 2 * PARTS; ++k) {
-            Frag<T> f;
-            read_row(kt, KEYS, 32 * n + (lane & 31), h, k, f);
-            multiply(s[n], f, qf[k]);
-        }
-    }
+    Ahead<T, NS * 2 * PARTS, kAhead<T>> ops;
+    auto read = [&](int i, Frag<T>& f) { read_row(kt, KEYS, 32 * (i % NS) + (lane & 31), h, i / NS, f); };
+    ops.start(read);
+    ops.run(read, [&](int i, const Frag<T>& f) { multiply(s[i % NS], f, qf[i / NS]); });
+    then();
     if (masked) {
 #pragma unroll
         for (int n = 0; n < NS; ++n)
@@ -93,28 +95,34 @@ __device__ __forceinline__ void pass_tile(const T* kt, const T* vt, int lane, in
             s[n][i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], c, -mc));
             st.l += s[n][i];
         }
-#pragma unroll
-    for (int k = 0; k < KEYS / 16; ++k) {
-        Frag<T> p;
-        from_result(s[k / 2], k % 2, p);
-#pragma unroll
-        for (int part = 0; part < PARTS; ++part) {
-            Frag<T> f;
-            read_column(vt, KEYS, 16 * k, lane, part, f);
-            multiply(st.o[part], f, p);
-        }
-    }
 }
+// Their values, times p.
+template <class T, int PARTS, int KEYS>
+struct Values {
+    Ahead<T, KEYS / 16 * PARTS, kAhead<T>> ops;
+    const T* vt;
+    const int lane;
+    __device__ __forceinline__ Values(const T* tile, int l) : vt(tile), lane(l) {}
+    __device__ __forceinline__ void start()
+    {
+        ops.start([&](int i, Frag<T>& f) { read_column(vt, KEYS, 16 * (i / PARTS), lane, i % PARTS, f); });
+    }
+    __device__ __forceinline__ void pass(const f32x16 (&s)[KEYS / 32], State<PARTS>& st)
+    {
+        Frag<T> p[KEYS / 16];
+#pragma unroll
+        for (int k = 0; k < KEYS / 16; ++k) from_result(s[k / 2], k % 2, p[k]);
+        ops.run([&](int i, Frag<T>& f) { read_column(vt, KEYS, 16 * (i / PARTS), lane, i % PARTS, f); },
+                [&](int i, const Frag<T>& f) { multiply(st.o[i % PARTS], f, p[i / PARTS]); });
+    }
+};
 
 template <class T, int PARTS>
 __device__ __forceinline__ void load_queries(const Args& g, const Rows& rows, const Row& row, int h, Frag<T> (&qf)[2 * PARTS])
 {
     const T* q = static_cast<const T*>(g.q.p) + rows.b * g.q.lb + row.t * g.q.lt + row.head * g.q.lh;
-#pragma unroll
-    for (int k = 0; k < 2 * PARTS; ++k) {
-        if (row.sees) load_frag(q, 16 * k + 8 * h, g.D, qf[k]);
-        else no_frag(qf[k]);
-    }
+    if (row.sees) load_frags<T, PARTS>(q, h, g.D, qf);
+    else clear_frags<T, PARTS>(qf);
 }
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
@@ -130,8 +138,8 @@ __global__ __launch_bounds__(kThreads, 2) void attention_rows_kernel(Args g)
     __shared__ __attribute__((aligned(16))) T k0[tile_elements<T>(KEYS, PARTS)], k1[tile_elements<T>(KEYS, PARTS)];
     __shared__ __attribute__((aligned(16))) T v0[tile_elements<T>(KEYS, PARTS)], v1[tile_elements<T>(KEYS, PARTS)];
     const int lane = threadIdx.x & 63, h = lane >> 5, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const Place at = place_of(g);
-    const int unit = at.unit, tile = g.tiles - 1 - (int)at.at;             // late rows see most keys: first
+    const Place at = place_of(g, g.tiles);
+    const int unit = at.unit, tile = g.tiles - 1 - at.at;            // late rows see most keys: first
     if (unit >= g.units) return;
     const Rows rows = rows_of(g, unit, tile * kRowsByRows, kRowsByRows);
     const Row row = row_of(g, rows, tile * kRowsByRows + wid * 32 + (lane & 31));
@@ -149,7 +157,11 @@ __global__ __launch_bounds__(kThreads, 2) void attention_rows_kernel(Args g)
     auto step = [&](int key0, T* kb, T* vb, T* next_k, T* next_v) {
         tiles_barrier();
         if (key0 + KEYS < rows.end) issue(key0 + KEYS, next_k, next_v);
-        if (key0 < most) pass_tile<T, PARTS, KEYS>(kb, vb, lane, key0, row.sees, key0 + KEYS > least, g.c, qf, st);
+        if (key0 >= most) return;
+        f32x16 p[KEYS / 32];
+        Values<T, PARTS, KEYS> values(vb, lane);
+        pass_keys<T, PARTS, KEYS>(kb, lane, key0, row.sees, key0 + KEYS > least, g.c, qf, st, p, [&] { values.start(); });
+        values.pass(p, st);
     };
     if (rows.end > 0) issue(0, k0, v0);
     for (int key0 = 0; key0 < rows.end; key0 += 2 * KEYS) {
@@ -170,97 +182,102 @@ __global__ __launch_bounds__(kThreads, 2) void attention_rows_kernel(Args g)
 }
 
 // ---- by keys ----
-template <class T, int PARTS>
-constexpr int kWavesByKeys = sizeof(T) == 4 && PARTS > 2 ? 2 : 4;   // as many as their tiles leave room for
-constexpr int kRowsByKeys = 32, kKeysByKeys = 32;
+constexpr int kRowsByKeys = 32, kKeysByKeys = 32, kRowsJoined = 4;
 
 // A split's part: sums relative to m, [32][parts of 32], then m and l of each row.
 __host__ __device__ constexpr int part_floats(int parts) { return kRowsByKeys * (parts * kPart + 2); }
 
-template <class T, int PARTS, bool ALIGNED>
-__global__ __launch_bounds__((64 * kWavesByKeys<T, PARTS>), 1) void attention_keys_kernel(Args g)
+// All but the N youngest loads of the wavefront have arrived, and all reads of LDS.
+template <int N>
+__device__ __forceinline__ void wait_loads()
 {
-    constexpr int W = kWavesByKeys<T, PARTS>, KEYS = kKeysByKeys, N = tile_elements<T>(KEYS, PARTS);
-    __shared__ __attribute__((aligned(16))) T k0[W][N], k1[W][N];
-    __shared__ __attribute__((aligned(16))) T v0[W][N], v1[W][N];
-    __shared__ float sums[W][kRowsByKeys][kPart + 1], tops[W][kRowsByKeys], ls[W][kRowsByKeys];
+    __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x0070);
+    asm volatile("" ::: "memory");
+}
+
+// Each wavefront has one K tile and one V tile: the next K tile is on its way while the values are passed, the next V tile while the keys
+// are, so that two workgroups' wavefronts fit a compute unit.
+template <class T, int PARTS, bool ALIGNED>
+__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_keys_kernel(Args g)
+{
+    constexpr int W = kWaves, KEYS = kKeysByKeys, N = tile_elements<T>(KEYS, PARTS), COLS = PARTS * kPart;
+    __shared__ __attribute__((aligned(16))) T kt[W][N];
+    __shared__ __attribute__((aligned(16))) T vt[W][N];
+    __shared__ float sums[W][kRowsJoined][COLS + 1], tops[W][kRowsByKeys], ls[W][kRowsByKeys];
     const int lane = threadIdx.x & 63, h = lane >> 5, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    int64_t id = blockIdx.x;
-    const int split = (int)(id % g.splits);
-    id /= g.splits;
-    const int tile = g.tiles - 1 - (int)(id % g.tiles), unit = (int)(id / g.tiles);
+    // units in turn: were it splits, those that only long entries have would all go to the same dies
+    const int unit = (int)(blockIdx.x % g.units), at = (int)(blockIdx.x / g.units);
+    const int tile = g.tiles - 1 - at % g.tiles, split = at / g.tiles;
     const Rows rows = rows_of(g, unit, tile * kRowsByKeys, kRowsByKeys);
     const Row row = row_of(g, rows, tile * kRowsByKeys + (lane & 31));
     const int begin = split * g.chunk, end = min(begin + g.chunk, rows.end);
     const int least = wave_min(row.sees);
     State<PARTS> st;
     if (begin + wid * KEYS < end) {
-        Frag<T> qf[2 * PARTS];
-        load_queries<T, PARTS>(g, rows, row, h, qf);
         const T* k = static_cast<const T*>(g.k.p) + rows.b * g.k.lb + rows.hk * g.k.lh;
         const T* v = static_cast<const T*>(g.v.p) + rows.b * g.v.lb + rows.hk * g.v.lh;
-        auto issue = [&](int key0, T* kb, T* vb) {
-            auto key = [&](int r) { return key0 + r < rows.nk ? key0 + r : rows.nk - 1; };
-            load_tile<T, KEYS, PARTS, 1, ALIGNED>(kb, 0, lane, g.D, [&](int r) { return k + key(r) * g.k.lt; });
-            load_tile<T, KEYS, PARTS, 1, ALIGNED>(vb, 0, lane, g.D, [&](int r) { return v + key(r) * g.v.lt; });
+        // (behind the last tile too, the last key again and again: under a condition the compiler waits for all loads before it reads)
+        auto load = [&](const T* from, int64_t lt, int key0, T* to) {
+            load_tile<T, KEYS, PARTS, 1, ALIGNED>(to, 0, lane, g.D, [&](int r) { return from + (key0 + r < rows.nk ? key0 + r : rows.nk - 1) * lt; });
         };
-        auto step = [&](int key0, T* kb, T* vb, T* next_k, T* next_v) {
-            __builtin_amdgcn_s_waitcnt(0xC07F);                    // lgkmcnt 0: the next buffers have been read
-            asm volatile("" ::: "memory");
-            if (key0 + W * KEYS < end) {
-                issue(key0 + W * KEYS, next_k, next_v);
-                constexpr int later = 2 * TileLoad<T, KEYS, PARTS, 1>::kLoads;
-                if constexpr (ALIGNED) __builtin_amdgcn_s_waitcnt((later & 15) | ((later >> 4) << 14) | 0x0F70);    // this tile is there
-            } else {
-                __builtin_amdgcn_s_waitcnt(0x0F70);
-            }
-            asm volatile("" ::: "memory");
-            pass_tile<T, PARTS, KEYS>(kb, vb, lane, key0, row.sees, key0 + KEYS > least, g.c, qf, st);
-        };
-        const int first = begin + wid * KEYS;
-        issue(first, k0[wid], v0[wid]);
-        for (int key0 = first; key0 < end; key0 += 2 * W * KEYS) {
-            step(key0, k0[wid], v0[wid], k1[wid], v1[wid]);
-            if (key0 + W * KEYS < end) step(key0 + W * KEYS, k1[wid], v1[wid], k0[wid], v0[wid]);
+        constexpr int later = ALIGNED ? TileLoad<T, KEYS, PARTS, 1>::kLoads : 0;
+        Frag<T> qf[2 * PARTS];
+        load_queries<T, PARTS>(g, rows, row, h, qf);
+        load(k, g.k.lt, begin + wid * KEYS, kt[wid]);
+        load(v, g.v.lt, begin + wid * KEYS, vt[wid]);
+        for (int key0 = begin + wid * KEYS; key0 < end; key0 += W * KEYS) {
+            f32x16 p[1];
+            Values<T, PARTS, KEYS> values(vt[wid], lane);
+            wait_loads<later>();
+            pass_keys<T, PARTS, KEYS>(kt[wid], lane, key0, row.sees, key0 + KEYS > least, g.c, qf, st, p, [] {});
+            wait_loads<later>();
+            load(k, g.k.lt, key0 + W * KEYS, kt[wid]);
+            wait_loads<later>();
+            values.start();
+            values.pass(p, st);
+            wait_loads<later>();
+            load(v, g.v.lt, key0 + W * KEYS, vt[wid]);
         }
     }
-    // the wavefronts' sums, 32 columns at a time
+    // the wavefronts' sums, a few rows at a time
     const float l = st.l + other_half(st.l);
     if (h == 0) {
         tops[wid][lane] = st.m;
         ls[wid][lane] = l;
     }
     float* const part = g.parts ? g.parts + (((int64_t)unit * g.tiles + tile) * g.splits + split) * part_floats(PARTS) : nullptr;
+    const int live = min(kRowsByKeys, g.rows - tile * kRowsByKeys);
+    for (int r0 = 0; r0 < live; r0 += kRowsJoined) {
+        const int mine = (lane & 31) - r0;
+        __syncthreads();                                           // (the last rows' sums have been read)
+        if (mine >= 0 && mine < kRowsJoined) {
 #pragma unroll
-    for (int p = 0; p < PARTS; ++p) {
+            for (int p = 0; p < PARTS; ++p)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sums[wid][lane & 31][8 * (i >> 2) + 4 * h + (i & 3)] = st.o[p][i];
+                for (int i = 0; i < 16; ++i) sums[wid][mine][p * kPart + 8 * (i >> 2) + 4 * h + (i & 3)] = st.o[p][i];
+        }
         __syncthreads();
-#pragma unroll
-        for (int i = threadIdx.x; i < kRowsByKeys * kPart; i += 64 * W) {
-            const int r = i / kPart, c = i % kPart;
+        for (int i = threadIdx.x; i < min(kRowsJoined, live - r0) * COLS; i += kThreads) {
+            const int q = i / COLS, c = i % COLS, r = r0 + q;
             float m = tops[0][r], o = 0.0f, n = 0.0f;
 #pragma unroll
             for (int w = 1; w < W; ++w) m = fmaxf(m, tops[w][r]);
 #pragma unroll
             for (int w = 0; w < W; ++w) {
                 const float a = tops[w][r] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((tops[w][r] - m) * g.c);
-                o += a * sums[w][r][c];
+                o += a * sums[w][q][c];
                 n += a * ls[w][r];
             }
-            const Row to = row_of(g, rows, tile * kRowsByKeys + r);
-            if (!to.there) continue;
             if (part) {
-                if (n > 0.0f) part[r * (PARTS * kPart) + p * kPart + c] = o;
-                if (p == 0 && c < 2) part[kRowsByKeys * PARTS * kPart + 2 * r + c] = c ? n : m;
+                if (n > 0.0f) part[r * COLS + c] = o;
+                if (c < 2) part[kRowsByKeys * COLS + 2 * r + c] = c ? n : m;
             } else {
-                if (p * kPart + c < g.D)
-                    put1(static_cast<T*>(g.out.p) + rows.b * g.out.lb + to.t * g.out.lt + to.head * g.out.lh + p * kPart + c, n > 0.0f ? o / n : 0.0f);
-                if (p == 0 && c == 0 && g.lse)
-                    g.lse[((int64_t)rows.b * g.Hq + to.head) * g.Tq + to.t] = n > 0.0f ? m * g.scale + logf(n) : -INFINITY;
+                const Row to = row_of(g, rows, tile * kRowsByKeys + r);
+                if (c < g.D)
+                    put1(static_cast<T*>(g.out.p) + rows.b * g.out.lb + to.t * g.out.lt + to.head * g.out.lh + c, n > 0.0f ? o / n : 0.0f);
+                if (c == 0 && g.lse) g.lse[((int64_t)rows.b * g.Hq + to.head) * g.Tq + to.t] = n > 0.0f ? m * g.scale + logf(n) : -INFINITY;
             }
         }
-        __syncthreads();
     }
 }
 
@@ -342,7 +359,7 @@ void launch(const Args& g, const Plan& p, bool aligned, hipStream_t s)
         else hipLaunchKernelGGL((attention_rows_kernel<T, PARTS, false>), grid, dim3(kThreads), 0, s, g);
         return;
     }
-    const dim3 grid((unsigned)((int64_t)g.units * g.tiles * g.splits)), threads(64 * kWavesByKeys<T, PARTS>);
+    const dim3 grid((unsigned)((int64_t)g.units * g.tiles * g.splits)), threads(kThreads);
     if (aligned) hipLaunchKernelGGL((attention_keys_kernel<T, PARTS, true>), grid, threads, 0, s, g);
     else hipLaunchKernelGGL((attention_keys_kernel<T, PARTS, false>), grid, threads, 0, s, g);
     if (g.splits > 1) hipLaunchKernelGGL((attention_join_kernel<T, PARTS>), dim3((unsigned)((int64_t)g.units * g.tiles)), dim3(kThreads), 0, s, g);

@@ -68,32 +68,66 @@ __device__ __forceinline__ void from_result(const f32x16& r, int k, Frag<float>&
     }
 }
 
-// 16 bytes of a row of D columns from column c on, zeros past its end; any alignment.
-template <class T>
+// 16 bytes of a row of D columns from column c on, zeros past its end; any alignment.  A piece that the row's end cuts is read so that
+// it ends with the row, and moved to its place.  EDGE: it may be cut, or lie behind the end.
+template <bool EDGE, class T>
 __device__ __forceinline__ v4u load16(const T* row, int c, int D)
 {
     constexpr int per = 16 / (int)sizeof(T);
-    if (c + per <= D) return *reinterpret_cast<const v4u_any*>(row + c);
-    v4u q = {0, 0, 0, 0};
-    if (c < D) {
+    if constexpr (!EDGE) return *reinterpret_cast<const v4u_any*>(row + c);
+    else if (D >= per) {
+        const int over = c + per - D;
+        v4u q = *reinterpret_cast<const v4u_any*>(row + (over > 0 ? D - per : c));
+        if (over > 0) {
+            const int bits = 8 * (int)sizeof(T) * over;
+            uint64_t lo = q[0] | (uint64_t)q[1] << 32, hi = q[2] | (uint64_t)q[3] << 32;
+            if (bits >= 128) lo = hi = 0;
+            else if (bits >= 64) {
+                lo = hi >> (bits - 64);
+                hi = 0;
+            } else {
+                lo = lo >> bits | hi << (64 - bits);
+                hi >>= bits;
+            }
+            q = v4u{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+        }
+        return q;
+    } else {
+        v4u q = {0, 0, 0, 0};
 #pragma unroll
         for (int e = 0; e < per - 1; ++e)
             if (c + e < D) {
                 if constexpr (sizeof(T) == 4) q[e] = __float_as_uint(row[c + e]);
                 else q[e / 2] |= (uint32_t)row[c + e] << (16 * (e & 1));
             }
+        return q;
     }
-    return q;
 }
 // An operand's eight elements from memory.
-__device__ __forceinline__ void load_frag(const uint16_t* row, int c, int D, Frag<uint16_t>& f) { f.v = __builtin_bit_cast(bf16x8, load16(row, c, D)); }
+template <bool EDGE>
+__device__ __forceinline__ void load_frag(const uint16_t* row, int c, int D, Frag<uint16_t>& f) { f.v = __builtin_bit_cast(bf16x8, load16<EDGE>(row, c, D)); }
+template <bool EDGE>
 __device__ __forceinline__ void load_frag(const float* row, int c, int D, Frag<float>& f)
 {
-    f.lo = __builtin_bit_cast(v4f, load16(row, c, D));
-    f.hi = __builtin_bit_cast(v4f, load16(row, c + 4, D));
+    f.lo = __builtin_bit_cast(v4f, load16<EDGE>(row, c, D));
+    f.hi = __builtin_bit_cast(v4f, load16<EDGE>(row, c + 4, D));
 }
-template <class T>
-__device__ __forceinline__ void no_frag(Frag<T>& f) { __builtin_memset(&f, 0, sizeof(f)); }
+// A lane's row as operands, contraction along its columns: zeros past the row's end.  All are asked for before any is waited for.
+template <class T, int PARTS>
+__device__ __forceinline__ void load_frags(const T* row, int h, int D, Frag<T> (&f)[2 * PARTS])
+{
+#pragma unroll
+    for (int k = 0; k < 2 * PARTS; ++k) {
+        if (16 * k + 16 <= D) load_frag<false>(row, 16 * k + 8 * h, D, f[k]);
+        else load_frag<true>(row, 16 * k + 8 * h, D, f[k]);
+    }
+}
+template <class T, int PARTS>
+__device__ __forceinline__ void clear_frags(Frag<T> (&f)[2 * PARTS])
+{
+#pragma unroll
+    for (int k = 0; k < 2 * PARTS; ++k) __builtin_memset(&f[k], 0, sizeof(f[k]));
+}
 
 // ---- tiles in LDS ----
 template <class T>
@@ -180,7 +214,7 @@ __device__ __forceinline__ void load_tile(T* tile, int wid, int lane, int D, F s
         for (int g = 0; g < L::kGroups; ++g) {
             const T* p = src(L::row(g, wid, lane));
 #pragma unroll
-            for (int part = 0; part < PARTS; ++part) q[g * PARTS + part] = load16(p, part * kPart + L::column(g, wid, lane), D);
+            for (int part = 0; part < PARTS; ++part) q[g * PARTS + part] = load16<true>(p, part * kPart + L::column(g, wid, lane), D);
         }
 #pragma unroll
         for (int g = 0; g < L::kGroups; ++g)
@@ -197,6 +231,33 @@ __device__ __forceinline__ void tiles_barrier()
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
+
+// N products whose operands read(i, f) gets from LDS, DEPTH of them ahead of multiply(i, f): left to itself the compiler reads each one
+// just before its product, into the same registers, and every product waits for LDS.  Instructions of the vector unit may be moved
+// between the steps.  start() may come earlier, with other work behind it.
+template <class T, int N, int DEPTH>
+struct Ahead {
+    static constexpr int kDepth = DEPTH < N ? DEPTH : N;
+    static constexpr int kMayMove = 0x2 | 0x4 | 0x400;            // vector, scalar, transcendental
+    Frag<T> f[kDepth];
+    template <class R>
+    __device__ __forceinline__ void start(R read)
+    {
+#pragma unroll
+        for (int i = 0; i < kDepth; ++i) read(i, f[i]);
+        __builtin_amdgcn_sched_barrier(kMayMove);
+    }
+    template <class R, class M>
+    __device__ __forceinline__ void run(R read, M mul)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            mul(i, f[i % kDepth]);
+            if (i + kDepth < N) read(i + kDepth, f[i % kDepth]);
+            __builtin_amdgcn_sched_barrier(kMayMove);
+        }
+    }
+};
 
 // ---- rows ----
 // x / d for x < 2^31
@@ -241,16 +302,18 @@ void set_shape(Shape& g, const A& p)
 }
 
 // A workgroup's unit, and its number among the unit's.  Workgroups go to the eight dies in turn, and each die has a cache of its own:
-// where units come out even, a die takes units of its own.
+// where units come out even, a die takes units of its own, every eighth, so that each has some of every part of the batch.  It goes
+// through them a few at a time, as many as fill it, whose keys and values its cache then holds.
 struct Place {
-    int unit;
-    int64_t at;
+    int unit, at;
 };
-__device__ __forceinline__ Place place_of(const Shape& g)
+constexpr int kFill = 64;                                         // workgroups at work on a die
+__device__ __forceinline__ Place place_of(const Shape& g, int each)
 {
-    if (g.per_die == 0) return Place{(int)(blockIdx.x % g.units), blockIdx.x / g.units};
-    const int at = blockIdx.x >> 3;
-    return Place{(int)(blockIdx.x & 7) * g.per_die + at % g.per_die, at / g.per_die};
+    if (g.per_die == 0) return Place{(int)(blockIdx.x % g.units), (int)(blockIdx.x / g.units)};
+    const int few = (kFill - 1) / each + 1, at = blockIdx.x >> 3, first = at / (few * each) * few, rest = at - first * each;
+    const int here = g.per_die - first < few ? g.per_die - first : few;
+    return Place{(int)(blockIdx.x & 7) + (first + rest % here) * 8, rest / here};
 }
 inline int64_t workgroups(const Shape& g, int64_t each) { return each * (g.per_die ? 8 * g.per_die : g.units); }
 __device__ __forceinline__ int length_of(const int32_t* lens, int b, int most)

@@ -40,15 +40,6 @@ constexpr int kPass = sizeof(T) == 2 ? 64 : 32;          // keys, or rows, of th
 template <class T>
 constexpr bool kFromZ = sizeof(T) == 2;                  // s begins with -z / c
 
-template <class T, int PARTS>
-__device__ __forceinline__ void load_frags(const T* row, bool live, int h, int D, Frag<T> (&f)[2 * PARTS])
-{
-#pragma unroll
-    for (int k = 0; k < 2 * PARTS; ++k) {
-        if (live) load_frag(row, 16 * k + 8 * h, D, f[k]);
-        else no_frag(f[k]);
-    }
-}
 __device__ __forceinline__ float dot(const Frag<uint16_t>& a, const Frag<uint16_t>& b)
 {
     float s = 0.0f;
@@ -118,9 +109,9 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(Args g)
     __shared__ __attribute__((aligned(16))) T k0[N], k1[N];
     __shared__ __attribute__((aligned(16))) T v0[N], v1[N];
     const int lane = threadIdx.x & 63, h = lane >> 5, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const Place at = place_of(g);
+    const Place at = place_of(g, g.row_tiles * g.row_splits);
     if (at.unit >= g.units) return;
-    const int split = (int)(at.at % g.row_splits), tile = g.row_tiles - 1 - (int)(at.at / g.row_splits);   // late rows see most keys: first
+    const int split = at.at % g.row_splits, tile = g.row_tiles - 1 - at.at / g.row_splits;   // late rows see most keys: first
     const Rows rows = rows_of(g, at.unit, tile * kMine, kMine);
     const int r = tile * kMine + wid * 32 + (lane & 31);
     const Row row = row_of(g, rows, r);
@@ -131,15 +122,16 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(Args g)
         const T* q = static_cast<const T*>(g.q.p) + rows.b * g.q.lb + row.t * g.q.lt + row.head * g.q.lh;
         const T* d = static_cast<const T*>(g.dout.p) + rows.b * g.dout.lb + row.t * g.dout.lt + row.head * g.dout.lh;
         const T* o = static_cast<const T*>(g.out.p) + rows.b * g.out.lb + row.t * g.out.lt + row.head * g.out.lh;
-        load_frags<T, PARTS>(q, row.sees > 0, h, g.D, qf);
-        load_frags<T, PARTS>(d, row.sees > 0, h, g.D, df);
-        if (row.sees > 0) {
+        Frag<T> of[2 * PARTS];
+        if (row.sees == 0) {
+            clear_frags<T, PARTS>(qf);
+            clear_frags<T, PARTS>(df);
+        } else {
+            load_frags<T, PARTS>(q, h, g.D, qf);
+            load_frags<T, PARTS>(d, h, g.D, df);
+            load_frags<T, PARTS>(o, h, g.D, of);
 #pragma unroll
-            for (int k = 0; k < 2 * PARTS; ++k) {
-                Frag<T> f;
-                load_frag(o, 16 * k + 8 * h, g.D, f);
-                delta -= dot(f, df[k]);
-            }
+            for (int k = 0; k < 2 * PARTS; ++k) delta -= dot(of[k], df[k]);
             z = -g.lse[((int64_t)rows.b * g.Hq + row.head) * g.Tq + row.t] * (kFromZ<T> ? g.inv_scale : kLog2e);
         }
         delta += other_half(delta);
@@ -211,16 +203,21 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dkv_kernel(Args g)
     __shared__ __attribute__((aligned(16))) T d0[N], d1[N];
     __shared__ __attribute__((aligned(16))) float z0[ROWS], z1[ROWS], e0[ROWS], e1[ROWS];
     const int lane = threadIdx.x & 63, h = lane >> 5, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const Place at = place_of(g);
+    const Place at = place_of(g, g.key_tiles * g.key_splits);
     if (at.unit >= g.units) return;
-    const int split = (int)(at.at % g.key_splits), tile = (int)(at.at / g.key_splits);
+    const int split = at.at % g.key_splits, tile = at.at / g.key_splits;
     const int b = at.unit / g.Hk, hk = at.unit % g.Hk;
     const int nq = length_of(g.q_lens, b, g.Tq), nk = length_of(g.k_lens, b, g.Tk);
     const int key0 = tile * kMine, key = key0 + wid * 32 + (lane & 31);
     const bool live = key < nk;
     Frag<T> kf[2 * PARTS], vf[2 * PARTS];
-    load_frags<T, PARTS>(static_cast<const T*>(g.k.p) + b * g.k.lb + (live ? key : 0) * g.k.lt + hk * g.k.lh, live, h, g.D, kf);
-    load_frags<T, PARTS>(static_cast<const T*>(g.v.p) + b * g.v.lb + (live ? key : 0) * g.v.lt + hk * g.v.lh, live, h, g.D, vf);
+    if (live) {
+        load_frags<T, PARTS>(static_cast<const T*>(g.k.p) + b * g.k.lb + key * g.k.lt + hk * g.k.lh, h, g.D, kf);
+        load_frags<T, PARTS>(static_cast<const T*>(g.v.p) + b * g.v.lb + key * g.v.lt + hk * g.v.lh, h, g.D, vf);
+    } else {
+        clear_frags<T, PARTS>(kf);
+        clear_frags<T, PARTS>(vf);
+    }
     // a key behind the last has zeros for k and v; what its lane adds up is not stored
     const int from = live ? first_row(g, nq, nk, key) : 0, least = first_row(g, nq, nk, key0 + wid * 32), most = wave_max(from);
     const int rows_live = nq * g.G;
