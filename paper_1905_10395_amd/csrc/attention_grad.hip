@@ -25,7 +25,7 @@ namespace {
 struct Args : Shape {
     Heads dout, q, k, v, out, dq, dk, dv;
     const float* lse;                // [B][Hq][Tq]
-    float *z, *delta;                // [units][row_tiles 128]: -z / c (fp32: -z), -inf for rows that see nothing, and -delta
+    float *z, *delta;                // [units][rows]: -z / c (fp32: -z), -inf for rows that see nothing, and -delta
     float *dq_parts, *dkv_parts;     // of splits, NULL: one
     int row_tiles, key_tiles;
     int row_splits, row_chunk;       // by rows: workgroups a tile, and the keys of one
@@ -33,12 +33,24 @@ struct Args : Shape {
     float scale, inv_scale, c;
 };
 
-constexpr int kWaves = 4, kThreads = 64 * kWaves;
-constexpr int kMine = 32 * kWaves;                       // rows, or keys, that a workgroup owns
-template <class T>
-constexpr int kPass = sizeof(T) == 2 ? 64 : 32;          // keys, or rows, of the tiles that pass
+// A workgroup owns 32 OWN rows, or keys, and SHARE of its wavefronts share each 32: of every tile that passes, each takes PASS of the rows
+// (keys), and their sums are added up in order at the end.  BUFFERS tiles, so that the next is on its way while one is passed.
+template <int OWN_, int SHARE_, int PASS_, int BUFFERS_>
+struct Form {
+    static constexpr int OWN = OWN_, SHARE = SHARE_, PASS = PASS_, BUFFERS = BUFFERS_;
+    static constexpr int WAVES = OWN * SHARE, THREADS = 64 * WAVES, TILE = SHARE * PASS, MINE = 32 * OWN;
+};
+// Many rows: 128 a workgroup.
+template <class T> using RowsMany = Form<4, 1, sizeof(T) == 2 ? 64 : 32, 2>;
+// Many keys: with a causal mask the first keys have all rows to pass and the last none, and two halves of a workgroup that take every
+// second tile halve the longest one's time (gradients of 4 x 4096 x 16 x 128: 1160 -> TODO us).
+template <class T> using KeysMany = Form<4, 2, sizeof(T) == 2 ? 64 : 32, 2>;
+// Few of either: 32 a workgroup.
+template <class T> using Few = Form<1, 4, 32, 1>;
+
 template <class T>
 constexpr bool kFromZ = sizeof(T) == 2;                  // s begins with -z / c
+constexpr int kChunk = 128;                              // chunks of a split are multiples of it
 
 __device__ __forceinline__ float dot(const Frag<uint16_t>& a, const Frag<uint16_t>& b)
 {
@@ -54,32 +66,29 @@ __device__ __forceinline__ float dot(const Frag<float>& a, const Frag<float>& b)
     for (int e = 0; e < 4; ++e) s += a.lo[e] * b.lo[e] + a.hi[e] * b.hi[e];
     return s;
 }
+// How far operands are read ahead; fp32's instructions take long enough without, and by keys registers are short.
+template <class T>
+constexpr int kAheadRows = sizeof(T) == 2 ? 4 : 1;
+template <class T>
+constexpr int kAheadKeys = sizeof(T) == 2 ? 2 : 1;
+
 // c += the product of 32 rows of a tile, from row r0 on, with an operand in registers.
-template <class T, int PARTS>
+template <int AHEAD, class T, int PARTS>
 __device__ __forceinline__ void rows_times(const T* tile, int rows, int r0, int lane, const Frag<T> (&b)[2 * PARTS], f32x16& c)
 {
-#pragma unroll
-    for (int k = 0; k < 2 * PARTS; ++k) {
-        Frag<T> f;
-        read_row(tile, rows, r0 + (lane & 31), lane >> 5, k, f);
-        multiply(c, f, b[k]);
-    }
+    Ahead<T, 2 * PARTS, AHEAD> ops;
+    auto read = [&](int k, Frag<T>& f) { read_row(tile, rows, r0 + (lane & 31), lane >> 5, k, f); };
+    ops.start(read);
+    ops.run(read, [&](int k, const Frag<T>& f) { multiply(c, f, b[k]); });
 }
-// sums += the columns of 32 rows of a tile times a result.
-template <class T, int PARTS>
-__device__ __forceinline__ void columns_times(const T* tile, int rows, int r0, int lane, const f32x16& r, f32x16 (&sums)[PARTS])
+// sums += the columns of 32 rows of a tile times a result made an operand.
+template <int AHEAD, class T, int PARTS>
+__device__ __forceinline__ void columns_times(const T* tile, int rows, int r0, int lane, const Frag<T> (&b)[2], f32x16 (&sums)[PARTS])
 {
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        Frag<T> b;
-        from_result(r, k, b);
-#pragma unroll
-        for (int p = 0; p < PARTS; ++p) {
-            Frag<T> f;
-            read_column(tile, rows, r0 + 16 * k, lane, p, f);
-            multiply(sums[p], f, b);
-        }
-    }
+    Ahead<T, 2 * PARTS, AHEAD> ops;
+    auto read = [&](int i, Frag<T>& f) { read_column(tile, rows, r0 + 16 * (i / PARTS), lane, i % PARTS, f); };
+    ops.start(read);
+    ops.run(read, [&](int i, const Frag<T>& f) { multiply(sums[i % PARTS], f, b[i / PARTS]); });
 }
 template <int PARTS>
 __device__ __forceinline__ void clear_sums(f32x16 (&s)[PARTS])
@@ -102,18 +111,49 @@ __device__ __forceinline__ void store_sums(T* row, int lane, int D, float factor
         }
 }
 
-template <class T, int PARTS, bool ALIGNED>
-__global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(Args g)
+// The sums of the wavefronts that share rows, in the first one's registers: areas of a wavefront's sums in the two tiles' memory.
+template <class F, int PARTS>
+__device__ __forceinline__ void join_shared(void* tile0, void* tile1, int own, int share, int lane, f32x16 (&s)[PARTS])
 {
-    constexpr int KEYS = kPass<T>, N = tile_elements<T>(KEYS, PARTS);
-    __shared__ __attribute__((aligned(16))) T k0[N], k1[N];
-    __shared__ __attribute__((aligned(16))) T v0[N], v1[N];
+    if constexpr (F::SHARE > 1) {
+        constexpr int kArea = PARTS * 16 * 64, kPerTile = 2;      // floats
+        static_assert((F::SHARE - 1) * F::OWN <= 2 * kPerTile, "areas");
+        auto area = [&](int k) {
+            const int a = k * F::OWN + own;
+            return reinterpret_cast<float*>(a < kPerTile ? tile0 : tile1) + a % kPerTile * kArea + lane;
+        };
+        __syncthreads();                                          // the tiles, or the last sums, have been read
+        if (share) {
+            float* to = area(share - 1);
+#pragma unroll
+            for (int i = 0; i < PARTS * 16; ++i) to[i * 64] = s[i / 16][i % 16];
+        }
+        __syncthreads();
+        if (!share) {
+#pragma unroll
+            for (int k = 0; k < F::SHARE - 1; ++k) {
+                const float* from = area(k);
+#pragma unroll
+                for (int i = 0; i < PARTS * 16; ++i) s[i / 16][i % 16] += from[i * 64];
+            }
+        }
+    }
+}
+
+template <class F, class T, int PARTS, bool ALIGNED>
+__global__ __launch_bounds__(F::THREADS, F::WAVES == 4 && F::BUFFERS == 1 ? 1 : 2) void attention_dq_kernel(Args g)
+{
+    constexpr int KEYS = F::TILE, N = tile_elements<T>(KEYS, PARTS);
+    static_assert(sizeof(T) * N >= 2 * 4 * PARTS * 16 * 64 || F::SHARE == 1, "two areas a tile");
+    __shared__ __attribute__((aligned(16))) T k0[N], k1[F::BUFFERS > 1 ? N : 8];
+    __shared__ __attribute__((aligned(16))) T v0[N], v1[F::BUFFERS > 1 ? N : 8];
+    const int own = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) % F::OWN), share = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) / F::OWN);
     const int lane = threadIdx.x & 63, h = lane >> 5, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Place at = place_of(g, g.row_tiles * g.row_splits);
     if (at.unit >= g.units) return;
     const int split = at.at % g.row_splits, tile = g.row_tiles - 1 - at.at / g.row_splits;   // late rows see most keys: first
-    const Rows rows = rows_of(g, at.unit, tile * kMine, kMine);
-    const int r = tile * kMine + wid * 32 + (lane & 31);
+    const Rows rows = rows_of(g, at.unit, tile * F::MINE, F::MINE);
+    const int r = tile * F::MINE + own * 32 + (lane & 31);
     const Row row = row_of(g, rows, r);
     const int least = wave_min(row.sees), most = wave_max(row.sees);
     Frag<T> qf[2 * PARTS], df[2 * PARTS];
@@ -135,10 +175,9 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(Args g)
             z = -g.lse[((int64_t)rows.b * g.Hq + row.head) * g.Tq + row.t] * (kFromZ<T> ? g.inv_scale : kLog2e);
         }
         delta += other_half(delta);
-        if (split == 0 && h == 0) {
-            const int64_t to = (int64_t)at.unit * g.row_tiles * kMine + r;
-            g.z[to] = row.there ? z : -INFINITY;
-            g.delta[to] = row.there ? delta : 0.0f;
+        if (split == 0 && share == 0 && h == 0 && row.there) {
+            g.z[(int64_t)at.unit * g.rows + r] = z;
+            g.delta[(int64_t)at.unit * g.rows + r] = delta;
         }
     }
     f32x16 dq[PARTS];
@@ -148,42 +187,58 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dq_kernel(Args g)
     const int begin = split * g.row_chunk, end = min(rows.end, begin + g.row_chunk);
     auto issue = [&](int key0, T* kb, T* vb) {
         auto key = [&](int i) { return key0 + i < rows.nk ? key0 + i : rows.nk - 1; };
-        load_tile<T, KEYS, PARTS, kWaves, ALIGNED>(kb, wid, lane, g.D, [&](int i) { return k + key(i) * g.k.lt; });
-        load_tile<T, KEYS, PARTS, kWaves, ALIGNED>(vb, wid, lane, g.D, [&](int i) { return v + key(i) * g.v.lt; });
+        load_tile<T, KEYS, PARTS, F::WAVES, ALIGNED>(kb, wid, lane, g.D, [&](int i) { return k + key(i) * g.k.lt; });
+        load_tile<T, KEYS, PARTS, F::WAVES, ALIGNED>(vb, wid, lane, g.D, [&](int i) { return v + key(i) * g.v.lt; });
     };
-    auto step = [&](int key0, T* kb, T* vb, T* next_k, T* next_v) {
-        tiles_barrier();
-        if (key0 + KEYS < end) issue(key0 + KEYS, next_k, next_v);
-        if (key0 >= most) return;
-        const bool masked = key0 + KEYS > least;
+    auto pass = [&](int key0, const T* kb, const T* vb) {
+        if (key0 + share * F::PASS >= most) return;
+        const bool masked = key0 + (share + 1) * F::PASS > least;
 #pragma unroll
-        for (int n = 0; n < KEYS / 32; ++n) {
+        for (int n = 0; n < F::PASS / 32; ++n) {
+            const int k0 = share * F::PASS + 32 * n;
             f32x16 s, dp;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 s[i] = kFromZ<T> ? z : 0.0f;
                 dp[i] = delta;
             }
-            rows_times<T, PARTS>(kb, KEYS, 32 * n, lane, qf, s);
-            rows_times<T, PARTS>(vb, KEYS, 32 * n, lane, df, dp);
+            rows_times<kAheadRows<T>, T, PARTS>(kb, KEYS, k0, lane, qf, s);
+            rows_times<kAheadRows<T>, T, PARTS>(vb, KEYS, k0, lane, df, dp);
 #pragma unroll
             for (int i = 0; i < 16; ++i) dp[i] *= __builtin_amdgcn_exp2f(kFromZ<T> ? s[i] * g.c : fmaf(s[i], g.c, z));
             if (masked) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) dp[i] = key0 + 32 * n + 8 * (i >> 2) + 4 * h + (i & 3) < row.sees ? dp[i] : 0.0f;
+                for (int i = 0; i < 16; ++i) dp[i] = key0 + k0 + 8 * (i >> 2) + 4 * h + (i & 3) < row.sees ? dp[i] : 0.0f;
             }
-            columns_times<T, PARTS>(kb, KEYS, 32 * n, lane, dp, dq);
+            Frag<T> ef[2];
+            from_result(dp, 0, ef[0]);
+            from_result(dp, 1, ef[1]);
+            columns_times<kAheadRows<T>, T, PARTS>(kb, KEYS, k0, lane, ef, dq);
         }
     };
-    if (begin < end) issue(begin, k0, v0);
-    for (int key0 = begin; key0 < end; key0 += 2 * KEYS) {
-        step(key0, k0, v0, k1, v1);
-        if (key0 + KEYS < end) step(key0 + KEYS, k1, v1, k0, v0);
+    if constexpr (F::BUFFERS > 1) {
+        auto step = [&](int key0, T* kb, T* vb, T* next_k, T* next_v) {
+            tiles_barrier();
+            if (key0 + KEYS < end) issue(key0 + KEYS, next_k, next_v);
+            pass(key0, kb, vb);
+        };
+        if (begin < end) issue(begin, k0, v0);
+        for (int key0 = begin; key0 < end; key0 += 2 * KEYS) {
+            step(key0, k0, v0, k1, v1);
+            if (key0 + KEYS < end) step(key0 + KEYS, k1, v1, k0, v0);
+        }
+    } else {
+        for (int key0 = begin; key0 < end; key0 += KEYS) {
+            if (key0 > begin) tiles_barrier();                     // the last tiles have been read
+            issue(key0, k0, v0);
+            tiles_barrier();
+            pass(key0, k0, v0);
+        }
     }
-    if (!row.there) return;
+    join_shared<F, PARTS>(k0, v0, own, share, lane, dq);
+    if (!row.there || share) return;
     if (g.dq_parts)
-        store_sums<float, PARTS>(g.dq_parts + ((((int64_t)at.unit * g.row_tiles + tile) * g.row_splits + split) * kMine + r - tile * kMine) * (PARTS * kPart),
-                                 lane, PARTS * kPart, g.scale, dq);
+        store_sums<float, PARTS>(g.dq_parts + (((int64_t)at.unit * g.rows + r) * g.row_splits + split) * (PARTS * kPart), lane, PARTS * kPart, g.scale, dq);
     else
         store_sums<T, PARTS>(static_cast<T*>(g.dq.p) + rows.b * g.dq.lb + row.t * g.dq.lt + row.head * g.dq.lh, lane, g.D, g.scale, dq);
 }
@@ -195,20 +250,22 @@ __device__ __forceinline__ int first_row(const Args& g, int nq, int nk, int key)
     return g.causal && t > 0 ? (t < nq ? t : nq) * g.G : 0;
 }
 
-template <class T, int PARTS, bool ALIGNED>
-__global__ __launch_bounds__(kThreads, 2) void attention_dkv_kernel(Args g)
+template <class F, class T, int PARTS, bool ALIGNED>
+__global__ __launch_bounds__(F::THREADS, F::WAVES == 4 && F::BUFFERS == 1 ? 1 : 2) void attention_dkv_kernel(Args g)
 {
-    constexpr int ROWS = kPass<T>, N = tile_elements<T>(ROWS, PARTS);
-    __shared__ __attribute__((aligned(16))) T q0[N], q1[N];
-    __shared__ __attribute__((aligned(16))) T d0[N], d1[N];
+    constexpr int ROWS = F::TILE, N = tile_elements<T>(ROWS, PARTS);
+    static_assert(sizeof(T) * N >= 2 * 4 * PARTS * 16 * 64 || F::SHARE == 1, "two areas a tile");
+    __shared__ __attribute__((aligned(16))) T q0[N], q1[F::BUFFERS > 1 ? N : 8];
+    __shared__ __attribute__((aligned(16))) T d0[N], d1[F::BUFFERS > 1 ? N : 8];
     __shared__ __attribute__((aligned(16))) float z0[ROWS], z1[ROWS], e0[ROWS], e1[ROWS];
+    const int own = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) % F::OWN), share = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) / F::OWN);
     const int lane = threadIdx.x & 63, h = lane >> 5, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Place at = place_of(g, g.key_tiles * g.key_splits);
     if (at.unit >= g.units) return;
     const int split = at.at % g.key_splits, tile = at.at / g.key_splits;
     const int b = at.unit / g.Hk, hk = at.unit % g.Hk;
     const int nq = length_of(g.q_lens, b, g.Tq), nk = length_of(g.k_lens, b, g.Tk);
-    const int key0 = tile * kMine, key = key0 + wid * 32 + (lane & 31);
+    const int key0 = tile * F::MINE, key = key0 + own * 32 + (lane & 31);
     const bool live = key < nk;
     Frag<T> kf[2 * PARTS], vf[2 * PARTS];
     if (live) {
@@ -219,7 +276,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dkv_kernel(Args g)
         clear_frags<T, PARTS>(vf);
     }
     // a key behind the last has zeros for k and v; what its lane adds up is not stored
-    const int from = live ? first_row(g, nq, nk, key) : 0, least = first_row(g, nq, nk, key0 + wid * 32), most = wave_max(from);
+    const int from = live ? first_row(g, nq, nk, key) : 0, least = first_row(g, nq, nk, key0 + own * 32), most = wave_max(from);
     const int rows_live = nq * g.G;
     int begin = first_row(g, nq, nk, key0) / ROWS * ROWS, end = key0 < nk ? rows_live : 0;
     begin = max(begin, split * g.key_chunk);
@@ -229,74 +286,98 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dkv_kernel(Args g)
     clear_sums<PARTS>(dv);
     const T* q = static_cast<const T*>(g.q.p) + b * g.q.lb + (int64_t)hk * g.G * g.q.lh;
     const T* d = static_cast<const T*>(g.dout.p) + b * g.dout.lb + (int64_t)hk * g.G * g.dout.lh;
-    const float* z = g.z + (int64_t)at.unit * g.row_tiles * kMine;
-    const float* delta = g.delta + (int64_t)at.unit * g.row_tiles * kMine;
+    const float* z = g.z + (int64_t)at.unit * g.rows;
+    const float* delta = g.delta + (int64_t)at.unit * g.rows;
     auto issue = [&](int r0, T* qb, T* db, float* zb, float* eb) {
         auto place = [&](int i, const Heads& a) {
             const int r = r0 + i < rows_live ? r0 + i : rows_live - 1, t = over(r, g.by_g);
             return t * a.lt + (r - t * g.G) * a.lh;
         };
-        load_tile<T, ROWS, PARTS, kWaves, ALIGNED>(qb, wid, lane, g.D, [&](int i) { return q + place(i, g.q); });
-        load_tile<T, ROWS, PARTS, kWaves, ALIGNED>(db, wid, lane, g.D, [&](int i) { return d + place(i, g.dout); });
-        // (z and delta have whole tiles of rows)
-        if (lane < ROWS && wid == 0) zb[lane] = z[r0 + lane];
-        if (lane < ROWS && wid == 1) eb[lane] = delta[r0 + lane];
+        load_tile<T, ROWS, PARTS, F::WAVES, ALIGNED>(qb, wid, lane, g.D, [&](int i) { return q + place(i, g.q); });
+        load_tile<T, ROWS, PARTS, F::WAVES, ALIGNED>(db, wid, lane, g.D, [&](int i) { return d + place(i, g.dout); });
+        static_assert(ROWS <= F::THREADS && kChunk % ROWS == 0, "a value a thread, whole tiles a chunk");
+        if ((int)threadIdx.x < ROWS) {
+            const int r = r0 + (int)threadIdx.x;
+            zb[threadIdx.x] = r < rows_live ? z[r] : -INFINITY;
+            eb[threadIdx.x] = r < rows_live ? delta[r] : 0.0f;
+        }
     };
-    auto step = [&](int r0, T* qb, T* db, float* zb, float* eb, T* next_q, T* next_d, float* next_z, float* next_e) {
-        tiles_barrier();
-        if (r0 + ROWS < end) issue(r0 + ROWS, next_q, next_d, next_z, next_e);
-        if (r0 + ROWS <= least) return;
-        const bool masked = r0 < most;
+    auto pass = [&](int r0, const T* qb, const T* db, const float* zb, const float* eb) {
+        if (r0 + (share + 1) * F::PASS <= least) return;
+        const bool masked = r0 + share * F::PASS < most;
 #pragma unroll 1
-        for (int n = 0; n < ROWS / 32; ++n) {
+        for (int n = 0; n < F::PASS / 32; ++n) {
+            const int i0 = share * F::PASS + 32 * n;
             f32x16 s, dp;
             auto begin_with = [&](const float* first, f32x16& c) {
 #pragma unroll
                 for (int i = 0; i < 16; i += 4) {
-                    const v4f x = *reinterpret_cast<const v4f*>(first + 32 * n + 2 * i + 4 * h);
+                    const v4f x = *reinterpret_cast<const v4f*>(first + i0 + 2 * i + 4 * h);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) c[i + e] = x[e];
                 }
             };
             if constexpr (kFromZ<T>) {
                 begin_with(zb, s);
-                rows_times<T, PARTS>(qb, ROWS, 32 * n, lane, kf, s);
+                rows_times<kAheadKeys<T>, T, PARTS>(qb, ROWS, i0, lane, kf, s);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i] * g.c);
             } else {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[i] = 0.0f;
-                rows_times<T, PARTS>(qb, ROWS, 32 * n, lane, kf, s);
+                rows_times<kAheadKeys<T>, T, PARTS>(qb, ROWS, i0, lane, kf, s);
                 begin_with(zb, dp);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], g.c, dp[i]));
             }
             if (masked) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = r0 + 32 * n + 8 * (i >> 2) + 4 * h + (i & 3) >= from ? s[i] : 0.0f;
+                for (int i = 0; i < 16; ++i) s[i] = r0 + i0 + 8 * (i >> 2) + 4 * h + (i & 3) >= from ? s[i] : 0.0f;
             }
-            columns_times<T, PARTS>(db, ROWS, 32 * n, lane, s, dv);
             begin_with(eb, dp);
-            rows_times<T, PARTS>(db, ROWS, 32 * n, lane, vf, dp);
+            rows_times<kAheadKeys<T>, T, PARTS>(db, ROWS, i0, lane, vf, dp);
+            // both become operands before either is passed on, so that the products' registers are free
+            Frag<T> pf[2], ef[2];
+            from_result(s, 0, pf[0]);
+            from_result(s, 1, pf[1]);
 #pragma unroll
             for (int i = 0; i < 16; ++i) dp[i] *= s[i];
-            columns_times<T, PARTS>(qb, ROWS, 32 * n, lane, dp, dk);
+            from_result(dp, 0, ef[0]);
+            from_result(dp, 1, ef[1]);
+            columns_times<kAheadKeys<T>, T, PARTS>(db, ROWS, i0, lane, pf, dv);
+            columns_times<kAheadKeys<T>, T, PARTS>(qb, ROWS, i0, lane, ef, dk);
         }
     };
-    if (begin < end) issue(begin, q0, d0, z0, e0);
-    for (int r0 = begin; r0 < end; r0 += 2 * ROWS) {
-        step(r0, q0, d0, z0, e0, q1, d1, z1, e1);
-        if (r0 + ROWS < end) step(r0 + ROWS, q1, d1, z1, e1, q0, d0, z0, e0);
+    if constexpr (F::BUFFERS > 1) {
+        auto step = [&](int r0, T* qb, T* db, float* zb, float* eb, T* next_q, T* next_d, float* next_z, float* next_e) {
+            tiles_barrier();
+            if (r0 + ROWS < end) issue(r0 + ROWS, next_q, next_d, next_z, next_e);
+            pass(r0, qb, db, zb, eb);
+        };
+        if (begin < end) issue(begin, q0, d0, z0, e0);
+        for (int r0 = begin; r0 < end; r0 += 2 * ROWS) {
+            step(r0, q0, d0, z0, e0, q1, d1, z1, e1);
+            if (r0 + ROWS < end) step(r0 + ROWS, q1, d1, z1, e1, q0, d0, z0, e0);
+        }
+    } else {
+        for (int r0 = begin; r0 < end; r0 += ROWS) {
+            if (r0 > begin) tiles_barrier();                       // the last tiles have been read
+            issue(r0, q0, d0, z0, e0);
+            tiles_barrier();
+            pass(r0, q0, d0, z0, e0);
+        }
     }
-    if (key >= g.Tk) return;
+    join_shared<F, PARTS>(q0, d0, own, share, lane, dk);
+    join_shared<F, PARTS>(q0, d0, own, share, lane, dv);
+    if (key >= g.Tk || share) return;
     if (!live) {
         clear_sums<PARTS>(dk);
         clear_sums<PARTS>(dv);
     }
     if (g.dkv_parts) {
-        float* part = g.dkv_parts + ((((int64_t)at.unit * g.key_tiles + tile) * g.key_splits + split) * 2 * kMine + key - key0) * (PARTS * kPart);
+        float* part = g.dkv_parts + (((int64_t)at.unit * g.Tk + key) * g.key_splits + split) * (2 * PARTS * kPart);
         store_sums<float, PARTS>(part, lane, PARTS * kPart, g.scale, dk);
-        store_sums<float, PARTS>(part + kMine * PARTS * kPart, lane, PARTS * kPart, 1.0f, dv);
+        store_sums<float, PARTS>(part + PARTS * kPart, lane, PARTS * kPart, 1.0f, dv);
     } else {
         store_sums<T, PARTS>(static_cast<T*>(g.dk.p) + b * g.dk.lb + key * g.dk.lt + hk * g.dk.lh, lane, g.D, g.scale, dk);
         store_sums<T, PARTS>(static_cast<T*>(g.dv.p) + b * g.dv.lb + key * g.dv.lt + hk * g.dv.lh, lane, g.D, 1.0f, dv);
@@ -304,20 +385,21 @@ __global__ __launch_bounds__(kThreads, 2) void attention_dkv_kernel(Args g)
 }
 
 // The sums of the splits' parts, in order.  KV: of dk and dv, else of dq.
+constexpr int kJoinThreads = 256;
 template <class T, int PARTS, bool KV>
-__global__ __launch_bounds__(kThreads) void attention_grad_join_kernel(Args g)
+__global__ __launch_bounds__(kJoinThreads) void attention_grad_join_kernel(Args g)
 {
     constexpr int COLS = PARTS * kPart, LISTS = KV ? 2 : 1;
-    const int tiles = KV ? g.key_tiles : g.row_tiles, splits = KV ? g.key_splits : g.row_splits, many = KV ? g.Tk : g.rows;
-    const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x, row = id / COLS;
+    const int splits = KV ? g.key_splits : g.row_splits, many = KV ? g.Tk : g.rows;
+    const int64_t id = (int64_t)blockIdx.x * kJoinThreads + threadIdx.x, row = id / COLS;
     const int c = (int)(id % COLS), unit = (int)(row / many), r = (int)(row % many);
     if (unit >= g.units || c >= g.D) return;
-    const float* p = (KV ? g.dkv_parts : g.dq_parts) + (((int64_t)unit * tiles + r / kMine) * splits * LISTS * kMine + r % kMine) * COLS + c;
+    const float* p = (KV ? g.dkv_parts : g.dq_parts) + row * splits * LISTS * COLS + c;
     const int b = unit / g.Hk, hk = unit % g.Hk;
 #pragma unroll
     for (int list = 0; list < LISTS; ++list) {
         float s = 0.0f;
-        for (int k = 0; k < splits; ++k) s += p[((int64_t)k * LISTS + list) * kMine * COLS];
+        for (int k = 0; k < splits; ++k) s += p[(k * LISTS + list) * COLS];
         const Heads& a = KV ? (list ? g.dv : g.dk) : g.dq;
         const int t = KV ? r : over(r, g.by_g), head = KV ? hk : hk * g.G + r - t * g.G;
         put1(static_cast<T*>(a.p) + b * a.lb + t * a.lt + head * a.lh + c, s);
@@ -327,16 +409,17 @@ __global__ __launch_bounds__(kThreads) void attention_grad_join_kernel(Args g)
 // ---- host ----
 constexpr int kComputeUnits = 256;
 struct Plan {
+    bool few_rows, few_keys;
     int row_tiles, key_tiles, row_splits, row_chunk, key_splits, key_chunk;
     size_t stat, dq, dkv, bytes;     // bytes of z (and of delta), of the parts, of all
 };
 constexpr size_t padded(size_t n) { return (n + kAlign - 1) / kAlign * kAlign; }
 
-// Splits of `many` into chunks, so that there are two workgroups a compute unit, but chunks of at least 512.
+// Splits of `many` into chunks, so that there is a workgroup a compute unit, but chunks of at least 512.
 void split(int64_t groups, int64_t many, int& splits, int& chunk)
 {
-    const int64_t least = 512, step = 128;
-    const int64_t n = std::max<int64_t>(1, std::min<int64_t>(2 * kComputeUnits / std::max<int64_t>(1, groups), (many + least - 1) / least));
+    const int64_t least = 512, step = kChunk;
+    const int64_t n = std::max<int64_t>(1, std::min<int64_t>(kComputeUnits / std::max<int64_t>(1, groups), (many + least - 1) / least));
     chunk = (int)std::max<int64_t>(step, ((many + n - 1) / n + step - 1) / step * step);
     splits = (int)std::max<int64_t>(1, (many + chunk - 1) / chunk);
 }
@@ -345,45 +428,58 @@ Plan plan_of(int B, int Tq, int Tk, int Hq, int Hk, int D)
     Plan p{};
     const int64_t rows = (int64_t)Tq * (Hq / Hk), units = (int64_t)B * Hk;
     const size_t cols = (size_t)parts_of(D) * kPart;
-    p.row_tiles = (int)((rows + kMine - 1) / kMine);
-    p.key_tiles = (Tk + kMine - 1) / kMine;
+    auto tiles = [&](int64_t many, bool& few) {
+        few = units * ((many + 127) / 128) < kComputeUnits;
+        const int mine = few ? 32 : 128;
+        return (int)((many + mine - 1) / mine);
+    };
+    p.row_tiles = tiles(rows, p.few_rows);
+    p.key_tiles = tiles(Tk, p.few_keys);
     split(units * p.row_tiles, Tk, p.row_splits, p.row_chunk);
     split(units * p.key_tiles, rows, p.key_splits, p.key_chunk);
-    p.stat = padded(sizeof(float) * (size_t)units * p.row_tiles * kMine);
-    p.dq = p.row_splits > 1 ? padded(sizeof(float) * (size_t)units * p.row_tiles * p.row_splits * kMine * cols) : 0;
-    p.dkv = p.key_splits > 1 ? padded(sizeof(float) * (size_t)units * p.key_tiles * p.key_splits * 2 * kMine * cols) : 0;
+    p.stat = padded(sizeof(float) * (size_t)(units * rows));
+    p.dq = p.row_splits > 1 ? padded(sizeof(float) * (size_t)(units * rows * p.row_splits) * cols) : 0;
+    p.dkv = p.key_splits > 1 ? padded(sizeof(float) * (size_t)(units * Tk * p.key_splits * 2) * cols) : 0;
     p.bytes = std::max(kAlign, 2 * p.stat + p.dq + p.dkv);
     return p;
 }
 
-template <class T, int PARTS>
-void launch(const Args& g, bool aligned_rows, bool aligned_keys, hipStream_t s)
+template <class T, int PARTS, bool ALIGNED>
+void launch_rows(const Args& g, bool few, hipStream_t s)
 {
-    const dim3 threads(kThreads);
+    const dim3 grid((unsigned)workgroups(g, (int64_t)g.row_tiles * g.row_splits));
+    if (few) hipLaunchKernelGGL((attention_dq_kernel<Few<T>, T, PARTS, ALIGNED>), grid, dim3(Few<T>::THREADS), 0, s, g);
+    else hipLaunchKernelGGL((attention_dq_kernel<RowsMany<T>, T, PARTS, ALIGNED>), grid, dim3(RowsMany<T>::THREADS), 0, s, g);
+}
+template <class T, int PARTS, bool ALIGNED>
+void launch_keys(const Args& g, bool few, hipStream_t s)
+{
+    const dim3 grid((unsigned)workgroups(g, (int64_t)g.key_tiles * g.key_splits));
+    if (few) hipLaunchKernelGGL((attention_dkv_kernel<Few<T>, T, PARTS, ALIGNED>), grid, dim3(Few<T>::THREADS), 0, s, g);
+    else hipLaunchKernelGGL((attention_dkv_kernel<KeysMany<T>, T, PARTS, ALIGNED>), grid, dim3(KeysMany<T>::THREADS), 0, s, g);
+}
+template <class T, int PARTS>
+void launch(const Args& g, const Plan& p, bool aligned_rows, bool aligned_keys, hipStream_t s)
+{
+    auto join_grid = [&](int64_t many) { return dim3((unsigned)((g.units * many * PARTS * kPart + kJoinThreads - 1) / kJoinThreads)); };
     if (g.rows) {
-        const dim3 grid((unsigned)workgroups(g, (int64_t)g.row_tiles * g.row_splits));
-        if (aligned_keys) hipLaunchKernelGGL((attention_dq_kernel<T, PARTS, true>), grid, threads, 0, s, g);
-        else hipLaunchKernelGGL((attention_dq_kernel<T, PARTS, false>), grid, threads, 0, s, g);
-        if (g.row_splits > 1)
-            hipLaunchKernelGGL((attention_grad_join_kernel<T, PARTS, false>), dim3((unsigned)(((int64_t)g.units * g.rows * PARTS * kPart + kThreads - 1) / kThreads)),
-                               threads, 0, s, g);
+        if (aligned_keys) launch_rows<T, PARTS, true>(g, p.few_rows, s);
+        else launch_rows<T, PARTS, false>(g, p.few_rows, s);
+        if (g.row_splits > 1) hipLaunchKernelGGL((attention_grad_join_kernel<T, PARTS, false>), join_grid(g.rows), dim3(kJoinThreads), 0, s, g);
     }
     if (g.Tk) {
-        const dim3 grid((unsigned)workgroups(g, (int64_t)g.key_tiles * g.key_splits));
-        if (aligned_rows) hipLaunchKernelGGL((attention_dkv_kernel<T, PARTS, true>), grid, threads, 0, s, g);
-        else hipLaunchKernelGGL((attention_dkv_kernel<T, PARTS, false>), grid, threads, 0, s, g);
-        if (g.key_splits > 1)
-            hipLaunchKernelGGL((attention_grad_join_kernel<T, PARTS, true>), dim3((unsigned)(((int64_t)g.units * g.Tk * PARTS * kPart + kThreads - 1) / kThreads)),
-                               threads, 0, s, g);
+        if (aligned_rows) launch_keys<T, PARTS, true>(g, p.few_keys, s);
+        else launch_keys<T, PARTS, false>(g, p.few_keys, s);
+        if (g.key_splits > 1) hipLaunchKernelGGL((attention_grad_join_kernel<T, PARTS, true>), join_grid(g.Tk), dim3(kJoinThreads), 0, s, g);
     }
 }
 
 // Launches of fewer than 2^32 threads.
 bool fits(const Plan& p, int64_t B, int64_t Tk, int64_t rows, int64_t Hk, int D)
 {
-    const double units = (double)(B * Hk + 7) * 1.2 * kThreads;
+    const double units = (double)(B * Hk + 7) * 1.2 * 512;
     return units * p.row_tiles * p.row_splits < 4294967296.0 && units * p.key_tiles * p.key_splits < 4294967296.0 &&
-           (double)(B * Hk) * (double)std::max(rows, Tk) * (parts_of(D) * kPart) < 4294967040.0;
+           (double)(B * Hk) * (double)std::max(p.row_splits > 1 ? rows : 0, p.key_splits > 1 ? Tk : 0) * (parts_of(D) * kPart) < 4294967040.0;
 }
 
 } // namespace
@@ -411,8 +507,9 @@ lsgd_status lsgd_attention_grad(const lsgd_attention_grad_args* p, void* workspa
     if (p->is_bf16 & ~1 || p->causal & ~1) return set_error(LSGD_ERR_INVALID_ARG, "%s: is_bf16 and causal must be 0 or 1", who);
     if (!std::isfinite(p->scale) || p->scale <= 0.0f) return set_error(LSGD_ERR_INVALID_ARG, "%s: scale must be finite and positive", who);
     if (Tq == 0 && Tk == 0) return LSGD_OK;
+    if ((int64_t)B * Hk > INT64_C(1) << 30) return set_error(LSGD_ERR_SHAPE, "%s: B=%d, Hk=%d are too large for one launch", who, B, Hk);
     const Plan plan = plan_of(B, Tq, Tk, Hq, Hk, D);
-    if ((int64_t)B * Hk > INT64_C(1) << 30 || !fits(plan, B, Tk, (int64_t)Tq * (Hq / Hk), Hk, D)) return set_error(LSGD_ERR_SHAPE, "%s: B=%d, Tq=%d, Tk=%d, Hk=%d are too large for one launch", who, B, Tq, Tk, Hk);
+    if ( !fits(plan, B, Tk, (int64_t)Tq * (Hq / Hk), Hk, D)) return set_error(LSGD_ERR_SHAPE, "%s: B=%d, Tq=%d, Tk=%d, Hk=%d are too large for one launch", who, B, Tq, Tk, Hk);
     const bool q = Tq > 0, k = Tk > 0;
     LSGD_TRY(check_heads(who, "dout", p->dout, B, Tq, Hq, D, es, q || p->dout.data, false));
     LSGD_TRY(check_heads(who, "q", p->q, B, Tq, Hq, D, es, q || p->q.data, false));
@@ -446,7 +543,7 @@ lsgd_status lsgd_attention_grad(const lsgd_attention_grad_args* p, void* workspa
     const bool aligned_rows = whole && wide_heads(p->q, B, Tq, Hq, es) && wide_heads(p->dout, B, Tq, Hq, es);
     const bool aligned_keys = whole && wide_heads(p->k, B, Tk, Hk, es) && wide_heads(p->v, B, Tk, Hk, es);
     by_type_and_parts(p->is_bf16, parts_of(D), [&](auto type, auto parts) {
-        launch<decltype(type), decltype(parts)::value>(g, aligned_rows, aligned_keys, static_cast<hipStream_t>(hip_stream));
+        launch<decltype(type), decltype(parts)::value>(g, plan, aligned_rows, aligned_keys, static_cast<hipStream_t>(hip_stream));
     });
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return set_error(LSGD_ERR_HIP, "%s: %s", who, hipGetErrorString(e));
