@@ -491,8 +491,9 @@ lsgd_status lsgd_qk_rotary_grad(const lsgd_qk_rotary_grad_args* args, void* work
  * A query that sees no key, or behind q_lens[b], has out = 0 and lse = -inf.  What lies in memory at keys from k_lens[b] and queries from
  * q_lens[b] on does not matter (NaN neither); a key that is merely not seen yet must be finite.  Scores, softmax and sums are
  * fp32; with bf16 data p is rounded to bf16 before the product with v.  out must not overlap the inputs.
- *   workspace  device, >= lsgd_attention_workspace_bytes, 256-byte aligned, not kept; may be NULL where that says 256.
- *              Few queries and long keys are split over the keys, and the parts joined from there.                          */
+ *   workspace  device, >= lsgd_attention_workspace_bytes, 256-byte aligned, not kept; may be NULL where that says 256, which it does up
+ *              to LSGD_ATTENTION_ONE_LAUNCH keys.  Few queries and longer keys are split over the keys, and the parts joined from there. */
+#define LSGD_ATTENTION_ONE_LAUNCH 1024
 typedef struct {
     int32_t B, Tq, Tk, Hq, Hk, D;
     int32_t is_bf16;              /* type of q, k, v, out: 0 fp32, 1 bf16 */

@@ -355,6 +355,8 @@ ADAMW_BLOCK = 256
 
 EMBED_GRAD_ONE_LAUNCH = 8192
 
+ATTENTION_ONE_LAUNCH = 1024
+
 _F32, _BF16, _I32 = torch.float32, torch.bfloat16, torch.int32
 _FLOATS = (_F32, _BF16)
 # the handle alone: a torch.cuda.Stream object takes longer to make than a small call
@@ -577,44 +579,56 @@ _NO_HEADS = (0, 0, 0, 0)
 
 
 def _heads(who, name, t, shape, dtype, index):
-    """lsgd_heads of an activation tensor [B, T, H, D]."""
+    """lsgd_heads of an activation tensor [B, T, H, D] (strides of a dimension of one element mean nothing, and are not looked at)."""
     if t is None:
         return _NO_HEADS
     if t.shape != shape or t.dtype is not dtype:
         raise ValueError(f"{who}: {name} must be {dtype} {list(shape)}")
     if t.get_device() != index:
         raise ValueError(f"{who}: {name} is not on the GPU of the others")
-    B, T, H, D = shape
     sb, st, sh, sd = t.stride()
-    if sd != 1 and D > 1 and t.numel():
+    if sd != 1 and shape[3] > 1 and t.numel():
         raise ValueError(f"{who}: columns of {name} must be dense")
-    # a dimension of one element has no stride that means anything
-    return t.data_ptr(), sb if B > 1 else 0, st if T > 1 else 0, sh if H > 1 else 0
+    return t.data_ptr(), sb, st, sh
+
+
+def _new_heads(like, shape, dtype, stream):
+    """A result of the call's own, and its lsgd_heads."""
+    t = _fresh(like, shape, dtype, stream)
+    row = shape[2] * shape[3]
+    return t, (t.data_ptr(), shape[1] * row, row, shape[3])
 
 
 def _vector(who, name, t, dtype, n, index):
     """Address of a dense vector, or of n things in any shape."""
     if t is None:
         return 0
-    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous() or t.get_device() != index:
+    if t.dtype is not dtype or t.numel() != n or t.get_device() != index or not t.is_contiguous():
         raise ValueError(f"{who}: {name} must be {n} contiguous {dtype}, on the GPU of the others")
     return t.data_ptr()
 
 
-def _positions(who, positions, W, T, index):
-    if positions is None:
+def _positions(who, t, W, T, index):
+    if t is None:
         return 0, 0
-    if positions.dtype is not _I32 or positions.shape not in ((W, T), (1, T)) or positions.get_device() != index:
+    if t.dtype is not _I32 or t.get_device() != index or t.shape not in ((W, T), (1, T)):
         raise ValueError(f"{who}: positions must be int32 [W, T] or [1, T], on the GPU of the others")
-    ld = _worker_stride(who, "positions", positions, "must be dense within a worker")
-    return positions.data_ptr(), ld if positions.shape[0] > 1 else 0
+    ld, st = t.stride()
+    if st != 1 and T > 1:
+        raise ValueError(f"{who}: positions must be dense within a worker")
+    return t.data_ptr(), ld if t.shape[0] > 1 else 0
 
 
 def _head_weights(who, name, w, W, D, index):
     """[W, D], or [1, D] for all workers."""
-    if w is not None and w.dim() == 2 and w.shape[0] == 1 < W:
-        return _weights(who, name, w, 1, D, index)[0], 0
-    return _weights(who, name, w, W, D, index)
+    if w is None:
+        return 0, 0
+    if w.dtype is not _F32 or w.get_device() != index or w.shape not in ((W, D), (1, D)):
+        raise ValueError(f"{who}: {name} must be float32 [W, D] or [1, D], on the GPU of the others")
+    ld, sd = w.stride()
+    if sd != 1 and D > 1:
+        raise ValueError(f"{who}: rows of {name} must be dense")
+    return w.data_ptr(), ld if w.shape[0] > 1 else 0
 
 
 def rotary_turns(columns, base=10000.0, stretch=1.0, keep=None, device="cuda"):
@@ -648,7 +662,9 @@ def qk_rotary(q, k=None, positions=None, turns=None, w_q=None, w_k=None, norm=Tr
     who = "qk_rotary"
     dt = q.dtype
     _need(q.dim() == 4 and dt in _FLOATS, "qk_rotary: q must be float32 or bfloat16 [W, T, H, D]")
-    index = _gpu(who, q, (("q", q),))
+    index = q.get_device()
+    if index < 0:
+        index = _gpu(who, q, (("q", q),))
     W, T, Hq, D = shape = q.shape
     _need(k is None or k.dim() == 4, "qk_rotary: k must be [W, T, H, D]")
     _need(k is not None or (w_k is None and k_out is None), "qk_rotary: w_k and k_out need k")
@@ -658,17 +674,20 @@ def qk_rotary(q, k=None, positions=None, turns=None, w_q=None, w_k=None, norm=Tr
     half = 0 if turns is None else turns.numel()
     _need(half * 2 <= D, "qk_rotary: more turns than pairs of columns")
     if q_out is None:
-        q_out = _fresh(q, shape, dt, stream)
+        q_out, to_q = _new_heads(q, shape, dt, stream)
+    else:
+        to_q = _heads(who, "q_out", q_out, shape, dt, index)
     if Hk and k_out is None:
-        k_out = _fresh(q, kshape, dt, stream)
+        k_out, to_k = _new_heads(q, kshape, dt, stream)
+    else:
+        to_k = _heads(who, "k_out", k_out, kshape, dt, index)
     if norm and stats is None:
         stats = _fresh(q, (W, T, Hq + Hk), _F32, stream)
     wq, lq = _head_weights(who, "w_q", w_q, W, D, index)
     wk, lk = _head_weights(who, "w_k", w_k, W, D, index)
     if T:
         a = _QK_ROTARY.pack(W, T, Hq, Hk, D, 2 * half, dt is _BF16, bool(norm), bool(interleaved), eps, magnitude, *_heads(who, "q", q, shape, dt, index),
-                            *_heads(who, "k", k, kshape, dt, index), *_heads(who, "q_out", q_out, shape, dt, index),
-                            *_heads(who, "k_out", k_out, kshape, dt, index), *_positions(who, positions, W, T, index),
+                            *_heads(who, "k", k, kshape, dt, index), *to_q, *to_k, *_positions(who, positions, W, T, index),
                             _vector(who, "turns", turns, torch.float64, half, index), wq, wk, lq, lk,
                             _vector(who, "stats", stats, _F32, W * T * (Hq + Hk), index))
         _call(index, stream, lib().lsgd_qk_rotary, a)
@@ -683,7 +702,9 @@ def qk_rotary_grad(dq_out, dk_out=None, q=None, k=None, stats=None, positions=No
     who = "qk_rotary_grad"
     dt = dq_out.dtype
     _need(dq_out.dim() == 4 and dt in _FLOATS, "qk_rotary_grad: dq_out must be float32 or bfloat16 [W, T, H, D]")
-    index = _gpu(who, dq_out, (("dq_out", dq_out),))
+    index = dq_out.get_device()
+    if index < 0:
+        index = _gpu(who, dq_out, (("dq_out", dq_out),))
     W, T, Hq, D = shape = dq_out.shape
     _need(dk_out is None or dk_out.dim() == 4, "qk_rotary_grad: dk_out must be [W, T, H, D]")
     _need(dk_out is not None or (k is None and w_k is None and dw_k is None and dk is None), "qk_rotary_grad: k, w_k, dw_k and dk need dk_out")
@@ -693,17 +714,20 @@ def qk_rotary_grad(dq_out, dk_out=None, q=None, k=None, stats=None, positions=No
     half = 0 if turns is None else turns.numel()
     _need(half * 2 <= D, "qk_rotary_grad: more turns than pairs of columns")
     if dq is None:
-        dq = _fresh(dq_out, shape, dt, stream)
+        dq, to_q = _new_heads(dq_out, shape, dt, stream)
+    else:
+        to_q = _heads(who, "dq", dq, shape, dt, index)
     if Hk and dk is None:
-        dk = _fresh(dq_out, kshape, dt, stream)
+        dk, to_k = _new_heads(dq_out, kshape, dt, stream)
+    else:
+        to_k = _heads(who, "dk", dk, kshape, dt, index)
     wq, lq = _head_weights(who, "w_q", w_q, W, D, index)
     wk, lk = _head_weights(who, "w_k", w_k, W, D, index)
     dwq, ldq = _weights(who, "dw_q", dw_q, W, D, index)
     dwk, ldk = _weights(who, "dw_k", dw_k, W, D, index)
     a = _QK_ROTARY_GRAD.pack(W, T, Hq, Hk, D, 2 * half, dt is _BF16, bool(norm), bool(interleaved), bool(accumulate), magnitude,
                              *_heads(who, "dq_out", dq_out, shape, dt, index), *_heads(who, "dk_out", dk_out, kshape, dt, index),
-                             *_heads(who, "q", q, shape, dt, index), *_heads(who, "k", k, kshape, dt, index), *_heads(who, "dq", dq, shape, dt, index),
-                             *_heads(who, "dk", dk, kshape, dt, index), *_positions(who, positions, W, T, index),
+                             *_heads(who, "q", q, shape, dt, index), *_heads(who, "k", k, kshape, dt, index), *to_q, *to_k, *_positions(who, positions, W, T, index),
                              _vector(who, "turns", turns, torch.float64, half, index), wq, wk, lq, lk,
                              _vector(who, "stats", stats, _F32, W * T * (Hq + Hk), index) if norm else 0, dwq, dwk, ldq, ldk)
     L = lib()
@@ -715,11 +739,13 @@ def qk_rotary_grad(dq_out, dk_out=None, q=None, k=None, stats=None, positions=No
     return dq, dk
 
 
-def _attention_shapes(who, q, k, v):
-    _need(q.dim() == 4 and q.dtype in _FLOATS, f"{who}: q must be float32 or bfloat16 [B, Tq, Hq, D]")
-    B, Tq, Hq, D = q.shape
-    _need(k.dim() == 4 and k.shape[0] == B and k.shape[3] == D, f"{who}: k must be [B, Tk, Hk, D] beside q")
-    return B, Tq, k.shape[1], Hq, k.shape[2], D
+def _attention_shapes(who, q, k):
+    qs, ks = q.shape, k.shape
+    if len(qs) != 4 or q.dtype not in _FLOATS:
+        raise ValueError(f"{who}: q must be float32 or bfloat16 [B, Tq, Hq, D]")
+    if len(ks) != 4 or ks[0] != qs[0] or ks[3] != qs[3]:
+        raise ValueError(f"{who}: k must be [B, Tk, Hk, D] beside q")
+    return qs, ks
 
 
 def attention(q, k, v, causal=False, scale=None, q_lens=None, k_lens=None, with_lse=True, out=None, lse=None, workspace=None, stream=None):
@@ -730,50 +756,51 @@ def attention(q, k, v, causal=False, scale=None, q_lens=None, k_lens=None, with_
     Returns (out, lse): out like q, lse float32 [B, Hq, Tq], which the gradient needs (None if not with_lse).  Queries that see nothing have zeros
     and -inf.  out, lse: optional buffers."""
     who = "attention"
-    B, Tq, Tk, Hq, Hk, D = _attention_shapes(who, q, k, v)
+    shape, kshape = _attention_shapes(who, q, k)
+    (B, Tq, Hq, D), (_, Tk, Hk, _) = shape, kshape
     dt = q.dtype
-    index = _gpu(who, q, (("q", q),))
-    shape, kshape = (B, Tq, Hq, D), (B, Tk, Hk, D)
+    index = q.get_device()
+    if index < 0:
+        index = _gpu(who, q, (("q", q),))
     if scale is None:
         scale = D ** -0.5
     if out is None:
-        out = _fresh(q, shape, dt, stream)
+        out, to = _new_heads(q, shape, dt, stream)
+    else:
+        to = _heads(who, "out", out, shape, dt, index)
     if lse is None and with_lse:
         lse = _fresh(q, (B, Hq, Tq), _F32, stream)
     a = _ATTENTION.pack(B, Tq, Tk, Hq, Hk, D, dt is _BF16, bool(causal), scale, *_heads(who, "q", q, shape, dt, index),
-                        *_heads(who, "k", k, kshape, dt, index), *_heads(who, "v", v, kshape, dt, index), *_heads(who, "out", out, shape, dt, index),
+                        *_heads(who, "k", k, kshape, dt, index), *_heads(who, "v", v, kshape, dt, index), *to,
                         _vector(who, "q_lens", q_lens, _I32, B, index), _vector(who, "k_lens", k_lens, _I32, B, index),
                         _vector(who, "lse", lse, _F32, B * Hq * Tq, index))
     L = lib()
     ws, nbytes = None, 0
-    need = L.lsgd_attention_workspace_bytes(B, Tq, Tk, Hq, Hk, D, dt is _BF16)
-    if need != _ATTENTION_NO_WORKSPACE:
-        workspace, nbytes = _workspace(who, need, q, workspace, stream)
+    if Tk > ATTENTION_ONE_LAUNCH or workspace is not None:
+        workspace, nbytes = _workspace(who, L.lsgd_attention_workspace_bytes(B, Tq, Tk, Hq, Hk, D, dt is _BF16), q, workspace, stream)
         ws = workspace.data_ptr()
     _call(index, stream, L.lsgd_attention, a, ws, nbytes)
     return out, lse
-
-
-_ATTENTION_NO_WORKSPACE = 256
 
 
 def attention_grad(dout, q, k, v, out, lse, causal=False, scale=None, q_lens=None, k_lens=None, dq=None, dk=None, dv=None, workspace=None, stream=None):
     """lsgd_attention_grad: (dq, dk, dv) from dout; out, lse: what attention returned; the rest as given to it.  dq, dk, dv: optional
     buffers (parts of one projection's gradient will do)."""
     who = "attention_grad"
-    B, Tq, Tk, Hq, Hk, D = _attention_shapes(who, q, k, v)
+    shape, kshape = _attention_shapes(who, q, k)
+    (B, Tq, Hq, D), (_, Tk, Hk, _) = shape, kshape
     dt = q.dtype
-    index = _gpu(who, q, (("q", q),))
-    shape, kshape = (B, Tq, Hq, D), (B, Tk, Hk, D)
+    index = q.get_device()
+    if index < 0:
+        index = _gpu(who, q, (("q", q),))
     if scale is None:
         scale = D ** -0.5
-    dq = _fresh(q, shape, dt, stream) if dq is None else dq
-    dk = _fresh(q, kshape, dt, stream) if dk is None else dk
-    dv = _fresh(q, kshape, dt, stream) if dv is None else dv
+    dq, to_q = _new_heads(q, shape, dt, stream) if dq is None else (dq, _heads(who, "dq", dq, shape, dt, index))
+    dk, to_k = _new_heads(q, kshape, dt, stream) if dk is None else (dk, _heads(who, "dk", dk, kshape, dt, index))
+    dv, to_v = _new_heads(q, kshape, dt, stream) if dv is None else (dv, _heads(who, "dv", dv, kshape, dt, index))
     a = _ATTENTION_GRAD.pack(B, Tq, Tk, Hq, Hk, D, dt is _BF16, bool(causal), scale, *_heads(who, "dout", dout, shape, dt, index),
                              *_heads(who, "q", q, shape, dt, index), *_heads(who, "k", k, kshape, dt, index), *_heads(who, "v", v, kshape, dt, index),
-                             *_heads(who, "out", out, shape, dt, index), *_heads(who, "dq", dq, shape, dt, index),
-                             *_heads(who, "dk", dk, kshape, dt, index), *_heads(who, "dv", dv, kshape, dt, index),
+                             *_heads(who, "out", out, shape, dt, index), *to_q, *to_k, *to_v,
                              _vector(who, "q_lens", q_lens, _I32, B, index), _vector(who, "k_lens", k_lens, _I32, B, index),
                              _vector(who, "lse", lse, _F32, B * Hq * Tq, index))
     L = lib()

@@ -340,7 +340,7 @@ Plan plan_of(int B, int Tq, int Tk, int Hq, int Hk, int D)
     }
     p.tiles = (int)((rows + kRowsByKeys - 1) / kRowsByKeys);
     const int64_t groups = units * p.tiles, wanted = std::max<int64_t>(1, 8 * kComputeUnits / std::max<int64_t>(1, groups));
-    const int least = 1024, step = 128;
+    const int least = LSGD_ATTENTION_ONE_LAUNCH, step = 128;
     const int64_t splits = std::min<int64_t>(wanted, (Tk + least - 1) / least);
     if (splits > 1) {
         p.chunk = (int)(((Tk + splits - 1) / splits + step - 1) / step * step);

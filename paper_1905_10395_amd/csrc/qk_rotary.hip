@@ -99,6 +99,9 @@ __device__ __forceinline__ float team_sum(float a, int lanes)
     return a;
 }
 
+// x^-1/2 to a last bit (of what is below the normal values: of the smallest of those; NaN stays).
+__device__ __forceinline__ float inverse_root(float x) { return __builtin_amdgcn_rsqf(x < 0x1p-126f ? 0x1p-126f : x); }
+
 // Where a lane's N units of two pieces lie in a row.
 template <int E, int N, bool NEIGHBOURS>
 struct Unit {
@@ -226,7 +229,7 @@ __global__ __launch_bounds__(kThreads) void qk_rotary_kernel(Args g)
             }
             float q = 1.0f;
             if (g.norm) {
-                q = 1.0f / sqrtf(team_sum(s, g.lanes) * g.inv_d + g.eps);
+                q = inverse_root(team_sum(s, g.lanes) * g.inv_d + g.eps);
                 if (g.stats && lane == 0) g.stats[((int64_t)w * g.T + t0 + r.token) * (g.H[0] + g.H[1]) + (which ? g.H[0] : 0) + r.head] = q;
             }
             T* y = row_of<T>(g.y[which], w, t0 + r.token, r.head);
@@ -252,25 +255,22 @@ __global__ __launch_bounds__(kThreads) void qk_rotary_grad_kernel(Args g)
     extern __shared__ v2f table[];
     const int lane = threadIdx.x & (g.lanes - 1), team = threadIdx.x / g.lanes, teams = kThreads / g.lanes, w = blockIdx.y;
     const Unit<E, N, NEIGHBOURS> at(g, lane);
-    float da[2][N][E], db[2][N][E];                        // the lane's part of both weights' gradients, over its rows
+    const int which = blockIdx.z, H = g.H[which];          // queries, or keys
+    if (H == 0) return;
+    float da[N][E], db[N][E];                              // the lane's part of the weight's gradient, over its rows
 #pragma unroll
-    for (int which = 0; which < 2; ++which)
+    for (int n = 0; n < N; ++n)
 #pragma unroll
-        for (int n = 0; n < N; ++n)
-#pragma unroll
-            for (int e = 0; e < E; ++e) da[which][n][e] = db[which][n][e] = 0.0f;
+        for (int e = 0; e < E; ++e) da[n][e] = db[n][e] = 0.0f;
+    const bool whole = g.x[which].p != nullptr;            // absent: neither a norm nor a weight's gradient needs it
+    float wa[N][E], wb[N][E];
+    weights<T, E, N>(g, which, w, at, wa, wb);
     for (int64_t t64 = (int64_t)blockIdx.x * g.tokens; t64 < g.T; t64 += (int64_t)gridDim.x * g.tokens) {
         const int t0 = (int)t64, tokens = g.T - t0 < g.tokens ? g.T - t0 : g.tokens;
         __syncthreads();                                   // the last tokens' table has been read
         make_table(g, w, t0, tokens, table);
         __syncthreads();
-#pragma unroll
-        for (int which = 0; which < 2; ++which) {
-            const int H = g.H[which];
-            if (H == 0) continue;
-            const bool whole = g.x[which].p != nullptr;    // absent: neither a norm nor a weight's gradient needs it
-            float wa[N][E], wb[N][E];
-            weights<T, E, N>(g, which, w, at, wa, wb);
+        {
             for (RowWalk r(team, teams, H); r.token < tokens; r.next()) {
                 const T* dy = row_of<const T>(g.y[which], w, t0 + r.token, r.head);
                 const T* x = whole ? row_of<const T>(g.x[which], w, t0 + r.token, r.head) : nullptr;
@@ -296,8 +296,8 @@ __global__ __launch_bounds__(kThreads) void qk_rotary_grad_kernel(Args g)
                     for (int e = 0; e < E; ++e) {
                         ha[n][e] *= q;
                         hb[n][e] *= q;
-                        da[which][n][e] += a[n][e] * ha[n][e];
-                        db[which][n][e] += b[n][e] * hb[n][e];
+                        da[n][e] += a[n][e] * ha[n][e];
+                        db[n][e] += b[n][e] * hb[n][e];
                         a[n][e] *= wa[n][e];
                         b[n][e] *= wb[n][e];
                         s += a[n][e] * ha[n][e] + b[n][e] * hb[n][e];
@@ -326,22 +326,19 @@ __global__ __launch_bounds__(kThreads) void qk_rotary_grad_kernel(Args g)
     // the workgroup's teams add up theirs in order
     __shared__ float sum[kThreads * 2 * E * N];
     float* part = g.parts + ((int64_t)w * gridDim.x + blockIdx.x) * 2 * g.Dp;
+    __syncthreads();
 #pragma unroll
-    for (int which = 0; which < 2; ++which) {
-        __syncthreads();
+    for (int n = 0; n < N; ++n)
 #pragma unroll
-        for (int n = 0; n < N; ++n)
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                if (at.has_a[n]) sum[team * g.D + at.a[n] + e] = da[which][n][e];
-                if (at.has_b[n]) sum[team * g.D + at.b[n] + e] = db[which][n][e];
-            }
-        __syncthreads();
-        for (int c = threadIdx.x; c < g.D; c += kThreads) {
-            float s = 0.0f;
-            for (int k = 0; k < teams; ++k) s += sum[k * g.D + c];
-            part[which * g.Dp + c] = s;
+        for (int e = 0; e < E; ++e) {
+            if (at.has_a[n]) sum[team * g.D + at.a[n] + e] = da[n][e];
+            if (at.has_b[n]) sum[team * g.D + at.b[n] + e] = db[n][e];
         }
+    __syncthreads();
+    for (int c = threadIdx.x; c < g.D; c += kThreads) {
+        float s = 0.0f;
+        for (int k = 0; k < teams; ++k) s += sum[k * g.D + c];
+        part[which * g.Dp + c] = s;
     }
 }
 
@@ -590,7 +587,7 @@ lsgd_status lsgd_qk_rotary_grad(const lsgd_qk_rotary_grad_args* p, void* workspa
         for (const lsgd_heads* a : {&p->dk_out, &p->k, &p->dk}) once = once && wide_heads(*a, W, T, p->Hk, es);
         dispatch(p->is_bf16, E, p->interleaved, once, [&](auto type, auto e, auto neighbours, auto streamed) {
             hipLaunchKernelGGL((qk_rotary_grad_kernel<decltype(type), decltype(e)::value, decltype(neighbours)::value, decltype(streamed)::value>),
-                               dim3((unsigned)plan.groups, (unsigned)W), dim3(kThreads), sizeof(v2f) * (size_t)std::max(1, g.tokens * g.half), s, g);
+                               dim3((unsigned)plan.groups, (unsigned)W, p->Hk ? 2 : 1), dim3(kThreads), sizeof(v2f) * (size_t)std::max(1, g.tokens * g.half), s, g);
         });
     }
     // (no tokens: the sums of nothing)
