@@ -51,7 +51,7 @@ constexpr int kAhead = sizeof(T) == 2 ? 4 : 1;
 
 // KEYS keys of a tile: their p of the lane's row, and the state's reference moved if need be.  masked: some row does not see some of
 // them.  then() is called when the products are on their way.
-template <class T, int PARTS, int KEYS, class F>
+template <int WIDTH, class T, int PARTS, int KEYS, class F>
 __device__ __forceinline__ void pass_keys(const T* kt, int lane, int key0, int sees, bool masked, float c, const Frag<T> (&qf)[2 * PARTS], State<PARTS>& st,
                                           f32x16 (&s)[KEYS / 32], F then)
 {
@@ -62,7 +62,7 @@ __device__ __forceinline__ void pass_keys(const T* kt, int lane, int key0, int s
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[n][i] = 0.0f;
     Ahead<T, NS * 2 * PARTS, kAhead<T>> ops;
-    auto read = [&](int i, Frag<T>& f) { read_row(kt, KEYS, 32 * (i % NS) + (lane & 31), h, i / NS, f); };
+    auto read = [&](int i, Frag<T>& f) { read_row<WIDTH>(kt, KEYS, 32 * (i % NS) + (lane & 31), h, i / NS, f); };
     ops.start(read);
     ops.run(read, [&](int i, const Frag<T>& f) { multiply(s[i % NS], f, qf[i / NS]); });
     then();
@@ -97,7 +97,7 @@ __device__ __forceinline__ void pass_keys(const T* kt, int lane, int key0, int s
         }
 }
 // Their values, times p.
-template <class T, int PARTS, int KEYS>
+template <int WIDTH, class T, int PARTS, int KEYS>
 struct Values {
     Ahead<T, KEYS / 16 * PARTS, kAhead<T>> ops;
     const T* vt;
@@ -105,14 +105,14 @@ struct Values {
     __device__ __forceinline__ Values(const T* tile, int l) : vt(tile), lane(l) {}
     __device__ __forceinline__ void start()
     {
-        ops.start([&](int i, Frag<T>& f) { read_column(vt, KEYS, 16 * (i / PARTS), lane, i % PARTS, f); });
+        ops.start([&](int i, Frag<T>& f) { read_column<WIDTH>(vt, KEYS, 16 * (i / PARTS), lane, i % PARTS, f); });
     }
     __device__ __forceinline__ void pass(const f32x16 (&s)[KEYS / 32], State<PARTS>& st)
     {
         Frag<T> p[KEYS / 16];
 #pragma unroll
         for (int k = 0; k < KEYS / 16; ++k) from_result(s[k / 2], k % 2, p[k]);
-        ops.run([&](int i, Frag<T>& f) { read_column(vt, KEYS, 16 * (i / PARTS), lane, i % PARTS, f); },
+        ops.run([&](int i, Frag<T>& f) { read_column<WIDTH>(vt, KEYS, 16 * (i / PARTS), lane, i % PARTS, f); },
                 [&](int i, const Frag<T>& f) { multiply(st.o[i % PARTS], f, p[i / PARTS]); });
     }
 };
@@ -159,8 +159,8 @@ __global__ __launch_bounds__(kThreads, 2) void attention_rows_kernel(Args g)
         if (key0 + KEYS < rows.end) issue(key0 + KEYS, next_k, next_v);
         if (key0 >= most) return;
         f32x16 p[KEYS / 32];
-        Values<T, PARTS, KEYS> values(vb, lane);
-        pass_keys<T, PARTS, KEYS>(kb, lane, key0, row.sees, key0 + KEYS > least, g.c, qf, st, p, [&] { values.start(); });
+        Values<kPart, T, PARTS, KEYS> values(vb, lane);
+        pass_keys<kPart, T, PARTS, KEYS>(kb, lane, key0, row.sees, key0 + KEYS > least, g.c, qf, st, p, [&] { values.start(); });
         values.pass(p, st);
     };
     if (rows.end > 0) issue(0, k0, v0);
@@ -201,6 +201,7 @@ template <class T, int PARTS, bool ALIGNED>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_keys_kernel(Args g)
 {
     constexpr int W = kWaves, KEYS = kKeysByKeys, N = tile_elements<T>(KEYS, PARTS), COLS = PARTS * kPart;
+    constexpr int WIDTH = sizeof(T) == 2 && PARTS % 2 == 0 ? 2 * kPart : kPart;
     __shared__ __attribute__((aligned(16))) T kt[W][N];
     __shared__ __attribute__((aligned(16))) T vt[W][N];
     __shared__ float sums[W][kRowsJoined][COLS + 1], tops[W][kRowsByKeys], ls[W][kRowsByKeys];
@@ -218,18 +219,18 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_ke
         const T* v = static_cast<const T*>(g.v.p) + rows.b * g.v.lb + rows.hk * g.v.lh;
         // (behind the last tile too, the last key again and again: under a condition the compiler waits for all loads before it reads)
         auto load = [&](const T* from, int64_t lt, int key0, T* to) {
-            load_tile<T, KEYS, PARTS, 1, ALIGNED>(to, 0, lane, g.D, [&](int r) { return from + (key0 + r < rows.nk ? key0 + r : rows.nk - 1) * lt; });
+            load_tile<T, KEYS, PARTS, 1, ALIGNED, WIDTH>(to, 0, lane, g.D, [&](int r) { return from + (key0 + r < rows.nk ? key0 + r : rows.nk - 1) * lt; });
         };
-        constexpr int later = ALIGNED ? TileLoad<T, KEYS, PARTS, 1>::kLoads : 0;
+        constexpr int later = ALIGNED ? TileLoad<T, KEYS, PARTS, 1, WIDTH>::kLoads : 0;
         Frag<T> qf[2 * PARTS];
         load_queries<T, PARTS>(g, rows, row, h, qf);
         load(k, g.k.lt, begin + wid * KEYS, kt[wid]);
         load(v, g.v.lt, begin + wid * KEYS, vt[wid]);
         for (int key0 = begin + wid * KEYS; key0 < end; key0 += W * KEYS) {
             f32x16 p[1];
-            Values<T, PARTS, KEYS> values(vt[wid], lane);
+            Values<WIDTH, T, PARTS, KEYS> values(vt[wid], lane);
             wait_loads<later>();
-            pass_keys<T, PARTS, KEYS>(kt[wid], lane, key0, row.sees, key0 + KEYS > least, g.c, qf, st, p, [] {});
+            pass_keys<WIDTH, T, PARTS, KEYS>(kt[wid], lane, key0, row.sees, key0 + KEYS > least, g.c, qf, st, p, [] {});
             wait_loads<later>();
             load(k, g.k.lt, key0 + W * KEYS, kt[wid]);
             wait_loads<later>();

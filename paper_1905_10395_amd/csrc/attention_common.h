@@ -9,9 +9,10 @@
 // registers, if the other operand's contraction places are taken in the same order: 4 h .. 4 h + 3, then 8 + 4 h .. 8 + 4 h + 3 (of
 // 16).  One operand of every product stays in registers that way, the other passes through LDS.
 //
-// Tiles.  R rows of a tile lie in LDS as parts of 32 columns, [part][row][32], in pieces of 16 bytes; loads straight to LDS write
-// consecutive pieces, so rows cannot be padded: a row's pieces are stored in another order (exclusive or with part of the row's
-// number), such that the reads along rows and those along columns both spread over all banks.
+// Tiles.  R rows of a tile lie in LDS as slabs of WIDTH columns, [slab][row][WIDTH], in pieces of 16 bytes; loads straight to LDS write
+// consecutive pieces, so rows cannot be padded: a row's pieces are stored in another order (exclusive or with bits of the row's
+// number), such that the reads along rows and those along columns both spread over all banks.  Slabs of 32 columns, or of 64 bf16
+// ones where the rows come from memory once: a load then takes whole lines (but the reads' addresses take more registers).
 #pragma once
 
 #include <type_traits>
@@ -130,96 +131,104 @@ __device__ __forceinline__ void clear_frags(Frag<T> (&f)[2 * PARTS])
 }
 
 // ---- tiles in LDS ----
-template <class T>
+template <class T, int WIDTH>
 struct Tile {
+    static_assert(WIDTH == kPart || (sizeof(T) == 2 && WIDTH == 2 * kPart), "slabs");
     static constexpr int kPer = 16 / (int)sizeof(T);              // elements a piece
-    static constexpr int kPieces = kPart / kPer;                  // pieces of a part's row: 4, or 8 of fp32
-    static __device__ __forceinline__ int order(int row) { return sizeof(T) == 2 ? (row >> 2) & 3 : (row >> 1) & 7; }
+    static constexpr int kPieces = WIDTH / kPer;                  // pieces of a slab's row
+    static __device__ __forceinline__ int order(int row)
+    {
+        if constexpr (sizeof(T) == 4) return (row >> 1) & 7;
+        else if constexpr (WIDTH == 64) return (row << 1 & 4) | (row >> 2 & 3);
+        else return row >> 2 & 3;
+    }
+    // piece `piece` of a row of slab `slab`
+    static __device__ __forceinline__ int at(int rows, int slab, int row, int piece) { return slab * rows * WIDTH + row * WIDTH + (piece ^ order(row)) * kPer; }
 };
 template <class T>
 constexpr int tile_elements(int rows, int parts) { return rows * parts * kPart; }
 
 // Rows as an operand whose contraction are the columns: columns 16 s + 8 h .. + 7 of row `row`.
+template <int WIDTH = kPart>
 __device__ __forceinline__ void read_row(const uint16_t* tile, int rows, int row, int h, int s, Frag<uint16_t>& f)
 {
-    const int piece = ((s & 1) * 2 + h) ^ Tile<uint16_t>::order(row);
-    f.v = *reinterpret_cast<const bf16x8*>(tile + ((s >> 1) * rows * kPart + row * kPart + piece * 8));
+    f.v = *reinterpret_cast<const bf16x8*>(tile + Tile<uint16_t, WIDTH>::at(rows, 16 * s / WIDTH, row, 16 * s % WIDTH / 8 + h));
 }
+template <int WIDTH = kPart>
 __device__ __forceinline__ void read_row(const float* tile, int rows, int row, int h, int s, Frag<float>& f)
 {
-    const int o = Tile<float>::order(row), p = (s & 1) * 4 + h * 2;
-    const int at = (s >> 1) * rows * kPart + row * kPart;
-    f.lo = *reinterpret_cast<const v4f*>(tile + (at + (p ^ o) * 4));
-    f.hi = *reinterpret_cast<const v4f*>(tile + (at + ((p + 1) ^ o) * 4));
+    f.lo = *reinterpret_cast<const v4f*>(tile + Tile<float, WIDTH>::at(rows, s >> 1, row, (s & 1) * 4 + h * 2));
+    f.hi = *reinterpret_cast<const v4f*>(tile + Tile<float, WIDTH>::at(rows, s >> 1, row, (s & 1) * 4 + h * 2 + 1));
 }
 // Columns as an operand whose contraction are the rows r0 .. r0 + 15 (a multiple of 16), in the order of a result's registers: column
 // 32 part + lane % 32.  bf16: the LDS transposing read (in every group of 16 lanes, lanes 4 k .. 4 k + 3 point at 16 elements of row k, and
 // lane i receives column i of the four rows).
+template <int WIDTH = kPart>
 __device__ __forceinline__ void read_column(const uint16_t* tile, int rows, int r0, int lane, int part, Frag<uint16_t>& f)
 {
-    const int h = lane >> 5, i = lane & 15, row = r0 + 4 * h + (i >> 2), piece = ((lane & 16) >> 3) + ((i & 3) >> 1);
-    const uint16_t* base = tile + part * rows * kPart;
-    const int lo = row * kPart + (piece ^ Tile<uint16_t>::order(4 * h)) * 8 + (i & 1) * 4;
-    const int hi = (row + 8) * kPart + (piece ^ Tile<uint16_t>::order(8 + 4 * h)) * 8 + (i & 1) * 4;
-    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(base + lo));
-    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(base + hi));
+    using L = Tile<uint16_t, WIDTH>;
+    const int h = lane >> 5, i = lane & 15, row = 4 * h + (i >> 2), slab = kPart * part / WIDTH;
+    const int piece = kPart * part % WIDTH / 8 + ((lane & 16) >> 3) + ((i & 3) >> 1);
+    const uint16_t* base = tile + (r0 * WIDTH + (i & 1) * 4);     // (orders repeat after 16 rows)
+    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(base + L::at(rows, slab, row, piece)));
+    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(base + L::at(rows, slab, row + 8, piece)));
     const s16x8 v = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
     f.v = __builtin_bit_cast(bf16x8, v);
 }
+template <int WIDTH = kPart>
 __device__ __forceinline__ void read_column(const float* tile, int rows, int r0, int lane, int part, Frag<float>& f)
 {
     const int h = lane >> 5, c = lane & 31;
-    const float* base = tile + part * rows * kPart;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const int row = r0 + (e & 3) + 4 * h + 8 * (e >> 2);
-        const float x = base[row * kPart + ((c >> 2) ^ Tile<float>::order(row)) * 4 + (c & 3)];
+        const float x = tile[r0 * kPart + Tile<float, WIDTH>::at(rows, part, (e & 3) + 4 * h + 8 * (e >> 2), c >> 2) + (c & 3)];
         if (e < 4) f.lo[e] = x;
         else f.hi[e - 4] = x;
     }
 }
 
 // Where the threads' pieces of a tile of R rows and PARTS parts come from.  A wavefront's load writes 64 consecutive pieces, all of one
-// part; wavefront `wid` of `WAVES` takes every WAVES-th 64, so a thread has the same GROUPS rows and the same piece of them in every part.
-template <class T, int R, int PARTS, int WAVES>
+// slab; wavefront `wid` of `WAVES` takes every WAVES-th 64, so a thread has the same GROUPS rows and the same piece of them in every slab.
+template <class T, int R, int PARTS, int WAVES, int WIDTH = kPart>
 struct TileLoad {
-    static constexpr int kPer = Tile<T>::kPer, kPieces = Tile<T>::kPieces;
-    static constexpr int kGroups = R * kPieces / (64 * WAVES), kLoads = kGroups * PARTS;
-    static_assert(kGroups * 64 * WAVES == R * kPieces, "whole wavefronts' loads");
-    static __device__ __forceinline__ int row(int group, int wid, int lane) { return ((group * WAVES + wid) * 64 + lane) / kPieces; }
-    static __device__ __forceinline__ int column(int group, int wid, int lane) { return ((lane % kPieces) ^ Tile<T>::order(row(group, wid, lane))) * kPer; }
-    static __device__ __forceinline__ int first(int group, int part, int wid) { return part * R * kPart + (group * WAVES + wid) * 64 * kPer; }
+    using L = Tile<T, WIDTH>;
+    static constexpr int kSlabs = PARTS * kPart / WIDTH, kGroups = R * L::kPieces / (64 * WAVES), kLoads = kGroups * kSlabs;
+    static_assert(kGroups * 64 * WAVES == R * L::kPieces && kSlabs * WIDTH == PARTS * kPart, "whole wavefronts' loads, whole slabs");
+    static __device__ __forceinline__ int row(int group, int wid, int lane) { return ((group * WAVES + wid) * 64 + lane) / L::kPieces; }
+    static __device__ __forceinline__ int column(int group, int wid, int lane) { return ((lane % L::kPieces) ^ L::order(row(group, wid, lane))) * L::kPer; }
+    static __device__ __forceinline__ int first(int group, int slab, int wid) { return slab * R * WIDTH + (group * WAVES + wid) * 64 * L::kPer; }
 };
 
 // Straight to LDS (16-byte aligned rows, a whole number of pieces: one past the row's end becomes its last one; what that multiplies is
 // zero, or is not stored), or through registers.  src(row): the row's address.
-template <class T, int R, int PARTS, int WAVES, bool ALIGNED, class F>
+template <class T, int R, int PARTS, int WAVES, bool ALIGNED, int WIDTH = kPart, class F>
 __device__ __forceinline__ void load_tile(T* tile, int wid, int lane, int D, F src)
 {
-    using L = TileLoad<T, R, PARTS, WAVES>;
+    using M = TileLoad<T, R, PARTS, WAVES, WIDTH>;
+    using L = Tile<T, WIDTH>;
     if constexpr (ALIGNED) {
 #pragma unroll
-        for (int g = 0; g < L::kGroups; ++g) {
-            const int c = L::column(g, wid, lane), end = D - L::kPer - (PARTS - 1) * kPart;
-            const T* p = src(L::row(g, wid, lane)) + c;
+        for (int g = 0; g < M::kGroups; ++g) {
+            const int c = M::column(g, wid, lane), end = D - L::kPer - (M::kSlabs - 1) * WIDTH;
+            const T* p = src(M::row(g, wid, lane)) + c;
 #pragma unroll
-            for (int part = 0; part < PARTS; ++part) {
-                if (part == PARTS - 1) p -= c > end ? c - end : 0;
-                __builtin_amdgcn_global_load_lds((global_ptr)(p + part * kPart), (lds_ptr)(tile + L::first(g, part, wid)), 16, 0, 0);
+            for (int s = 0; s < M::kSlabs; ++s) {
+                if (s == M::kSlabs - 1) p -= c > end ? c - end : 0;
+                __builtin_amdgcn_global_load_lds((global_ptr)(p + s * WIDTH), (lds_ptr)(tile + M::first(g, s, wid)), 16, 0, 0);
             }
         }
     } else {
-        v4u q[L::kLoads];
+        v4u q[M::kLoads];
 #pragma unroll
-        for (int g = 0; g < L::kGroups; ++g) {
-            const T* p = src(L::row(g, wid, lane));
+        for (int g = 0; g < M::kGroups; ++g) {
+            const T* p = src(M::row(g, wid, lane));
 #pragma unroll
-            for (int part = 0; part < PARTS; ++part) q[g * PARTS + part] = load16<true>(p, part * kPart + L::column(g, wid, lane), D);
+            for (int s = 0; s < M::kSlabs; ++s) q[g * M::kSlabs + s] = load16<true>(p, s * WIDTH + M::column(g, wid, lane), D);
         }
 #pragma unroll
-        for (int g = 0; g < L::kGroups; ++g)
+        for (int g = 0; g < M::kGroups; ++g)
 #pragma unroll
-            for (int part = 0; part < PARTS; ++part) *reinterpret_cast<v4u*>(tile + (L::first(g, part, wid) + lane * L::kPer)) = q[g * PARTS + part];
+            for (int s = 0; s < M::kSlabs; ++s) *reinterpret_cast<v4u*>(tile + (M::first(g, s, wid) + lane * L::kPer)) = q[g * M::kSlabs + s];
     }
 }
 
