@@ -25,6 +25,7 @@ namespace attention {
 
 constexpr int kPart = 32;                   // columns of a part of a tile
 constexpr int kMaxColumns = 128;            // of a head
+constexpr int kNonTemporal = 2;             // cache policy of a load
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -200,8 +201,8 @@ struct TileLoad {
 };
 
 // Straight to LDS (16-byte aligned rows, a whole number of pieces: one past the row's end becomes its last one; what that multiplies is
-// zero, or is not stored), or through registers.  src(row): the row's address.
-template <class T, int R, int PARTS, int WAVES, bool ALIGNED, int WIDTH = kPart, class F>
+// zero, or is not stored), or through registers.  src(row): the row's address.  ONCE: past the caches.
+template <class T, int R, int PARTS, int WAVES, bool ALIGNED, int WIDTH = kPart, bool ONCE = false, class F>
 __device__ __forceinline__ void load_tile(T* tile, int wid, int lane, int D, F src)
 {
     using M = TileLoad<T, R, PARTS, WAVES, WIDTH>;
@@ -214,7 +215,7 @@ __device__ __forceinline__ void load_tile(T* tile, int wid, int lane, int D, F s
 #pragma unroll
             for (int s = 0; s < M::kSlabs; ++s) {
                 if (s == M::kSlabs - 1) p -= c > end ? c - end : 0;
-                __builtin_amdgcn_global_load_lds((global_ptr)(p + s * WIDTH), (lds_ptr)(tile + M::first(g, s, wid)), 16, 0, 0);
+                __builtin_amdgcn_global_load_lds((global_ptr)(p + s * WIDTH), (lds_ptr)(tile + M::first(g, s, wid)), 16, 0, ONCE ? kNonTemporal : 0);
             }
         }
     } else {
