@@ -45,9 +45,9 @@ struct State {
 
 constexpr float kSlack = 8.0f;       // powers of two
 
-// How far operands are read ahead; fp32's instructions take long enough without.
+// How far operands are read ahead.
 template <class T>
-constexpr int kAhead = sizeof(T) == 2 ? 4 : 1;
+constexpr int kAhead = sizeof(T) == 2 ? 4 : 2;
 
 // KEYS keys of a tile: their p of the lane's row, and the state's reference moved if need be.  masked: some row does not see some of
 // them.  then() is called when the products are on their way.
@@ -182,7 +182,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_rows_kernel(Args g)
 }
 
 // ---- by keys ----
-constexpr int kRowsByKeys = 32, kKeysByKeys = 32, kRowsJoined = 4;
+constexpr int kRowsByKeys = 32, kKeysByKeys = 32;
 
 // A split's part: sums relative to m, [32][parts of 32], then m and l of each row.
 __host__ __device__ constexpr int part_floats(int parts) { return kRowsByKeys * (parts * kPart + 2); }
@@ -206,7 +206,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_ke
     constexpr int WIDTH = sizeof(T) == 2 && PARTS % 2 == 0 ? 2 * kPart : kPart;
     __shared__ __attribute__((aligned(16))) T kt[W][N];
     __shared__ __attribute__((aligned(16))) T vt[W][N];
-    __shared__ float sums[W][kRowsJoined][COLS + 1], tops[W][kRowsByKeys], ls[W][kRowsByKeys];
+    __shared__ float tops[W][kRowsByKeys], ls[W][kRowsByKeys];
     const int lane = threadIdx.x & 63, h = lane >> 5, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // units in turn: were it splits, those that only long entries have would all go to the same dies; those first
     const int unit = (int)(blockIdx.x % g.units), at = (int)(blockIdx.x / g.units);
@@ -242,45 +242,57 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_ke
             load(v, g.v.lt, key0 + W * KEYS, vt[wid]);
         }
     }
-    // the wavefronts' sums, a few rows at a time
+    // the wavefronts' sums, through the tiles' memory: each wavefront adds up every fourth of the groups of four columns
+    constexpr int HELD = N * sizeof(T) / (64 * sizeof(float));     // registers of the sums that a tile holds
+    static_assert(2 * HELD >= PARTS * 16, "both hold all");
+    float* const in_k = reinterpret_cast<float*>(kt[wid]) + lane;
+    float* const in_v = reinterpret_cast<float*>(vt[wid]) + lane;
     const float l = st.l + other_half(st.l);
+    wait_loads<0>();
+#pragma unroll
+    for (int i = 0; i < PARTS * 16; ++i) (i < HELD ? in_k : in_v - HELD * 64)[i * 64] = st.o[i / 16][i % 16];
     if (h == 0) {
         tops[wid][lane] = st.m;
         ls[wid][lane] = l;
     }
+    __syncthreads();
+    if (!row.there) return;
+    float m = tops[0][lane & 31], n = 0.0f, a[W];
+#pragma unroll
+    for (int w = 1; w < W; ++w) m = fmaxf(m, tops[w][lane & 31]);
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+        const float mw = tops[w][lane & 31];
+        a[w] = mw == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((mw - m) * g.c);
+        n += a[w] * ls[w][lane & 31];
+    }
     float* const part = g.parts ? g.parts + (((int64_t)unit * g.tiles + tile) * g.splits + split) * part_floats(PARTS) : nullptr;
-    const int live = min(kRowsByKeys, g.rows - tile * kRowsByKeys);
-    for (int r0 = 0; r0 < live; r0 += kRowsJoined) {
-        const int mine = (lane & 31) - r0;
-        __syncthreads();                                           // (the last rows' sums have been read)
-        if (mine >= 0 && mine < kRowsJoined) {
+    T* const out = static_cast<T*>(g.out.p) + rows.b * g.out.lb + row.t * g.out.lt + row.head * g.out.lh;
+    const float inv = n > 0.0f ? 1.0f / n : 0.0f;
 #pragma unroll
-            for (int p = 0; p < PARTS; ++p)
+    for (int k = 0; k < PARTS; ++k) {
+        const int i0 = 4 * (k * W + wid), c = 8 * (k * W + wid) + 4 * h;
+        float o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                for (int i = 0; i < 16; ++i) sums[wid][mine][p * kPart + 8 * (i >> 2) + 4 * h + (i & 3)] = st.o[p][i];
+        for (int w = 0; w < W; ++w) {
+            const float* from = (i0 < HELD ? reinterpret_cast<const float*>(kt[w]) : reinterpret_cast<const float*>(vt[w]) - HELD * 64) + lane;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] += a[w] * from[(i0 + e) * 64];
         }
-        __syncthreads();
-        for (int i = threadIdx.x; i < min(kRowsJoined, live - r0) * COLS; i += kThreads) {
-            const int q = i / COLS, c = i % COLS, r = r0 + q;
-            float m = tops[0][r], o = 0.0f, n = 0.0f;
+        if (part) {
+            if (n > 0.0f) put4(part + (lane & 31) * COLS + c, o);
+        } else {
 #pragma unroll
-            for (int w = 1; w < W; ++w) m = fmaxf(m, tops[w][r]);
-#pragma unroll
-            for (int w = 0; w < W; ++w) {
-                const float a = tops[w][r] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((tops[w][r] - m) * g.c);
-                o += a * sums[w][q][c];
-                n += a * ls[w][r];
-            }
-            if (part) {
-                if (n > 0.0f) part[r * COLS + c] = o;
-                if (c < 2) part[kRowsByKeys * COLS + 2 * r + c] = c ? n : m;
-            } else {
-                const Row to = row_of(g, rows, tile * kRowsByKeys + r);
-                if (c < g.D)
-                    put1(static_cast<T*>(g.out.p) + rows.b * g.out.lb + to.t * g.out.lt + to.head * g.out.lh + c, n > 0.0f ? o / n : 0.0f);
-                if (c == 0 && g.lse) g.lse[((int64_t)rows.b * g.Hq + to.head) * g.Tq + to.t] = n > 0.0f ? m * g.scale + logf(n) : -INFINITY;
-            }
+            for (int e = 0; e < 4; ++e) o[e] *= inv;
+            store4(out, c, g.D, o);
         }
+    }
+    if (wid || h) return;
+    if (part) {
+        part[kRowsByKeys * COLS + 2 * lane] = m;
+        part[kRowsByKeys * COLS + 2 * lane + 1] = n;
+    } else if (g.lse) {
+        g.lse[((int64_t)rows.b * g.Hq + row.head) * g.Tq + row.t] = n > 0.0f ? m * g.scale + logf(n) : -INFINITY;
     }
 }
 

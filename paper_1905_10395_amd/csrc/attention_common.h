@@ -35,22 +35,42 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) void* lds_ptr;
 typedef const __attribute__((address_space(1))) void* global_ptr;
 
-// Eight elements of an operand.
+// Eight elements of an operand.  fp32: as the sum of three bf16 values, each of which takes the next eight bits of what is left (to
+// 2^-24 of the element); of the nine products of two such sums the six largest are made, and what is left out is below 2^-24 of the
+// whole.  Six bf16 instructions take 6 / 16 of the time of the fp32 ones of the same products; the parts are made on the way from LDS.
 template <class T> struct Frag;
 template <> struct Frag<uint16_t> { bf16x8 v; };
-template <> struct Frag<float> { v4f lo, hi; };
+template <> struct Frag<float> { bf16x8 v[3]; };
 
 __device__ __forceinline__ void multiply(f32x16& c, const Frag<uint16_t>& a, const Frag<uint16_t>& b)
 {
     c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, b.v, c, 0, 0, 0);
 }
-// fp32: instructions of a contraction of two, element e of both halves in each
 __device__ __forceinline__ void multiply(f32x16& c, const Frag<float>& a, const Frag<float>& b)
 {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.lo[e], b.lo[e], c, 0, 0, 0);
+    for (int k = 2; k >= 0; --k)                              // the smallest first
 #pragma unroll
-    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.hi[e], b.hi[e], c, 0, 0, 0);
+        for (int i = 0; i <= k; ++i) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v[i], b.v[k - i], c, 0, 0, 0);
+}
+__device__ __forceinline__ void split(const float (&x)[8], Frag<float>& f)
+{
+    float r[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = x[e];
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+        v4u q;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            q[e] = f32x2_to_bf16x2(r[2 * e], r[2 * e + 1]);
+            if (k < 2) {
+                r[2 * e] -= __uint_as_float(q[e] << 16);
+                r[2 * e + 1] -= __uint_as_float(q[e] & 0xFFFF0000u);
+            }
+        }
+        f.v[k] = __builtin_bit_cast(bf16x8, q);
+    }
 }
 
 // Half of a result's column as an operand: registers 8 k .. 8 k + 7.
@@ -63,11 +83,10 @@ __device__ __forceinline__ void from_result(const f32x16& r, int k, Frag<uint16_
 }
 __device__ __forceinline__ void from_result(const f32x16& r, int k, Frag<float>& f)
 {
+    float x[8];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        f.lo[e] = r[8 * k + e];
-        f.hi[e] = r[8 * k + 4 + e];
-    }
+    for (int e = 0; e < 8; ++e) x[e] = r[8 * k + e];
+    split(x, f);
 }
 
 // 16 bytes of a row of D columns from column c on, zeros past its end; any alignment.  A piece that the row's end cuts is read so that
@@ -108,11 +127,15 @@ __device__ __forceinline__ v4u load16(const T* row, int c, int D)
 // An operand's eight elements from memory.
 template <bool EDGE>
 __device__ __forceinline__ void load_frag(const uint16_t* row, int c, int D, Frag<uint16_t>& f) { f.v = __builtin_bit_cast(bf16x8, load16<EDGE>(row, c, D)); }
+__device__ __forceinline__ void split(v4f lo, v4f hi, Frag<float>& f)
+{
+    const float x[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    split(x, f);
+}
 template <bool EDGE>
 __device__ __forceinline__ void load_frag(const float* row, int c, int D, Frag<float>& f)
 {
-    f.lo = __builtin_bit_cast(v4f, load16<EDGE>(row, c, D));
-    f.hi = __builtin_bit_cast(v4f, load16<EDGE>(row, c + 4, D));
+    split(__builtin_bit_cast(v4f, load16<EDGE>(row, c, D)), __builtin_bit_cast(v4f, load16<EDGE>(row, c + 4, D)), f);
 }
 // A lane's row as operands, contraction along its columns: zeros past the row's end.  All are asked for before any is waited for.
 template <class T, int PARTS>
@@ -158,8 +181,9 @@ __device__ __forceinline__ void read_row(const uint16_t* tile, int rows, int row
 template <int WIDTH = kPart>
 __device__ __forceinline__ void read_row(const float* tile, int rows, int row, int h, int s, Frag<float>& f)
 {
-    f.lo = *reinterpret_cast<const v4f*>(tile + Tile<float, WIDTH>::at(rows, s >> 1, row, (s & 1) * 4 + h * 2));
-    f.hi = *reinterpret_cast<const v4f*>(tile + Tile<float, WIDTH>::at(rows, s >> 1, row, (s & 1) * 4 + h * 2 + 1));
+    const v4f lo = *reinterpret_cast<const v4f*>(tile + Tile<float, WIDTH>::at(rows, s >> 1, row, (s & 1) * 4 + h * 2));
+    const v4f hi = *reinterpret_cast<const v4f*>(tile + Tile<float, WIDTH>::at(rows, s >> 1, row, (s & 1) * 4 + h * 2 + 1));
+    split(lo, hi, f);
 }
 // Columns as an operand whose contraction are the rows r0 .. r0 + 15 (a multiple of 16), in the order of a result's registers: column
 // 32 part + lane % 32.  bf16: the LDS transposing read (in every group of 16 lanes, lanes 4 k .. 4 k + 3 point at 16 elements of row k, and
@@ -180,12 +204,10 @@ template <int WIDTH = kPart>
 __device__ __forceinline__ void read_column(const float* tile, int rows, int r0, int lane, int part, Frag<float>& f)
 {
     const int h = lane >> 5, c = lane & 31;
+    float x[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float x = tile[r0 * kPart + Tile<float, WIDTH>::at(rows, part, (e & 3) + 4 * h + 8 * (e >> 2), c >> 2) + (c & 3)];
-        if (e < 4) f.lo[e] = x;
-        else f.hi[e - 4] = x;
-    }
+    for (int e = 0; e < 8; ++e) x[e] = tile[r0 * kPart + Tile<float, WIDTH>::at(rows, part, (e & 3) + 4 * h + 8 * (e >> 2), c >> 2) + (c & 3)];
+    split(x, f);
 }
 
 // Where the threads' pieces of a tile of R rows and PARTS parts come from.  A wavefront's load writes 64 consecutive pieces, all of one

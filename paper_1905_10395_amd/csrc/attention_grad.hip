@@ -63,7 +63,7 @@ __device__ __forceinline__ float dot(const Frag<float>& a, const Frag<float>& b)
 {
     float s = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) s += a.lo[e] * b.lo[e] + a.hi[e] * b.hi[e];
+    for (int e = 0; e < 8; ++e) s += ((float)a.v[0][e] + ((float)a.v[1][e] + (float)a.v[2][e])) * ((float)b.v[0][e] + ((float)b.v[1][e] + (float)b.v[2][e]));
     return s;
 }
 // How far operands are read ahead; fp32's instructions take long enough without, and by keys registers are short.
