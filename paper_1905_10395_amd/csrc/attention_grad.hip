@@ -43,8 +43,11 @@ struct Form {
 // Many rows: 128 a workgroup.
 template <class T> using RowsMany = Form<4, 1, sizeof(T) == 2 ? 64 : 32, 2>;
 // Many keys: with a causal mask the first keys have all rows to pass and the last none, and two halves of a workgroup that take every
-// second tile halve the longest one's time (gradients of 4 x 4096 x 16 x 128: 1160 -> TODO us).
-template <class T> using KeysMany = Form<4, 2, sizeof(T) == 2 ? 64 : 32, 2>;
+// second tile halve the longest one's time (gradients of 4 x 4096 x 16 x 128: 1160 -> 955 us).  The parts of wide fp32 leave registers for
+// one wavefront a SIMD, so four in all (4 x 1024 x 8 x 128: 345 us, 475 with eight; but 64 columns 169, 192 with four).
+template <class T, int PARTS> constexpr bool kWide = sizeof(T) == 4 && PARTS > 2;
+template <class T, int PARTS>
+using KeysMany = std::conditional_t<kWide<T, PARTS>, Form<2, 2, 32, 2>, Form<4, 2, sizeof(T) == 2 ? 64 : 32, 2>>;
 // Few of either: 32 a workgroup.
 template <class T> using Few = Form<1, 4, 32, 1>;
 
@@ -66,11 +69,14 @@ __device__ __forceinline__ float dot(const Frag<float>& a, const Frag<float>& b)
     for (int e = 0; e < 8; ++e) s += ((float)a.v[0][e] + ((float)a.v[1][e] + (float)a.v[2][e])) * ((float)b.v[0][e] + ((float)b.v[1][e] + (float)b.v[2][e]));
     return s;
 }
-// How far operands are read ahead; fp32's instructions take long enough without, and by keys registers are short.
+// How far operands are read ahead; by keys registers are short.
 template <class T>
-constexpr int kAheadRows = sizeof(T) == 2 ? 4 : 1;
+constexpr int kAheadRows = sizeof(T) == 2 ? 4 : 2;
 template <class T>
-constexpr int kAheadKeys = sizeof(T) == 2 ? 2 : 1;
+constexpr int kAheadKeys = 2;
+// Wavefronts a SIMD.
+template <class F, class T, int PARTS>
+constexpr int kOccupancy = kWide<T, PARTS> || F::BUFFERS == 1 ? 1 : 2;
 
 // c += the product of 32 rows of a tile, from row r0 on, with an operand in registers.
 template <int AHEAD, class T, int PARTS>
@@ -141,7 +147,7 @@ __device__ __forceinline__ void join_shared(void* tile0, void* tile1, int own, i
 }
 
 template <class F, class T, int PARTS, bool ALIGNED>
-__global__ __launch_bounds__(F::THREADS, F::WAVES == 4 && F::BUFFERS == 1 ? 1 : 2) void attention_dq_kernel(Args g)
+__global__ __launch_bounds__(F::THREADS, (kOccupancy<F, T, PARTS>)) void attention_dq_kernel(Args g)
 {
     constexpr int KEYS = F::TILE, N = tile_elements<T>(KEYS, PARTS);
     static_assert(sizeof(T) * N >= 2 * 4 * PARTS * 16 * 64 || F::SHARE == 1, "two areas a tile");
@@ -251,7 +257,7 @@ __device__ __forceinline__ int first_row(const Args& g, int nq, int nk, int key)
 }
 
 template <class F, class T, int PARTS, bool ALIGNED>
-__global__ __launch_bounds__(F::THREADS, F::WAVES == 4 && F::BUFFERS == 1 ? 1 : 2) void attention_dkv_kernel(Args g)
+__global__ __launch_bounds__(F::THREADS, (kOccupancy<F, T, PARTS>)) void attention_dkv_kernel(Args g)
 {
     constexpr int ROWS = F::TILE, N = tile_elements<T>(ROWS, PARTS);
     static_assert(sizeof(T) * N >= 2 * 4 * PARTS * 16 * 64 || F::SHARE == 1, "two areas a tile");
@@ -384,18 +390,18 @@ __global__ __launch_bounds__(F::THREADS, F::WAVES == 4 && F::BUFFERS == 1 ? 1 : 
     }
 }
 
-// The sums of the splits' parts, in order.  KV: of dk and dv, else of dq.
+// The sums of the splits' parts, in order: of dq, and of dk and dv.
 constexpr int kJoinThreads = 256;
 template <class T, int PARTS, bool KV>
-__global__ __launch_bounds__(kJoinThreads) void attention_grad_join_kernel(Args g)
+__device__ __forceinline__ void join_parts(const Args& g)
 {
     constexpr int COLS = PARTS * kPart, LISTS = KV ? 2 : 1;
     const int splits = KV ? g.key_splits : g.row_splits, many = KV ? g.Tk : g.rows;
     const int64_t id = (int64_t)blockIdx.x * kJoinThreads + threadIdx.x, row = id / COLS;
-    const int c = (int)(id % COLS), unit = (int)(row / many), r = (int)(row % many);
-    if (unit >= g.units || c >= g.D) return;
+    const int c = (int)(id % COLS), r = (int)(row % many);
+    if (row >= (int64_t)g.units * many || c >= g.D) return;
+    const int unit = (int)(row / many), b = unit / g.Hk, hk = unit % g.Hk;
     const float* p = (KV ? g.dkv_parts : g.dq_parts) + row * splits * LISTS * COLS + c;
-    const int b = unit / g.Hk, hk = unit % g.Hk;
 #pragma unroll
     for (int list = 0; list < LISTS; ++list) {
         float s = 0.0f;
@@ -403,6 +409,15 @@ __global__ __launch_bounds__(kJoinThreads) void attention_grad_join_kernel(Args 
         const Heads& a = KV ? (list ? g.dv : g.dk) : g.dq;
         const int t = KV ? r : over(r, g.by_g), head = KV ? hk : hk * g.G + r - t * g.G;
         put1(static_cast<T*>(a.p) + b * a.lb + t * a.lt + head * a.lh + c, s);
+    }
+}
+template <class T, int PARTS>
+__global__ __launch_bounds__(kJoinThreads) void attention_grad_join_kernel(Args g)
+{
+    if (blockIdx.y) {
+        if (g.dkv_parts) join_parts<T, PARTS, true>(g);
+    } else {
+        if (g.dq_parts) join_parts<T, PARTS, false>(g);
     }
 }
 
@@ -430,13 +445,13 @@ Plan plan_of(int B, int Tq, int Tk, int Hq, int Hk, int D, int is_bf16)
     Plan p{};
     const int64_t rows = (int64_t)Tq * (Hq / Hk), units = (int64_t)B * Hk;
     const size_t cols = (size_t)parts_of(D) * kPart;
-    auto tiles = [&](int64_t many, bool& few) {
-        few = units * ((many + 127) / 128) < kComputeUnits;
-        const int mine = few ? 32 : 128;
+    auto tiles = [&](int64_t many, int each, bool& few) {
+        few = units * ((many + each - 1) / each) < kComputeUnits;
+        const int mine = few ? Few<float>::MINE : each;
         return (int)((many + mine - 1) / mine);
     };
-    p.row_tiles = tiles(rows, p.few_rows);
-    p.key_tiles = tiles(Tk, p.few_keys);
+    p.row_tiles = tiles(rows, RowsMany<float>::MINE, p.few_rows);
+    p.key_tiles = tiles(Tk, !is_bf16 && parts_of(D) > 2 ? KeysMany<float, 4>::MINE : KeysMany<uint16_t, 4>::MINE, p.few_keys);
     const int64_t least = is_bf16 ? 512 : 128;
     split(units * p.row_tiles, Tk, least, p.row_splits, p.row_chunk);
     split(units * p.key_tiles, rows, least, p.key_splits, p.key_chunk);
@@ -459,21 +474,23 @@ void launch_keys(const Args& g, bool few, hipStream_t s)
 {
     const dim3 grid((unsigned)workgroups(g, (int64_t)g.key_tiles * g.key_splits));
     if (few) hipLaunchKernelGGL((attention_dkv_kernel<Few<T>, T, PARTS, ALIGNED>), grid, dim3(Few<T>::THREADS), 0, s, g);
-    else hipLaunchKernelGGL((attention_dkv_kernel<KeysMany<T>, T, PARTS, ALIGNED>), grid, dim3(KeysMany<T>::THREADS), 0, s, g);
+    else hipLaunchKernelGGL((attention_dkv_kernel<KeysMany<T, PARTS>, T, PARTS, ALIGNED>), grid, dim3(KeysMany<T, PARTS>::THREADS), 0, s, g);
 }
 template <class T, int PARTS>
 void launch(const Args& g, const Plan& p, bool aligned_rows, bool aligned_keys, hipStream_t s)
 {
-    auto join_grid = [&](int64_t many) { return dim3((unsigned)((g.units * many * PARTS * kPart + kJoinThreads - 1) / kJoinThreads)); };
     if (g.rows) {
         if (aligned_keys) launch_rows<T, PARTS, true>(g, p.few_rows, s);
         else launch_rows<T, PARTS, false>(g, p.few_rows, s);
-        if (g.row_splits > 1) hipLaunchKernelGGL((attention_grad_join_kernel<T, PARTS, false>), join_grid(g.rows), dim3(kJoinThreads), 0, s, g);
     }
     if (g.Tk) {
         if (aligned_rows) launch_keys<T, PARTS, true>(g, p.few_keys, s);
         else launch_keys<T, PARTS, false>(g, p.few_keys, s);
-        if (g.key_splits > 1) hipLaunchKernelGGL((attention_grad_join_kernel<T, PARTS, true>), join_grid(g.Tk), dim3(kJoinThreads), 0, s, g);
+    }
+    if (g.dq_parts || g.dkv_parts) {
+        const int64_t many = std::max<int64_t>(g.dq_parts ? g.rows : 0, g.dkv_parts ? g.Tk : 0);
+        const dim3 grid((unsigned)((g.units * many * PARTS * kPart + kJoinThreads - 1) / kJoinThreads), 2);
+        hipLaunchKernelGGL((attention_grad_join_kernel<T, PARTS>), grid, dim3(kJoinThreads), 0, s, g);
     }
 }
 
