@@ -27,6 +27,7 @@ struct Args : Shape {
     int tiles;                       // of rows
     int splits, chunk;               // by keys: workgroups a tile of rows, and the keys of one
     float scale, c;                  // c: scale log2 e
+    int wide_out;                    // rows of out are whole 16-byte pieces
 };
 
 // What a wavefront holds of 32 rows: their sums so far, relative to m.
@@ -168,17 +169,23 @@ __global__ __launch_bounds__(kThreads, 2) void attention_rows_kernel(Args g)
         step(key0, k0, v0, k1, v1);
         if (key0 + KEYS < rows.end) step(key0 + KEYS, k1, v1, k0, v0);
     }
-    if (!row.there) return;
     const float l = st.l + other_half(st.l), inv = l > 0.0f ? 1.0f / l : 0.0f;
-    T* out = static_cast<T*>(g.out.p) + rows.b * g.out.lb + row.t * g.out.lt + row.head * g.out.lh;
-#pragma unroll
-    for (int p = 0; p < PARTS; ++p)
-#pragma unroll
-        for (int i = 0; i < 16; i += 4) {
-            const float o[4] = {st.o[p][i] * inv, st.o[p][i + 1] * inv, st.o[p][i + 2] * inv, st.o[p][i + 3] * inv};
-            store4(out, p * kPart + 2 * i + 4 * h, g.D, o);
-        }
-    if (g.lse && h == 0) g.lse[((int64_t)rows.b * g.Hq + row.head) * g.Tq + row.t] = l > 0.0f ? st.m * g.scale + logf(l) : -INFINITY;
+    if (g.lse && row.there && h == 0) g.lse[((int64_t)rows.b * g.Hq + row.head) * g.Tq + row.t] = l > 0.0f ? st.m * g.scale + logf(l) : -INFINITY;
+    T* const out = static_cast<T*>(g.out.p) + rows.b * g.out.lb + (int64_t)rows.hk * g.G * g.out.lh;
+    auto place = [&](int r) {
+        const int t = over(r, g.by_g);
+        return out + t * g.out.lt + (r - t * g.G) * g.out.lh;
+    };
+    const int r0 = tile * kRowsByRows + wid * 32;
+    if (g.wide_out) {
+        __syncthreads();                                           // the tiles have been read
+        constexpr int kMine = PARTS * kPart * 32, kFit = KEYS / 32;    // elements of a wavefront; how many a tile holds
+        const int tile_of = wid / kFit;
+        T* const mine = (tile_of == 0 ? k0 : tile_of == 1 ? k1 : tile_of == 2 ? v0 : v1) + wid % kFit * kMine;
+        store_rows<T, PARTS>(mine, lane, g.D, inv, st.o, [&](int i) { return r0 + i < g.rows ? place(r0 + i) : nullptr; });
+    } else if (row.there) {
+        store_sums<T, PARTS>(place(r0 + (lane & 31)), lane, g.D, inv, st.o);
+    }
 }
 
 // ---- by keys ----
@@ -448,6 +455,7 @@ lsgd_status lsgd_attention(const lsgd_attention_args* p, void* workspace, size_t
     g.scale = p->scale; g.c = p->scale * kLog2e;
     // what is read by 16 bytes straight to LDS has to lie on them
     const bool aligned = D % (16 / es) == 0 && wide_heads(p->k, B, Tk, Hk, es) && wide_heads(p->v, B, Tk, Hk, es);
+    g.wide_out = D % (16 / es) == 0 && wide_heads(p->out, B, Tq, Hq, es);
     by_type_and_parts(p->is_bf16, parts_of(D), [&](auto type, auto parts) {
         launch<decltype(type), decltype(parts)::value>(g, plan, aligned, static_cast<hipStream_t>(hip_stream));
     });

@@ -417,6 +417,43 @@ __device__ __forceinline__ void store4(T* row, int c, int D, const float (&v)[4]
             if (c + e < D) put1(row + c + e, v[e]);
 }
 
+// The lane's columns of its row, times a factor, any alignment.
+template <class T, int PARTS>
+__device__ __forceinline__ void store_sums(T* row, int lane, int D, float factor, const f32x16 (&s)[PARTS])
+{
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            const float o[4] = {s[p][i] * factor, s[p][i + 1] * factor, s[p][i + 2] * factor, s[p][i + 3] * factor};
+            store4(row, p * kPart + 2 * i + 4 * (lane >> 5), D, o);
+        }
+}
+// The same of 16-byte aligned rows, a whole number of pieces: through LDS ([32][PARTS 32] of the wavefront's own), so that rows are written
+// by 16 bytes a lane, one after the other, and not by 8 of 32 rows at a time.  row(i): the address of row i of the 32, NULL: not stored.
+template <class T, int PARTS, class F>
+__device__ __forceinline__ void store_rows(T* lds, int lane, int D, float factor, const f32x16 (&s)[PARTS], F row)
+{
+    constexpr int kPer = 16 / (int)sizeof(T), kPieces = PARTS * kPart / kPer;
+    auto at = [](int r, int piece) { return (r * kPieces + (piece + r) % kPieces) * kPer; };      // rotated: over all banks
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            const float o[4] = {s[p][i] * factor, s[p][i + 1] * factor, s[p][i + 2] * factor, s[p][i + 3] * factor};
+            const int c = p * kPart + 2 * i + 4 * (lane >> 5);
+            put4(lds + (at(lane & 31, c / kPer) + c % kPer), o);
+        }
+    asm volatile("" ::: "memory");                                // (LDS serves a wavefront in order)
+#pragma unroll
+    for (int k = 0; k < 32 * kPieces / 64; ++k) {
+        const int slot = k * 64 + lane, r = slot / kPieces, piece = slot % kPieces;
+        T* to = row(r);
+        if (to && piece * kPer < D) *reinterpret_cast<v4u*>(to + piece * kPer) = *reinterpret_cast<const v4u*>(lds + at(r, piece));
+    }
+    asm volatile("" ::: "memory");
+}
+
 // ---- host ----
 constexpr size_t kAlign = 256;
 constexpr int kMaxEntries = 1 << 20, kMaxTokens = 1 << 24, kMaxHeads = 1024;

@@ -104,19 +104,6 @@ __device__ __forceinline__ void clear_sums(f32x16 (&s)[PARTS])
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[p][i] = 0.0f;
 }
-// The lane's columns of its row, times a factor, in the tensor's type or, for a part, fp32.
-template <class T, int PARTS>
-__device__ __forceinline__ void store_sums(T* row, int lane, int D, float factor, const f32x16 (&s)[PARTS])
-{
-#pragma unroll
-    for (int p = 0; p < PARTS; ++p)
-#pragma unroll
-        for (int i = 0; i < 16; i += 4) {
-            const float o[4] = {s[p][i] * factor, s[p][i + 1] * factor, s[p][i + 2] * factor, s[p][i + 3] * factor};
-            store4(row, p * kPart + 2 * i + 4 * (lane >> 5), D, o);
-        }
-}
-
 // The sums of the wavefronts that share rows, in the first one's registers: areas of a wavefront's sums in the two tiles' memory.
 template <class F, int PARTS>
 __device__ __forceinline__ void join_shared(void* tile0, void* tile1, int own, int share, int lane, f32x16 (&s)[PARTS])
