@@ -498,7 +498,7 @@ typedef struct {
     int32_t B, Tq, Tk, Hq, Hk, D;
     int32_t is_bf16;              /* type of q, k, v, out: 0 fp32, 1 bf16 */
     int32_t causal;
-    float scale;                  /* positive                            */
+    float scale;                  /* within [1e-30, 1e30]                 */
     lsgd_heads q, k, v, out;
     const int32_t *q_lens, *k_lens;
     float* lse;

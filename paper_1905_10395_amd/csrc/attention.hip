@@ -431,7 +431,7 @@ lsgd_status lsgd_attention(const lsgd_attention_args* p, void* workspace, size_t
     const int B = p->B, Tq = p->Tq, Tk = p->Tk, Hq = p->Hq, Hk = p->Hk, D = p->D, es = p->is_bf16 ? 2 : 4;
     LSGD_TRY(check_attention_shape(who, B, Tq, Tk, Hq, Hk, D));
     if (p->is_bf16 & ~1 || p->causal & ~1) return set_error(LSGD_ERR_INVALID_ARG, "%s: is_bf16 and causal must be 0 or 1", who);
-    if (!std::isfinite(p->scale) || p->scale <= 0.0f) return set_error(LSGD_ERR_INVALID_ARG, "%s: scale must be finite and positive", who);
+    if (!scale_ok(p->scale)) return set_error(LSGD_ERR_INVALID_ARG, "%s: scale must be within [1e-30, 1e30]", who);
     if (Tq == 0) return LSGD_OK;
     if ((int64_t)B * Hk > INT64_C(1) << 30 || !fits(B, Tq, Tk, Hq, Hk, D)) return set_error(LSGD_ERR_SHAPE, "%s: B=%d, Tq=%d, Hk=%d are too large for one launch", who, B, Tq, Hk);
     LSGD_TRY(check_heads(who, "q", p->q, B, Tq, Hq, D, es, true, false));

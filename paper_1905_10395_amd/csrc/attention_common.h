@@ -464,6 +464,8 @@ constexpr int kMaxEntries = 1 << 20, kMaxTokens = 1 << 24, kMaxHeads = 1024;
         if (st_ != LSGD_OK) return st_;     \
     } while (0)
 
+// A scale whose inverse is a normal value as well, with room for scores.
+inline bool scale_ok(float scale) { return scale >= 1e-30f && scale <= 1e30f; }
 lsgd_status check_attention_shape(const char* who, int64_t B, int64_t Tq, int64_t Tk, int64_t Hq, int64_t Hk, int64_t D);
 inline int parts_of(int D) { return (D + kPart - 1) / kPart; }
 

@@ -511,7 +511,7 @@ lsgd_status lsgd_attention_grad(const lsgd_attention_grad_args* p, void* workspa
     const int B = p->B, Tq = p->Tq, Tk = p->Tk, Hq = p->Hq, Hk = p->Hk, D = p->D, es = p->is_bf16 ? 2 : 4;
     LSGD_TRY(check_attention_shape(who, B, Tq, Tk, Hq, Hk, D));
     if (p->is_bf16 & ~1 || p->causal & ~1) return set_error(LSGD_ERR_INVALID_ARG, "%s: is_bf16 and causal must be 0 or 1", who);
-    if (!std::isfinite(p->scale) || p->scale <= 0.0f) return set_error(LSGD_ERR_INVALID_ARG, "%s: scale must be finite and positive", who);
+    if (!scale_ok(p->scale)) return set_error(LSGD_ERR_INVALID_ARG, "%s: scale must be within [1e-30, 1e30]", who);
     if (Tq == 0 && Tk == 0) return LSGD_OK;
     if ((int64_t)B * Hk > INT64_C(1) << 30) return set_error(LSGD_ERR_SHAPE, "%s: B=%d, Hk=%d are too large for one launch", who, B, Hk);
     const Plan plan = plan_of(B, Tq, Tk, Hq, Hk, D, p->is_bf16);

@@ -516,6 +516,7 @@ lsgd_status lsgd_qk_rotary(const lsgd_qk_rotary_args* p, void* hip_stream)
     for (const lsgd_heads* a : {&p->q, &p->q_out}) once = once && wide_heads(*a, W, T, p->Hq, es);
     for (const lsgd_heads* a : {&p->k, &p->k_out}) once = once && wide_heads(*a, W, T, p->Hk, es);
     const dim3 grid((unsigned)((T + g.tokens - 1) / g.tokens), (unsigned)W);
+    if ((double)grid.x * W * kThreads >= 4294967296.0) return set_error(LSGD_ERR_SHAPE, "%s: W=%d, T=%d are too large for one launch", who, W, T);
     dispatch(p->is_bf16, E, p->interleaved, once, [&](auto type, auto e, auto neighbours, auto streamed) {
         hipLaunchKernelGGL((qk_rotary_kernel<decltype(type), decltype(e)::value, decltype(neighbours)::value, decltype(streamed)::value>), grid,
                            dim3(kThreads), sizeof(v2f) * (size_t)std::max(1, g.tokens * g.half), static_cast<hipStream_t>(hip_stream), g);

@@ -49,6 +49,8 @@ def test_qk_rotary_arguments():
         assert f(qk(**bad), None) == status and word in error(), (bad, error())
     assert f(None, None) == INVALID
     assert f(qk(T=0), None) == OK
+    assert f(qk(W=32768, T=2 ** 24, Hq=1, Hk=0, k=NONE, k_out=NONE, wk=0, D=1, R=0, turns=0, ld_pos=0, q=(P, 2 ** 24, 1, 1), q_out=(P, 2 ** 24, 1, 1)), None) == SHAPE
+    assert "too large" in error()
     # without a norm eps has no meaning, without a rotation turns have none
     assert f(qk(T=0, norm=0, eps=0.0, R=0, turns=0), None) == OK
 
@@ -81,7 +83,8 @@ def attention(B=2, Tq=3, Tk=5, Hq=4, Hk=2, D=8, bf16=0, causal=0, scale=1.0, q=N
 
 BAD = [(dict(B=0), SHAPE, "B="), (dict(B=2 ** 20 + 1), SHAPE, "B="), (dict(Tq=-1), SHAPE, "Tq="), (dict(Tk=2 ** 24 + 1), SHAPE, "Tk="), (dict(Hk=0), SHAPE, "Hk="),
        (dict(Hq=5), SHAPE, "multiple"), (dict(Hq=2048), SHAPE, "Hq="), (dict(D=0), SHAPE, "D="), (dict(D=129), UNSUPPORTED, "128"), (dict(bf16=2), INVALID, "is_bf16"),
-       (dict(causal=-1), INVALID, "causal"), (dict(scale=0.0), INVALID, "scale"), (dict(scale=-1.0), INVALID, "scale"), (dict(scale=float("inf")), INVALID, "scale"),
+       (dict(causal=-1), INVALID, "causal"), (dict(scale=0.0), INVALID, "scale"), (dict(scale=-1.0), INVALID, "scale"), (dict(scale=float("inf")), INVALID, "scale"), (dict(scale=float("nan")), INVALID, "scale"),
+       (dict(scale=1e-39), INVALID, "scale"),
        (dict(q=NONE), INVALID, "q is required"), (dict(v=NONE), INVALID, "v is required"), (dict(k=heads(5, 2, 8, P + 2)), INVALID, "k is not aligned"),
        (dict(k=(P, 80, -16, 8)), SHAPE, "negative"), (dict(q_lens=P + 2), INVALID, "q_lens"), (dict(k_lens=P + 1), INVALID, "k_lens"),
        (dict(Hq=1024, Hk=1, Tq=2 ** 21), SHAPE, "too large"), (dict(B=2 ** 20, Tq=2 ** 20), SHAPE, "too large")]

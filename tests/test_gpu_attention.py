@@ -53,7 +53,7 @@ class Reference:
         self.k, self.v = (x.masked_fill(~self.seen.any(2)[..., None], 0.0) for x in (self.k, self.v))
         self.q = self.q.masked_fill(~self.seen.any(3)[..., None], 0.0)
         s = scale * self.q @ self.k.transpose(2, 3)
-        # a score: D products and sums; its exponent: the difference to another of its row, rounded; exp2: 2 last bits
+        # a score: four roundings a product (fp32 in three parts) and D sums; its exponent: the difference to another of its row, rounded; exp2: 2 last bits
         es = scale * (self.q.abs() @ self.k.abs().transpose(2, 3)) * (D + 4) * EPS
         s = s.masked_fill(hidden, -math.inf)
         self.lse = torch.logsumexp(s, 3) if Tk else torch.full((B, Hq, Tq), -math.inf, dtype=torch.float64)
