@@ -347,12 +347,22 @@ struct Plan {
     size_t bytes;
 };
 constexpr int kComputeUnits = 256;
-Plan plan_of(int B, int Tq, int Tk, int Hq, int Hk, int D)
+// By keys where by rows would leave compute units without a workgroup (heads of 128, 16 query and 4 key heads; us by rows, by keys):
+// 1024 causal tokens, 128 workgroups, bf16 24.4, 18.2, fp32 114, 47; 1536, 192 workgroups, bf16 33, 29, fp32 163, 89; but 2048, 256
+// workgroups, 42, 40 and 216, 138, and 8 x 512 x 8 x 8, as many, 17, 23 and 65, 62.  Without a causal mask rows' workgroups all have as
+// much to do, and bf16, bound by the products, gains up to half as many: 1024 tokens 23.5, 21.3; 1152, 144 workgroups, 26.7, 33.5.
+//
+// Splits of the keys cost their parts' way through memory.  Tiles of many rows: as many splits as compute units take (1152 causal
+// tokens in 576 workgroups: 20 us, in two splits 45; 64 x 16 rows to 16384 keys, 128 workgroups: unsplit 142, two splits 93, eight 128).
+// One tile, where reading the keys is all there is, and lengths differ: six a compute unit (32 x 8 key heads to up to 16384 keys: 267 us
+// with one, 212 with four, 209 with six, 207 with eight; 128 x 4 heads to 4096 keys each: 185, 210, 218, 226).  None of fewer
+// than 1024 keys (2 x 4 key heads, one query, 2048 keys: 15.9 us, unsplit 19.2; 16384: 27.5, splits of 2048 35).
+Plan plan_of(int B, int Tq, int Tk, int Hq, int Hk, int D, int is_bf16, int causal)
 {
     Plan p{};
     const int64_t rows = (int64_t)Tq * (Hq / Hk), units = (int64_t)B * Hk;
     const int64_t by_rows = units * ((rows + kRowsByRows - 1) / kRowsByRows);
-    p.by_keys = rows <= kRowsByKeys || by_rows < kComputeUnits / 2;
+    p.by_keys = rows <= kRowsByKeys || by_rows < (is_bf16 && !causal ? kComputeUnits / 2 + 1 : kComputeUnits);
     p.splits = 1;
     p.chunk = std::max(Tk, 1);
     p.bytes = kAlign;
@@ -361,7 +371,7 @@ Plan plan_of(int B, int Tq, int Tk, int Hq, int Hk, int D)
         return p;
     }
     p.tiles = (int)((rows + kRowsByKeys - 1) / kRowsByKeys);
-    const int64_t groups = units * p.tiles, wanted = std::max<int64_t>(1, 8 * kComputeUnits / std::max<int64_t>(1, groups));
+    const int64_t groups = units * p.tiles, wanted = std::max<int64_t>(1, (p.tiles == 1 ? 6 : 1) * kComputeUnits / std::max<int64_t>(1, groups));
     const int least = LSGD_ATTENTION_ONE_LAUNCH, step = 128;
     const int64_t splits = std::min<int64_t>(wanted, (Tk + least - 1) / least);
     if (splits > 1) {
@@ -389,9 +399,8 @@ void launch(const Args& g, const Plan& p, bool aligned, hipStream_t s)
 }
 
 // Launches of at most 2^31 workgroups and fewer than 2^32 threads.
-bool fits(int B, int Tq, int Tk, int Hq, int Hk, int D)
+bool fits(const Plan& p, int B, int Hk)
 {
-    const Plan p = plan_of(B, Tq, Tk, Hq, Hk, D);
     return (double)((int64_t)B * Hk + 7) * 1.2 * p.tiles * p.splits * kThreads < 4294967296.0;
 }
 
@@ -419,9 +428,8 @@ extern "C" {
 
 size_t lsgd_attention_workspace_bytes(int32_t B, int32_t Tq, int32_t Tk, int32_t Hq, int32_t Hk, int32_t D, int32_t is_bf16)
 {
-    (void)is_bf16;
     if (check_attention_shape("attention", B, Tq, Tk, Hq, Hk, D) != LSGD_OK) return 0;
-    return plan_of(B, Tq, Tk, Hq, Hk, D).bytes;
+    return plan_of(B, Tq, Tk, Hq, Hk, D, is_bf16, 1).bytes;  // where keys are split, they are with either mask
 }
 
 lsgd_status lsgd_attention(const lsgd_attention_args* p, void* workspace, size_t workspace_bytes, void* hip_stream)
@@ -433,13 +441,13 @@ lsgd_status lsgd_attention(const lsgd_attention_args* p, void* workspace, size_t
     if (p->is_bf16 & ~1 || p->causal & ~1) return set_error(LSGD_ERR_INVALID_ARG, "%s: is_bf16 and causal must be 0 or 1", who);
     if (!scale_ok(p->scale)) return set_error(LSGD_ERR_INVALID_ARG, "%s: scale must be within [1e-30, 1e30]", who);
     if (Tq == 0) return LSGD_OK;
-    if ((int64_t)B * Hk > INT64_C(1) << 30 || !fits(B, Tq, Tk, Hq, Hk, D)) return set_error(LSGD_ERR_SHAPE, "%s: B=%d, Tq=%d, Hk=%d are too large for one launch", who, B, Tq, Hk);
+    const Plan plan = plan_of(B, Tq, Tk, Hq, Hk, D, p->is_bf16, p->causal);
+    if ((int64_t)B * Hk > INT64_C(1) << 30 || !fits(plan, B, Hk)) return set_error(LSGD_ERR_SHAPE, "%s: B=%d, Tq=%d, Hk=%d are too large for one launch", who, B, Tq, Hk);
     LSGD_TRY(check_heads(who, "q", p->q, B, Tq, Hq, D, es, true, false));
     LSGD_TRY(check_heads(who, "k", p->k, B, Tk, Hk, D, es, Tk > 0 || p->k.data, false));
     LSGD_TRY(check_heads(who, "v", p->v, B, Tk, Hk, D, es, Tk > 0 || p->v.data, false));
     LSGD_TRY(check_heads(who, "out", p->out, B, Tq, Hq, D, es, true, true));
     if (!on(p->q_lens, 4) || !on(p->k_lens, 4) || !on(p->lse, 4)) return set_error(LSGD_ERR_INVALID_ARG, "%s: q_lens, k_lens or lse is not aligned to its element", who);
-    const Plan plan = plan_of(B, Tq, Tk, Hq, Hk, D);
     if (plan.splits > 1) {
         if (!workspace) return set_error(LSGD_ERR_INVALID_ARG, "%s: workspace is NULL", who);
         if (!on(workspace, kAlign)) return set_error(LSGD_ERR_INVALID_ARG, "%s: workspace must be 256-byte aligned", who);

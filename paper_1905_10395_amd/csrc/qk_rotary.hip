@@ -408,9 +408,10 @@ int lanes_of(int D, int R, int E)
     while (lanes < units && lanes < kWave) lanes *= 2;
     return lanes;
 }
-// Tokens whose table a workgroup makes at a time: about eight rows a team, or one table entry a thread, but no more than leave two workgroups a
-// compute unit.
-constexpr int kRowsPerTeam = 8, kComputeUnits = 256;
+// Tokens whose table a workgroup makes at a time: about four rows a team, or one table entry a thread, but no more than leave two workgroups a
+// compute unit.  (8 x 8192 tokens, 32 and 8 heads of 128: two rows 321 us, four 255, eight 257, 16 269; gradients of 8 x 4096: 205,
+// 191, 201, 208.)
+constexpr int kRowsPerTeam = 4, kComputeUnits = 256;
 int tokens_of(int W, int T, int H, int R, int lanes)
 {
     const int teams = kThreads / lanes;

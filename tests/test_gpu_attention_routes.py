@@ -19,6 +19,16 @@ def test_many_rows_and_keys(D, dtype, causal):
     both(*inputs(B, T, T, 6, 6, D, dtype), causal=causal, q_lens=lens, k_lens=lens)
 
 
+@pytest.mark.parametrize("D", [64, 90, 128])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("causal", [False, True])
+def test_many_rows_of_shared_keys(D, dtype, causal):
+    B, T = 24, 150
+    lens = [(43 * b) % (T + 1) for b in range(B)]
+    lens[2] = T
+    both(*inputs(B, T, T, 12, 4, D, dtype), causal=causal, q_lens=lens, k_lens=lens)
+
+
 @pytest.mark.parametrize("Tq,Tk,Hq,Hk,D,k_lens", [(50, 3000, 3, 1, 64, [2990]), (9, 2100, 8, 1, 128, [2100]), (40, 1100, 2, 2, 52, [1025])])
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("causal", [False, True])
