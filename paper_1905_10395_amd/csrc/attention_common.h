@@ -89,62 +89,85 @@ __device__ __forceinline__ void from_result(const f32x16& r, int k, Frag<float>&
     split(x, f);
 }
 
-// 16 bytes of a row of D columns from column c on, zeros past its end; any alignment.  A piece that the row's end cuts is read so that
-// it ends with the row, and moved to its place.  EDGE: it may be cut, or lie behind the end.
-template <bool EDGE, class T>
-__device__ __forceinline__ v4u load16(const T* row, int c, int D)
+// Rows of any alignment and length, by 16 bytes from column c on, zeros past the row's end.  A piece that the end cuts is read so that it ends
+// with the row, and then moved to its place: all pieces are asked for before the first is moved, without a branch between (branches between
+// them had every piece wait for the one before: 3 x 5161 x 2 x 89 bf16 gradients 468 us, now 355; 4 queries to 4000 keys of 59 columns 39, 23).
+template <class T>
+__device__ __forceinline__ v4u fetch16(const T* row, int c, int D)
 {
     constexpr int per = 16 / (int)sizeof(T);
-    if constexpr (!EDGE) return *reinterpret_cast<const v4u_any*>(row + c);
-    else if (D >= per) {
-        const int over = c + per - D;
-        v4u q = *reinterpret_cast<const v4u_any*>(row + (over > 0 ? D - per : c));
-        if (over > 0) {
-            const int bits = 8 * (int)sizeof(T) * over;
-            uint64_t lo = q[0] | (uint64_t)q[1] << 32, hi = q[2] | (uint64_t)q[3] << 32;
-            if (bits >= 128) lo = hi = 0;
-            else if (bits >= 64) {
-                lo = hi >> (bits - 64);
-                hi = 0;
-            } else {
-                lo = lo >> bits | hi << (64 - bits);
-                hi >>= bits;
-            }
-            q = v4u{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
-        }
-        return q;
-    } else {
-        v4u q = {0, 0, 0, 0};
-#pragma unroll
-        for (int e = 0; e < per - 1; ++e)
-            if (c + e < D) {
-                if constexpr (sizeof(T) == 4) q[e] = __float_as_uint(row[c + e]);
-                else q[e / 2] |= (uint32_t)row[c + e] << (16 * (e & 1));
-            }
-        return q;
-    }
+    return *reinterpret_cast<const v4u_any*>(row + (c < D - per ? c : D - per));
 }
-// An operand's eight elements from memory.
-template <bool EDGE>
-__device__ __forceinline__ void load_frag(const uint16_t* row, int c, int D, Frag<uint16_t>& f) { f.v = __builtin_bit_cast(bf16x8, load16<EDGE>(row, c, D)); }
+template <class T>
+__device__ __forceinline__ v4u place16(v4u q, int c, int D)
+{
+    constexpr int per = 16 / (int)sizeof(T);
+    const int over = c + per - D, halves = over > 0 ? over * (int)sizeof(T) / 2 : 0;
+    if constexpr (sizeof(T) == 2) {
+        if (halves & 1) q = v4u{q[0] >> 16 | q[1] << 16, q[1] >> 16 | q[2] << 16, q[2] >> 16 | q[3] << 16, q[3] >> 16};
+    }
+    if (halves & 2) q = v4u{q[1], q[2], q[3], 0};
+    if (halves & 4) q = v4u{q[2], q[3], 0, 0};
+    return halves < 8 ? q : v4u{0, 0, 0, 0};
+}
+// Rows shorter than a piece.
+template <class T>
+__device__ __forceinline__ v4u few16(const T* row, int c, int D)
+{
+    constexpr int per = 16 / (int)sizeof(T);
+    v4u q = {0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < per - 1; ++e)
+        if (c + e < D) {
+            if constexpr (sizeof(T) == 4) q[e] = __float_as_uint(row[c + e]);
+            else q[e / 2] |= (uint32_t)row[c + e] << (16 * (e & 1));
+        }
+    return q;
+}
 __device__ __forceinline__ void split(v4f lo, v4f hi, Frag<float>& f)
 {
     const float x[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
     split(x, f);
 }
-template <bool EDGE>
-__device__ __forceinline__ void load_frag(const float* row, int c, int D, Frag<float>& f)
-{
-    split(__builtin_bit_cast(v4f, load16<EDGE>(row, c, D)), __builtin_bit_cast(v4f, load16<EDGE>(row, c + 4, D)), f);
-}
-// A lane's row as operands, contraction along its columns: zeros past the row's end.  All are asked for before any is waited for.
+// A lane's row in pieces: of every 16 columns those from 8 h on.  Only those of the last part can lie behind the row's end.
+template <class T, int PARTS>
+struct Pieces {
+    static constexpr int kPer = 16 / (int)sizeof(T), kEach = 8 / kPer;
+    v4u q[2 * PARTS][kEach];
+    __device__ __forceinline__ void load(const T* row, int h, int D)
+    {
+        if (PARTS == 1 && D < kPer) {
+#pragma unroll
+            for (int i = 0; i < 2 * PARTS * kEach; ++i) q[i / kEach][i % kEach] = few16(row, column(i, h), D);
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < 2 * PARTS * kEach; ++i) {
+            const int c = column(i, h);
+            if (i < (2 * PARTS - 2) * kEach) q[i / kEach][i % kEach] = *reinterpret_cast<const v4u_any*>(row + c);
+            else q[i / kEach][i % kEach] = fetch16(row, c, D);
+        }
+#pragma unroll
+        for (int i = (2 * PARTS - 2) * kEach; i < 2 * PARTS * kEach; ++i) q[i / kEach][i % kEach] = place16<T>(q[i / kEach][i % kEach], column(i, h), D);
+    }
+    static __device__ __forceinline__ int column(int i, int h) { return 16 * (i / kEach) + 8 * h + i % kEach * kPer; }
+    // the elements of 8 columns
+    __device__ __forceinline__ float at(int k, int e) const
+    {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(q[k][e / 4][e % 4]);
+        else return __uint_as_float(e & 1 ? q[k][0][e / 2] & 0xffff0000u : q[k][0][e / 2] << 16);
+    }
+};
+// A lane's row as operands, contraction along its columns.
 template <class T, int PARTS>
 __device__ __forceinline__ void load_frags(const T* row, int h, int D, Frag<T> (&f)[2 * PARTS])
 {
+    Pieces<T, PARTS> p;
+    p.load(row, h, D);
 #pragma unroll
     for (int k = 0; k < 2 * PARTS; ++k) {
-        if (16 * k + 16 <= D) load_frag<false>(row, 16 * k + 8 * h, D, f[k]);
-        else load_frag<true>(row, 16 * k + 8 * h, D, f[k]);
+        if constexpr (sizeof(T) == 2) f[k].v = __builtin_bit_cast(bf16x8, p.q[k][0]);
+        else split(__builtin_bit_cast(v4f, p.q[k][0]), __builtin_bit_cast(v4f, p.q[k][1]), f[k]);
     }
 }
 template <class T, int PARTS>
@@ -242,11 +265,22 @@ __device__ __forceinline__ void load_tile(T* tile, int wid, int lane, int D, F s
         }
     } else {
         v4u q[M::kLoads];
+        if (PARTS == 1 && D < L::kPer) {
 #pragma unroll
-        for (int g = 0; g < M::kGroups; ++g) {
-            const T* p = src(M::row(g, wid, lane));
+            for (int g = 0; g < M::kGroups; ++g) q[g] = few16(src(M::row(g, wid, lane)), M::column(g, wid, lane), D);
+        } else {
 #pragma unroll
-            for (int s = 0; s < M::kSlabs; ++s) q[g * M::kSlabs + s] = load16<true>(p, s * WIDTH + M::column(g, wid, lane), D);
+            for (int g = 0; g < M::kGroups; ++g) {
+                const T* p = src(M::row(g, wid, lane));
+                const int c = M::column(g, wid, lane);
+#pragma unroll
+                for (int s = 0; s < M::kSlabs; ++s) q[g * M::kSlabs + s] = s < M::kSlabs - 1 ? *reinterpret_cast<const v4u_any*>(p + (s * WIDTH + c)) : fetch16(p, s * WIDTH + c, D);
+            }
+#pragma unroll
+            for (int g = 0; g < M::kGroups; ++g) {
+                v4u& last = q[g * M::kSlabs + M::kSlabs - 1];
+                last = place16<T>(last, (M::kSlabs - 1) * WIDTH + M::column(g, wid, lane), D);
+            }
         }
 #pragma unroll
         for (int g = 0; g < M::kGroups; ++g)
@@ -335,11 +369,13 @@ void set_shape(Shape& g, const A& p)
 
 // A workgroup's unit, and its number among the unit's.  Workgroups go to the eight dies in turn, and each die has a cache of its own:
 // where units come out even, a die takes units of its own, every eighth, so that each has some of every part of the batch.  It goes
-// through them a few at a time, as many as fill it, whose keys and values its cache then holds.
+// through them a few at a time, as many as fill it, whose keys and values its cache then holds.  (32 x 2048 tokens of 16 heads of 128, 1.1 GB
+// of keys and values: 1143 us, 1915 with all units at once; their gradients for 16 entries 1237 and 1350; where all fit the memory-side
+// cache no difference, 2 x 8192 of 32 and 8 heads 1055 and 1058.)
 struct Place {
     int unit, at;
 };
-constexpr int kFill = 64;                                         // workgroups at work on a die
+constexpr int kFill = 64;                                         // workgroups at work on a die (16: 16 x 2048 x 8 x 64 101 -> 114 us; 256: the first of the above 1197)
 __device__ __forceinline__ Place place_of(const Shape& g, int each)
 {
     if (g.per_die == 0) return Place{(int)(blockIdx.x % g.units), (int)(blockIdx.x / g.units)};

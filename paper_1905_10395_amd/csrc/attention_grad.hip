@@ -13,6 +13,9 @@
 //
 // In both, results become operands in registers (attention_common.h): by rows s^T and dp^T, keys becoming the contraction, by
 // keys s and dp, rows becoming it.  Where a pass has few workgroups, further ones split its contraction, and a launch adds up their sums.
+//
+// Bound by the products: 4 x 4096 causal tokens of 16 and 4 heads of 128 bf16 0.95 to 1.0 ms, 1.05 PFLOP/s of the products made (0.35 to 0.4
+// ms by rows, 0.6 by keys); small ones by the chain of one workgroup's tiles (3 x 100 to 259 keys of 72 columns fp32: 17 + 17 + 4 us).
 #include <algorithm>
 #include <cmath>
 
@@ -55,21 +58,10 @@ template <class T>
 constexpr bool kFromZ = sizeof(T) == 2;                  // s begins with -z / c
 constexpr int kChunk = 128;                              // chunks of a split are multiples of it
 
-__device__ __forceinline__ float dot(const Frag<uint16_t>& a, const Frag<uint16_t>& b)
-{
-    float s = 0.0f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) s += (float)a.v[e] * (float)b.v[e];
-    return s;
-}
-__device__ __forceinline__ float dot(const Frag<float>& a, const Frag<float>& b)
-{
-    float s = 0.0f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) s += ((float)a.v[0][e] + ((float)a.v[1][e] + (float)a.v[2][e])) * ((float)b.v[0][e] + ((float)b.v[1][e] + (float)b.v[2][e]));
-    return s;
-}
-// How far operands are read ahead; by keys registers are short.
+// An operand's element as it was.
+__device__ __forceinline__ float value(const Frag<uint16_t>& a, int e) { return (float)a.v[e]; }
+__device__ __forceinline__ float value(const Frag<float>& a, int e) { return (float)a.v[0][e] + ((float)a.v[1][e] + (float)a.v[2][e]); }
+// How far operands are read ahead; by keys registers are short.  (4 x 4096 x 16 x 128: 967 us; two by rows and four by keys 1006.)
 template <class T>
 constexpr int kAheadRows = sizeof(T) == 2 ? 4 : 2;
 template <class T>
@@ -155,16 +147,16 @@ __global__ __launch_bounds__(F::THREADS, (kOccupancy<F, T, PARTS>)) void attenti
         const T* q = static_cast<const T*>(g.q.p) + rows.b * g.q.lb + row.t * g.q.lt + row.head * g.q.lh;
         const T* d = static_cast<const T*>(g.dout.p) + rows.b * g.dout.lb + row.t * g.dout.lt + row.head * g.dout.lh;
         const T* o = static_cast<const T*>(g.out.p) + rows.b * g.out.lb + row.t * g.out.lt + row.head * g.out.lh;
-        Frag<T> of[2 * PARTS];
         if (row.sees == 0) {
             clear_frags<T, PARTS>(qf);
             clear_frags<T, PARTS>(df);
         } else {
             load_frags<T, PARTS>(q, h, g.D, qf);
             load_frags<T, PARTS>(d, h, g.D, df);
-            load_frags<T, PARTS>(o, h, g.D, of);
+            Pieces<T, PARTS> of;
+            of.load(o, h, g.D);
 #pragma unroll
-            for (int k = 0; k < 2 * PARTS; ++k) delta -= dot(of[k], df[k]);
+            for (int i = 0; i < 16 * PARTS; ++i) delta -= of.at(i / 8, i % 8) * value(df[i / 8], i % 8);
             z = -g.lse[((int64_t)rows.b * g.Hq + row.head) * g.Tq + row.t] * (kFromZ<T> ? g.inv_scale : kLog2e);
         }
         delta += other_half(delta);
@@ -432,6 +424,8 @@ Plan plan_of(int B, int Tq, int Tk, int Hq, int Hk, int D, int is_bf16)
     Plan p{};
     const int64_t rows = (int64_t)Tq * (Hq / Hk), units = (int64_t)B * Hk;
     const size_t cols = (size_t)parts_of(D) * kPart;
+    // Few where 128 a workgroup would leave compute units without one (8 causal heads, us of few and of many: 128 columns bf16, 1024 tokens 48
+    // and 66, 2048 91 and 96, 4096, 256 workgroups, 241 and 223; fp32, 2048 tokens, 254 and 338; 64 columns bf16, 2048 tokens, 53 and 61).
     auto tiles = [&](int64_t many, int each, bool& few) {
         few = units * ((many + each - 1) / each) < kComputeUnits;
         const int mine = few ? Few<float>::MINE : each;

