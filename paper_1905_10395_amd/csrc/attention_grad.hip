@@ -105,21 +105,25 @@ __device__ __forceinline__ void join_shared(void* tile0, void* tile1, int own, i
         static_assert((F::SHARE - 1) * F::OWN <= 2 * kPerTile, "areas");
         auto area = [&](int k) {
             const int a = k * F::OWN + own;
-            return reinterpret_cast<float*>(a < kPerTile ? tile0 : tile1) + a % kPerTile * kArea + lane;
+            return reinterpret_cast<v4f*>(a < kPerTile ? tile0 : tile1) + a % kPerTile * (kArea / 4) + lane;
         };
         __syncthreads();                                          // the tiles, or the last sums, have been read
         if (share) {
-            float* to = area(share - 1);
+            v4f* to = area(share - 1);
 #pragma unroll
-            for (int i = 0; i < PARTS * 16; ++i) to[i * 64] = s[i / 16][i % 16];
+            for (int i = 0; i < PARTS * 4; ++i) {
+                const f32x16& f = s[i / 4];
+                const int e = i % 4 * 4;
+                to[i * 64] = v4f{f[e], f[e + 1], f[e + 2], f[e + 3]};
+            }
         }
         __syncthreads();
         if (!share) {
 #pragma unroll
             for (int k = 0; k < F::SHARE - 1; ++k) {
-                const float* from = area(k);
+                const v4f* from = area(k);
 #pragma unroll
-                for (int i = 0; i < PARTS * 16; ++i) s[i / 16][i % 16] += from[i * 64];
+                for (int i = 0; i < PARTS * 16; ++i) s[i / 16][i % 16] += from[i / 4 * 64][i % 4];
             }
         }
     }
