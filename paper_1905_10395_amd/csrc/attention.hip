@@ -382,7 +382,7 @@ Plan plan_of(int B, int Tq, int Tk, int Hq, int Hk, int D, int is_bf16, int caus
     if (splits > 1) {
         p.chunk = (int)(((Tk + splits - 1) / splits + step - 1) / step * step);
         p.splits = (Tk + p.chunk - 1) / p.chunk;
-        p.bytes = sizeof(float) * (size_t)groups * (size_t)p.splits * (size_t)part_floats(parts_of(D));
+        p.bytes = std::max(kAlign, sizeof(float) * (size_t)groups * (size_t)p.splits * (size_t)part_floats(parts_of(D)));   // (groups 0: no queries)
     }
     return p;
 }

@@ -106,6 +106,12 @@ def test_attention_arguments():
     assert f(attention(**long), P, need - 1, None) == NOMEM
 
 
+def test_no_queries_need_no_parts():
+    size = b.lib().lsgd_attention_workspace_bytes
+    for Tk in (0, 5, 1024, 1025, 100000):
+        assert size(2, 0, Tk, 4, 2, 64, 1) == 256
+
+
 def test_attention_grad_arguments():
     f, size = b.lib().lsgd_attention_grad, b.lib().lsgd_attention_grad_workspace_bytes
 

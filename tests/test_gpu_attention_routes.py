@@ -42,6 +42,15 @@ def test_many_heads_share_a_key_head(dtype):
     both(*inputs(1, 20, 33, 67, 1, 64, dtype))
 
 
+@pytest.mark.parametrize("Tk", [0, 7, 5000])
+def test_no_queries(Tk):
+    q, k, v, do = inputs(2, 0, Tk, 4, 2, 64, BF16)
+    out, lse = L.attention(q, k, v, causal=True)
+    assert out.shape == q.shape and lse.shape == (2, 4, 0)
+    dq, dk, dv = L.attention_grad(do, q, k, v, out, lse, causal=True)
+    assert dq.shape == q.shape and not bool(dk.any()) and not bool(dv.any())
+
+
 def test_shared_keys_by_strides():
     """Keys of one entry for all entries and heads, by strides of zero."""
     q, k, v, do = inputs(3, 20, 70, 4, 4, 64, BF16)
