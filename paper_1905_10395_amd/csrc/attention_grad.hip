@@ -14,8 +14,8 @@
 // In both, results become operands in registers (attention_common.h): by rows s^T and dp^T, keys becoming the contraction, by
 // keys s and dp, rows becoming it.  Where a pass has few workgroups, further ones split its contraction, and a launch adds up their sums.
 //
-// Bound by the products: 4 x 4096 causal tokens of 16 and 4 heads of 128 bf16 0.95 to 1.0 ms, 1.05 PFLOP/s of the products made (0.35 to 0.4
-// ms by rows, 0.6 by keys); small ones by the chain of one workgroup's tiles (3 x 100 to 259 keys of 72 columns fp32: 17 + 17 + 4 us).
+// Bound by the products: 4 x 4096 causal tokens of 16 and 4 heads of 128 bf16 0.95 to 1.02 ms, 0.95 to 1.0 PFLOP/s of the seven products (0.35 to 0.4
+// ms by rows, 0.6 by keys); small ones by the chain of one workgroup's tiles (3 x 100 to 259 keys of 72 columns fp32: 14 + 16 + 4 us).
 #include <algorithm>
 #include <cmath>
 

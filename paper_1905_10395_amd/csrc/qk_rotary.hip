@@ -7,7 +7,7 @@
 //   backward, from dy, with h = q x:  dz = R' dy;  dx = q (dz o w - h mean(dz o w o h));  dw = sum over tokens and heads dz o h
 //
 // Bound by memory: 8 x 8192 tokens of 32 and 8 heads of 128 bf16 in 236 to 260 us, 5.2 to 5.7 TB/s, as a copy of the same bytes (245); gradients of
-// 8 x 4096 193 us, 5.2 TB/s, and 5 more for the weights'.  Angles: a position far into a text times a frequency is thousands of turns, of which fp32 keeps too few
+// 8 x 4096 182 us in all, 5.6 TB/s.  Angles: a position far into a text times a frequency is thousands of turns, of which fp32 keeps too few
 // bits; the product is made in 64 bits, whole turns are taken off, and the rest goes through sincospi in fp32.  All heads of a
 // token turn alike, so a workgroup makes the table of its tokens once, in LDS, and its rows read it there.
 //
