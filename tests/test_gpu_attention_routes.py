@@ -51,6 +51,26 @@ def test_no_queries(Tk):
     assert dq.shape == q.shape and not bool(dk.any()) and not bool(dv.any())
 
 
+@pytest.mark.parametrize("B,Tq,Tk,D", [(24, 150, 150, 64), (24, 150, 150, 90), (2, 40, 90, 64), (2, 1, 5000, 64), (1, 3, 3000, 45), (1, 50, 3000, 128)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_nan_is_not_hidden(B, Tq, Tk, D, dtype):
+    """A query with NaN, or one that sees a key with NaN, has NaN and says so; others have what they had."""
+    H, t = 6, Tq // 2
+    q, k, v, _ = inputs(B, Tq, Tk, H, H, D, dtype)
+    want, wlse = L.attention(q, k, v)
+    q[0, t, 1, D // 2] = float("nan")
+    k[B - 1, Tk // 3, 2] = float("nan")
+    out, lse = L.attention(q, k, v)
+    bad = torch.zeros((B, Tq, H), dtype=torch.bool, device=DEV)
+    bad[0, t, 1] = True
+    bad[B - 1, :, 2] = True
+    rest = ~bad.cpu()
+    assert bool(out[bad].isnan().all()) and bool(lse.transpose(1, 2)[bad].isnan().all())
+    # (rows of a wavefront are rescaled together, so other rows' sums may round elsewhere: values of up to 5 once to their type, twice)
+    lim = 2e-5 if dtype is F32 else 5 * 2 ** -7
+    assert float((d(out) - d(want))[rest].abs().max()) <= lim and float((d(lse) - d(wlse)).transpose(1, 2)[rest].abs().max()) <= 2e-5
+
+
 def test_shared_keys_by_strides():
     """Keys of one entry for all entries and heads, by strides of zero."""
     q, k, v, do = inputs(3, 20, 70, 4, 4, 64, BF16)
