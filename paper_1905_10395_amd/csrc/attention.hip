@@ -136,6 +136,8 @@ __device__ __forceinline__ void load_queries(const Args& g, const Rows& rows, co
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr int kRowsByRows = 32 * kWaves;
 template <class T>
+constexpr bool kLate = sizeof(T) == 2;                    // rows off 16 bytes wait in registers while a tile is passed (16 x 700 x 8 x 59 32 -> 29 us; fp32 83, late 88)
+template <class T>
 constexpr int kKeysByRows = sizeof(T) == 2 ? 64 : 32;     // 64 rows of 32 bf16 are a load of each wavefront; two buffers of K and V leave two workgroups a compute unit
 
 template <class T, int PARTS, bool ALIGNED>
@@ -157,21 +159,34 @@ __global__ __launch_bounds__(kThreads, 2) void attention_rows_kernel(Args g)
     State<PARTS> st;
     const T* k = static_cast<const T*>(g.k.p) + rows.b * g.k.lb + rows.hk * g.k.lh;
     const T* v = static_cast<const T*>(g.v.p) + rows.b * g.v.lb + rows.hk * g.v.lh;
+    TileOnItsWay<T, KEYS, PARTS, kWaves, ALIGNED> kt, vt;
     auto issue = [&](int key0, T* kb, T* vb) {
         auto key = [&](int r) { return key0 + r < rows.nk ? key0 + r : rows.nk - 1; };
-        load_tile<T, KEYS, PARTS, kWaves, ALIGNED>(kb, wid, lane, g.D, [&](int r) { return k + key(r) * g.k.lt; });
-        load_tile<T, KEYS, PARTS, kWaves, ALIGNED>(vb, wid, lane, g.D, [&](int r) { return v + key(r) * g.v.lt; });
+        kt.fetch(kb, wid, lane, g.D, [&](int r) { return k + key(r) * g.k.lt; });
+        vt.fetch(vb, wid, lane, g.D, [&](int r) { return v + key(r) * g.v.lt; });
+    };
+    auto put = [&](T* kb, T* vb) {
+        kt.put(kb, wid, lane, g.D);
+        vt.put(vb, wid, lane, g.D);
     };
     auto step = [&](int key0, T* kb, T* vb, T* next_k, T* next_v) {
         tiles_barrier();
-        if (key0 + KEYS < rows.end) issue(key0 + KEYS, next_k, next_v);
-        if (key0 >= most) return;
-        f32x16 p[KEYS / 32];
-        Values<kPart, T, PARTS, KEYS> values(vb, lane);
-        pass_keys<kPart, T, PARTS, KEYS>(kb, lane, key0, row.sees, key0 + KEYS > least, g.c, qf, st, p, [&] { values.start(); });
-        values.pass(p, st);
+        if (key0 + KEYS < rows.end) {
+            issue(key0 + KEYS, next_k, next_v);
+            if (!kLate<T>) put(next_k, next_v);
+        }
+        if (key0 < most) {
+            f32x16 p[KEYS / 32];
+            Values<kPart, T, PARTS, KEYS> values(vb, lane);
+            pass_keys<kPart, T, PARTS, KEYS>(kb, lane, key0, row.sees, key0 + KEYS > least, g.c, qf, st, p, [&] { values.start(); });
+            values.pass(p, st);
+        }
+        if (kLate<T> && key0 + KEYS < rows.end) put(next_k, next_v);
     };
-    if (rows.end > 0) issue(0, k0, v0);
+    if (rows.end > 0) {
+        issue(0, k0, v0);
+        put(k0, v0);
+    }
     for (int key0 = 0; key0 < rows.end; key0 += 2 * KEYS) {
         step(key0, k0, v0, k1, v1);
         if (key0 + KEYS < rows.end) step(key0 + KEYS, k1, v1, k0, v0);

@@ -246,26 +246,28 @@ struct TileLoad {
 };
 
 // Straight to LDS (16-byte aligned rows, a whole number of pieces: one past the row's end becomes its last one; what that multiplies is
-// zero, or is not stored), or through registers.  src(row): the row's address.  ONCE: past the caches.
-template <class T, int R, int PARTS, int WAVES, bool ALIGNED, int WIDTH = kPart, bool ONCE = false, class F>
-__device__ __forceinline__ void load_tile(T* tile, int wid, int lane, int D, F src)
-{
+// zero, or is not stored), or through registers, where the loads can be on their way while another tile is passed: fetch() asks for them, put()
+// lays them down.  src(row): the row's address.  ONCE: past the caches.
+template <class T, int R, int PARTS, int WAVES, bool ALIGNED, int WIDTH = kPart, bool ONCE = false>
+struct TileOnItsWay {
     using M = TileLoad<T, R, PARTS, WAVES, WIDTH>;
     using L = Tile<T, WIDTH>;
-    if constexpr (ALIGNED) {
+    v4u q[ALIGNED ? 1 : M::kLoads];
+    template <class F>
+    __device__ __forceinline__ void fetch(T* tile, int wid, int lane, int D, F src)
+    {
+        if constexpr (ALIGNED) {
 #pragma unroll
-        for (int g = 0; g < M::kGroups; ++g) {
-            const int c = M::column(g, wid, lane), end = D - L::kPer - (M::kSlabs - 1) * WIDTH;
-            const T* p = src(M::row(g, wid, lane)) + c;
+            for (int g = 0; g < M::kGroups; ++g) {
+                const int c = M::column(g, wid, lane), end = D - L::kPer - (M::kSlabs - 1) * WIDTH;
+                const T* p = src(M::row(g, wid, lane)) + c;
 #pragma unroll
-            for (int s = 0; s < M::kSlabs; ++s) {
-                if (s == M::kSlabs - 1) p -= c > end ? c - end : 0;
-                __builtin_amdgcn_global_load_lds((global_ptr)(p + s * WIDTH), (lds_ptr)(tile + M::first(g, s, wid)), 16, 0, ONCE ? kNonTemporal : 0);
+                for (int s = 0; s < M::kSlabs; ++s) {
+                    if (s == M::kSlabs - 1) p -= c > end ? c - end : 0;
+                    __builtin_amdgcn_global_load_lds((global_ptr)(p + s * WIDTH), (lds_ptr)(tile + M::first(g, s, wid)), 16, 0, ONCE ? kNonTemporal : 0);
+                }
             }
-        }
-    } else {
-        v4u q[M::kLoads];
-        if (PARTS == 1 && D < L::kPer) {
+        } else if (PARTS == 1 && D < L::kPer) {
 #pragma unroll
             for (int g = 0; g < M::kGroups; ++g) q[g] = few16(src(M::row(g, wid, lane)), M::column(g, wid, lane), D);
         } else {
@@ -276,17 +278,29 @@ __device__ __forceinline__ void load_tile(T* tile, int wid, int lane, int D, F s
 #pragma unroll
                 for (int s = 0; s < M::kSlabs; ++s) q[g * M::kSlabs + s] = s < M::kSlabs - 1 ? *reinterpret_cast<const v4u_any*>(p + (s * WIDTH + c)) : fetch16(p, s * WIDTH + c, D);
             }
-#pragma unroll
-            for (int g = 0; g < M::kGroups; ++g) {
-                v4u& last = q[g * M::kSlabs + M::kSlabs - 1];
-                last = place16<T>(last, (M::kSlabs - 1) * WIDTH + M::column(g, wid, lane), D);
-            }
         }
-#pragma unroll
-        for (int g = 0; g < M::kGroups; ++g)
-#pragma unroll
-            for (int s = 0; s < M::kSlabs; ++s) *reinterpret_cast<v4u*>(tile + (M::first(g, s, wid) + lane * L::kPer)) = q[g * M::kSlabs + s];
     }
+    __device__ __forceinline__ void put(T* tile, int wid, int lane, int D)
+    {
+        if constexpr (!ALIGNED) {
+            const bool few = PARTS == 1 && D < L::kPer;            // those lie in their places
+#pragma unroll
+            for (int g = 0; g < M::kGroups; ++g)
+#pragma unroll
+                for (int s = 0; s < M::kSlabs; ++s) {
+                    v4u p = q[g * M::kSlabs + s];
+                    if (s == M::kSlabs - 1 && !few) p = place16<T>(p, s * WIDTH + M::column(g, wid, lane), D);
+                    *reinterpret_cast<v4u*>(tile + (M::first(g, s, wid) + lane * L::kPer)) = p;
+                }
+        }
+    }
+};
+template <class T, int R, int PARTS, int WAVES, bool ALIGNED, int WIDTH = kPart, bool ONCE = false, class F>
+__device__ __forceinline__ void load_tile(T* tile, int wid, int lane, int D, F src)
+{
+    TileOnItsWay<T, R, PARTS, WAVES, ALIGNED, WIDTH, ONCE> t;
+    t.fetch(tile, wid, lane, D, src);
+    t.put(tile, wid, lane, D);
 }
 
 // The tile handed over: this wavefront's loads have arrived, everyone's part is there, and nobody reads the buffer that is filled next.

@@ -61,6 +61,10 @@ constexpr int kChunk = 128;                              // chunks of a split ar
 // An operand's element as it was.
 __device__ __forceinline__ float value(const Frag<uint16_t>& a, int e) { return (float)a.v[e]; }
 __device__ __forceinline__ float value(const Frag<float>& a, int e) { return (float)a.v[0][e] + ((float)a.v[1][e] + (float)a.v[2][e]); }
+// Rows off 16 bytes wait in registers while a tile is passed, if those suffice (3 x 5161 x 2 x 89 354 -> 325 us; but 8 x 1000 x 8 x 125 154, late
+// 203, fp32 475 and 496).
+template <class T, int PARTS>
+constexpr bool kLate = sizeof(T) == 2 && PARTS < 4;
 // How far operands are read ahead; by keys registers are short.  (4 x 4096 x 16 x 128: 967 us; two by rows and four by keys 1006.)
 template <class T>
 constexpr int kAheadRows = sizeof(T) == 2 ? 4 : 2;
@@ -174,10 +178,15 @@ __global__ __launch_bounds__(F::THREADS, (kOccupancy<F, T, PARTS>)) void attenti
     const T* k = static_cast<const T*>(g.k.p) + rows.b * g.k.lb + rows.hk * g.k.lh;
     const T* v = static_cast<const T*>(g.v.p) + rows.b * g.v.lb + rows.hk * g.v.lh;
     const int begin = split * g.row_chunk, end = min(rows.end, begin + g.row_chunk);
+    TileOnItsWay<T, KEYS, PARTS, F::WAVES, ALIGNED> kt, vt;
     auto issue = [&](int key0, T* kb, T* vb) {
         auto key = [&](int i) { return key0 + i < rows.nk ? key0 + i : rows.nk - 1; };
-        load_tile<T, KEYS, PARTS, F::WAVES, ALIGNED>(kb, wid, lane, g.D, [&](int i) { return k + key(i) * g.k.lt; });
-        load_tile<T, KEYS, PARTS, F::WAVES, ALIGNED>(vb, wid, lane, g.D, [&](int i) { return v + key(i) * g.v.lt; });
+        kt.fetch(kb, wid, lane, g.D, [&](int i) { return k + key(i) * g.k.lt; });
+        vt.fetch(vb, wid, lane, g.D, [&](int i) { return v + key(i) * g.v.lt; });
+    };
+    auto put = [&](T* kb, T* vb) {
+        kt.put(kb, wid, lane, g.D);
+        vt.put(vb, wid, lane, g.D);
     };
     auto pass = [&](int key0, const T* kb, const T* vb) {
         if (key0 + share * F::PASS >= most) return;
@@ -208,10 +217,17 @@ __global__ __launch_bounds__(F::THREADS, (kOccupancy<F, T, PARTS>)) void attenti
     if constexpr (F::BUFFERS > 1) {
         auto step = [&](int key0, T* kb, T* vb, T* next_k, T* next_v) {
             tiles_barrier();
-            if (key0 + KEYS < end) issue(key0 + KEYS, next_k, next_v);
+            if (key0 + KEYS < end) {
+                issue(key0 + KEYS, next_k, next_v);
+                if (!kLate<T, PARTS>) put(next_k, next_v);
+            }
             pass(key0, kb, vb);
+            if (kLate<T, PARTS> && key0 + KEYS < end) put(next_k, next_v);
         };
-        if (begin < end) issue(begin, k0, v0);
+        if (begin < end) {
+            issue(begin, k0, v0);
+            put(k0, v0);
+        }
         for (int key0 = begin; key0 < end; key0 += 2 * KEYS) {
             step(key0, k0, v0, k1, v1);
             if (key0 + KEYS < end) step(key0 + KEYS, k1, v1, k0, v0);
@@ -220,6 +236,7 @@ __global__ __launch_bounds__(F::THREADS, (kOccupancy<F, T, PARTS>)) void attenti
         for (int key0 = begin; key0 < end; key0 += KEYS) {
             if (key0 > begin) tiles_barrier();                     // the last tiles have been read
             issue(key0, k0, v0);
+            put(k0, v0);
             tiles_barrier();
             pass(key0, k0, v0);
         }
@@ -277,13 +294,18 @@ __global__ __launch_bounds__(F::THREADS, (kOccupancy<F, T, PARTS>)) void attenti
     const T* d = static_cast<const T*>(g.dout.p) + b * g.dout.lb + (int64_t)hk * g.G * g.dout.lh;
     const float* z = g.z + (int64_t)at.unit * g.rows;
     const float* delta = g.delta + (int64_t)at.unit * g.rows;
+    TileOnItsWay<T, ROWS, PARTS, F::WAVES, ALIGNED> qt, dt;
+    auto put = [&](T* qb, T* db) {
+        qt.put(qb, wid, lane, g.D);
+        dt.put(db, wid, lane, g.D);
+    };
     auto issue = [&](int r0, T* qb, T* db, float* zb, float* eb) {
         auto place = [&](int i, const Heads& a) {
             const int r = r0 + i < rows_live ? r0 + i : rows_live - 1, t = over(r, g.by_g);
             return t * a.lt + (r - t * g.G) * a.lh;
         };
-        load_tile<T, ROWS, PARTS, F::WAVES, ALIGNED>(qb, wid, lane, g.D, [&](int i) { return q + place(i, g.q); });
-        load_tile<T, ROWS, PARTS, F::WAVES, ALIGNED>(db, wid, lane, g.D, [&](int i) { return d + place(i, g.dout); });
+        qt.fetch(qb, wid, lane, g.D, [&](int i) { return q + place(i, g.q); });
+        dt.fetch(db, wid, lane, g.D, [&](int i) { return d + place(i, g.dout); });
         static_assert(ROWS <= F::THREADS && kChunk % ROWS == 0, "a value a thread, whole tiles a chunk");
         if ((int)threadIdx.x < ROWS) {
             const int r = r0 + (int)threadIdx.x;
@@ -340,10 +362,17 @@ __global__ __launch_bounds__(F::THREADS, (kOccupancy<F, T, PARTS>)) void attenti
     if constexpr (F::BUFFERS > 1) {
         auto step = [&](int r0, T* qb, T* db, float* zb, float* eb, T* next_q, T* next_d, float* next_z, float* next_e) {
             tiles_barrier();
-            if (r0 + ROWS < end) issue(r0 + ROWS, next_q, next_d, next_z, next_e);
+            if (r0 + ROWS < end) {
+                issue(r0 + ROWS, next_q, next_d, next_z, next_e);
+                if (!kLate<T, PARTS>) put(next_q, next_d);
+            }
             pass(r0, qb, db, zb, eb);
+            if (kLate<T, PARTS> && r0 + ROWS < end) put(next_q, next_d);
         };
-        if (begin < end) issue(begin, q0, d0, z0, e0);
+        if (begin < end) {
+            issue(begin, q0, d0, z0, e0);
+            put(q0, d0);
+        }
         for (int r0 = begin; r0 < end; r0 += 2 * ROWS) {
             step(r0, q0, d0, z0, e0, q1, d1, z1, e1);
             if (r0 + ROWS < end) step(r0 + ROWS, q1, d1, z1, e1, q0, d0, z0, e0);
@@ -352,6 +381,7 @@ __global__ __launch_bounds__(F::THREADS, (kOccupancy<F, T, PARTS>)) void attenti
         for (int r0 = begin; r0 < end; r0 += ROWS) {
             if (r0 > begin) tiles_barrier();                       // the last tiles have been read
             issue(r0, q0, d0, z0, e0);
+            put(q0, d0);
             tiles_barrier();
             pass(r0, q0, d0, z0, e0);
         }
