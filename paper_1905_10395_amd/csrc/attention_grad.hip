@@ -283,7 +283,9 @@ __global__ __launch_bounds__(F::THREADS, (kOccupancy<F, T, PARTS>)) void attenti
     }
     // a key behind the last has zeros for k and v; what its lane adds up is not stored
     const int from = live ? first_row(g, nq, nk, key) : 0, least = first_row(g, nq, nk, key0 + own * 32), most = wave_max(from);
-    const int rows_live = nq * g.G;
+    // rows that see no key, causal ones before the first that does among them, and places behind the last: p = 0, times what a row that
+    // sees some holds, so that NaN in theirs is not passed
+    const int rows_live = nq * g.G, row_first = first_row(g, nq, nk, 0);
     int begin = first_row(g, nq, nk, key0) / ROWS * ROWS, end = key0 < nk ? rows_live : 0;
     begin = max(begin, split * g.key_chunk);
     end = min(end, (split + 1) * g.key_chunk);
@@ -301,7 +303,7 @@ __global__ __launch_bounds__(F::THREADS, (kOccupancy<F, T, PARTS>)) void attenti
     };
     auto issue = [&](int r0, T* qb, T* db, float* zb, float* eb) {
         auto place = [&](int i, const Heads& a) {
-            const int r = r0 + i < rows_live ? r0 + i : rows_live - 1, t = over(r, g.by_g);
+            const int r = min(max(r0 + i, row_first), rows_live - 1), t = over(r, g.by_g);
             return t * a.lt + (r - t * g.G) * a.lh;
         };
         qt.fetch(qb, wid, lane, g.D, [&](int i) { return q + place(i, g.q); });
