@@ -2,7 +2,8 @@
 //
 //   s = q . k,  c = scale log2 e,  p = 2^(c (s - m)),  l = sum p,  out = (sum p v) / l,  lse = scale m + log l
 //
-// l = 0 marks a row that sees nothing; a row with NaN among its scores has l = NaN, and so its results.
+// A row that sees nothing has zeros by its mask, not by its sums: those may hold 0 x infinity from keys that rows beside it see.  A row
+// with NaN among its scores has l = NaN, and so its results; one whose scores are all -inf has l = 0, and 0 / 0.
 //
 // One pass over the keys.  m is a running reference of the scores, not always their maximum: sums are rescaled only when a score
 // exceeds it by 8 or more powers of two, so most tiles need no rescaling, and p stays below 2^8.  s^T = K Q^T and out^T = V^T P^T:
@@ -191,7 +192,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_rows_kernel(Args g)
         step(key0, k0, v0, k1, v1);
         if (key0 + KEYS < rows.end) step(key0 + KEYS, k1, v1, k0, v0);
     }
-    const float l = st.l + other_half(st.l), inv = l != 0.0f ? 1.0f / l : 0.0f;
+    const float l = st.l + other_half(st.l), inv = 1.0f / l;
     if (g.lse && row.there && h == 0) g.lse[((int64_t)rows.b * g.Hq + row.head) * g.Tq + row.t] = l != 0.0f ? st.m * g.scale + logf(l) : -INFINITY;
     T* const out = static_cast<T*>(g.out.p) + rows.b * g.out.lb + (int64_t)rows.hk * g.G * g.out.lh;
     auto place = [&](int r) {
@@ -204,9 +205,9 @@ __global__ __launch_bounds__(kThreads, 2) void attention_rows_kernel(Args g)
         constexpr int kMine = PARTS * kPart * 32, kFit = KEYS / 32;    // elements of a wavefront; how many a tile holds
         const int tile_of = wid / kFit;
         T* const mine = (tile_of == 0 ? k0 : tile_of == 1 ? k1 : tile_of == 2 ? v0 : v1) + wid % kFit * kMine;
-        store_rows<T, PARTS>(mine, lane, g.D, inv, st.o, [&](int i) { return r0 + i < g.rows ? place(r0 + i) : nullptr; });
+        store_rows<T, PARTS>(mine, lane, g.D, inv, st.o, row.sees > 0, [&](int i) { return r0 + i < g.rows ? place(r0 + i) : nullptr; });
     } else if (row.there) {
-        store_sums<T, PARTS>(place(r0 + (lane & 31)), lane, g.D, inv, st.o);
+        store_sums<T, PARTS>(place(r0 + (lane & 31)), lane, g.D, inv, st.o, row.sees > 0);
     }
 }
 
@@ -297,7 +298,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_ke
     }
     float* const part = g.parts ? g.parts + (((int64_t)unit * g.tiles + tile) * g.splits + split) * part_floats(PARTS) : nullptr;
     T* const out = static_cast<T*>(g.out.p) + rows.b * g.out.lb + row.t * g.out.lt + row.head * g.out.lh;
-    const float inv = n != 0.0f ? 1.0f / n : 0.0f;
+    const float inv = 1.0f / n;
 #pragma unroll
     for (int k = 0; k < PARTS; ++k) {
         const int i0 = 4 * (k * W + wid), c = 8 * (k * W + wid) + 4 * h;
@@ -312,7 +313,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_ke
             if (n != 0.0f) put4(part + (lane & 31) * COLS + c, o);
         } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] *= inv;
+            for (int e = 0; e < 4; ++e) o[e] = row.sees ? o[e] * inv : 0.0f;
             store4(out, c, g.D, o);
         }
     }
@@ -357,7 +358,7 @@ __global__ __launch_bounds__(kThreads) void attention_join_kernel(Args g)
         T* out = static_cast<T*>(g.out.p) + rows.b * g.out.lb + to.t * g.out.lt + to.head * g.out.lh;
 #pragma unroll
         for (int k = 0; k < COLS; ++k)
-            if (lane + 64 * k < g.D) put1(out + lane + 64 * k, n != 0.0f ? o[k] / n : 0.0f);
+            if (lane + 64 * k < g.D) put1(out + lane + 64 * k, to.sees ? o[k] / n : 0.0f);
         if (g.lse && lane == 0) g.lse[((int64_t)rows.b * g.Hq + to.head) * g.Tq + to.t] = n != 0.0f ? m * g.scale + logf(n) : -INFINITY;
     }
 }

@@ -467,22 +467,29 @@ __device__ __forceinline__ void store4(T* row, int c, int D, const float (&v)[4]
             if (c + e < D) put1(row + c + e, v[e]);
 }
 
-// The lane's columns of its row, times a factor, any alignment.
+// Four sums times a factor, or zeros, whatever the sums are.
+__device__ __forceinline__ void scaled(const f32x16& s, int i, float factor, bool live, float (&o)[4])
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = live ? s[i + e] * factor : 0.0f;
+}
+// The lane's columns of its row, times a factor, any alignment.  live: not zeros.
 template <class T, int PARTS>
-__device__ __forceinline__ void store_sums(T* row, int lane, int D, float factor, const f32x16 (&s)[PARTS])
+__device__ __forceinline__ void store_sums(T* row, int lane, int D, float factor, const f32x16 (&s)[PARTS], bool live = true)
 {
 #pragma unroll
     for (int p = 0; p < PARTS; ++p)
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
-            const float o[4] = {s[p][i] * factor, s[p][i + 1] * factor, s[p][i + 2] * factor, s[p][i + 3] * factor};
+            float o[4];
+            scaled(s[p], i, factor, live, o);
             store4(row, p * kPart + 2 * i + 4 * (lane >> 5), D, o);
         }
 }
 // The same of 16-byte aligned rows, a whole number of pieces: through LDS ([32][PARTS 32] of the wavefront's own), so that rows are written
 // by 16 bytes a lane, one after the other, and not by 8 of 32 rows at a time.  row(i): the address of row i of the 32, NULL: not stored.
 template <class T, int PARTS, class F>
-__device__ __forceinline__ void store_rows(T* lds, int lane, int D, float factor, const f32x16 (&s)[PARTS], F row)
+__device__ __forceinline__ void store_rows(T* lds, int lane, int D, float factor, const f32x16 (&s)[PARTS], bool live, F row)
 {
     constexpr int kPer = 16 / (int)sizeof(T), kPieces = PARTS * kPart / kPer;
     auto at = [](int r, int piece) { return (r * kPieces + (piece + r) % kPieces) * kPer; };      // rotated: over all banks
@@ -490,7 +497,8 @@ __device__ __forceinline__ void store_rows(T* lds, int lane, int D, float factor
     for (int p = 0; p < PARTS; ++p)
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
-            const float o[4] = {s[p][i] * factor, s[p][i + 1] * factor, s[p][i + 2] * factor, s[p][i + 3] * factor};
+            float o[4];
+            scaled(s[p], i, factor, live, o);
             const int c = p * kPart + 2 * i + 4 * (lane >> 5);
             put4(lds + (at(lane & 31, c / kPer) + c % kPer), o);
         }

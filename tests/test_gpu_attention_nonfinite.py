@@ -42,3 +42,45 @@ def test_queries_that_see_no_key_have_no_effect(shape, dtype, lens):
     for name, a, b in zip(("dq", "dk", "dv"), grads, got):
         assert torch.equal(a, b), name
     assert bool((got[0][blind] == 0).all())
+
+
+# by rows; by keys; keys split: B, Tq, Tk, H, D
+ROUTES = [(24, 150, 150, 6, 64), (24, 150, 150, 6, 90), (24, 150, 150, 6, 128), (2, 40, 90, 6, 64), (2, 40, 90, 6, 45), (1, 20, 3000, 2, 64), (1, 20, 3000, 2, 101)]
+
+
+def some_rows(B, Tq, Tk):
+    """Lengths that leave each entry queries that see nothing and queries that see all keys of its length, and a key of each that is marked."""
+    q_lens, k_lens = [1 + 5 * b % (Tq - 1) for b in range(B)], [Tk - b % 3 for b in range(B)]
+    where = torch.zeros((B, Tk), dtype=torch.bool)
+    for b in range(B):
+        where[b, k_lens[b] // 2] = True
+    blind = torch.arange(Tq)[None] >= torch.tensor(q_lens)[:, None]
+    return lengths(q_lens), lengths(k_lens), where.to("cuda:0"), blind.to("cuda:0")
+
+
+@pytest.mark.parametrize("B,Tq,Tk,H,D", ROUTES)
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("which", ["v", "k"])
+def test_queries_that_see_no_key_have_zeros(B, Tq, Tk, H, D, dtype, which):
+    """Beside queries that see an infinity or NaN."""
+    q, k, v, _ = inputs(B, Tq, Tk, H, H, D, dtype)
+    q_lens, k_lens, where, blind = some_rows(B, Tq, Tk)
+    args = dict(q_lens=q_lens, k_lens=k_lens)
+    _, clean = L.attention(q, k, v, **args)
+    out, lse = L.attention(q, *((k, poison(v, where)) if which == "v" else (poison(k, where), v)), **args)
+    assert bool((out[blind] == 0).all()) and bool((lse.transpose(1, 2)[blind] == -math.inf).all())
+    if which == "v":
+        assert torch.equal(lse, clean)
+        # 0, 3, ...: NaN; 1, 2: infinities, which may come out as NaN
+        assert bool(out[~blind][:, :, ::4].isnan().all()) and not bool(out[~blind][:, :, 1::4].isfinite().any())
+
+
+@pytest.mark.parametrize("B,Tq,Tk,H", [(24, 150, 150, 6), (2, 40, 90, 6), (1, 20, 3000, 2)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_scores_of_minus_infinity(B, Tq, Tk, H, dtype):
+    """A query whose scores are all minus infinity sees keys: 0 / 0, not the zeros of one that sees none."""
+    q, k, v, _ = inputs(B, Tq, Tk, H, H, 32, dtype)
+    k[0] = -INF
+    out, lse = L.attention(q.abs() + 1, k, v)
+    assert bool(out[0].isnan().all()) and not bool(lse[0].isfinite().any())
+    assert bool(out[1:].isfinite().all()) and bool(lse[1:].isfinite().all())
