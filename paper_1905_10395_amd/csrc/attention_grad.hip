@@ -243,10 +243,11 @@ __global__ __launch_bounds__(F::THREADS, (kOccupancy<F, T, PARTS>)) void attenti
     }
     join_shared<F, PARTS>(k0, v0, own, share, lane, dq);
     if (!row.there || share) return;
+    // (a row that sees nothing: zeros, not 0 x infinity of keys that rows beside it see)
     if (g.dq_parts)
-        store_sums<float, PARTS>(g.dq_parts + (((int64_t)at.unit * g.rows + r) * g.row_splits + split) * (PARTS * kPart), lane, PARTS * kPart, g.scale, dq);
+        store_sums<float, PARTS>(g.dq_parts + (((int64_t)at.unit * g.rows + r) * g.row_splits + split) * (PARTS * kPart), lane, PARTS * kPart, g.scale, dq, row.sees > 0);
     else
-        store_sums<T, PARTS>(static_cast<T*>(g.dq.p) + rows.b * g.dq.lb + row.t * g.dq.lt + row.head * g.dq.lh, lane, g.D, g.scale, dq);
+        store_sums<T, PARTS>(static_cast<T*>(g.dq.p) + rows.b * g.dq.lb + row.t * g.dq.lt + row.head * g.dq.lh, lane, g.D, g.scale, dq, row.sees > 0);
 }
 
 // The first row that sees a key.

@@ -84,3 +84,20 @@ def test_scores_of_minus_infinity(B, Tq, Tk, H, dtype):
     out, lse = L.attention(q.abs() + 1, k, v)
     assert bool(out[0].isnan().all()) and not bool(lse[0].isfinite().any())
     assert bool(out[1:].isfinite().all()) and bool(lse[1:].isfinite().all())
+
+
+@pytest.mark.parametrize("B,Tq,Tk,H,D", ROUTES)
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("which", ["v", "k", "do"])
+def test_gradients_of_queries_that_see_no_key_are_zeros(B, Tq, Tk, H, D, dtype, which):
+    """Beside queries that see an infinity or NaN, or have one; as those of keys that nobody sees."""
+    q, k, v, do = inputs(B, Tq, Tk, H, H, D, dtype)
+    q_lens, k_lens, where, blind = some_rows(B, Tq, Tk)
+    args = dict(q_lens=q_lens, k_lens=k_lens)
+    k, v = (k, poison(v, where)) if which == "v" else (poison(k, where), v) if which == "k" else (k, v)
+    out, lse = L.attention(q, k, v, **args)
+    first = torch.arange(Tq, device=q.device)[None].expand(B, Tq) == 0
+    dq, dk, dv = L.attention_grad(poison(do, first) if which == "do" else do, q, k, v, out, lse, **args)
+    assert bool((dq[blind] == 0).all()) and not bool(dq[:, 0].isfinite().all())
+    unseen = torch.arange(Tk, device=q.device)[None] >= k_lens[:, None]
+    assert bool((dk[unseen] == 0).all()) and bool((dv[unseen] == 0).all())
