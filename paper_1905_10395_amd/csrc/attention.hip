@@ -256,7 +256,9 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_ke
         constexpr int later = ALIGNED ? TileLoad<T, KEYS, PARTS, 1, WIDTH>::kLoads : 0;
         Frag<T> qf[2 * PARTS];
         load_queries<T, PARTS>(g, rows, row, h, qf);
+        // every wait below counts on the order K, V, K, V, ...: the tiles are objects of their own, which the compiler may load in either order
         load(k, g.k.lt, begin + wid * KEYS, kt[wid]);
+        asm volatile("" ::: "memory");
         load(v, g.v.lt, begin + wid * KEYS, vt[wid]);
         for (int key0 = begin + wid * KEYS; key0 < end; key0 += W * KEYS) {
             f32x16 p[1];
