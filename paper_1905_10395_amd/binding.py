@@ -608,6 +608,15 @@ def _vector(who, name, t, dtype, n, index):
     return t.data_ptr()
 
 
+def _statistics(who, name, t, shape, index):
+    """Address of float32 statistics without gaps, laid out as one of these calls writes them."""
+    if t is None:
+        return 0
+    if t.shape != shape or t.dtype is not _F32 or t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"{who}: {name} must be contiguous {_F32} {list(shape)}, on the GPU of the others")
+    return t.data_ptr()
+
+
 def _positions(who, t, W, T, index):
     if t is None:
         return 0, 0
@@ -689,7 +698,7 @@ def qk_rotary(q, k=None, positions=None, turns=None, w_q=None, w_k=None, norm=Tr
         a = _QK_ROTARY.pack(W, T, Hq, Hk, D, 2 * half, dt is _BF16, bool(norm), bool(interleaved), eps, magnitude, *_heads(who, "q", q, shape, dt, index),
                             *_heads(who, "k", k, kshape, dt, index), *to_q, *to_k, *_positions(who, positions, W, T, index),
                             _vector(who, "turns", turns, torch.float64, half, index), wq, wk, lq, lk,
-                            _vector(who, "stats", stats, _F32, W * T * (Hq + Hk), index))
+                            _statistics(who, "stats", stats, (W, T, Hq + Hk), index))
         _call(index, stream, lib().lsgd_qk_rotary, a)
     return q_out, k_out, stats
 
@@ -729,7 +738,7 @@ def qk_rotary_grad(dq_out, dk_out=None, q=None, k=None, stats=None, positions=No
                              *_heads(who, "dq_out", dq_out, shape, dt, index), *_heads(who, "dk_out", dk_out, kshape, dt, index),
                              *_heads(who, "q", q, shape, dt, index), *_heads(who, "k", k, kshape, dt, index), *to_q, *to_k, *_positions(who, positions, W, T, index),
                              _vector(who, "turns", turns, torch.float64, half, index), wq, wk, lq, lk,
-                             _vector(who, "stats", stats, _F32, W * T * (Hq + Hk), index) if norm else 0, dwq, dwk, ldq, ldk)
+                             _statistics(who, "stats", stats, (W, T, Hq + Hk), index) if norm else 0, dwq, dwk, ldq, ldk)
     L = lib()
     ws, nbytes = None, 0
     if T and (dwq or dwk):
@@ -773,7 +782,7 @@ def attention(q, k, v, causal=False, scale=None, q_lens=None, k_lens=None, with_
     a = _ATTENTION.pack(B, Tq, Tk, Hq, Hk, D, dt is _BF16, bool(causal), scale, *_heads(who, "q", q, shape, dt, index),
                         *_heads(who, "k", k, kshape, dt, index), *_heads(who, "v", v, kshape, dt, index), *to,
                         _vector(who, "q_lens", q_lens, _I32, B, index), _vector(who, "k_lens", k_lens, _I32, B, index),
-                        _vector(who, "lse", lse, _F32, B * Hq * Tq, index))
+                        _statistics(who, "lse", lse, (B, Hq, Tq), index))
     L = lib()
     ws, nbytes = None, 0
     if Tk > ATTENTION_ONE_LAUNCH or workspace is not None:
@@ -802,7 +811,7 @@ def attention_grad(dout, q, k, v, out, lse, causal=False, scale=None, q_lens=Non
                              *_heads(who, "q", q, shape, dt, index), *_heads(who, "k", k, kshape, dt, index), *_heads(who, "v", v, kshape, dt, index),
                              *_heads(who, "out", out, shape, dt, index), *to_q, *to_k, *to_v,
                              _vector(who, "q_lens", q_lens, _I32, B, index), _vector(who, "k_lens", k_lens, _I32, B, index),
-                             _vector(who, "lse", lse, _F32, B * Hq * Tq, index))
+                             _statistics(who, "lse", lse, (B, Hq, Tq), index))
     L = lib()
     workspace, nbytes = _workspace(who, L.lsgd_attention_grad_workspace_bytes(B, Tq, Tk, Hq, Hk, D, dt is _BF16), q, workspace, stream)
     _call(index, stream, L.lsgd_attention_grad, a, workspace.data_ptr(), nbytes)
