@@ -754,6 +754,8 @@ def _attention_shapes(who, q, k):
         raise ValueError(f"{who}: q must be float32 or bfloat16 [B, Tq, Hq, D]")
     if len(ks) != 4 or ks[0] != qs[0] or ks[3] != qs[3]:
         raise ValueError(f"{who}: k must be [B, Tk, Hk, D] beside q")
+    if qs[3] == 0:
+        raise ValueError(f"{who}: q has no columns")
     return qs, ks
 
 

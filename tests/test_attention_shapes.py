@@ -40,3 +40,10 @@ def test_stats_have_their_own_layout(as_if_on_a_gpu):
             L.qk_rotary(q, k, stats=stats)
     L.qk_rotary_grad(q, k, q, k, f(B, Tq, Hq + Hk))
     assert L.qk_rotary(q, k, stats=f(B, Tq, Hq + Hk))[2].shape == (B, Tq, Hq + Hk)
+
+
+def test_heads_without_columns_are_refused(as_if_on_a_gpu):
+    q, k = f(B, Tq, Hq, 0), f(B, Tk, Hk, 0)
+    for call in (lambda: L.attention(q, k, k), lambda: L.attention_grad(q, q, k, k, q, f(B, Hq, Tq))):
+        with pytest.raises(ValueError, match="columns"):
+            call()
