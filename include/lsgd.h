@@ -489,8 +489,11 @@ lsgd_status lsgd_qk_rotary_grad(const lsgd_qk_rotary_grad_args* args, void* work
  *   q_lens, k_lens  device int32 [B], read on the device and taken as within [0, Tq], [0, Tk]; NULL: all Tq, all Tk
  *   lse         device fp32 [B, Hq, Tq]: log of the sum of exp(scale q.k), which the gradient needs; NULL: not wanted
  * A query that sees no key, or behind q_lens[b], has out = 0 and lse = -inf.  What lies in memory at such queries and at keys from
- * k_lens[b] on does not matter (NaN neither); a key that is merely not seen yet must be finite.  Scores, softmax and sums are
- * fp32; with bf16 data p is rounded to bf16 before the product with v.  out must not overlap the inputs.
+ * k_lens[b] on does not matter (NaN neither); a key that is merely not seen yet must be finite, or queries beside may get NaN from it.
+ * NaN in a query, or in keys that it sees, makes its results NaN, and in their values those columns.  Infinities there make them
+ * infinite or NaN; a score of -inf counts nothing, or makes them NaN.  fp32 elements above the largest bf16 (3.39e38) count as infinite.
+ * Scores, softmax and sums are fp32; sums of p v before their division reach 2^8 Tk max|v|, which must be finite.  With bf16 data p is
+ * rounded to bf16 before the product with v.  out must not overlap the inputs.
  *   workspace  device, >= lsgd_attention_workspace_bytes, 256-byte aligned, not kept; may be NULL where that says 256, which it does up
  *              to LSGD_ATTENTION_ONE_LAUNCH keys.  Few queries and longer keys are split over the keys, and the parts joined from there. */
 #define LSGD_ATTENTION_ONE_LAUNCH 1024
@@ -508,8 +511,9 @@ lsgd_status lsgd_attention(const lsgd_attention_args* args, void* workspace, siz
 
 /* Its gradients dq, dk, dv from dout, given what the forward call read and gave (out, lse): sums over queries, and over the heads that
  * share a key head, in an order that depends on the sizes and lengths alone.  Zeros at queries that see nothing, at queries from q_lens
- * and keys from k_lens on; what lies there (in dout, q, out, k, v) does not matter.  With bf16 data p and its gradient are rounded to bf16 before their products.  dq, dk, dv must not overlap
- * the inputs or each other.
+ * and keys from k_lens on; what lies there (in dout, q, out, k, v) does not matter.  With bf16 data p and its gradient are rounded to
+ * bf16 before their products.  NaN or infinities at a query that sees some key, or at a key that is seen, may reach gradients of keys
+ * and queries of its entry that do not see each other.  dq, dk, dv must not overlap the inputs or each other.
  *   workspace  device, >= lsgd_attention_grad_workspace_bytes, 256-byte aligned, not kept                                  */
 typedef struct {
     int32_t B, Tq, Tk, Hq, Hk, D;

@@ -101,3 +101,16 @@ def test_gradients_of_queries_that_see_no_key_are_zeros(B, Tq, Tk, H, D, dtype, 
     assert bool((dq[blind] == 0).all()) and not bool(dq[:, 0].isfinite().all())
     unseen = torch.arange(Tk, device=q.device)[None] >= k_lens[:, None]
     assert bool((dk[unseen] == 0).all()) and bool((dv[unseen] == 0).all())
+
+
+@pytest.mark.parametrize("B,Tq,Tk,H,D", ROUTES)
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("power", [-60, 106])
+def test_values_of_any_size(B, Tq, Tk, H, D, dtype, power):
+    """Powers of two in v are powers of two in the results, as long as 2^8 Tk max|v| is finite (3000 keys of up to 4 2^106 with p up to 2^8:
+    below 2^128) and what fp32's third part of an element holds, 2^-24 of it, times a p of 2^-20, is a normal value."""
+    q, k, v, _ = inputs(B, Tq, Tk, H, H, D, dtype)
+    v = torch.where(v.abs() < 2.0 ** -10, torch.ones_like(v), v).clamp(-4.0, 4.0)
+    out, lse = L.attention(q, k, v)
+    got, glse = L.attention(q, k, v * 2.0 ** power)
+    assert torch.equal(lse, glse) and torch.equal(got / 2.0 ** power, out)
