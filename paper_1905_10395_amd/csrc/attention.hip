@@ -15,9 +15,12 @@
 // a workgroup takes 32 of them, and its wavefronts and further workgroups split the keys; each wavefront has tiles of its own and waits
 // for nobody, and the parts are joined at the end.
 //
-// By rows is bound by the products (2 x 8192 causal tokens of 32 and 8 heads of 128 bf16 1.02 to 1.06 ms, 1.04 to 1.08 PFLOP/s where a large
-// product alone reaches 1.22), short and narrow rows by the exponentials and by filling and draining (64 x 512 of 16 heads of 64 with lengths of all
-// kinds 53 to 57 us); a single query to a cache by memory (32 entries of up to 16384 keys, 8 heads of 128, 205 to 225 us, 4.9 to 5.4 TB/s).
+// By rows is bound by the products (2 x 8192 causal tokens of 32 and 8 heads of 128 bf16 1.02 to 1.11 ms, 0.99 to 1.08 PFLOP/s where a large
+// product alone reaches 1.22), short rows by loading, computing and storing one after the other (64 x 512 of 16 heads of 64 with lengths of
+// all kinds 52 to 57 us: its bytes take 31, its exponentials and products some 20); fp32 by splitting operands beside the products, and of 97
+// to 128 columns by registers that do not suffice, 108 to 124 bytes of scratch a lane (4 x 2048 causal tokens of 16 and 4 heads of 128 472 us, 146
+// TFLOP/s, of 16 heads of 64 249, 138); a single query to a cache by memory (32 entries of up to 16384 keys, 8 heads of 128, 205 to 225 us, 4.9
+// to 5.4 TB/s).
 #include <algorithm>
 #include <cmath>
 
@@ -374,7 +377,8 @@ struct Plan {
 constexpr int kComputeUnits = 256;
 // By keys where by rows would leave compute units without a workgroup (heads of 128, 16 query and 4 key heads; us by rows, by keys):
 // 1024 causal tokens, 128 workgroups, bf16 24.4, 18.2, fp32 114, 47; 1536, 192 workgroups, bf16 33, 29, fp32 163, 89; but 2048, 256
-// workgroups, 42, 40 and 216, 138, and 8 x 512 x 8 x 8, as many, 17, 23 and 65, 62.  Without a causal mask rows' workgroups all have as
+// workgroups, 42, 40 and 216, 138, and 8 x 512 x 8 x 8, as many, 17, 23 and 65, 62.  The limit is bf16's: fp32's two lie beyond it, and how far was
+// not measured.  Without a causal mask rows' workgroups all have as
 // much to do, and bf16, bound by the products, gains up to half as many: 1024 tokens 23.5, 21.3; 1152, 144 workgroups, 26.7, 33.5.
 //
 // Splits of the keys cost their parts' way through memory.  Tiles of many rows: as many splits as compute units take (1152 causal

@@ -26,7 +26,7 @@ namespace attention {
 constexpr int kPart = 32;                   // columns of a part of a tile
 constexpr int kMaxColumns = 128;            // of a head
 constexpr int kNonTemporal = 2;             // cache policy of a load
-constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
+constexpr float kLog2e = 1.44269504088896341f;
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -37,7 +37,9 @@ typedef const __attribute__((address_space(1))) void* global_ptr;
 
 // Eight elements of an operand.  fp32: as the sum of three bf16 values, each of which takes the next eight bits of what is left (to
 // 2^-24 of the element); of the nine products of two such sums the six largest are made, and what is left out is below 2^-24 of the
-// whole.  Six bf16 instructions take 6 / 16 of the time of the fp32 ones of the same products; the parts are made on the way from LDS.
+// whole.  Six bf16 instructions take 6 / 16 of the time of the fp32 ones of the same products; the parts are made on the way from LDS,
+// by every wavefront that reads an element, in about as long as its products.  An infinite element, and one that rounds to an infinity
+// of bf16, has NaN for its second part.
 template <class T> struct Frag;
 template <> struct Frag<uint16_t> { bf16x8 v; };
 template <> struct Frag<float> { bf16x8 v[3]; };

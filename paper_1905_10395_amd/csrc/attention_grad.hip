@@ -14,8 +14,13 @@
 // In both, results become operands in registers (attention_common.h): by rows s^T and dp^T, keys becoming the contraction, by
 // keys s and dp, rows becoming it.  Where a pass has few workgroups, further ones split its contraction, and a launch adds up their sums.
 //
-// Bound by the products: 4 x 4096 causal tokens of 16 and 4 heads of 128 bf16 0.95 to 1.02 ms, 0.95 to 1.0 PFLOP/s of the seven products (0.35 to 0.4
-// ms by rows, 0.6 by keys); small ones by the chain of one workgroup's tiles (3 x 100 to 259 keys of 72 columns fp32: 14 + 16 + 4 us).
+// By rows bound by the products, by keys also by loads that are waited for: 4 x 4096 causal tokens of 16 and 4 heads of 128 bf16 0.95 to 1.02 ms,
+// 0.95 to 1.0 PFLOP/s of the seven products, the three by rows in 0.35 to 0.4 ms, the four by keys in 0.6.  By keys z and delta are asked
+// for after the next tile and laid down at once, and loads arrive in order, so the wavefronts that bring them wait for that tile before they
+// pass the present one.  Registers that do not suffice, in bytes of scratch a lane (aligned, off alignment): by keys bf16 of 97 to 128 columns
+// 56 and 64, reloaded between the tile's loads; fp32 of 33 to 64 columns 272 and 288, of 97 to 128 16 and 24, few of them off alignment 84; by
+// rows fp32 of 33 to 64 columns 12.  fp32: 4 x 2048 causal tokens of 16 and 4 heads of 128 1.56 ms, 110 TFLOP/s of the five products
+// counted, of 16 heads of 64 0.9, 96.  Small ones by the chain of one workgroup's tiles (3 x 100 to 259 keys of 72 columns fp32: 14 + 16 + 4 us).
 #include <algorithm>
 #include <cmath>
 
@@ -37,7 +42,7 @@ struct Args : Shape {
 };
 
 // A workgroup owns 32 OWN rows, or keys, and SHARE of its wavefronts share each 32: of every tile that passes, each takes PASS of the rows
-// (keys), and their sums are added up in order at the end.  BUFFERS tiles, so that the next is on its way while one is passed.
+// (keys), and their sums are added up in order at the end.  BUFFERS tiles: 2, the next is asked for before one is passed.
 template <int OWN_, int SHARE_, int PASS_, int BUFFERS_>
 struct Form {
     static constexpr int OWN = OWN_, SHARE = SHARE_, PASS = PASS_, BUFFERS = BUFFERS_;
